@@ -358,6 +358,58 @@ int32_t psd_decode_block_cached(psd_handle *h, int32_t *tokens, int32_t B, int32
                                 const psd_policy *policy, const psd_graph *graph, psd_stats *stats, void *cache,
                                 int32_t capacity, void *ws, int64_t ws_bytes, void *stream);
 
+/* ---- Keys that a batch shares, the weights they draw, and eviction by those weights ------------
+ * Requests that begin with the same text need its keys and values once.  Here the keys that a row attends to come in segments,
+ * coarse to fine: a prefix of the whole batch, the cache of a request (shared by its drafts), the rows of a block.  A segment
+ * has S / seqs_per_unit units; sequences u * seqs_per_unit .. + seqs_per_unit - 1 see unit u of it, all of its keys.
+ * Unit u: keys k + u * stride_k, key j in row j (row stride ld_k), channels of KV head g from g * d_head on; values transposed,
+ * vt + u * stride_vt, row g * d_head + c (row stride ld_vt) the values of channel c with the keys of every group of 16 in the order
+ * 0-3, 8-11, 4-7, 12-15 -- one layer of a KV cache as psd_kv_cache_bytes lays it out is such a unit.  What lies behind the
+ * last key is never used.  Strides are in elements.  Rows are 16-byte aligned, rows of values hold whole groups of 16 keys. */
+#define PSD_MAX_SEGMENTS 4
+typedef struct {
+    const void *k, *vt;          /* device, in the dtype of the call */
+    const int32_t *lens;         /* device int32, keys of every unit (cut to 0 .. len), or NULL: each unit holds len */
+    float *weights;              /* device: [units] stride_w apart, [n_kv_heads] ld_w apart, one per key; or NULL */
+    int64_t stride_k, stride_vt, stride_w;
+    int32_t ld_k, ld_vt, ld_w;
+    int32_t len;                 /* keys of a unit, or the most that any unit holds (0: the segment is skipped) */
+    int32_t seqs_per_unit;       /* a multiple of the next segment's; that of the first divides S */
+    int32_t reserved;            /* 0 */
+} psd_kv_segment;
+/* Rows of the attention: S sequences of L rows (1 .. 64), row i of sequence s at q + (s*L + i) * ld_q, n_heads heads of d_head.
+ * dtype PSD_DTYPE_BF16: d_head 64 or 128; PSD_DTYPE_FP32: 16, 32, 64 or 128. */
+typedef struct {
+    int32_t S, L, n_heads, n_kv_heads, d_head, dtype;
+    int64_t ld_q, ld_out;
+} psd_attention_shape;
+/* sizeof psd_kv_segment, psd_attention_shape and psd_kv_shared, as psd_struct_sizes gives those of the structures above. */
+int32_t psd_shared_struct_sizes(int32_t *out, int32_t n);
+/* psd_attention_shared: softmax(q k^T / sqrt(d_head)) v of every row over all keys of the units it sees.  out as q (row stride
+ *   ld_out, may not overlap an input); lse device float [S*L, n_heads], ln of the sum of the exponentials of its scores, or NULL.  A row
+ *   without a key (all lengths 0) gets zeros and lse -inf.  ws: device, 256-byte aligned, psd_attention_shared_bytes of the same
+ *   shape and segments (which looks at shapes and len only, not at device memory); calls that overlap need one each.  Sums and statistics are
+ *   fp32; with bf16 the probabilities are rounded to bf16 before they meet the values.
+ * psd_attention_weights: what each key drew: weights[u][g][j] = sum over the rows of the unit's sequences and the query heads of KV head g
+ *   of exp(score - lse), lse from psd_attention_shared over all segments.  Segments without `weights` are skipped; accumulate = 1
+ *   adds to what is there, 0 overwrites.  Weights behind a unit's last key are left as they are.  ws likewise
+ *   (psd_attention_weights_bytes; may be NULL where that is 0). */
+int64_t psd_attention_shared_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments);
+int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments, void *out,
+                             float *lse, void *ws, int64_t ws_bytes, void *stream);
+int64_t psd_attention_weights_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments);
+int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments,
+                              const float *lse, int32_t accumulate, void *ws, int64_t ws_bytes, void *stream);
+/* psd_kv_evict: of `units` units of src (seqs_per_unit is ignored) and every KV head the keep >= 1 positions with the largest weights: the first n_first
+ *   and the last n_last positions of a unit always (n_first + n_last <= keep), then by src->weights, descending, equal ones the
+ *   lowest position first (both zeros are equal, NaN is below everything).  They go to dst in ascending order of their positions: keys, values and, where
+ *   dst->weights is set, weights; a unit of at most `keep` positions is copied whole.  dst must hold min(keep, src->len) positions (its `len`), have
+ *   lens NULL, and not overlap src; what lies behind the positions written is left as it is.  kept device int32 [units][n_kv_heads][keep]: the source position of
+ *   each, -1 behind the last; kept_lens device int32 [units] (or NULL): positions of each unit now.
+ *   The layers of the caches of n sequences are n * n_layers units in a row.  d_head * element size a multiple of 16 bytes. */
+int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32_t units, int32_t n_kv_heads, int32_t d_head, int32_t dtype,
+                     int32_t keep, int32_t n_first, int32_t n_last, int32_t *kept, int32_t *kept_lens, void *stream);
+
 /* ---- Approximate KV cache for fully bidirectional models -----------------------------------------
  * Sec. 3.2 stage 3 notes that KV-cache sharing can cut redundant computation; with bidirectional
  * attention any cache is an approximation, and the paper fixes no scheme.  The one offered here is the

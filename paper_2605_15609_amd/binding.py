@@ -66,6 +66,17 @@ class _Work(C.Structure):
                 ("head_bytes", C.c_double), ("weight_bytes", C.c_double)]
 
 
+class _Segment(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("vt", C.c_void_p), ("lens", C.c_void_p), ("weights", C.c_void_p), ("stride_k", C.c_int64),
+                ("stride_vt", C.c_int64), ("stride_w", C.c_int64), ("ld_k", C.c_int32), ("ld_vt", C.c_int32), ("ld_w", C.c_int32),
+                ("len", C.c_int32), ("seqs_per_unit", C.c_int32), ("reserved", C.c_int32)]
+
+
+class _AttentionShape(C.Structure):
+    _fields_ = [("S", C.c_int32), ("L", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32),
+                ("dtype", C.c_int32), ("ld_q", C.c_int64), ("ld_out", C.c_int64)]
+
+
 class _DebugLayout(C.Structure):
     _fields_ = [("off_a", C.c_int64), ("off_qkv", C.c_int64), ("off_vt", C.c_int64), ("off_o", C.c_int64),
                 ("off_act", C.c_int64), ("ld_qkv", C.c_int32), ("ld_act", C.c_int32), ("ld_vt", C.c_int32),
@@ -151,6 +162,12 @@ def load_library():
         "psd_kernel_gemm_tile_count": (i32, []),
         "psd_kernel_gemm_tile_name": (C.c_char_p, [i32]),
         "psd_forward_work": (i32, [C.POINTER(_Config), i32, i32, i32, C.POINTER(_Work)]),
+        "psd_shared_struct_sizes": (i32, [C.POINTER(i32), i32]),
+        "psd_attention_shared_bytes": (i64, [vp, vp, i32]),
+        "psd_attention_shared": (i32, [vp, vp, vp, i32, vp, vp, vp, i64, vp]),
+        "psd_attention_weights_bytes": (i64, [vp, vp, i32]),
+        "psd_attention_weights": (i32, [vp, vp, vp, i32, vp, i32, vp, i64, vp]),
+        "psd_kv_evict": (i32, [vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -160,6 +177,10 @@ def load_library():
     theirs = (i32 * len(mine))()
     if lib.psd_struct_sizes(theirs, len(mine)) != len(mine) or list(theirs) != mine:
         raise PsdError(f"binding and libpsd.so disagree on the structure layouts: {mine} vs {list(theirs)} (rebuild the library)")
+    mine = [C.sizeof(t) for t in (_Segment, _AttentionShape)]
+    theirs = (i32 * len(mine))()
+    if lib.psd_shared_struct_sizes(theirs, len(mine)) != len(mine) or list(theirs) != mine:
+        raise PsdError(f"binding and libpsd.so disagree on the segment layouts: {mine} vs {list(theirs)} (rebuild the library)")
     _lib = lib
     return lib
 
@@ -658,6 +679,184 @@ def psd_decode_block_approx(model: Model, tokens: torch.Tensor, block_start: int
     _check(model.lib.psd_decode_block_approx(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(pol), C.byref(g), cstats,
                                              _ptr(cache.mem), cache.capacity, _ptr(ws), nb, _stream()))
     return _add_stats(stats, cstats, B)
+
+
+# ---- keys that a batch shares, the weights they draw, eviction by those weights (see psd.h) ----
+
+_DTYPES = {torch.bfloat16: 1, torch.float32: 0}
+
+
+class KvSegment:
+    """Keys that the sequences of a batch attend to, one unit of them for every seqs_per_unit consecutive sequences.
+
+    k [units, positions, n_kv_heads * d_head] and vt [units, n_kv_heads * d_head, at least the positions rounded up to 16] (values
+    transposed, keys of every group of 16 in the order 0-3, 8-11, 4-7, 12-15), bf16 or fp32, dense along the last dimension; the
+    first `length` positions are keys (default: all), or lens[unit] of them (int32 [units]; what is outside 0 .. length is cut).
+    weights fp32 [units, n_kv_heads, positions]: what psd_attention_weights writes and psd_kv_evict goes by."""
+
+    def __init__(self, k: torch.Tensor, vt: torch.Tensor, d_head: int, length: Optional[int] = None, seqs_per_unit: int = 1,
+                 lens: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None):
+        if k.dim() != 3 or vt.dim() != 3 or k.dtype not in _DTYPES or vt.dtype != k.dtype or k.shape[0] != vt.shape[0] \
+                or k.shape[2] != vt.shape[1] or d_head < 1 or k.shape[2] % d_head or k.stride(2) != 1 or vt.stride(2) != 1:
+            raise PsdError(f"keys [units, positions, heads * d_head] and values [units, heads * d_head, slots] of one type, dense along the "
+                           f"last dimension, not {k.dtype} {tuple(k.shape)} {k.stride()} and {vt.dtype} {tuple(vt.shape)} {vt.stride()}")
+        units, positions, width = k.shape
+        n = positions if length is None else int(length)
+        if not 0 <= n <= positions or (n + 15) // 16 * 16 > vt.shape[2]:
+            raise PsdError(f"{n} keys of {positions} positions, value rows of {vt.shape[2]}")
+        if lens is not None and (lens.dtype != torch.int32 or tuple(lens.shape) != (units,) or not lens.is_contiguous()):
+            raise PsdError(f"lens: dense int32 [{units}], not {lens.dtype} {tuple(lens.shape)}")
+        if weights is not None and (weights.dtype != torch.float32 or weights.dim() != 3 or tuple(weights.shape[:2]) != (units, width // d_head)
+                                    or weights.shape[2] < n or weights.stride(2) != 1):
+            raise PsdError(f"weights: float32 [{units}, {width // d_head}, at least {n}] dense along the last dimension, not "
+                           f"{weights.dtype} {tuple(weights.shape)} {weights.stride()}")
+        for t in (vt, lens, weights):
+            if t is not None and t.device != k.device:
+                raise PsdError(f"a segment on {k.device} and {t.device}")
+        self.k, self.vt, self.lens, self.weights = k, vt, lens, weights
+        self.units, self.length, self.d_head, self.n_kv_heads = units, n, int(d_head), width // d_head
+        self.seqs_per_unit, self.device, self.dtype = int(seqs_per_unit), k.device, k.dtype
+        def address(t):
+            return None if t is None or t.numel() == 0 else t.data_ptr()
+        # (strides of dimensions of one entry mean nothing, and torch gives any)
+        self.c = _Segment(address(k), address(vt), address(lens), address(weights), k.stride(0) if units > 1 else 0,
+                          vt.stride(0) if units > 1 else 0, 0 if weights is None or units == 1 else weights.stride(0),
+                          k.stride(1) if positions > 1 else width, vt.stride(1) if width > 1 else vt.shape[2],
+                          0 if weights is None else weights.stride(1) if self.n_kv_heads > 1 else weights.shape[2], n, self.seqs_per_unit, 0)
+
+
+class KvSegments:
+    """The segments of a batch, coarse to fine, as the calls take them (built once, used by many calls)."""
+
+    def __init__(self, segments: Sequence[KvSegment]):
+        self.segments = list(segments)
+        if not self.segments:
+            raise PsdError("no segments")
+        first = self.segments[0]
+        for s in self.segments:
+            if (s.device, s.dtype, s.d_head, s.n_kv_heads) != (first.device, first.dtype, first.d_head, first.n_kv_heads):
+                raise PsdError("segments of different devices, types or heads")
+        self.c = (_Segment * len(self.segments))(*[s.c for s in self.segments])
+        self.n, self.device, self.dtype, self.d_head, self.n_kv_heads = len(self.segments), first.device, first.dtype, first.d_head, first.n_kv_heads
+
+
+def _rows(t: torch.Tensor, what: str) -> int:
+    """Row stride of [S, L, heads, d_head] whose S * L rows are evenly spaced and hold their heads densely."""
+    S, L, H, d = t.shape
+    row = t.stride(1) if L > 1 else t.stride(0) if S > 1 else H * d
+    if (d > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != d) or (S > 1 and t.stride(0) != L * row):
+        raise PsdError(f"{what}: heads of a row one behind the other, rows evenly spaced, not {tuple(t.shape)} with strides {t.stride()}")
+    return row
+
+
+def _attention_shape(q: torch.Tensor, keys: KvSegments, out: Optional[torch.Tensor] = None) -> _AttentionShape:
+    if q.dim() != 4 or q.dtype != keys.dtype or q.device != keys.device or q.shape[3] != keys.d_head:
+        raise PsdError(f"q [S, L, heads, {keys.d_head}] {keys.dtype} on {keys.device}, not {q.dtype} {tuple(q.shape)} on {q.device}")
+    S, L, H, d = q.shape
+    if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != q.device):
+        raise PsdError(f"out like q, not {out.dtype} {tuple(out.shape)} on {out.device}")
+    for s in keys.segments:
+        if s.seqs_per_unit < 1 or s.units * s.seqs_per_unit != S:
+            raise PsdError(f"{s.units} units of {s.seqs_per_unit} sequences for a batch of {S}")
+    return _AttentionShape(S, L, H, keys.n_kv_heads, d, _DTYPES[q.dtype], _rows(q, "q"), H * d if out is None else _rows(out, "out"))
+
+
+def _check_lse(lse: torch.Tensor, q: torch.Tensor) -> None:
+    if lse.dtype != torch.float32 or lse.shape != q.shape[:3] or not lse.is_contiguous() or lse.device != q.device:
+        raise PsdError(f"lse: dense float32 {tuple(q.shape[:3])} on {q.device}, not {lse.dtype} {tuple(lse.shape)} on {lse.device}")
+
+
+def _bytes(n: int, device, given: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    if given is not None:
+        if given.device != device or not given.is_contiguous():
+            raise PsdError(f"a dense workspace on {device}, not on {given.device}")
+        return given
+    return torch.empty((n,), dtype=torch.uint8, device=device) if n else None
+
+
+class _on_device:
+    """The stream of a tensor's device, whichever device is current."""
+
+    def __init__(self, device):
+        if device.type != "cuda":
+            raise PsdError(f"tensors on a GPU, not on {device}")
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return _stream()
+
+    def __exit__(self, *what):
+        if self.guard is not None:
+            self.guard.__exit__(*what)
+
+
+def psd_attention_workspace(q: torch.Tensor, keys: KvSegments) -> torch.Tensor:
+    """What psd_attention_shared needs for q and keys, to be kept and passed on as ws."""
+    shape = _attention_shape(q, keys)
+    return torch.empty((max(256, _check(load_library().psd_attention_shared_bytes(C.byref(shape), keys.c, keys.n))),), dtype=torch.uint8,
+                       device=q.device)
+
+
+def psd_attention_weights_bytes(q: torch.Tensor, keys: KvSegments) -> int:
+    """Bytes of workspace that psd_attention_weights needs for q and keys (possibly 0)."""
+    shape = _attention_shape(q, keys)
+    return int(_check(load_library().psd_attention_weights_bytes(C.byref(shape), keys.c, keys.n)))
+
+
+def psd_attention_shared(q: torch.Tensor, keys: KvSegments, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                         ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of q [S, L, n_heads, d_head] over the keys of all segments -> out [S, L, n_heads, d_head]; lse fp32 [S, L, n_heads]
+    receives the log of each row's sum of exponentials."""
+    lib = load_library()
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    shape = _attention_shape(q, keys, out)
+    if lse is not None:
+        _check_lse(lse, q)
+    if ws is None:
+        ws = _bytes(_check(lib.psd_attention_shared_bytes(C.byref(shape), keys.c, keys.n)), q.device)
+    else:
+        _bytes(0, q.device, ws)
+    with _on_device(q.device) as stream:
+        _check(lib.psd_attention_shared(C.byref(shape), q.data_ptr(), keys.c, keys.n, out.data_ptr(), _ptr(lse), _ptr(ws),
+                                        0 if ws is None else ws.numel() * ws.element_size(), stream))
+    return out
+
+
+def psd_attention_weights(q: torch.Tensor, keys: KvSegments, lse: torch.Tensor, accumulate: bool = True,
+                          ws: Optional[torch.Tensor] = None) -> None:
+    """What every key of the segments with weights drew from the rows of q under the lse of psd_attention_shared, added to their
+    weights (accumulate) or in their place."""
+    lib = load_library()
+    shape = _attention_shape(q, keys)
+    _check_lse(lse, q)
+    need = _check(lib.psd_attention_weights_bytes(C.byref(shape), keys.c, keys.n))
+    ws = _bytes(need, q.device, ws)
+    with _on_device(q.device) as stream:
+        _check(lib.psd_attention_weights(C.byref(shape), q.data_ptr(), keys.c, keys.n, lse.data_ptr(), int(bool(accumulate)), _ptr(ws),
+                                         0 if ws is None else ws.numel() * ws.element_size(), stream))
+
+
+def psd_kv_evict(src: KvSegment, dst: KvSegment, keep: int, first: int = 0, last: int = 0, kept: Optional[torch.Tensor] = None,
+                 kept_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The `keep` positions of every unit and KV head of src that drew most (the first and last ones always) into dst, in ascending
+    order -> kept int32 [units, n_kv_heads, keep], their positions in src, -1 behind the last; kept_lens int32 [units]."""
+    shape = (src.units, src.n_kv_heads, int(keep))
+    if (dst.units, dst.n_kv_heads, dst.d_head, dst.dtype, dst.device) != (src.units, src.n_kv_heads, src.d_head, src.dtype, src.device):
+        raise PsdError("source and destination differ in units, heads, type or device")
+    if keep < 1:
+        raise PsdError(f"keep {keep}")
+    if kept is None:
+        kept = torch.empty(shape, dtype=torch.int32, device=src.device)
+    for name, t, want in (("kept", kept, shape), ("kept_lens", kept_lens, shape[:1])):
+        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != want or not t.is_contiguous() or t.device != src.device):
+            raise PsdError(f"{name}: dense int32 {want} on {src.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    with _on_device(src.device) as stream:
+        _check(load_library().psd_kv_evict(C.byref(src.c), C.byref(dst.c), src.units, src.n_kv_heads, src.d_head, _DTYPES[src.dtype], int(keep),
+                                           int(first), int(last), kept.data_ptr(), _ptr(kept_lens), stream))
+    return kept
 
 
 def psd_calibrate_graph(model: Model, tokens: torch.Tensor, prompt_len: int, L: int, policy: Policy,

@@ -1013,6 +1013,163 @@ int32_t psd_decode_block_cached(psd_handle *h, int32_t *tokens, int32_t B, int32
     return decode_block_impl(h, tokens, B, N, block_start, L, policy, graph, stats, ws, ws_bytes, stream, &a);
 }
 
+// ---- keys that a batch shares, the weights they draw, eviction by those weights ----
+
+namespace {
+
+int32_t check_segment(const psd_kv_segment &s, int i, int32_t units, int32_t n_kv_heads, int32_t d_head, int32_t dtype, SharedSegment *out) {
+    if (s.reserved != 0) PSD_FAIL(PSD_ERR_INVALID_ARG, "segment %d: reserved is not 0", i);
+    if (s.len < 0) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: %d keys", i, s.len);
+    if (s.stride_k < 0 || s.stride_vt < 0 || s.stride_w < 0) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: negative stride", i);
+    if (s.len > 0 && s.ld_k < n_kv_heads * d_head) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: key rows of %d elements", i, s.ld_k);
+    if (s.weights && s.len > 0 && (s.ld_w < s.len || (units > 1 && s.stride_w < (int64_t)(n_kv_heads - 1) * s.ld_w + s.len)))
+        PSD_FAIL(PSD_ERR_SHAPE, "segment %d: weights of %d keys do not fit their strides", i, s.len);
+    out->k = s.k;
+    out->vt = s.vt;
+    out->lens = s.lens;
+    out->weights = s.weights;
+    out->stride_k = s.stride_k;
+    out->stride_vt = s.stride_vt;
+    out->stride_w = s.stride_w;
+    out->ld_k = s.ld_k;
+    out->ld_vt = s.ld_vt;
+    out->ld_w = s.ld_w;
+    out->len = s.len;
+    out->seqs_per_unit = s.seqs_per_unit;
+    if (const char *why = shared_segment_fault(dtype, *out)) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: %s", i, why);
+    return PSD_OK;
+}
+
+int32_t check_shared(const psd_attention_shape *a, const psd_kv_segment *segs, int32_t n, SharedShape *sh, SharedSegment *out) {
+    if (!a || !segs) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL shape / segments");
+    if (n < 1 || n > PSD_MAX_SEGMENTS) PSD_FAIL(PSD_ERR_SHAPE, "%d segments (1..%d)", n, PSD_MAX_SEGMENTS);
+    if (a->dtype != PSD_DTYPE_BF16 && a->dtype != PSD_DTYPE_FP32) PSD_FAIL(PSD_ERR_UNSUPPORTED, "dtype %d", a->dtype);
+    if (!shared_attention_takes(a->dtype, a->d_head))
+        PSD_FAIL(PSD_ERR_UNSUPPORTED, "d_head %d (bf16: 64, 128; fp32: 16, 32, 64, 128)", a->d_head);
+    if (a->S < 1 || a->L < 1 || a->L > PSD_MAX_BLOCK) PSD_FAIL(PSD_ERR_SHAPE, "%d sequences of %d rows (1..%d)", a->S, a->L, PSD_MAX_BLOCK);
+    if (a->n_heads < 1 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads)
+        PSD_FAIL(PSD_ERR_SHAPE, "%d heads on %d KV heads", a->n_heads, a->n_kv_heads);
+    if ((int64_t)a->n_heads * a->d_head >= 1 << 24 || (int64_t)a->S * a->L * a->n_heads >= 1ll << 31)
+        PSD_FAIL(PSD_ERR_SHAPE, "%d sequences of %d rows of %d heads are too many", a->S, a->L, a->n_heads);
+    const int chunk = a->dtype == PSD_DTYPE_BF16 ? 8 : 4;
+    if (a->ld_q < (int64_t)a->n_heads * a->d_head || a->ld_q % chunk) PSD_FAIL(PSD_ERR_SHAPE, "query rows of %lld elements", (long long)a->ld_q);
+    if (a->ld_out < (int64_t)a->n_heads * a->d_head || a->ld_out % chunk) PSD_FAIL(PSD_ERR_SHAPE, "output rows of %lld elements", (long long)a->ld_out);
+    *sh = {a->S, a->L, a->n_heads, a->n_kv_heads, a->d_head, a->dtype, a->ld_q, a->ld_out, (int64_t)a->S * a->L * a->n_heads};
+    int32_t above = a->S;
+    for (int i = 0; i < n; ++i) {
+        const int32_t per = segs[i].seqs_per_unit;
+        if (per < 1 || above % per) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: units of %d sequences do not divide those of %d before it", i, per, above);
+        above = per;
+        CHECK(check_segment(segs[i], i, a->S / per, a->n_kv_heads, a->d_head, a->dtype, out + i));
+    }
+    if (!shared_attention_fits(*sh, out, n)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    return PSD_OK;
+}
+
+bool misaligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+
+// [first, last) byte that a segment's units occupy
+struct Extent {
+    uintptr_t first, last;
+    bool meets(const Extent &o) const { return first < o.last && o.first < last; }
+};
+Extent extent(const void *p, int64_t units, int64_t stride, int64_t rows, int64_t ld, int64_t width, int64_t esz) {
+    const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+    return {b, b + (uintptr_t)(((units - 1) * stride + (rows - 1) * ld + width) * esz)};
+}
+
+}   // namespace
+
+int32_t psd_shared_struct_sizes(int32_t *out, int32_t n) {
+    const int32_t sizes[] = {(int32_t)sizeof(psd_kv_segment), (int32_t)sizeof(psd_attention_shape)};
+    const int32_t count = (int32_t)(sizeof(sizes) / sizeof(sizes[0]));
+    for (int32_t i = 0; i < n && i < count && out; ++i) out[i] = sizes[i];
+    return count;
+}
+
+int64_t psd_attention_shared_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments) {
+    SharedShape sh;
+    SharedSegment seg[kMaxSegments];
+    CHECK(check_shared(shape, segments, n_segments, &sh, seg));
+    return shared_attention_bytes(sh, seg, n_segments);
+}
+
+int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments, void *out,
+                             float *lse, void *ws, int64_t ws_bytes, void *stream) {
+    SharedShape sh;
+    SharedSegment seg[kMaxSegments];
+    CHECK(check_shared(shape, segments, n_segments, &sh, seg));
+    if (!q || !out) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL q / out");
+    if (misaligned16(q) || misaligned16(out)) PSD_FAIL(PSD_ERR_SHAPE, "q and out must be 16-byte aligned");
+    const int64_t need = shared_attention_bytes(sh, seg, n_segments);
+    if (need > 0 && (!ws || ws_bytes < need)) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
+    if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 255) != 0) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    launch_attention_shared(q, sh, seg, n_segments, out, lse, ws, (hipStream_t)stream);
+    PSD_HIP(hipGetLastError());
+    return PSD_OK;
+}
+
+int64_t psd_attention_weights_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments) {
+    SharedShape sh;
+    SharedSegment seg[kMaxSegments];
+    CHECK(check_shared(shape, segments, n_segments, &sh, seg));
+    return shared_weights_bytes(sh, seg, n_segments);
+}
+
+int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments,
+                              const float *lse, int32_t accumulate, void *ws, int64_t ws_bytes, void *stream) {
+    SharedShape sh;
+    SharedSegment seg[kMaxSegments];
+    CHECK(check_shared(shape, segments, n_segments, &sh, seg));
+    if (!q || !lse) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL q / lse");
+    if (misaligned16(q)) PSD_FAIL(PSD_ERR_SHAPE, "q must be 16-byte aligned");
+    if (accumulate != 0 && accumulate != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "accumulate %d", accumulate);
+    const int64_t need = shared_weights_bytes(sh, seg, n_segments);
+    if (need > 0 && (!ws || ws_bytes < need)) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
+    if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 255) != 0) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    launch_attention_weights(q, sh, seg, n_segments, lse, accumulate, ws, (hipStream_t)stream);
+    PSD_HIP(hipGetLastError());
+    return PSD_OK;
+}
+
+int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32_t units, int32_t n_kv_heads, int32_t d_head, int32_t dtype,
+                     int32_t keep, int32_t n_first, int32_t n_last, int32_t *kept, int32_t *kept_lens, void *stream) {
+    if (!src || !dst || !kept) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL src / dst / kept");
+    if (dtype != PSD_DTYPE_BF16 && dtype != PSD_DTYPE_FP32) PSD_FAIL(PSD_ERR_UNSUPPORTED, "dtype %d", dtype);
+    const int64_t esz = dtype == PSD_DTYPE_BF16 ? 2 : 4;
+    if (units < 1 || n_kv_heads < 1 || d_head < 1 || (int64_t)n_kv_heads * d_head >= 1 << 24) PSD_FAIL(PSD_ERR_SHAPE, "%d units of %d x %d", units, n_kv_heads, d_head);
+    if (d_head * esz % 16) PSD_FAIL(PSD_ERR_UNSUPPORTED, "d_head %d: rows of a head are whole 16 bytes", d_head);
+    if (keep < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > keep)
+        PSD_FAIL(PSD_ERR_SHAPE, "keep %d with the first %d and the last %d", keep, n_first, n_last);
+    SharedSegment from, to;
+    CHECK(check_segment(*src, 0, units, n_kv_heads, d_head, dtype, &from));
+    CHECK(check_segment(*dst, 1, units, n_kv_heads, d_head, dtype, &to));
+    if (!src->weights && src->len > 0) PSD_FAIL(PSD_ERR_INVALID_ARG, "the source has no weights");
+    if (dst->lens) PSD_FAIL(PSD_ERR_INVALID_ARG, "the destination has lengths of its own");
+    const int32_t most = std::min(keep, src->len);
+    if (dst->len < most) PSD_FAIL(PSD_ERR_SHAPE, "a destination of %d positions for %d", dst->len, most);
+    if (kv_evict_workgroups(from, units, n_kv_heads, d_head, dtype, keep) >= 1ll << 31 || (int64_t)units * n_kv_heads >= 1ll << 31)
+        PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    if (most > 0) {
+        const int64_t w = (int64_t)n_kv_heads * d_head;
+        const Extent in[] = {extent(src->k, units, src->stride_k, src->len, src->ld_k, w, esz),
+                             extent(src->vt, units, src->stride_vt, w, src->ld_vt, src->ld_vt, esz),
+                             extent(src->weights, units, src->stride_w, n_kv_heads, src->ld_w, src->len, 4)};
+        // (what is written: `most` positions, value rows up to the group of 16 that the last one is in)
+        const Extent written[] = {extent(dst->k, units, dst->stride_k, most, dst->ld_k, w, esz),
+                                  extent(dst->vt, units, dst->stride_vt, w, dst->ld_vt, (most + 15) / 16 * 16, esz),
+                                  dst->weights ? extent(dst->weights, units, dst->stride_w, n_kv_heads, dst->ld_w, most, 4) : Extent{0, 0},
+                                  extent(kept, 1, 0, 1, 0, (int64_t)units * n_kv_heads * keep, 4)};
+        for (const Extent &a : in)
+            for (const Extent &b : written)
+                if (a.meets(b)) PSD_FAIL(PSD_ERR_INVALID_ARG, "the destination overlaps the source");
+        if (units > 1 && (dst->stride_k < 1 || dst->stride_vt < 1)) PSD_FAIL(PSD_ERR_SHAPE, "the units of the destination lie on each other");
+    }
+    launch_kv_evict(from, to, units, n_kv_heads, d_head, dtype, keep, n_first, n_last, kept, kept_lens, (hipStream_t)stream);
+    PSD_HIP(hipGetLastError());
+    return PSD_OK;
+}
+
 // ---- approximate prefix + suffix KV cache for bidirectional models ----
 
 int32_t psd_forward_confidence_approx(psd_handle *h, const int32_t *tokens, int32_t S, int32_t N, int32_t block_start, int32_t L,

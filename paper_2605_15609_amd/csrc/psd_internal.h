@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <atomic>
 #include <vector>
 
@@ -399,6 +400,45 @@ void launch_attention_block(const bf16_t *qkv, int ld_qkv, int S, int N, int n_h
 // their own block and of everything before it, all of them (their own included) in the cache
 void launch_attention_causal_bf16(const bf16_t *qkv, int ld_qkv, int S, int N, int n_heads, int n_kv_heads, int d_head, bf16_t *out,
                                   const KvPrefix &cache, int pos0, int block_len, hipStream_t st);
+// attention_shared.hip: attention over segments of keys that the sequences of a batch share, coarse to fine (psd_kv_segment)
+struct SharedSegment {
+    const void *k = nullptr, *vt = nullptr;
+    const int32_t *lens = nullptr;       // device, one per unit; NULL: every unit holds len keys
+    const int32_t *rows = nullptr;       // device: unit u is cache rows[u * seqs_per_unit] / rows_div (NULL: cache u)
+    float *weights = nullptr;
+    int64_t stride_k = 0, stride_vt = 0, stride_w = 0;
+    int ld_k = 0, ld_vt = 0, ld_w = 0, len = 0, seqs_per_unit = 1, rows_div = 1;
+};
+struct SharedShape {
+    int S, L, n_heads, n_kv_heads, d_head, dtype;
+    int64_t ld_q, ld_out, n_rows;        // n_rows = S * L * n_heads
+};
+constexpr int kMaxSegments = PSD_MAX_SEGMENTS;
+// what one launch does: jobs behind one another in the grid, each with the segment of its number
+struct SharedJob {
+    int units, tiles, splits, block0, part0;
+};
+struct SharedLaunch {
+    int n_jobs = 0, parts = 0;
+    int64_t blocks = 0;
+    SharedJob job[kMaxSegments] = {};
+    SharedSegment seg[kMaxSegments];
+    float *o = nullptr;                  // [parts][n_rows][d_head] sums relative to the part's maximum
+    float2 *ml = nullptr;                // [parts][n_rows] maximum of the scores, sum of the exponentials (0: no keys, o not written)
+};
+bool shared_attention_takes(int dtype, int d_head);
+const char *shared_segment_fault(int dtype, const SharedSegment &s);
+int64_t shared_attention_bytes(const SharedShape &sh, const SharedSegment *seg, int n);
+bool shared_attention_fits(const SharedShape &sh, const SharedSegment *seg, int n);   // (its grid)
+void launch_attention_shared(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, void *out, float *lse /* or NULL */, void *ws,
+                             hipStream_t st);
+int64_t shared_weights_bytes(const SharedShape &sh, const SharedSegment *seg, int n);
+void launch_attention_weights(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, const float *lse, int accumulate, void *ws,
+                              hipStream_t st);
+// kv_evict.hip
+int64_t kv_evict_workgroups(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep);
+void launch_kv_evict(const SharedSegment &src, const SharedSegment &dst, int units, int n_kv_heads, int d_head, int dtype, int keep, int n_first,
+                     int n_last, int32_t *kept, int32_t *kept_lens, hipStream_t st);
 // lm_head.hip (bf16): LM-head fused with the online top-1 / sum-exp reduction
 int64_t head_partial_bytes(int rows, int V);
 // fragment-order copies: [ceil(R/32)][K/16][64 lanes][8 bf16]

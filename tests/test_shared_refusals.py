@@ -1,0 +1,143 @@
+"""What the shared-key operators refuse, on the CPU: nothing is launched, so no GPU is needed."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2605_15609_amd as psd
+from paper_2605_15609_amd import binding as B
+
+BF = torch.bfloat16
+BASE = 1 << 40       # an address that is never read
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import os
+    if not os.path.exists(psd.library_path()):
+        from paper_2605_15609_amd import build
+        build.build()
+    return psd.load_library()
+
+
+def shape(**kw):
+    return B._AttentionShape(**dict(dict(S=4, L=2, n_heads=8, n_kv_heads=4, d_head=64, dtype=1, ld_q=512, ld_out=512), **kw))
+
+
+def seg(**kw):
+    f = dict(k=BASE, vt=BASE + (1 << 30), lens=None, weights=None, stride_k=64 * 256, stride_vt=256 * 64, stride_w=0, ld_k=256, ld_vt=64, ld_w=0,
+             len=50, seqs_per_unit=4, reserved=0)
+    f.update(kw)
+    return B._Segment(**f)
+
+
+def ask(lib, sh, *segs):
+    return lib.psd_attention_shared_bytes(C.byref(sh), (B._Segment * len(segs))(*segs), len(segs))
+
+
+def test_the_shapes_that_are_taken(lib):
+    assert ask(lib, shape(), seg()) > 0
+    assert ask(lib, shape(), seg(), seg(seqs_per_unit=2), seg(seqs_per_unit=1)) > 0
+    assert ask(lib, shape(), seg(len=0, k=None, vt=None)) >= 0
+    for d in (16, 32, 64, 128):
+        assert ask(lib, shape(dtype=0, d_head=d, ld_q=8 * d, ld_out=8 * d), seg(ld_k=4 * d)) > 0
+    assert lib.psd_attention_weights_bytes(C.byref(shape()), (B._Segment * 1)(seg(weights=BASE, ld_w=50)), 1) >= 0
+
+
+@pytest.mark.parametrize("change", [dict(S=0), dict(L=0), dict(L=65), dict(n_heads=6), dict(n_kv_heads=0), dict(d_head=32), dict(d_head=96),
+                                    dict(dtype=2), dict(ld_q=511), dict(ld_q=516), dict(ld_out=8), dict(S=1 << 30), dict(dtype=0, d_head=24)])
+def test_shapes_that_are_not(lib, change):
+    assert ask(lib, shape(**change), seg()) < 0
+    assert B.load_library().psd_last_error()
+
+
+@pytest.mark.parametrize("change", [dict(k=None), dict(vt=None), dict(k=BASE + 2), dict(vt=BASE + 8), dict(ld_k=255), dict(ld_k=260), dict(ld_vt=48),
+                                    dict(ld_vt=56), dict(ld_vt=72), dict(stride_k=4), dict(stride_vt=4), dict(stride_k=-256), dict(len=-1),
+                                    dict(seqs_per_unit=0), dict(seqs_per_unit=3), dict(seqs_per_unit=8), dict(reserved=1),
+                                    dict(weights=BASE, ld_w=49), dict(weights=BASE, ld_w=50, stride_w=100, seqs_per_unit=1)])
+def test_segments_that_are_not(lib, change):
+    assert ask(lib, shape(), seg(**change)) < 0
+    assert B.load_library().psd_last_error()
+
+
+def test_order_and_number_of_segments(lib):
+    assert ask(lib, shape(), seg(seqs_per_unit=1), seg(seqs_per_unit=4)) < 0      # fine before coarse
+    assert ask(lib, shape(S=12), seg(seqs_per_unit=6), seg(seqs_per_unit=4)) < 0  # units that cross
+    assert ask(lib, shape(), *[seg() for _ in range(5)]) < 0
+    assert lib.psd_attention_shared_bytes(C.byref(shape()), None, 1) < 0
+    assert lib.psd_attention_shared_bytes(None, (B._Segment * 1)(seg()), 1) < 0
+    assert lib.psd_attention_shared_bytes(C.byref(shape()), (B._Segment * 1)(seg()), 0) < 0
+
+
+def test_calls_check_pointers_and_workspace_before_anything_runs(lib):
+    s, one = shape(), (B._Segment * 1)(seg())
+    need = ask(lib, s, seg())
+    ok = dict(q=BASE, out=BASE, ws=BASE, n=need)
+
+    def call(**kw):
+        a = dict(ok, **kw)
+        return lib.psd_attention_shared(C.byref(s), a["q"], one, 1, a["out"], None, a["ws"], a["n"], None)
+    for bad in (dict(q=None), dict(out=None), dict(q=BASE + 2), dict(out=BASE + 8), dict(ws=None), dict(ws=BASE + 128), dict(n=need - 1), dict(n=0)):
+        assert call(**bad) < 0, bad
+    assert lib.psd_attention_weights(C.byref(s), BASE, one, 1, None, 0, None, 0, None) < 0
+    assert lib.psd_attention_weights(C.byref(s), None, one, 1, BASE, 0, None, 0, None) < 0
+    assert lib.psd_attention_weights(C.byref(s), BASE, one, 1, BASE, 2, None, 0, None) < 0
+
+
+def evict(lib, src=None, dst=None, units=2, heads=4, d=64, dtype=1, keep=20, first=2, last=3, kept=BASE + (7 << 30)):
+    base = dict(weights=BASE + (2 << 30), ld_w=50, stride_w=200, len=50)
+    s = seg(**dict(base, **(src or {})))
+    t = seg(**dict(dict(k=BASE + (4 << 30), vt=BASE + (5 << 30), weights=BASE + (6 << 30), ld_w=50, stride_w=200, len=50), **(dst or {})))
+    return lib.psd_kv_evict(C.byref(s), C.byref(t), units, heads, d, dtype, keep, first, last, kept, None, None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(keep=0), dict(keep=-1), dict(first=-1), dict(last=-1), dict(first=18, last=3), dict(first=1 << 30, last=1 << 30), dict(units=0), dict(heads=0),
+    dict(d=0), dict(d=60), dict(dtype=7), dict(kept=None), dict(src=dict(weights=None)), dict(src=dict(ld_w=20)), dict(src=dict(k=None)),
+    dict(dst=dict(len=19)), dict(dst=dict(lens=BASE)), dict(dst=dict(k=BASE)), dict(dst=dict(vt=BASE + (1 << 30))), dict(dst=dict(weights=BASE + (2 << 30))),
+    dict(dst=dict(k=BASE + 1024)), dict(kept=BASE + 64), dict(dst=dict(stride_k=0)), dict(dst=dict(ld_vt=24)), dict(keep=1 << 30, heads=1 << 17),
+])
+def test_evictions_that_are_not(lib, change):
+    assert evict(lib, **change) < 0
+    assert lib.psd_last_error()
+
+
+def test_the_binding_refuses_tensors_that_the_library_would_misread(lib):
+    k, vt = torch.zeros((2, 20, 256), dtype=BF), torch.zeros((2, 256, 32), dtype=BF)
+    ok = psd.KvSegment(k, vt, 64, seqs_per_unit=2)
+    assert (ok.units, ok.n_kv_heads, ok.c.len, ok.c.ld_k, ok.c.ld_vt) == (2, 4, 20, 256, 32)
+    for args in ((k.float(), vt), (k.half(), vt.half()), (k[0], vt), (k, vt[:1]), (k, vt[:, :128]), (k, vt[:, :, :16]), (k[..., ::2], vt[:, ::2]),
+                 (k.transpose(1, 2).contiguous().transpose(1, 2), vt)):
+        with pytest.raises(psd.PsdError):
+            psd.KvSegment(*args, 64)
+    for kw in (dict(length=21), dict(length=-1), dict(lens=torch.zeros(2)), dict(lens=torch.zeros(3, dtype=torch.int32)),
+               dict(weights=torch.zeros((2, 4, 19))), dict(weights=torch.zeros((2, 3, 20))), dict(weights=torch.zeros((2, 4, 20), dtype=BF))):
+        with pytest.raises(psd.PsdError):
+            psd.KvSegment(k, vt, 64, **kw)
+    with pytest.raises(psd.PsdError):
+        psd.KvSegment(k, vt, 48)
+    with pytest.raises(psd.PsdError):
+        psd.KvSegments([])
+    with pytest.raises(psd.PsdError):
+        psd.KvSegments([ok, psd.KvSegment(k.float(), vt.float(), 64)])
+    keys = psd.KvSegments([ok])
+    q = torch.zeros((4, 3, 8, 64), dtype=BF)
+    for bad in (q.float(), q[..., :32], q[:3], q[0], q[:, :, ::2], q.transpose(1, 2).contiguous().transpose(1, 2)):
+        with pytest.raises(psd.PsdError):
+            psd.psd_attention_shared(bad, keys)
+    with pytest.raises(psd.PsdError):
+        psd.psd_attention_shared(q, keys, lse=torch.zeros((4, 3, 8), dtype=torch.float64))
+    with pytest.raises(psd.PsdError):
+        psd.psd_attention_shared(q, keys, out=torch.zeros((4, 3, 8, 64)))
+    with pytest.raises(psd.PsdError, match="on a GPU"):
+        psd.psd_attention_shared(q, keys)
+    with pytest.raises(psd.PsdError):
+        psd.psd_attention_weights(q, keys, torch.zeros((4, 3, 7)))
+    with pytest.raises(psd.PsdError, match="on a GPU"):
+        psd.psd_attention_weights(q, keys, torch.zeros((4, 3, 8)))
+    with pytest.raises(psd.PsdError, match="on a GPU"):
+        psd.psd_kv_evict(ok, ok, 5)
+    with pytest.raises(psd.PsdError):
+        psd.psd_kv_evict(ok, ok, 0)
+    with pytest.raises(psd.PsdError):
+        psd.psd_kv_evict(ok, ok, 5, kept=torch.zeros((2, 4, 6), dtype=torch.int32))
