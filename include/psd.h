@@ -410,6 +410,36 @@ int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, c
 int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32_t units, int32_t n_kv_heads, int32_t d_head, int32_t dtype,
                      int32_t keep, int32_t n_first, int32_t n_last, int32_t *kept, int32_t *kept_lens, void *stream);
 
+/* Model calls whose block rows attend to a prefix that the whole batch shares, then to the cache of their sequence, then to their block.
+ * Both caches are laid out like the exact one (psd_kv_cache_bytes(cfg, capacity) per sequence; the prefix is one), and their positions
+ * count as they lie: rotary positions are in the keys, so a cache may have gaps (psd_kv_evict), and the block's rows sit at positions block_start .. of
+ * tokens whatever the caches hold.  A prefix is filled by psd_kv_prefill with B = 1, a sequence's cache behind it by psd_kv_extend_shared.
+ * Block-causal models: exact while nothing is evicted.  Bidirectional models: the caches of psd_forward_confidence_approx, whole or evicted.
+ *   psd_forward_confidence_shared: as psd_forward_confidence_cached; sequence s uses cache s / seqs_per_cache.  What every cached
+ *     position drew from the block rows, layer by layer, is added to prefix_weights / cache_weights (zero them first) where set.
+ *   psd_kv_extend_shared: one forward over the block rows of B sequences (seqs_per_cache 1), whose keys and values go to positions len ..
+ *     len + L - 1 of their caches.  Block-causal models only; adds no weights.
+ *   psd_decode_block_shared: psd_decode_block with such model calls; afterwards the block is appended as by psd_kv_extend_shared.
+ * L a multiple of 16.  Workspace: psd_shared_workspace_bytes(cfg, S, L, kv), 256-byte aligned; for psd_decode_block_shared with S = B*K and
+ * kv->seqs_per_cache = K there (1 in the call), plus psd_decode_scratch_bytes(B, N, L, K). */
+typedef struct {
+    const void *prefix;          /* device, one cache; may be NULL where prefix_len is 0 */
+    void *cache;                 /* device, one per seqs_per_cache sequences; may be NULL where len is 0 and nothing is stored */
+    float *prefix_weights;       /* device [n_layers][n_kv_heads][prefix_capacity], or NULL */
+    float *cache_weights;        /* device [caches][n_layers][n_kv_heads][capacity], or NULL */
+    int32_t prefix_capacity, prefix_len, capacity, len, seqs_per_cache;
+    int32_t reserved;            /* 0 */
+} psd_kv_shared;
+int64_t psd_shared_workspace_bytes(const psd_model_config *cfg, int32_t S, int32_t L, const psd_kv_shared *kv);
+int32_t psd_forward_confidence_shared(psd_handle *h, const int32_t *tokens, int32_t S, int32_t N, int32_t block_start, int32_t L,
+                                      const psd_kv_shared *kv, int32_t *top1, float *conf, float *logits, void *ws, int64_t ws_bytes,
+                                      void *stream);
+int32_t psd_kv_extend_shared(psd_handle *h, const int32_t *tokens, int32_t B, int32_t N, int32_t block_start, int32_t L,
+                             const psd_kv_shared *kv, void *ws, int64_t ws_bytes, void *stream);
+int32_t psd_decode_block_shared(psd_handle *h, int32_t *tokens, int32_t B, int32_t N, int32_t block_start, int32_t L,
+                                const psd_policy *policy, const psd_graph *graph, psd_stats *stats, const psd_kv_shared *kv, void *ws,
+                                int64_t ws_bytes, void *stream);
+
 /* ---- Approximate KV cache for fully bidirectional models -----------------------------------------
  * Sec. 3.2 stage 3 notes that KV-cache sharing can cut redundant computation; with bidirectional
  * attention any cache is an approximation, and the paper fixes no scheme.  The one offered here is the

@@ -77,6 +77,12 @@ class _AttentionShape(C.Structure):
                 ("dtype", C.c_int32), ("ld_q", C.c_int64), ("ld_out", C.c_int64)]
 
 
+class _KvShared(C.Structure):
+    _fields_ = [("prefix", C.c_void_p), ("cache", C.c_void_p), ("prefix_weights", C.c_void_p), ("cache_weights", C.c_void_p),
+                ("prefix_capacity", C.c_int32), ("prefix_len", C.c_int32), ("capacity", C.c_int32), ("len", C.c_int32),
+                ("seqs_per_cache", C.c_int32), ("reserved", C.c_int32)]
+
+
 class _DebugLayout(C.Structure):
     _fields_ = [("off_a", C.c_int64), ("off_qkv", C.c_int64), ("off_vt", C.c_int64), ("off_o", C.c_int64),
                 ("off_act", C.c_int64), ("ld_qkv", C.c_int32), ("ld_act", C.c_int32), ("ld_vt", C.c_int32),
@@ -167,6 +173,11 @@ def load_library():
         "psd_attention_shared": (i32, [vp, vp, vp, i32, vp, vp, vp, i64, vp]),
         "psd_attention_weights_bytes": (i64, [vp, vp, i32]),
         "psd_attention_weights": (i32, [vp, vp, vp, i32, vp, i32, vp, i64, vp]),
+        "psd_shared_workspace_bytes": (i64, [C.POINTER(_Config), i32, i32, C.POINTER(_KvShared)]),
+        "psd_forward_confidence_shared": (i32, [vp, vp, i32, i32, i32, i32, C.POINTER(_KvShared), vp, vp, vp, vp, i64, vp]),
+        "psd_kv_extend_shared": (i32, [vp, vp, i32, i32, i32, i32, C.POINTER(_KvShared), vp, i64, vp]),
+        "psd_decode_block_shared": (i32, [vp, vp, i32, i32, i32, i32, C.POINTER(_Policy), C.POINTER(_Graph), C.POINTER(_Stats),
+                                          C.POINTER(_KvShared), vp, i64, vp]),
         "psd_kv_evict": (i32, [vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -177,7 +188,7 @@ def load_library():
     theirs = (i32 * len(mine))()
     if lib.psd_struct_sizes(theirs, len(mine)) != len(mine) or list(theirs) != mine:
         raise PsdError(f"binding and libpsd.so disagree on the structure layouts: {mine} vs {list(theirs)} (rebuild the library)")
-    mine = [C.sizeof(t) for t in (_Segment, _AttentionShape)]
+    mine = [C.sizeof(t) for t in (_Segment, _AttentionShape, _KvShared)]
     theirs = (i32 * len(mine))()
     if lib.psd_shared_struct_sizes(theirs, len(mine)) != len(mine) or list(theirs) != mine:
         raise PsdError(f"binding and libpsd.so disagree on the segment layouts: {mine} vs {list(theirs)} (rebuild the library)")
@@ -588,6 +599,28 @@ class KvCache:
     def reset(self):
         _check(self.model.lib.psd_kv_reset(self.model.handle, _ptr(self.mem), self.n_seqs, self.capacity, _stream()))
 
+    def new_weights(self) -> torch.Tensor:
+        """fp32 zeros [n_seqs, n_layers, n_kv_heads, capacity]: what the positions draw (SharedKv, segment)."""
+        s = self.model.shape
+        return torch.zeros((self.n_seqs, s.n_layers, s.n_kv_heads, self.capacity), dtype=torch.float32, device=self.mem.device)
+
+    def segment(self, length: int, weights: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None) -> "KvSegment":
+        """The layers of all caches as the units of one segment (sequence by sequence), `length` positions each: what psd_kv_evict
+        takes from and gives to.  weights as new_weights makes them; lens int32 [n_seqs * n_layers]."""
+        s = self.model.shape
+        dtype = torch.bfloat16 if s.dtype == "bf16" else torch.float32
+        width, ld_vt, units = s.n_kv_heads * s.d_head, (self.capacity + 63) // 64 * 64, self.n_seqs * s.n_layers
+        unit = self.capacity * width + width * ld_vt
+        flat = self.mem[:self.mem.numel() // 16 * 16].view(dtype)
+        if weights is not None:
+            want = (self.n_seqs, s.n_layers, s.n_kv_heads, self.capacity)
+            if tuple(weights.shape) != want or not weights.is_contiguous():
+                raise PsdError(f"weights: dense float32 {want}, not {tuple(weights.shape)}")
+            weights = weights.view(units, s.n_kv_heads, self.capacity)
+        return KvSegment(flat.as_strided((units, self.capacity, width), (unit, width, 1)),
+                         flat.as_strided((units, width, ld_vt), (unit, ld_vt, 1), self.capacity * width), s.d_head, length=length, lens=lens,
+                         weights=weights)
+
 
 # A prompt's rows go into the cache in passes of up to PREFILL_ROWS rows whose workspace, which the model keeps, stays within
 # PREFILL_WORKSPACE bytes.  16 sequences of 1024: 8B shape, 8 layers 43.0 ms with 4096 rows (664 MB) and with 16384 (1.8 GB);
@@ -857,6 +890,80 @@ def psd_kv_evict(src: KvSegment, dst: KvSegment, keep: int, first: int = 0, last
         _check(load_library().psd_kv_evict(C.byref(src.c), C.byref(dst.c), src.units, src.n_kv_heads, src.d_head, _DTYPES[src.dtype], int(keep),
                                            int(first), int(last), kept.data_ptr(), _ptr(kept_lens), stream))
     return kept
+
+
+@dataclass
+class SharedKv:
+    """What the block rows of a shared call attend to besides their block: prefix_len positions of `prefix` (a cache of one sequence), then
+    `length` positions of their sequence's cache.  prefix_weights / cache_weights (KvCache.new_weights): collect what the positions draw."""
+    prefix: Optional[KvCache] = None
+    prefix_len: int = 0
+    cache: Optional[KvCache] = None
+    length: int = 0
+    prefix_weights: Optional[torch.Tensor] = None
+    cache_weights: Optional[torch.Tensor] = None
+
+    def c(self, model: Model, n_caches: int, seqs_per_cache: int = 1) -> _KvShared:
+        for what, cache, weights, n in (("prefix", self.prefix, self.prefix_weights, 1), ("cache", self.cache, self.cache_weights, n_caches)):
+            if cache is not None and cache.n_seqs < n:
+                raise PsdError(f"{what}: {cache.n_seqs} sequences, {n} needed")
+            if cache is not None and (cache.model.shape, cache.mem.device) != (model.shape, model.device):
+                raise PsdError(f"{what}: the cache of another model or device")
+            if weights is not None:
+                want = None if cache is None else (cache.n_seqs, model.shape.n_layers, model.shape.n_kv_heads, cache.capacity)
+                if tuple(weights.shape) != want or weights.dtype != torch.float32 or not weights.is_contiguous() or weights.device != model.device:
+                    raise PsdError(f"{what} weights: dense float32 {want} on {model.device}, not {weights.dtype} {tuple(weights.shape)} on {weights.device}")
+
+        def address(t):
+            return None if t is None else t.data_ptr()
+        return _KvShared(None if self.prefix is None else self.prefix.mem.data_ptr(), None if self.cache is None else self.cache.mem.data_ptr(),
+                         address(self.prefix_weights), address(self.cache_weights), 0 if self.prefix is None else self.prefix.capacity,
+                         int(self.prefix_len), 0 if self.cache is None else self.cache.capacity, int(self.length), int(seqs_per_cache), 0)
+
+
+def _shared_ws(model: Model, S: int, L: int, kv: _KvShared, extra: int = 0):
+    need = _check(model.lib.psd_shared_workspace_bytes(C.byref(model.cfg), S, L, C.byref(kv))) + extra
+    return model.workspace(need), need
+
+
+def psd_forward_confidence_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, kv: SharedKv, seqs_per_cache: int = 1,
+                                  want_logits: bool = False):
+    """tokens int32 [S, N]; the block rows against a prefix of the whole batch and their caches -> (top1 [S, L], conf [S, L][, logits])."""
+    S, N = tokens.shape
+    if seqs_per_cache < 1 or S % seqs_per_cache:
+        raise PsdError(f"{S} sequences, {seqs_per_cache} to a cache")
+    c = kv.c(model, S // seqs_per_cache, seqs_per_cache)
+    ws, nb = _shared_ws(model, S, L, c)
+    top1 = torch.empty((S, L), dtype=torch.int32, device=tokens.device)
+    conf = torch.empty((S, L), dtype=torch.float32, device=tokens.device)
+    logits = torch.empty((S * L, model.shape.vocab), dtype=torch.float32, device=tokens.device) if want_logits else None
+    _check(model.lib.psd_forward_confidence_shared(model.handle, _ptr(tokens), S, N, block_start, L, C.byref(c), _ptr(top1), _ptr(conf),
+                                                   _ptr(logits), _ptr(ws), nb, _stream()))
+    return (top1, conf, logits) if want_logits else (top1, conf)
+
+
+def psd_kv_extend_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, kv: SharedKv) -> None:
+    """The block of every sequence of tokens [B, N] behind the first kv.length positions of its cache (kv.length is then L more: the
+    caller's to count)."""
+    B, N = tokens.shape
+    c = kv.c(model, B)
+    ws, nb = _shared_ws(model, B, L, c)
+    _check(model.lib.psd_kv_extend_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(c), _ptr(ws), nb, _stream()))
+
+
+def psd_decode_block_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, policy: Policy, graph: Graph, kv: SharedKv,
+                            stats: Optional[Sequence[Stats]] = None) -> List[Stats]:
+    """psd_decode_block with shared model calls; the finished block is appended to the caches (kv.length is then L more)."""
+    B, N = tokens.shape
+    K = graph.K
+    c = kv.c(model, B)
+    extra = _check(model.lib.psd_decode_scratch_bytes(B, N, L, K))
+    ws, nb = _shared_ws(model, B * K, L, kv.c(model, B, K), extra=extra)
+    cstats = (_Stats * B)()
+    g, pol = graph.c(), policy.c()
+    _check(model.lib.psd_decode_block_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(pol), C.byref(g), cstats, C.byref(c),
+                                             _ptr(ws), nb, _stream()))
+    return _add_stats(stats, cstats, B)
 
 
 def psd_calibrate_graph(model: Model, tokens: torch.Tensor, prompt_len: int, L: int, policy: Policy,

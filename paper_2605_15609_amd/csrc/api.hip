@@ -110,6 +110,27 @@ int32_t check_policy(const psd_policy *p) {
         if (rc_ != PSD_OK) return rc_; \
     } while (0)
 
+// Workspace of model calls with shared keys over up to S sequences, one or seqs_per_cache of them to a cache, and of the call that extends
+// the caches: how the attention is cut, and with it the scratch, depends on how many there are
+int64_t shared_workspace(const psd_model_config &cfg, int64_t S, int L, const KvCacheArg &kv, int seqs_per_cache) {
+    int64_t most = 0;
+    KvCacheArg a = kv;
+    for (int64_t n = 1; n <= S; ++n) {
+        const int64_t fwd = plan_forward(cfg, n, L, L).total;
+        for (int per : {1, seqs_per_cache}) {
+            if (n % per) continue;
+            a.seqs_per_cache = per;
+            a.append = false;
+            most = std::max(most, fwd + shared_call_bytes(cfg, (int)n, L, a));
+            if (per == 1) {
+                a.append = true;
+                most = std::max(most, fwd + shared_call_bytes(cfg, (int)n, L, a));
+            }
+        }
+    }
+    return most;
+}
+
 struct DecodeScratch {
     int64_t top1, conf, sigma, m, n_left, drafts, v_top1, v_conf, k_star, accepted, devstats, rows, starts, flags, total;
 };
@@ -522,6 +543,7 @@ int32_t decode_impl(psd_handle *h, int32_t *tokens, int32_t B, int32_t N, int32_
     const bool dual = kv && kv->dual;  // approximate cache: the first model call runs over whole sequences and fills it
     const int plan_N = kv ? L : N;     // rows per sequence that a model call runs over
     int64_t fwd_bytes = plan_forward(h->cfg, (int64_t)B * K, plan_N, L).total;
+    if (kv && kv->shared) fwd_bytes = shared_workspace(h->cfg, B * K, L, *kv, K);
     if (dual) fwd_bytes = std::max(fwd_bytes, plan_forward(h->cfg, B, N, L).total);
     const DecodeScratch sc = plan_decode(B, N, L, K);
     if (!ws || ws_bytes < fwd_bytes + sc.total)
@@ -1081,7 +1103,7 @@ Extent extent(const void *p, int64_t units, int64_t stride, int64_t rows, int64_
 }   // namespace
 
 int32_t psd_shared_struct_sizes(int32_t *out, int32_t n) {
-    const int32_t sizes[] = {(int32_t)sizeof(psd_kv_segment), (int32_t)sizeof(psd_attention_shape)};
+    const int32_t sizes[] = {(int32_t)sizeof(psd_kv_segment), (int32_t)sizeof(psd_attention_shape), (int32_t)sizeof(psd_kv_shared)};
     const int32_t count = (int32_t)(sizeof(sizes) / sizeof(sizes[0]));
     for (int32_t i = 0; i < n && i < count && out; ++i) out[i] = sizes[i];
     return count;
@@ -1168,6 +1190,86 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
     launch_kv_evict(from, to, units, n_kv_heads, d_head, dtype, keep, n_first, n_last, kept, kept_lens, (hipStream_t)stream);
     PSD_HIP(hipGetLastError());
     return PSD_OK;
+}
+
+namespace {
+
+// what a psd_kv_shared says, checked; append: the block goes behind the cache
+int32_t check_kv_shared(const psd_model_config &c, const psd_kv_shared *kv, int32_t S, int32_t L, bool append, KvCacheArg *out) {
+    if (!kv) PSD_FAIL(PSD_ERR_INVALID_ARG, "kv is NULL");
+    if (kv->reserved != 0) PSD_FAIL(PSD_ERR_INVALID_ARG, "reserved is not 0");
+    if (!shared_attention_takes(c.dtype, c.d_head))
+        PSD_FAIL(PSD_ERR_UNSUPPORTED, "d_head %d (bf16: 64, 128; fp32: 16, 32, 64, 128)", c.d_head);
+    if (L < 1 || L > PSD_MAX_BLOCK || L % 16) PSD_FAIL(PSD_ERR_SHAPE, "a cached block length must be a multiple of 16 (value layout) up to %d, not %d", PSD_MAX_BLOCK, L);
+    if (kv->prefix_len < 0 || kv->len < 0) PSD_FAIL(PSD_ERR_SHAPE, "%d and %d cached positions", kv->prefix_len, kv->len);
+    auto cache = [&](const void *p, int32_t capacity, int64_t len, const char *what) -> int32_t {
+        if (!p) PSD_FAIL(PSD_ERR_INVALID_ARG, "%s is NULL", what);
+        if ((reinterpret_cast<uintptr_t>(p) & 255) != 0) PSD_FAIL(PSD_ERR_WORKSPACE, "%s must be 256-byte aligned", what);
+        if (capacity < 1 || capacity > c.max_seq) PSD_FAIL(PSD_ERR_SHAPE, "%s capacity %d outside 1..max_seq", what, capacity);
+        if (len > capacity) PSD_FAIL(PSD_ERR_SHAPE, "%s of %d positions is too small for %lld", what, capacity, (long long)len);
+        return PSD_OK;
+    };
+    if (kv->prefix_len > 0) CHECK(cache(kv->prefix, kv->prefix_capacity, kv->prefix_len, "prefix"));
+    if (kv->len > 0 || append) CHECK(cache(kv->cache, kv->capacity, (int64_t)kv->len + (append ? L : 0), "cache"));
+    if (kv->seqs_per_cache < 1 || S % kv->seqs_per_cache) PSD_FAIL(PSD_ERR_SHAPE, "%d sequences, %d to a cache", S, kv->seqs_per_cache);
+    if (append && c.attention != PSD_ATTN_BLOCK_CAUSAL)
+        PSD_FAIL(PSD_ERR_UNSUPPORTED, "only the blocks of context-causal block attention become context (config.attention)");
+    KvCacheArg a;
+    a.shared = true;
+    a.base = kv->cache;
+    a.capacity = kv->cache ? kv->capacity : 0;
+    a.len = kv->len;
+    a.seqs_per_cache = kv->seqs_per_cache;
+    a.prefix = kv->prefix;
+    a.prefix_capacity = kv->prefix_capacity;
+    a.prefix_len = kv->prefix_len;
+    a.prefix_weights = kv->prefix_weights;
+    a.cache_weights = kv->cache_weights;
+    *out = a;
+    return PSD_OK;
+}
+
+}   // namespace
+
+int64_t psd_shared_workspace_bytes(const psd_model_config *cfg, int32_t S, int32_t L, const psd_kv_shared *kv) {
+    CHECK(check_cfg(cfg));
+    if (S < 1) PSD_FAIL(PSD_ERR_SHAPE, "batch %d", S);
+    KvCacheArg a;
+    CHECK(check_kv_shared(*cfg, kv, S, L, false, &a));
+    return shared_workspace(*cfg, S, L, a, a.seqs_per_cache);
+}
+
+int32_t psd_forward_confidence_shared(psd_handle *h, const int32_t *tokens, int32_t S, int32_t N, int32_t block_start, int32_t L,
+                                      const psd_kv_shared *kv, int32_t *top1, float *conf, float *logits, void *ws, int64_t ws_bytes, void *stream) {
+    CHECK(check_block(h, S, N, block_start, L));
+    KvCacheArg a;
+    CHECK(check_kv_shared(h->cfg, kv, S, L, false, &a));
+    if (!tokens || (!logits && (!top1 || !conf))) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL tokens/top1/conf");
+    hipStream_t st = (hipStream_t)stream;
+    CHECK(run_forward_cached(h, tokens, nullptr, S, N, block_start, L, a, ws, ws_bytes, st));
+    if (logits) CHECK(run_head_logits(h, S, L, L, logits, ws, st));
+    if (top1 && conf) return run_head_confidence(h, tokens, nullptr, S, N, block_start, L, top1, conf, nullptr, ws, st, L);
+    return PSD_OK;
+}
+
+int32_t psd_kv_extend_shared(psd_handle *h, const int32_t *tokens, int32_t B, int32_t N, int32_t block_start, int32_t L, const psd_kv_shared *kv,
+                             void *ws, int64_t ws_bytes, void *stream) {
+    CHECK(check_block(h, B, N, block_start, L));
+    KvCacheArg a;
+    CHECK(check_kv_shared(h->cfg, kv, B, L, true, &a));
+    if (!tokens) PSD_FAIL(PSD_ERR_INVALID_ARG, "tokens is NULL");
+    if (a.seqs_per_cache != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "extending needs one sequence per cache");
+    a.append = true;
+    return run_forward_cached(h, tokens, nullptr, B, N, block_start, L, a, ws, ws_bytes, (hipStream_t)stream);
+}
+
+int32_t psd_decode_block_shared(psd_handle *h, int32_t *tokens, int32_t B, int32_t N, int32_t block_start, int32_t L, const psd_policy *policy,
+                                const psd_graph *graph, psd_stats *stats, const psd_kv_shared *kv, void *ws, int64_t ws_bytes, void *stream) {
+    CHECK(check_block(h, B, N, block_start, L));
+    KvCacheArg a;
+    CHECK(check_kv_shared(h->cfg, kv, B, L, true, &a));
+    if (a.seqs_per_cache != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "decoding needs one sequence per cache");
+    return decode_block_impl(h, tokens, B, N, block_start, L, policy, graph, stats, ws, ws_bytes, stream, &a);
 }
 
 // ---- approximate prefix + suffix KV cache for bidirectional models ----

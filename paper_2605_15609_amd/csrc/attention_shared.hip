@@ -305,6 +305,13 @@ __global__ __launch_bounds__(NW * 64) void shared_weights_kernel(const T *__rest
     }
 }
 
+__global__ __launch_bounds__(256) void block_values_kernel(const float *__restrict__ qkv, int ld_qkv, int v_col, int L, int width, float *__restrict__ vT,
+                                                           int ld_vt) {
+    const int64_t s = blockIdx.x / L;
+    const int i = blockIdx.x % L;
+    for (int c = threadIdx.x; c < width; c += 256) vT[(s * width + c) * ld_vt + vt_key_slot(i)] = qkv[(int64_t)blockIdx.x * ld_qkv + v_col + c];
+}
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 template <typename T, int DH>
@@ -391,6 +398,10 @@ void launch_attention_shared(const void *q, const SharedShape &sh, const SharedS
     ln.o = (float *)ws;
     ln.ml = (float2 *)((char *)ws + align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256));
     PSD_SHARED_DISPATCH((run_attention<T, DH>((const T *)q, sh, ln, (T *)out, lse, st)))
+}
+
+void launch_block_values(const float *qkv, int ld_qkv, int v_col, int S, int L, int width, float *vT, int ld_vt, hipStream_t st) {
+    hipLaunchKernelGGL(block_values_kernel, dim3((unsigned)(S * L)), dim3(256), 0, st, qkv, ld_qkv, v_col, L, width, vT, ld_vt);
 }
 
 int64_t shared_weights_bytes(const SharedShape &, const SharedSegment *, int) { return 0; }

@@ -77,6 +77,11 @@ struct Dispatch<float> {
         launch_plain_attention<float>(qkv, ld_qkv, S, N, H, Hkv, dh, out, pre, block_len, st);
         return false;
     }
+    // rotary on q and k (row i of a sequence at position pos0 + i) and the values transposed
+    static void rope_values(psd_handle *h, float *qkv, int ld_qkv, int S, int R, int pos0, int H, int Hkv, int dh, float *vT, hipStream_t st) {
+        launch_rope<float>(qkv, ld_qkv, (int64_t)S * R, R, pos0, H, Hkv, dh, h->rope_cos, h->rope_sin, st);
+        launch_block_values(qkv, ld_qkv, (H + Hkv) * dh, S, R, Hkv * dh, vT, (int)vt_row_stride(R), st);
+    }
     static bool store_outside_fits(psd_handle *, const float *, int, const float *, int, int, const float *, const float *, const KvPrefix &) { return false; }
     static void store_outside(const float *, int, const float *, int, int, int, int, int, int, int, float *, float *, const KvPrefix &, hipStream_t) {}
 };
@@ -166,6 +171,9 @@ struct Dispatch<bf16_t> {
             launch_attention_bf16(qkv, ld_qkv, vT, S, N, H, Hkv, dh, out, pre, st);
         }
         return true;
+    }
+    static void rope_values(psd_handle *h, bf16_t *qkv, int ld_qkv, int S, int R, int pos0, int H, int Hkv, int dh, bf16_t *vT, hipStream_t st) {
+        launch_rope_transpose_v(qkv, ld_qkv, S, R, pos0, H, Hkv, dh, h->rope_cos, h->rope_sin, vT, st);
     }
     // whether the refreshed entries of the approximate cache can be taken from the transposed values (bit 4 of the debug switch: not)
     static bool store_outside_fits(psd_handle *h, const bf16_t *qkv, int ld_qkv, const bf16_t *vT, int N, int dh, const bf16_t *k_cache,
@@ -285,6 +293,54 @@ int32_t forward_hidden_impl(psd_handle *h, const int32_t *tokens, const int32_t 
     return PSD_OK;
 }
 
+// What the rows of a `shared` call see in layer li, coarse to fine: the prefix of the batch, their cache's positions, and (k not NULL)
+// the R rows of their own block.  Returns how many segments there are.
+int shared_segments(const psd_model_config &c, const KvCacheArg &kv, int li, const int32_t *seq_rows, int S, int cache_len, const void *k, int ld_k,
+                    const void *vt, int R, SharedSegment *seg) {
+    const int64_t esz = c.dtype == PSD_DTYPE_BF16 ? 2 : 4;
+    const int w = c.n_kv_heads * c.d_head;
+    int n = 0;
+    auto cached = [&](const void *base, int capacity, int len, int per_unit, float *weights) {
+        const KvLayout lay = kv_layout(c, capacity);
+        SharedSegment &s = seg[n++];
+        s.k = (const char *)base + li * (lay.k_elems + lay.vt_elems) * esz;
+        s.vt = (const char *)s.k + lay.k_elems * esz;
+        s.ld_k = (int)lay.ld_k;
+        s.ld_vt = (int)lay.ld_vt;
+        s.len = len;
+        s.seqs_per_unit = per_unit;
+        s.ld_w = capacity;
+        if (weights) s.weights = weights + (int64_t)li * c.n_kv_heads * capacity;
+        return lay.per_seq;
+    };
+    if (kv.prefix_len > 0) cached(kv.prefix, kv.prefix_capacity, kv.prefix_len, S, kv.prefix_weights);
+    if (cache_len > 0) {
+        const int64_t per_seq = cached(kv.base, kv.capacity, cache_len, kv.seqs_per_cache, kv.cache_weights);
+        SharedSegment &s = seg[n - 1];
+        s.stride_k = s.stride_vt = per_seq;
+        s.stride_w = (int64_t)c.n_layers * c.n_kv_heads * kv.capacity;
+        s.rows = seq_rows;
+        s.rows_div = kv.seqs_per_cache;
+    }
+    if (k) {
+        SharedSegment &s = seg[n++];
+        s.k = k;
+        s.vt = vt;
+        s.ld_k = ld_k;
+        s.ld_vt = (int)vt_row_stride(R);
+        s.stride_k = (int64_t)R * ld_k;
+        s.stride_vt = (int64_t)w * s.ld_vt;
+        s.len = R;
+        s.seqs_per_unit = 1;
+    }
+    return n;
+}
+
+SharedShape shared_shape(const psd_model_config &c, int S, int R) {
+    const int w = c.n_heads * c.d_head;
+    return {S, R, c.n_heads, c.n_kv_heads, c.d_head, c.dtype, qkv_row_stride(w + 2 * c.n_kv_heads * c.d_head), w, (int64_t)S * R * c.n_heads};
+}
+
 // The same model call on block rows alone, for context-causal block attention: everything before the block is finished, its
 // keys and values sit in the sequence's KV cache (kv.len positions), and nothing after the block is visible.  S sequences of
 // R rows, one block of L.  With kv.append the rows' keys and values are stored behind the cache and become context; R may then
@@ -310,6 +366,11 @@ int32_t forward_cached_impl(psd_handle *h, const int32_t *tokens, const int32_t 
     pre.stride_k = pre.stride_vt = lay.per_seq;
     pre.seq_rows = seq_rows;
     pre.seqs_per_cache = kv.seqs_per_cache;
+
+    // shared calls: the row sums, then what the attention and its weights need
+    const bool weighed = kv.shared && !kv.append && (kv.prefix_weights || kv.cache_weights);
+    float *lse = weighed ? (float *)(ws + p.total) : nullptr;
+    char *scratch = ws + p.total + (weighed ? align_up(nrow * H * 4, 256) : 0);
 
     float *ksplit = c.dtype == PSD_DTYPE_BF16 ? (float *)(ws + p.off_ksplit) : nullptr;
     PendingSums pend;
@@ -337,9 +398,9 @@ int32_t forward_cached_impl(psd_handle *h, const int32_t *tokens, const int32_t 
         const bool fused = kv_joined && wk == wq + (int64_t)H * dh * d && (!c.qkv_bias || lw.bk == lw.bq + H * dh);
         const bool kv_only = kv.append && li + 1 == h->layers.size();
         bool stored = false;
-        if (kv.append && !kv_only && fused && !seq_rows && ld_qkv == qkv_w) {   // keys and values go from the projection into the cache
+        if (kv.append && !kv_only && fused && !seq_rows && ld_qkv == qkv_w && kv.len % 16 == 0) {   // keys and values go from the projection into the cache
             KvDest to;
-            to.vT = (bf16_t *)vt_cache + kv.len;      // (kv.len is a multiple of 16: whole groups of key slots)
+            to.vT = (bf16_t *)vt_cache + kv.len;      // (whole groups of key slots)
             to.ld_vt = pre.ld_vt;
             to.vt_seq = to.k_seq = lay.per_seq;
             to.k = (bf16_t *)k_cache + (int64_t)kv.len * lay.ld_k;
@@ -364,8 +425,19 @@ int32_t forward_cached_impl(psd_handle *h, const int32_t *tokens, const int32_t 
             if (kv_only) return PSD_OK;
             KvPrefix all = pre;
             all.len = kv.len + R;
-            if (!Dispatch<T>::append_attention(h, qkv, ld_qkv, S, R, H, Hkv, dh, o, all, block_start, L, st))
+            if (kv.shared) {
+                SharedSegment seg[kMaxSegments];
+                const int n = shared_segments(c, kv, (int)li, seq_rows, S, all.len, nullptr, 0, nullptr, 0, seg);
+                launch_attention_shared(qkv, shared_shape(c, S, R), seg, n, o, nullptr, scratch, st);
+            } else if (!Dispatch<T>::append_attention(h, qkv, ld_qkv, S, R, H, Hkv, dh, o, all, block_start, L, st))
                 launch_plain_attention<T>(qkv, ld_qkv, S, R, H, Hkv, dh, o, pre, L, st);
+        } else if (kv.shared) {
+            Dispatch<T>::rope_values(h, qkv, ld_qkv, S, R, block_start, H, Hkv, dh, vT, st);
+            SharedSegment seg[kMaxSegments];
+            const int n = shared_segments(c, kv, (int)li, seq_rows, S, kv.len, qkv + H * dh, ld_qkv, vT, R, seg);
+            const SharedShape sh = shared_shape(c, S, R);
+            launch_attention_shared(qkv, sh, seg, n, o, lse, scratch, st);
+            if (weighed) launch_attention_weights(qkv, sh, seg, n, lse, 1, scratch, st);
         } else if (!Dispatch<T>::block_attention(h, qkv, ld_qkv, S, R, block_start, H, Hkv, dh, o, pre, st)) {
             Dispatch<T>::rope_attention(h, qkv, ld_qkv, vT, S, R, block_start, H, Hkv, dh, o, pre, 0, st);
         }
@@ -409,6 +481,15 @@ int32_t debug_layer_impl(psd_handle *h, int li, float *hbuf, int S, int N, int L
 
 }   // namespace
 
+int64_t shared_call_bytes(const psd_model_config &cfg, int S, int L, const KvCacheArg &kv) {
+    SharedSegment seg[kMaxSegments];
+    static const char own = 0;   // (an address for the block's rows: only lengths count here)
+    const int n = shared_segments(cfg, kv, 0, nullptr, S, kv.append ? kv.len + L : kv.len, kv.append ? nullptr : &own, 0, nullptr, L, seg);
+    const SharedShape sh = shared_shape(cfg, S, L);
+    const bool weighed = !kv.append && (kv.prefix_weights || kv.cache_weights);
+    return (weighed ? align_up(sh.n_rows * 4, 256) : 0) + std::max(shared_attention_bytes(sh, seg, n), weighed ? shared_weights_bytes(sh, seg, n) : 0);
+}
+
 int32_t run_debug_layer(psd_handle *h, int layer, float *hidden, int S, int N, int L, int stop_after, void *ws, int64_t ws_bytes,
                         hipStream_t st) {
     const ForwardPlan p = plan_forward(h->cfg, S, N, L);
@@ -435,10 +516,14 @@ int32_t run_forward_cached(psd_handle *h, const int32_t *tokens, const int32_t *
         PSD_FAIL(PSD_ERR_WORKSPACE, "workspace of %lld bytes, cached forward over %d x %d rows needs %lld", (long long)ws_bytes,
                  S, R, (long long)p.total);
     if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-    if (!kv.dual && kv.len != block_start)
+    if (kv.shared && ws_bytes < p.total + shared_call_bytes(h->cfg, S, R, kv))
+        PSD_FAIL(PSD_ERR_WORKSPACE, "workspace of %lld bytes, a forward over %d x %d rows with shared keys needs %lld", (long long)ws_bytes, S, R,
+                 (long long)(p.total + shared_call_bytes(h->cfg, S, R, kv)));
+    if (kv.shared && R > L) PSD_FAIL(PSD_ERR_INVALID_ARG, "%d rows per sequence in blocks of %d", R, L);
+    if (!kv.dual && !kv.shared && kv.len != block_start)
         PSD_FAIL(PSD_ERR_SHAPE, "the cache holds %d positions, the block starts at %d", kv.len, block_start);
     if (kv.dual && (kv.len != N - L || kv.append)) PSD_FAIL(PSD_ERR_SHAPE, "a cache of the %d positions outside the block", N - L);
-    if (kv.len + (kv.dual ? 0 : R) > kv.capacity) PSD_FAIL(PSD_ERR_SHAPE, "cache of %d positions is too small", kv.capacity);
+    if (kv.len + (kv.dual || (kv.shared && !kv.append) ? 0 : R) > kv.capacity) PSD_FAIL(PSD_ERR_SHAPE, "cache of %d positions is too small", kv.capacity);
     if (kv.append && kv.seqs_per_cache != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "appending needs one sequence per cache");
     int32_t rc;
     if (h->cfg.dtype == PSD_DTYPE_BF16)

@@ -231,7 +231,15 @@ struct KvCacheArg {
     bool dual = false;         // approximate cache of a bidirectional model: the len = N - L entries are the positions
                                // OUTSIDE the block (prefix, then suffix), frozen by the whole-sequence call that
                                // entered the block; the block rows keep their positions block_start ..
+    // shared: the rows see a prefix of the whole batch, then the len positions of their sequence's cache (base may be NULL where that is
+    // 0), then their block; positions in the caches need not be those of the sequence (evicted ones are missing)
+    bool shared = false;
+    const void *prefix = nullptr;
+    int prefix_capacity = 0, prefix_len = 0;
+    float *prefix_weights = nullptr, *cache_weights = nullptr;   // [n_layers][n_kv_heads][prefix_capacity], [caches][n_layers][n_kv_heads][capacity]
 };
+// scratch behind a cached forward's own workspace for the attention of a `shared` call over S sequences of L rows
+int64_t shared_call_bytes(const psd_model_config &cfg, int S, int L, const KvCacheArg &kv);
 
 // ---------------------------------------------------------------- kernel launchers
 // elementwise.hip
@@ -432,6 +440,8 @@ int64_t shared_attention_bytes(const SharedShape &sh, const SharedSegment *seg, 
 bool shared_attention_fits(const SharedShape &sh, const SharedSegment *seg, int n);   // (its grid)
 void launch_attention_shared(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, void *out, float *lse /* or NULL */, void *ws,
                              hipStream_t st);
+// values of the L rows of every sequence of qkv [S * L, ld_qkv] (columns from v_col on) transposed, for fp32 models
+void launch_block_values(const float *qkv, int ld_qkv, int v_col, int S, int L, int width, float *vT, int ld_vt, hipStream_t st);
 int64_t shared_weights_bytes(const SharedShape &sh, const SharedSegment *seg, int n);
 void launch_attention_weights(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, const float *lse, int accumulate, void *ws,
                               hipStream_t st);

@@ -1,0 +1,298 @@
+"""Model calls over keys that a batch shares: a common prefix, the sequences' own caches, weights of the cached positions, eviction.
+
+Checked against the oracle: (1) prefix + extended caches + block rows equal its masked forward over the whole sequence, stage-1 shape
+and a verification batch, fp32 within 1e-4 and bf16 within 2e-2 (the bounds of the cached calls); (2) a free-running fp32 decode
+reproduces its decode token for token; (3) the weights are its attention probabilities, summed; (4) a bidirectional model under
+an evicted approximate cache equals its forward over the entries that stayed.  And that the model calls, eviction and decoding run
+as one program, in any order that the documentation allows."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+import psd_inputs as inp
+from oracle import psd_oracle as orc
+from tests.shared_common import kept_positions
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _bc(shape, **kw):
+    return dataclasses.replace(shape, attention="block_causal", **kw)
+
+
+FP32 = inp.cut_down(inp.WORKLOADS[4].shape, name="sh-fp32", dtype="fp32", n_layers=2, d_model=96, n_heads=6, n_kv_heads=2, d_head=16, d_ffn=160,
+                    vocab=211, seed=61)
+BF16 = {
+    "mha-dh64": inp.cut_down(inp.WORKLOADS[2].shape, n_layers=2, vocab=5000, seed=62),
+    "gqa-bias-dh128": inp.cut_down(inp.WORKLOADS[4].shape, n_layers=2, d_model=512, n_heads=4, n_kv_heads=2, d_ffn=640, vocab=3001, seed=63),
+}
+MODELS = {"fp32": (FP32, 1e-4), **{k: (v, 2e-2) for k, v in BF16.items()}}
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def _batch(shape, B, P, own, L, seed, n_committed=5, blocks_behind=1):
+    """B sequences: P common tokens, `own` of their own, a block with some tokens committed, masked blocks behind."""
+    N = P + own + (1 + blocks_behind) * L
+    common = inp.draw_prompt(shape.vocab, P, seed) if P else np.zeros(0, dtype=np.int32)
+    rng = np.random.default_rng(seed)
+    rows = []
+    for b in range(B):
+        t = np.full(N, shape.mask_id, dtype=np.int32)
+        t[:P] = common
+        if own:
+            t[P:P + own] = inp.draw_prompt(shape.vocab, own, seed + 10 + b)
+        idx = rng.choice(L, size=n_committed + b, replace=False)
+        t[P + own + idx] = rng.integers(0, shape.vocab - 1, size=n_committed + b)
+        rows.append(t)
+    return np.stack(rows), P + own
+
+
+def _check(shape, host, logits, top1, conf, t, start, L, tol, label):
+    from tests.test_gpu_forward import check_sequence
+    o_top1, o_conf, z = orc.forward_confidence(host, t, start, L, return_logits=True, block_causal=True)
+    return check_sequence((o_top1, o_conf, z, None), logits, top1, conf, t, shape.mask_id, start, L, tol, label)
+
+
+def _prefilled(psd, model, d, P, own, L, capacity):
+    """SharedKv of a batch: the first sequence's prefix for all, everything behind it block by block into the caches."""
+    B = d.shape[0]
+    kv = psd.SharedKv(cache=psd.KvCache(model, B, capacity))
+    if P:
+        kv.prefix, kv.prefix_len = psd.KvCache(model, 1, P + 16), P
+        psd.psd_kv_prefill(model, d[:1], P, L, kv.prefix)
+    for at in range(0, own, L):
+        psd.psd_kv_extend_shared(model, d, P + at, L, kv)
+        kv.length += L
+    return kv
+
+
+@pytest.mark.parametrize("name", list(MODELS))
+@pytest.mark.parametrize("L,P,own", [(16, 48, 32), (32, 96, 64), (64, 64, 0), (32, 0, 32)])
+def test_shared_calls_match_the_oracle(name, L, P, own):
+    import paper_2605_15609_amd as psd
+    shape, tol = MODELS[name]
+    shape = _bc(shape)
+    B, K = 2, 3
+    t, start = _batch(shape, B, P, own, L, 7)
+    N = t.shape[1]
+    host = inp.draw_model(shape, N)
+    model = psd.Model.from_host(host, DEV)
+    d = _dev(t)
+    kv = _prefilled(psd, model, d, P, own, L, own + L)
+    print(f"[shared model] {name} L={L} P={P} own={own}", flush=True)
+    top1, conf, logits = psd.psd_forward_confidence_shared(model, d, start, L, kv, want_logits=True)
+    logits = logits.cpu().numpy().reshape(B, L, -1)
+    for b in range(B):
+        err = _check(shape, host, logits[b], top1[b].cpu().numpy(), conf[b].cpu().numpy(), t[b], start, L, tol, f"{name} sequence {b}")[0]
+        print(f"[shared model]   sequence {b}: logits off by {err:.2e}", flush=True)
+    # a verification batch: K drafts to a cache
+    rng = np.random.default_rng(5)
+    drafts = np.repeat(t, K, axis=0)
+    for i, row in enumerate(drafts):
+        masked = np.nonzero(row[start:start + L] == shape.mask_id)[0][:2 * (i % K)]
+        row[start + masked] = rng.integers(0, shape.vocab - 1, size=len(masked))
+    top1, conf, logits = psd.psd_forward_confidence_shared(model, _dev(drafts), start, L, kv, seqs_per_cache=K, want_logits=True)
+    logits = logits.cpu().numpy().reshape(B * K, L, -1)
+    for i in (1, 2, K, 2 * K - 1):
+        _check(shape, host, logits[i], top1[i].cpu().numpy(), conf[i].cpu().numpy(), drafts[i], start, L, tol, f"{name} draft {i}")
+
+
+@pytest.mark.parametrize("graph_kind", ["chain", "lattice"])
+def test_free_running_decode_reproduces_the_oracle(graph_kind):
+    import paper_2605_15609_amd as psd
+    from tests.gpu_common import oracle_graph
+    shape = _bc(FP32, logit_scale=6.0)
+    L, P, own, B = 16, 32, 16, 3
+    t, start = _batch(shape, B, P, own, L, 21, n_committed=0)
+    t[:, start:] = shape.mask_id
+    N = t.shape[1]
+    host = inp.draw_model(shape, N)
+    model = psd.Model.from_host(host, DEV)
+    d = _dev(t)
+    kv = _prefilled(psd, model, d, P, own, L, own + 2 * L)
+    graph = psd.chain_graph(3) if graph_kind == "chain" else psd.lattice_graph(2)
+    policy = psd.Policy(0.5, 1)
+    stats = None
+    for block in range(2):
+        stats = psd.psd_decode_block_shared(model, d, start + block * L, L, policy, graph, kv, stats)
+        kv.length += L
+    out = d.cpu().numpy()
+    for b in range(B):
+        want, ostats = orc.decode(orc.model_confidence_fn(host, block_causal=True), t[b], start, L, orc.Policy(0.5, 1), oracle_graph(graph), shape.mask_id)
+        assert (out[b] == want).all(), f"sequence {b}"
+        assert stats[b].invocations == ostats.invocations and stats[b].tokens == ostats.tokens == 2 * L
+    print(f"[shared model] decode {graph_kind}: {[s.invocations for s in stats]} invocations", flush=True)
+
+
+def _record_probabilities(monkeypatch):
+    """What the oracle's attention gives every key: a list of [H, Nq, Nk] arrays, one per call."""
+    seen = []
+    plain = orc.attention
+
+    def attention(q, k, v, operands=None, visible=None):
+        group = q.shape[1] // k.shape[1]
+        p = []
+        for j in range(q.shape[1]):
+            s = q[:, j] @ k[:, j // group].T / np.sqrt(q.shape[2])
+            if visible is not None:
+                s = np.where(visible, s, -np.inf)
+            e = np.exp(s - s.max(axis=-1, keepdims=True))
+            p.append(e / e.sum(axis=-1, keepdims=True))
+        seen.append(np.stack(p))
+        return plain(q, k, v, operands, visible)
+    monkeypatch.setattr(orc, "attention", attention)
+    return seen
+
+
+def test_weights_are_the_probabilities_of_every_layer(monkeypatch):
+    import paper_2605_15609_amd as psd
+    shape = _bc(FP32)
+    L, P, own, B = 16, 48, 32, 2
+    t, start = _batch(shape, B, P, own, L, 31)
+    host = inp.draw_model(shape, t.shape[1])
+    model = psd.Model.from_host(host, DEV)
+    d = _dev(t)
+    kv = _prefilled(psd, model, d, P, own, L, own + L)
+    kv.prefix_weights, kv.cache_weights = kv.prefix.new_weights(), kv.cache.new_weights()
+    psd.psd_forward_confidence_shared(model, d, start, L, kv)
+    first = kv.cache_weights.clone()
+    psd.psd_forward_confidence_shared(model, d, start, L, kv)
+    assert torch.allclose(kv.cache_weights, 2 * first, rtol=1e-6, atol=0)      # a second call adds as much again
+    H, Hkv = shape.n_heads, shape.n_kv_heads
+    prefix = np.zeros((shape.n_layers, Hkv, P))
+    for b in range(B):
+        seen = _record_probabilities(monkeypatch)
+        orc.forward_hidden(host, t[b], None, L)
+        monkeypatch.undo()
+        for li in range(shape.n_layers):
+            w = seen[li][:, start:start + L].sum(1).reshape(Hkv, H // Hkv, -1).sum(1)      # [Hkv, positions]
+            prefix[li] += w[:, :P]
+            got = first[b, li].double().cpu().numpy()
+            # fp32 through two layers: scores off by 1e-5 (the logits are held to 1e-4), so probabilities by that factor
+            assert np.abs(got[:, :own] / w[:, P:P + own] - 1).max() < 1e-4, (b, li)
+            assert (got[:, own:] == 0).all()
+    got = kv.prefix_weights[0, :, :, :P].double().cpu().numpy() / 2
+    assert np.abs(got / prefix - 1).max() < 1e-4
+    assert (kv.prefix_weights[..., P:] == 0).all()
+
+
+@pytest.mark.parametrize("name", list(MODELS))
+def test_bidirectional_model_under_an_evicted_approximate_cache(name):
+    import paper_2605_15609_amd as psd
+    from tests.test_gpu_forward import check_sequence
+    shape, tol = MODELS[name]
+    L, P, G, keep, first, last = 32, 70, 64, 41, 4, 8
+    N, start = P + G, P
+    host = inp.draw_model(shape, N)
+    model = psd.Model.from_host(host, DEV)
+    t0 = np.full(N, shape.mask_id, dtype=np.int32)
+    t0[:P] = inp.draw_prompt(shape.vocab, P, 41)
+    t = t0.copy()
+    t[start:start + 9] = inp.draw_prompt(shape.vocab, 9, 42)
+    cache = psd.KvCache(model, 1, N - L)
+    psd.psd_forward_confidence_approx(model, _dev(t0[None]), start, L, cache, refresh=True)
+    kv = psd.SharedKv(cache=cache, length=N - L, cache_weights=cache.new_weights())
+    d = _dev(t[None])
+    # whole: the approximate cache's own call
+    top1, conf, logits = psd.psd_forward_confidence_shared(model, d, start, L, kv, want_logits=True)
+    _, _, same = psd.psd_forward_confidence_approx(model, d, start, L, cache, refresh=False, want_logits=True)
+    assert float((logits - same).abs().max()) < tol
+    # evicted: the oracle's forward over the entries that stayed, head by head
+    small = psd.KvCache(model, 1, 48)
+    weights = small.new_weights()
+    kept = psd.psd_kv_evict(cache.segment(N - L, kv.cache_weights), small.segment(48, weights), keep, first, last)
+    w = kv.cache_weights[0].cpu().numpy()
+    kept = kept.cpu().numpy().reshape(shape.n_layers, shape.n_kv_heads, keep)
+    for li in range(shape.n_layers):
+        for g in range(shape.n_kv_heads):
+            assert kept[li, g].tolist() == kept_positions(w[li, g], N - L, keep, first, last)
+            assert np.array_equal(weights[0, li, g, :keep].cpu().numpy(), w[li, g, kept[li, g]])
+    ocache = orc.ApproximateCache(host)
+    ocache(t0, start, L)
+    frozen = [(np.stack([k[kept[li, g], g] for g in range(shape.n_kv_heads)], 1), np.stack([v[kept[li, g], g] for g in range(shape.n_kv_heads)], 1))
+              for li, (k, v) in enumerate(ocache.frozen)]
+    y = orc.forward_hidden_frozen(host, t, start, L, frozen)
+    z = shape.logit_scale * (y @ np.asarray(host.lm_head, dtype=np.float64).T)
+    x_hat, c = orc.top1_confidence(z, shape.mask_id)
+    masked = t[start:start + L] == shape.mask_id
+    ref = (np.where(masked, x_hat, t[start:start + L]).astype(np.int32), np.where(masked, c, -1.0).astype(np.float32))
+    kv2 = psd.SharedKv(cache=small, length=keep)
+    top1, conf, logits = psd.psd_forward_confidence_shared(model, d, start, L, kv2, want_logits=True)
+    err = check_sequence((*ref, z, None), logits.cpu().numpy(), top1[0].cpu().numpy(), conf[0].cpu().numpy(), t, shape.mask_id, start, L, tol,
+                         f"{name} evicted")[0]
+    print(f"[shared model] {name} evicted {N - L} -> {keep}: logits off by {err:.2e}", flush=True)
+
+
+@pytest.mark.parametrize("name", list(BF16))
+def test_a_served_batch_under_a_budget(name):
+    """A common prompt, four requests behind it, decoded block by block; after every block the requests' caches are cut to a budget by
+    what their positions drew.  Equal to the same requests decoded one at a time on the fp32-exact parts (positions, lengths),
+    every token resolved, the prefix untouched."""
+    import paper_2605_15609_amd as psd
+    shape = _bc(BF16[name])
+    L, P, own, B, blocks, keep = 32, 96, 32, 4, 3, 40
+    t, start = _batch(shape, B, P, own, L, 51, n_committed=0, blocks_behind=blocks - 1)
+    model = psd.Model.from_host(inp.draw_model(shape, t.shape[1]), DEV)
+    d = _dev(t)
+    kv = _prefilled(psd, model, d, P, own, L, keep + L)
+    before = kv.prefix.mem.clone()
+    other = psd.KvCache(model, B, keep + L)
+    kv.cache_weights = kv.cache.new_weights()
+    other_weights = other.new_weights()
+    for block in range(blocks):
+        psd.psd_decode_block_shared(model, d, start + block * L, L, psd.Policy(0.9, 4), psd.chain_graph(3), kv)
+        kv.length += L
+        assert (kv.cache_weights[..., :kv.length - L] > 0).all() and (kv.cache_weights[..., kv.length:] == 0).all()
+        if kv.length > keep:
+            other_weights.zero_()
+            kept = psd.psd_kv_evict(kv.cache.segment(kv.length, kv.cache_weights), other.segment(keep + L, other_weights), keep, 4, L)
+            kept = kept.cpu().numpy()
+            assert (np.diff(kept, axis=-1) > 0).all() and (kept[..., :4] == np.arange(4)).all() and (kept[..., -L:] == np.arange(kv.length - L, kv.length)).all()
+            kv.cache, other = other, kv.cache
+            kv.cache_weights, other_weights = other_weights, kv.cache_weights
+            kv.length = keep
+    assert not (d == shape.mask_id).any()
+    assert torch.equal(kv.prefix.mem, before)
+
+
+def test_shared_calls_refuse():
+    import paper_2605_15609_amd as psd
+    shape = _bc(BF16["mha-dh64"])
+    L = 32
+    model = psd.Model.from_host(inp.draw_model(shape, 256), DEV)
+    bid = psd.Model.from_host(inp.draw_model(BF16["mha-dh64"], 256), DEV)
+    d = torch.zeros((2, 256), dtype=torch.int32, device=DEV)
+    cache, prefix = psd.KvCache(model, 2, 64), psd.KvCache(model, 1, 64)
+    ok = dict(prefix=prefix, prefix_len=64, cache=cache, length=32)
+
+    def kv(**kw):
+        return psd.SharedKv(**dict(ok, **kw))
+    psd.psd_forward_confidence_shared(model, d, 96, L, kv())
+    psd.psd_forward_confidence_shared(model, d, 96, L, kv(length=64))
+    for bad in (kv(prefix_len=65), kv(prefix_len=-1), kv(length=65), kv(length=-1), kv(prefix=None), kv(cache=None), kv(cache=psd.KvCache(model, 1, 64)),
+                kv(cache_weights=prefix.new_weights()), kv(prefix_weights=prefix.new_weights().double()), kv(prefix=psd.KvCache(bid, 1, 64))):
+        with pytest.raises(psd.PsdError):
+            psd.psd_forward_confidence_shared(model, d, 96, L, bad)
+    for start, length in ((96, 24), (240, 32), (-1, 32), (96, 0)):
+        with pytest.raises(psd.PsdError):
+            psd.psd_forward_confidence_shared(model, d, start, length, kv())
+    with pytest.raises(psd.PsdError):
+        psd.psd_forward_confidence_shared(model, d, 96, L, kv(), seqs_per_cache=3)
+    with pytest.raises(psd.PsdError):
+        psd.psd_kv_extend_shared(model, d, 96, L, kv(length=33))
+    with pytest.raises(psd.PsdError):
+        psd.psd_decode_block_shared(model, d, 96, L, psd.Policy(), psd.chain_graph(2), kv(length=33))
+    with pytest.raises(psd.PsdError):
+        psd.psd_kv_extend_shared(bid, d, 96, L, psd.SharedKv(cache=psd.KvCache(bid, 2, 64), length=0))
+    small = torch.empty(4096, dtype=torch.uint8, device=DEV)
+    import ctypes as C
+    c = kv().c(model, 2)
+    top1, conf = torch.empty((2, L), dtype=torch.int32, device=DEV), torch.empty((2, L), device=DEV)
+    assert model.lib.psd_forward_confidence_shared(model.handle, d.data_ptr(), 2, 256, 96, L, C.byref(c), top1.data_ptr(), conf.data_ptr(), None,
+                                                   small.data_ptr(), 4096, None) == -3
