@@ -18,10 +18,13 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void lds_void;
 
-constexpr int TR = 32;    // rows per tile
+constexpr int TR = 32;    // rows of a tile where there are few
+constexpr int MT = 128;   // rows of a tile where there are many
 constexpr int BK = 32;    // keys that a wavefront takes at a time
 constexpr int NW = 4;     // wavefronts of a workgroup, which deal a tile's keys among themselves
+constexpr float SLACK = 8.f;   // (see many_rows)
 constexpr float LOG2E = 1.4426950408889634f;
 
 // A row of 8 slots of T, as a lane of a 32x32 product holds it: bf16 in one 16-byte load, fp32 in two.
@@ -104,26 +107,56 @@ struct RowOf {
     }
 };
 
-// One workgroup: a tile of TR rows of a unit against a part of the unit's keys.  The wavefronts deal the keys, BK at a time, operands
+// Where a row's result over the keys of one workgroup goes: a part that the join reads, or, where it is the only one, the output
+template <typename T, int DH>
+struct PartOut {
+    const SharedLaunch &ln;
+    const bool direct;
+    int64_t at;      // of the row in [parts][n_rows], or among the rows
+    float *o;
+    T *out;
+    __device__ PartOut(const SharedShape &sh, const SharedLaunch &l, int part, const RowOf &row) : ln(l), direct(l.parts == 0) {
+        const int64_t r = row.token * sh.n_heads + row.head;
+        at = direct ? r : part * sh.n_rows + r;
+        o = l.o + at * DH;
+        out = (T *)l.out + row.token * sh.ld_out + row.head * DH;
+    }
+    // m, l of the row, m_s = m in units of log2 (0 for -inf)
+    __device__ void sums(float m, float l, float m_s) const {
+        if (!direct) ln.ml[at] = make_float2(m, l);
+        else if (ln.lse) ln.lse[at] = log_sum(m_s, l);
+    }
+    __device__ static float log_sum(float m_s, float l) { return l == 0.f ? -INFINITY : m_s / LOG2E + logf(l); }
+    // what values() multiplies by; 0 where there were no keys
+    __device__ float factor(float l) const { return l == 0.f ? 0.f : direct ? 1.0f / l : 1.0f; }
+    __device__ void values(int c, const float *v, float f) const {
+        if (!direct) {
+            *reinterpret_cast<float4 *>(o + c) = make_float4(v[0], v[1], v[2], v[3]);
+        } else if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint2 *>(out + c) = make_uint2(pack_bf16x2(v[0] * f, v[1] * f), pack_bf16x2(v[2] * f, v[3] * f));
+        } else {
+            *reinterpret_cast<float4 *>(out + c) = make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+        }
+    }
+};
+
+// The lane's partner in the other half of the wavefront
+__device__ __forceinline__ float other_half(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// Few rows: a tile of TR rows of a unit against a part of the unit's keys.  The wavefronts deal the keys, BK at a time, operands
 // straight from memory, and merge in LDS in wavefront order.
 template <typename T, int DH>
-__global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *__restrict__ q, SharedShape sh, SharedLaunch ln, float sl2) {
+__device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedShape &sh, const SharedLaunch &ln, const SharedJob &jb, int u, int kvh,
+                                         int tile, int split, float sl2, float *part /* [wavefront][max, sum, NF values][64 lanes] */) {
     constexpr int KS = DH / 16, CT = (DH + 31) / 32, NF = CT * 16;   // contraction steps of the scores, channel subtiles, output values per lane
-    extern __shared__ __align__(16) float part[];                   // [wavefront][max, sum, NF values][64 lanes]
-    int j = 0;
-    while (j + 1 < ln.n_jobs && (int)blockIdx.x >= ln.job[j + 1].block0) ++j;
-    const SharedJob &jb = ln.job[j];
-    const SharedSegment &seg = ln.seg[j];
-    // (unit, KV head, part) groups are dealt to the XCDs, all tiles of a group to one: they read the same keys
-    const int local = blockIdx.x - jb.block0, slot = local >> 3;
-    const int grp = slot / jb.tiles * 8 + (local & 7), tile = slot % jb.tiles;
-    if (grp >= jb.units * sh.n_kv_heads * jb.splits) return;
-    const int split = grp % jb.splits, kvh = grp / jb.splits % sh.n_kv_heads, u = grp / jb.splits / sh.n_kv_heads;
+    const SharedSegment &seg = ln.seg[jb.seg];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
     const Keys<T> keys = keys_of<T>(seg, u, kvh, DH);
     const int n_steps = (keys.len + BK - 1) / BK;
     const int first = (int)((int64_t)n_steps * split / jb.splits), last = (int)((int64_t)n_steps * (split + 1) / jb.splits);
-
     const int rows = seg.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads), r = tile * TR + lrow;
     const RowOf row(sh, (int64_t)u * seg.seqs_per_unit, kvh, min(r, rows - 1));   // (rows past the last repeat it and store nothing)
     Frag<T> qf[KS];
@@ -157,7 +190,7 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
         float mx = x[0];
 #pragma unroll
         for (int v = 1; v < 16; ++v) mx = fmaxf(mx, x[v]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        mx = fmaxf(mx, other_half(mx));
         const float m_new = fmaxf(m_run, mx);
         const float m_s = m_new == -INFINITY ? 0.f : m_new * sl2;   // (scores of -inf alone: infinite keys)
         const float alpha = __builtin_amdgcn_exp2f(__builtin_fmaf(m_run, sl2, -m_s));
@@ -212,10 +245,10 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
         l_all += part[(w * (2 + NF) + 1) * 64 + lane] * scale[w];
     }
     if (r >= rows) return;
-    const int64_t at = (int64_t)(jb.part0 + split) * sh.n_rows + row.token * sh.n_heads + row.head;
-    if (wave == 0 && half == 0) ln.ml[at] = make_float2(l_all > 0.f || l_all != l_all ? m_all : -INFINITY, l_all);
-    if (l_all == 0.f) return;   // (no keys: the join reads no values)
-    float *op = ln.o + at * DH;
+    const PartOut<T, DH> to(sh, ln, jb.part0 + split, row);
+    if (wave == 0 && half == 0) to.sums(m_all, l_all, m_s);
+    const float inv = to.factor(l_all);
+    if (inv == 0.f && !to.direct) return;   // (no keys: the join reads no values)
 #pragma unroll
     for (int g = 0; g < NF / 4; ++g) {   // 4 values of a row: subtile g / 4, channels 8 (g % 4) + 4 half ..
         if (g % NW != wave) continue;
@@ -226,13 +259,246 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
         for (int w = 0; w < NW; ++w)
 #pragma unroll
             for (int v = 0; v < 4; ++v) o[v] += part[(w * (2 + NF) + 2 + g * 4 + v) * 64 + lane] * scale[w];
-        *reinterpret_cast<float4 *>(op + c) = make_float4(o[0], o[1], o[2], o[3]);
+        to.values(c, o, inv);
     }
+}
+
+// Many rows (bf16): a tile of 128 rows, 32 to a wavefront, walks tiles of 64 keys that pass through LDS, fetched a tile ahead by
+// loads that go to LDS directly (chunks of 16 bytes swizzled on the way, as in attention_mfma.hip).  The rows of the tile share the unit
+// of the job's first segment; of the others the tile walks every unit that one of its rows sees, and hides it from the rows that do not.
+struct Walk {   // the key tiles of a row tile, in order
+    int seg, u, u_last, k0, len;      // segment, unit, last unit that the tile's rows see, first key, keys of the unit
+};
+
+template <int DH>
+__device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const SharedShape &sh, const SharedLaunch &ln, const SharedJob &jb, int u0,
+                                          int kvh, int tile, int split, float sl2, unsigned char *lds) {
+    constexpr int KT = 64, KROW = DH * 2, VROW = KT * 2, K_BYTES = KT * KROW, STAGE = K_BYTES + DH * VROW, CT = DH / 32, KS = DH / 16;
+    constexpr int KRPI = 1024 / KROW, KLPR = 64 / KRPI;      // key rows of a load instruction, lanes to a row
+    constexpr int KG = KT / KRPI / NW, VG = DH / 8 / NW;     // load instructions per wavefront and tile
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
+    const int group = sh.n_heads / sh.n_kv_heads, per_seq = sh.L * group;
+    const SharedSegment &top = ln.seg[jb.seg];
+    const int rows = top.seqs_per_unit * per_seq, r = tile * MT + wave * 32 + lrow;
+    const int s0 = u0 * top.seqs_per_unit;
+    const int s_first = s0 + tile * MT / per_seq, s_last = s0 + (min(tile * MT + MT, rows) - 1) / per_seq;
+    const RowOf row(sh, s0, kvh, min(r, rows - 1));   // (rows past the last repeat it and store nothing)
+    const int my_seq = s0 + min(r, rows - 1) / per_seq;
+    const bool any_rows = tile * MT + wave * 32 < rows;
+
+    auto unit_len = [&](const SharedSegment &s, int u) {
+        if (!s.lens) return s.len;
+        const int64_t cache = s.rows ? s.rows[(int64_t)u * s.seqs_per_unit] / s.rows_div : u;
+        return __builtin_amdgcn_readfirstlane(min(max(s.lens[cache], 0), s.len));
+    };
+    // this workgroup's share of the key tiles
+    int n_tiles = 0;
+    for (int i = jb.seg; i < jb.seg + jb.segs; ++i)
+        for (int u = s_first / ln.seg[i].seqs_per_unit; u <= s_last / ln.seg[i].seqs_per_unit; ++u) n_tiles += (unit_len(ln.seg[i], u) + KT - 1) / KT;
+    const int first = (int)((int64_t)n_tiles * split / jb.splits), last = (int)((int64_t)n_tiles * (split + 1) / jb.splits);
+    Walk at;
+    auto enter = [&](int seg) {   // the first unit of a segment
+        at.seg = seg;
+        if (seg >= jb.seg + jb.segs) return;
+        at.u = s_first / ln.seg[seg].seqs_per_unit;
+        at.u_last = s_last / ln.seg[seg].seqs_per_unit;
+        at.k0 = 0;
+        at.len = unit_len(ln.seg[seg], at.u);
+    };
+    auto settle = [&]() {         // on to the next unit with keys left
+        while (at.seg < jb.seg + jb.segs && at.k0 >= at.len) {
+            if (at.u < at.u_last) {
+                ++at.u;
+                at.k0 = 0;
+                at.len = unit_len(ln.seg[at.seg], at.u);
+            } else {
+                enter(at.seg + 1);
+            }
+        }
+    };
+    enter(jb.seg);
+    settle();
+    for (int skip = first; skip > 0;) {
+        const int here = min(skip, (at.len - at.k0 + KT - 1) / KT);
+        at.k0 += here * KT;
+        skip -= here;
+        settle();
+    }
+
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+        qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(q + row.token * sh.ld_q + row.head * DH + ks * 16 + half * 8));
+
+    auto kkey = [](int x) { return DH == 128 ? (x & 15) : ((x >> 1) & 7); };   // swizzle keys, as in attention_mfma.hip
+    auto fetch = [&](int stage) {   // the tile `at` into a stage; what lies behind its keys is rejected by the descriptors or never used
+        const SharedSegment &s = ln.seg[at.seg];
+        const Keys<bf16_t> k = keys_of<bf16_t>(s, at.u, kvh, DH);
+        const int left = min(at.len - at.k0, KT), ld_k = s.ld_k, ld_vt = s.ld_vt;
+        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(k.k) + (int64_t)at.k0 * ld_k, 0,
+                                                                            ((left - 1) * ld_k + DH) * 2, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(k.vt) + at.k0, 0,
+                                                                            ((DH - 1) * ld_vt + (left + 15) / 16 * 16) * 2, 0x00020000);
+        unsigned char *sk = lds + stage * STAGE + wave * 1024, *sv = sk + K_BYTES;
+#pragma unroll
+        for (int j = 0; j < KG; ++j) {
+            const int x = (j * NW + wave) * KRPI + lane / KLPR;
+            const int voff = (lane / KLPR) * ld_k * 2 + (((lane % KLPR) ^ kkey(x)) << 4);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void *)(sk + j * (NW * 1024)), 16, voff, (j * NW + wave) * KRPI * ld_k * 2, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < VG; ++j) {
+            const int x = (j * NW + wave) * 8 + (lane >> 3);
+            const int voff = (lane >> 3) * ld_vt * 2 + (((lane & 7) ^ ((x >> 1) & 7)) << 4);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void *)(sv + j * (NW * 1024)), 16, voff, (j * NW + wave) * 8 * ld_vt * 2, 0, 0);
+        }
+    };
+
+    floatx16 acc_o[CT];
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc_o[i][v] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    if (first < last) fetch(0);
+    for (int t = first; t < last; ++t) {
+        const int stage = (t - first) & 1;
+        const int left = at.len - at.k0, per = ln.seg[at.seg].seqs_per_unit;
+        const bool vis = my_seq / per == at.u;
+        // this tile has landed for every wavefront, and every wavefront is done with the stage that the next one goes to
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        at.k0 += KT;
+        settle();
+        if (t + 1 < last) fetch(stage ^ 1);
+        const uint64_t seen = __ballot(vis);
+        if (!any_rows || seen == 0) continue;
+        const unsigned char *sk = lds + stage * STAGE, *sv = sk + K_BYTES;
+        floatx16 x[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[kt][v] = 0.f;
+            const int kr = kt * 32 + lrow;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    *reinterpret_cast<const bf16x8 *>(sk + kr * KROW + (((ks * 2 + half) ^ kkey(kr)) << 4)), qf[ks], x[kt], 0, 0, 0);
+        }
+        if (left < KT || seen != ~0ull) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (!vis || kt * 32 + 8 * (v >> 2) + 4 * half + (v & 3) >= left) x[kt][v] = -INFINITY;
+        }
+        float mx = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+        for (int v = 1; v < 16; ++v) mx = fmaxf(fmaxf(mx, x[0][v]), x[1][v]);
+        mx = fmaxf(mx, other_half(mx));
+        // The sums are kept relative to a running reference, raised to the maximum only where that has grown by more than 2^SLACK in a
+        // probability: bf16 and fp32 are as exact there, and the outputs are not touched in most tiles.
+        if (__any(mx * sl2 > m_run * sl2 + SLACK)) {
+            const float m_new = fmaxf(m_run, mx);
+            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * sl2);
+            l_run *= alpha;
+            m_run = m_new;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc_o[ct][v] *= alpha;
+        }
+        const float m_s = m_run == -INFINITY ? 0.f : m_run * sl2;
+        bf16x8 pf[4];
+        float psum = 0.f;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            float p[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][v], sl2, -m_s));
+                psum += p[v];
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                pf[kt * 2 + e] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(p[8 * e + 0], p[8 * e + 1]), pack_bf16x2(p[8 * e + 2], p[8 * e + 3]),
+                                                                       pack_bf16x2(p[8 * e + 4], p[8 * e + 5]), pack_bf16x2(p[8 * e + 6], p[8 * e + 7])));
+        }
+        l_run += psum;
+        auto values = [&](int kg, int ct) {
+            const int c = ct * 32 + lrow;
+            return *reinterpret_cast<const uint4 *>(sv + c * VROW + (((kg * 2 + half) ^ ((c >> 1) & 7)) << 4));
+        };
+        if (left >= KT && seen == ~0ull) {
+#pragma unroll
+            for (int kg = 0; kg < 4; ++kg)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    acc_o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(kg, ct)), pf[kg], acc_o[ct], 0, 0, 0);
+        } else {
+            // the last tile of a unit, or one that some rows do not see: 0 x NaN is NaN, so slots behind the last key are cleared and
+            // what a row does not see stays out of its sums
+#pragma unroll
+            for (int kg = 0; kg < 4; ++kg) {
+                if (kg * 16 >= left) break;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    Frag<bf16_t> vf;
+                    vf.v = values(kg, ct);
+                    vf.keep(left - kg * 16 - 4 * half);
+                    const floatx16 sums = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf.v), pf[kg], acc_o[ct], 0, 0, 0);
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc_o[ct][v] = vis ? sums[v] : acc_o[ct][v];
+                }
+            }
+        }
+    }
+    l_run += other_half(l_run);   // the halves of a row hold disjoint keys
+    if (r >= rows) return;
+    const PartOut<bf16_t, DH> to(sh, ln, jb.part0 + split, row);
+    if (half == 0) to.sums(m_run, l_run, m_run == -INFINITY ? 0.f : m_run * sl2);
+    const float f = to.factor(l_run);
+    if (f == 0.f && !to.direct) return;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float o[4] = {acc_o[ct][4 * g], acc_o[ct][4 * g + 1], acc_o[ct][4 * g + 2], acc_o[ct][4 * g + 3]};
+            to.values(ct * 32 + 8 * g + 4 * half, o, f);
+        }
+}
+
+template <typename T, int DH>
+constexpr int attention_lds() {
+    constexpr int merge = NW * (2 + (DH + 31) / 32 * 16) * 64 * 4, ring = sizeof(T) == 2 ? 2 * (64 * DH * 2 + DH * 128) : 0;
+    return merge > ring ? merge : ring;
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *__restrict__ q, SharedShape sh, SharedLaunch ln, float sl2) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    int j = 0;
+    while (j + 1 < ln.n_jobs && (int)blockIdx.x >= ln.job[j + 1].block0) ++j;
+    const SharedJob &jb = ln.job[j];
+    // (unit, KV head, part) groups are dealt to the XCDs, all tiles of a group to one: they read the same keys
+    const int local = blockIdx.x - jb.block0, slot = local >> 3;
+    const int grp = slot / jb.tiles * 8 + (local & 7), tile = slot % jb.tiles;
+    if (grp >= jb.units * sh.n_kv_heads * jb.splits) return;
+    const int split = grp % jb.splits, kvh = grp / jb.splits % sh.n_kv_heads, u = grp / jb.splits / sh.n_kv_heads;
+    if constexpr (sizeof(T) == 2) {
+        if (jb.tiled) {
+            many_rows<DH>(q, sh, ln, jb, u, kvh, tile, split, sl2, lds);
+            return;
+        }
+    }
+    few_rows<T, DH>(q, sh, ln, jb, u, kvh, tile, split, sl2, reinterpret_cast<float *>(lds));
 }
 
 // The parts of a row joined, in their order: a thread takes 4 channels.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, SharedLaunch ln, T *__restrict__ out, float *__restrict__ lse, float sl2) {
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, SharedLaunch ln, float sl2) {
     constexpr int TPR = DH / 4;   // threads per row
     const int64_t r = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
     if (r >= sh.n_rows) return;
@@ -250,10 +516,10 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, Shared
         o[0] += w * v.x, o[1] += w * v.y, o[2] += w * v.z, o[3] += w * v.w;
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;   // (a row without keys: zeros)
-    T *op = out + r / sh.n_heads * sh.ld_out + r % sh.n_heads * DH + c;
+    T *op = (T *)ln.out + r / sh.n_heads * sh.ld_out + r % sh.n_heads * DH + c;
 #pragma unroll
     for (int v = 0; v < 4; ++v) op[v] = from_float<T>(o[v] * inv);
-    if (lse && c == 0) lse[r] = l == 0.f ? -INFINITY : m_s / LOG2E + logf(l);
+    if (ln.lse && c == 0) ln.lse[r] = PartOut<T, DH>::log_sum(m_s, l);
 }
 
 // w[j] (+)= sum over the rows of the unit of exp(x_j - lse).  A wavefront keeps 32 keys in registers and walks all rows; a lane adds
@@ -265,7 +531,7 @@ __global__ __launch_bounds__(NW * 64) void shared_weights_kernel(const T *__rest
     int j = 0;
     while (j + 1 < ln.n_jobs && (int)blockIdx.x >= ln.job[j + 1].block0) ++j;
     const SharedJob &jb = ln.job[j];
-    const SharedSegment &seg = ln.seg[j];
+    const SharedSegment &seg = ln.seg[jb.seg];
     const int local = blockIdx.x - jb.block0;
     const int u = local / (jb.splits * sh.n_kv_heads), kvh = local / jb.splits % sh.n_kv_heads, part = local % jb.splits;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
@@ -315,15 +581,16 @@ __global__ __launch_bounds__(256) void block_values_kernel(const float *__restri
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 template <typename T, int DH>
-void run_attention(const T *q, const SharedShape &sh, const SharedLaunch &ln, T *out, float *lse, hipStream_t st) {
-    constexpr int smem = NW * (2 + (DH + 31) / 32 * 16) * 64 * 4;
+void run_attention(const T *q, const SharedShape &sh, const SharedLaunch &ln, hipStream_t st) {
+    constexpr int smem = attention_lds<T, DH>();
     const float sl2 = LOG2E / sqrtf((float)DH);
     auto kern = shared_attention_kernel<T, DH>;
     static std::atomic<uint64_t> lds_raised{0};   // one per instantiation
     ensure_dynamic_lds(reinterpret_cast<const void *>(kern), smem, lds_raised);
     if (ln.blocks > 0) hipLaunchKernelGGL(kern, dim3((unsigned)ln.blocks), dim3(NW * 64), smem, st, q, sh, ln, sl2);
+    if (ln.blocks > 0 && ln.parts == 0) return;
     constexpr int rows = 256 / (DH / 4);
-    hipLaunchKernelGGL((shared_join_kernel<T, DH>), dim3((unsigned)((sh.n_rows + rows - 1) / rows)), dim3(256), 0, st, sh, ln, out, lse, sl2);
+    hipLaunchKernelGGL((shared_join_kernel<T, DH>), dim3((unsigned)((sh.n_rows + rows - 1) / rows)), dim3(256), 0, st, sh, ln, sl2);
 }
 
 template <typename T, int DH>
@@ -333,25 +600,90 @@ void run_weights(const T *q, const float *lse, const SharedShape &sh, const Shar
                            LOG2E / sqrtf((float)DH));
 }
 
-// the work of one launch: a job per segment, its workgroups behind those of the one before
-SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *seg, int n) {
+// The work of one launch.  Segments with keys, in order, are cut into jobs: those that a job takes together need no parts, but its
+// tiles walk the keys of every finer unit that they touch.
+struct JobCost {
+    double steps;     // (tile of rows, 64 keys) pairs, or what costs as much
+    int keys;         // of one tile of rows, in steps
+};
+int rows_per_unit(const SharedShape &sh, const SharedSegment &s) { return s.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads); }
+
+// segments [a, b] as tiles of MT rows; steps < 0: not possible
+JobCost tiled_cost(const SharedShape &sh, const SharedSegment *seg, int a, int b) {
+    const int64_t rows = rows_per_unit(sh, seg[a]);
+    int64_t keys = 0;
+    for (int i = a; i <= b; ++i) {
+        if (sh.dtype != PSD_DTYPE_BF16 || seg[i].ld_k >= 1 << 23 || seg[i].ld_vt >= 1 << 22) return {-1.0, 0};   // (32-bit offsets within a tile)
+        const int64_t fine = rows_per_unit(sh, seg[i]);
+        const int64_t touched = i == a ? 1 : std::min<int64_t>((std::min<int64_t>(rows, MT) + fine - 1) / fine + (MT % fine && fine % MT ? 1 : 0), rows / fine);
+        if (touched > 8) return {-1.0, 0};
+        keys += touched * ((seg[i].len + 63) / 64);
+    }
+    if (keys > 1 << 30) return {-1.0, 0};
+    return {(double)(sh.S / seg[a].seqs_per_unit) * sh.n_kv_heads * ((rows + MT - 1) / MT) * (double)keys, (int)keys};
+}
+JobCost few_cost(const SharedShape &sh, const SharedSegment &s) {
+    const int64_t tiles = ((int64_t)rows_per_unit(sh, s) + TR - 1) / TR, keys = (s.len + NW * BK - 1) / (NW * BK);
+    return {(double)(sh.S / s.seqs_per_unit) * sh.n_kv_heads * tiles * (double)keys, (int)keys};
+}
+
+SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, int n_given) {
     SharedLaunch ln;
-    int64_t blocks = 0;
-    for (int i = 0; i < n; ++i) {
-        if (seg[i].len == 0) continue;
+    for (int i = 0; i < n_given; ++i)
+        if (given[i].len > 0) ln.seg[ln.n_segs++] = given[i];
+    const int n = ln.n_segs;
+    if (n == 0) return ln;
+    // every way to cut the segments into runs (bit i of cut: a job ends with segment i); a part costs its way through memory: row bytes
+    // written and read, in steps of 4.7 ns
+    const double part_cost = (double)sh.n_rows * sh.d_head * 8 / 5e12 / 4.7e-9;
+    double best = -1.0;
+    int best_cut = 0;
+    for (int cut = 0; cut < 1 << (n - 1); ++cut) {
+        double cost = 0.0;
+        int jobs = 0;
+        bool possible = true;
+        for (int a = 0, b = 0; a < n && possible; a = b + 1, ++jobs) {
+            b = a;
+            while (b < n - 1 && !(cut >> b & 1)) ++b;
+            const JobCost t = tiled_cost(sh, ln.seg, a, b);
+            const bool few = a == b && (t.steps < 0 || rows_per_unit(sh, ln.seg[a]) <= TR);
+            if (!few && t.steps < 0) possible = false;
+            cost += few ? few_cost(sh, ln.seg[a]).steps : t.steps;
+        }
+        cost += jobs > 1 ? jobs * part_cost : 0.0;
+        if (possible && (best < 0 || cost < best)) best = cost, best_cut = cut;
+    }
+    double total = 0.0;
+    int64_t row_tiles = 0;
+    int keys[kMaxSegments];
+    for (int a = 0, b = 0; a < n; a = b + 1) {
+        b = a;
+        while (b < n - 1 && !(best_cut >> b & 1)) ++b;
         SharedJob &jb = ln.job[ln.n_jobs];
-        ln.seg[ln.n_jobs++] = seg[i];
-        const int rows = seg[i].seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads);
-        jb.units = sh.S / seg[i].seqs_per_unit;
-        jb.tiles = (rows + TR - 1) / TR;
-        jb.block0 = (int)blocks;
+        const JobCost t = tiled_cost(sh, ln.seg, a, b);
+        jb.seg = a;
+        jb.segs = b - a + 1;
+        jb.tiled = !(a == b && (t.steps < 0 || rows_per_unit(sh, ln.seg[a]) <= TR));
+        jb.units = sh.S / ln.seg[a].seqs_per_unit;
+        const int rows = rows_per_unit(sh, ln.seg[a]), per = jb.tiled ? MT : TR;
+        jb.tiles = (rows + per - 1) / per;
+        const JobCost c = jb.tiled ? t : few_cost(sh, ln.seg[a]);
+        keys[ln.n_jobs++] = c.keys;
+        total += c.steps;
+        row_tiles += (int64_t)jb.units * jb.tiles * sh.n_kv_heads;
+    }
+    // two workgroups to a CU, each with as much to do
+    const int share = std::max(2, (int)std::min(total / 512.0 + 0.999, 1e9));
+    int64_t blocks = 0;
+    for (int j = 0; j < ln.n_jobs; ++j) {
+        SharedJob &jb = ln.job[j];
+        jb.splits = std::max(1, (keys[j] + share - 1) / share);
+        jb.block0 = (int)blocks;   // (grids of 2^31 workgroups and more are refused)
         jb.part0 = ln.parts;
-        const int64_t base = (int64_t)jb.units * sh.n_kv_heads * jb.tiles;
-        const int most = (seg[i].len + NW * BK - 1) / (NW * BK);   // every wavefront has a step
-        jb.splits = (int)std::min<int64_t>(most, std::max<int64_t>(1, 1024 / base));
         ln.parts += jb.splits;
         blocks += align_up((int64_t)jb.units * sh.n_kv_heads * jb.splits, 8) * jb.tiles;
     }
+    if (ln.parts == 1) ln.parts = 0;
     ln.blocks = blocks;
     return ln;
 }
@@ -397,7 +729,9 @@ void launch_attention_shared(const void *q, const SharedShape &sh, const SharedS
     SharedLaunch ln = plan_attention(sh, seg, n);
     ln.o = (float *)ws;
     ln.ml = (float2 *)((char *)ws + align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256));
-    PSD_SHARED_DISPATCH((run_attention<T, DH>((const T *)q, sh, ln, (T *)out, lse, st)))
+    ln.out = out;
+    ln.lse = lse;
+    PSD_SHARED_DISPATCH((run_attention<T, DH>((const T *)q, sh, ln, st)))
 }
 
 void launch_block_values(const float *qkv, int ld_qkv, int v_col, int S, int L, int width, float *vT, int ld_vt, hipStream_t st) {
@@ -413,6 +747,7 @@ void launch_attention_weights(const void *q, const SharedShape &sh, const Shared
     for (int i = 0; i < n; ++i) {
         if (!seg[i].weights || seg[i].len == 0) continue;
         SharedJob &jb = ln.job[ln.n_jobs];
+        jb.seg = ln.n_jobs;
         ln.seg[ln.n_jobs++] = seg[i];
         jb.units = sh.S / seg[i].seqs_per_unit;
         jb.splits = (seg[i].len + NW * BK - 1) / (NW * BK);

@@ -422,17 +422,20 @@ struct SharedShape {
     int64_t ld_q, ld_out, n_rows;        // n_rows = S * L * n_heads
 };
 constexpr int kMaxSegments = PSD_MAX_SEGMENTS;
-// what one launch does: jobs behind one another in the grid, each with the segment of its number
+// what one launch does: jobs behind one another in the grid.  A job's workgroups take a tile of rows of a unit of its first segment
+// against the keys of `segs` segments from `seg` on, or a part of them
 struct SharedJob {
-    int units, tiles, splits, block0, part0;
+    int seg, segs, tiled, units, tiles, splits, block0, part0;
 };
 struct SharedLaunch {
-    int n_jobs = 0, parts = 0;
+    int n_jobs = 0, n_segs = 0, parts = 0;   // parts = 0: every row's one part goes straight to the output
     int64_t blocks = 0;
     SharedJob job[kMaxSegments] = {};
     SharedSegment seg[kMaxSegments];
     float *o = nullptr;                  // [parts][n_rows][d_head] sums relative to the part's maximum
     float2 *ml = nullptr;                // [parts][n_rows] maximum of the scores, sum of the exponentials (0: no keys, o not written)
+    void *out = nullptr;
+    float *lse = nullptr;
 };
 bool shared_attention_takes(int dtype, int d_head);
 const char *shared_segment_fault(int dtype, const SharedSegment &s);

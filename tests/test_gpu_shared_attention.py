@@ -80,9 +80,11 @@ def test_large_scores_and_one_key_that_takes_everything(dtype, H, Hkv, dh):
     check(case, weights=(0, 1))
 
 
-def test_infinite_and_nan_keys_reach_only_those_who_see_them():
+@pytest.mark.parametrize("L", [2, 20, 32, 64])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_infinite_and_nan_keys_reach_only_those_who_see_them(L, dh):
     import paper_2605_15609_amd as psd
-    case = Case(BF, 4, 4, 64, 4, 2, [(4, 80, None), (1, 40, None)], seed=9)
+    case = Case(BF, 4, 4, dh, 4, L, [(4, 80, None), (1, 40, None)], seed=9)
     want = case.reference()
     case.segments[1]["k"][1, 3] = float("nan")
     case.segments[1]["vt"][2][:, 5] = float("inf")
