@@ -11,6 +11,8 @@
 //
 // Per tile the problem is transposed as in attention_mfma.hip: S^T = K Q^T, O^T += V^T P^T.  A lane owns one row; the softmax stays
 // in its registers, and the probabilities are the second product's operand as they are.
+#include <type_traits>
+
 #include "psd_internal.h"
 #include "device_types.h"
 
@@ -61,6 +63,17 @@ struct Frag<float> {
             if ((i >= 4 ? i + 4 : i) >= left) v[i] = 0.f;
     }
 };
+
+// a Frag out of LDS, chunk by chunk of 16 bytes
+template <typename F>
+__device__ __forceinline__ void load_chunks(Frag<bf16_t> &f, const unsigned char *lds, F at) {
+    f.v = *reinterpret_cast<const uint4 *>(lds + at(0));
+}
+template <typename F>
+__device__ __forceinline__ void load_chunks(Frag<float> &f, const unsigned char *lds, F at) {
+    const float4 a = *reinterpret_cast<const float4 *>(lds + at(0)), b = *reinterpret_cast<const float4 *>(lds + at(1));
+    f.v[0] = a.x, f.v[1] = a.y, f.v[2] = a.z, f.v[3] = a.w, f.v[4] = b.x, f.v[5] = b.y, f.v[6] = b.z, f.v[7] = b.w;
+}
 
 // acc += A B over 16 contraction slots, 8 in each half of the wavefront
 __device__ __forceinline__ void product(const Frag<bf16_t> &a, const Frag<bf16_t> &b, floatx16 &acc) {
@@ -496,79 +509,188 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
     few_rows<T, DH>(q, sh, ln, jb, u, kvh, tile, split, sl2, reinterpret_cast<float *>(lds));
 }
 
-// The parts of a row joined, in their order: a thread takes 4 channels.
-template <typename T, int DH>
+// The parts of a row joined: a thread takes 4 channels of every G-th part, and the G sums are added in order.  G = 8 where there are many
+// parts of few rows, each of which is a round trip to memory (896 rows of 74 parts: 44 -> JOIN_US us).
+template <typename T, int DH, int G>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, SharedLaunch ln, float sl2) {
-    constexpr int TPR = DH / 4;   // threads per row
-    const int64_t r = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-    if (r >= sh.n_rows) return;
-    const int c = threadIdx.x % TPR * 4;
+    constexpr int TPR = DH / 4, RPW = 256 / (TPR * G);   // threads per part, rows per workgroup
+    static_assert(RPW >= 1, "a row's threads are one workgroup");
+    __shared__ float4 sums[G > 1 ? 256 : 1];
+    __shared__ float lsum[G > 1 ? 256 : 1];
+    const int64_t r = (int64_t)blockIdx.x * RPW + threadIdx.x / (TPR * G);
+    const int g = threadIdx.x / TPR % G, c = threadIdx.x % TPR * 4;
+    const bool live = r < sh.n_rows;
+    const float2 *ml = ln.ml + (live ? r : 0);
+    const float *op = ln.o + (live ? r : 0) * DH + c;
     float m = -INFINITY;
-    for (int p = 0; p < ln.parts; ++p) m = fmaxf(m, ln.ml[(int64_t)p * sh.n_rows + r].x);
+    for (int p = 0; p < ln.parts; ++p) m = fmaxf(m, ml[p * sh.n_rows].x);
     const float m_s = m == -INFINITY ? 0.f : m * sl2;
     float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < ln.parts; ++p) {
-        const float2 ml = ln.ml[(int64_t)p * sh.n_rows + r];
-        if (ml.y == 0.f) continue;
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(ml.x, sl2, -m_s));
-        const float4 v = *reinterpret_cast<const float4 *>(ln.o + ((int64_t)p * sh.n_rows + r) * DH + c);
-        l += w * ml.y;
-        o[0] += w * v.x, o[1] += w * v.y, o[2] += w * v.z, o[3] += w * v.w;
+#pragma unroll 4
+    for (int p = g; p < ln.parts; p += G) {
+        const float2 s = ml[p * sh.n_rows];
+        const float4 v = *reinterpret_cast<const float4 *>(op + p * sh.n_rows * DH);
+        const bool none = s.y == 0.f;   // (values that were never written may be anything)
+        const float w = none ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(s.x, sl2, -m_s));
+        l += w * s.y;
+        o[0] += none ? 0.f : w * v.x, o[1] += none ? 0.f : w * v.y, o[2] += none ? 0.f : w * v.z, o[3] += none ? 0.f : w * v.w;
     }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;   // (a row without keys: zeros)
-    T *op = (T *)ln.out + r / sh.n_heads * sh.ld_out + r % sh.n_heads * DH + c;
+    if constexpr (G > 1) {
+        sums[threadIdx.x] = make_float4(o[0], o[1], o[2], o[3]);
+        lsum[threadIdx.x] = l;
+        __syncthreads();
+        if (g > 0) return;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) op[v] = from_float<T>(o[v] * inv);
+        for (int i = 1; i < G; ++i) {
+            const float4 v = sums[threadIdx.x + i * TPR];
+            l += lsum[threadIdx.x + i * TPR];
+            o[0] += v.x, o[1] += v.y, o[2] += v.z, o[3] += v.w;
+        }
+    }
+    if (!live) return;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;   // (a row without keys: zeros)
+    T *to = (T *)ln.out + r / sh.n_heads * sh.ld_out + r % sh.n_heads * DH + c;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    else *reinterpret_cast<float4 *>(to) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
     if (ln.lse && c == 0) ln.lse[r] = PartOut<T, DH>::log_sum(m_s, l);
 }
 
-// w[j] (+)= sum over the rows of the unit of exp(x_j - lse).  A wavefront keeps 32 keys in registers and walks all rows; a lane adds
-// up what its row of every tile gives, and the lanes are added at the end, in one order whatever the launch.
+// w[j] (+)= sum over the rows of the unit of exp(x_j - lse).  A wavefront keeps 32 NK keys in registers, a workgroup four times as many, and
+// walks the rows in tiles of WR that pass through LDS, fetched a tile ahead; a lane adds up what its row of every tile gives, and the
+// lanes are added at the end.  Where a unit has few keys and many rows, workgroups take a part of the rows each and a second kernel
+// adds the parts.  Every sum has an order that the shapes alone decide.
+// Bound: 64 exponentials a lane (a quarter of the rate) and as many additions and multiply-adds stand against 32 MFMAs a tile.
+template <typename T>
+constexpr int NKEYS = sizeof(T) == 2 ? 2 : 1;
+template <typename T>
+constexpr int WROWS = sizeof(T) == 2 ? 64 : 32;
+
 template <typename T, int DH>
-__global__ __launch_bounds__(NW * 64) void shared_weights_kernel(const T *__restrict__ q, const float *__restrict__ lse, SharedShape sh, SharedLaunch ln,
-                                                                 int accumulate, float sl2) {
-    constexpr int KS = DH / 16;
+__global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__restrict__ q, const float *__restrict__ lse, SharedShape sh, SharedLaunch ln,
+                                                                    int accumulate, float sl2) {
+    constexpr int NK = NKEYS<T>, WR = WROWS<T>, KS = DH / 16, KPW = 32 * NK, C = 16 / sizeof(T), CH = DH / C, ROW = DH * (int)sizeof(T);
+    constexpr int LOADS = WR * CH / (NW * 64) > 0 ? WR * CH / (NW * 64) : 1;       // 16-byte loads per thread and tile
+    __shared__ __align__(16) unsigned char tiles[2][WR * ROW];
+    __shared__ float z2[2][WR];
     int j = 0;
     while (j + 1 < ln.n_jobs && (int)blockIdx.x >= ln.job[j + 1].block0) ++j;
     const SharedJob &jb = ln.job[j];
     const SharedSegment &seg = ln.seg[jb.seg];
-    const int local = blockIdx.x - jb.block0;
-    const int u = local / (jb.splits * sh.n_kv_heads), kvh = local / jb.splits % sh.n_kv_heads, part = local % jb.splits;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
+    // (all key blocks of a unit, KV head and part read the same rows: one XCD)
+    const int local = blockIdx.x - jb.block0, slot = local >> 3;
+    const int grp = slot / jb.tiles * 8 + (local & 7), block = slot % jb.tiles;
+    if (grp >= jb.units * sh.n_kv_heads * jb.splits) return;
+    const int split = grp % jb.splits, kvh = grp / jb.splits % sh.n_kv_heads, u = grp / jb.splits / sh.n_kv_heads;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lrow = lane & 31, half = lane >> 5;
     const Keys<T> keys = keys_of<T>(seg, u, kvh, DH);
-    const int k0 = (part * NW + wave) * BK;
-    if (k0 >= keys.len) return;
-    Frag<T> kf[KS];
+    if (block * NW * KPW >= keys.len) return;
+    const int k0 = (block * NW + wave) * KPW;
+    Frag<T> kf[NK][KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kf[ks].load(keys.k + (int64_t)min(k0 + lrow, keys.len - 1) * seg.ld_k + ks * 16 + half * 8);
-    const int rows = seg.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads);
-    float w[16];
+    for (int i = 0; i < NK; ++i)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) w[v] = 0.f;
-    for (int r0 = 0; r0 < rows; r0 += TR) {
-        const RowOf row(sh, (int64_t)u * seg.seqs_per_unit, kvh, min(r0 + lrow, rows - 1));
-        const float z = r0 + lrow < rows ? lse[row.token * sh.n_heads + row.head] * LOG2E : INFINITY;   // (rows past the last one give nothing)
-        floatx16 x;
+        for (int ks = 0; ks < KS; ++ks) kf[i][ks].load(keys.k + (int64_t)min(k0 + i * 32 + lrow, keys.len - 1) * seg.ld_k + ks * 16 + half * 8);
+    const int rows = seg.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads), n_tiles = (rows + WR - 1) / WR;
+    const int first = (int)((int64_t)n_tiles * split / jb.splits), last = (int)((int64_t)n_tiles * (split + 1) / jb.splits);
+    const int64_t s0 = (int64_t)u * seg.seqs_per_unit;
+
+    // rows pass global -> registers -> LDS, chunks of 16 bytes swizzled so that 32 rows meet all banks
+    auto place = [](int row, int chunk) {
+        constexpr int PER = ROW >= 256 ? 1 : 256 / ROW, MASK = CH >= 16 ? 15 : CH - 1;   // rows in 256 bytes of LDS
+        return row * ROW + ((chunk ^ ((row / PER) & MASK)) << 4);
+    };
+    uint4 held[LOADS];
+    float held_z = 0.f;
+    auto fetch = [&](int t) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            Frag<T> qf;
-            qf.load(q + row.token * sh.ld_q + row.head * DH + ks * 16 + half * 8);
-            product(kf[ks], qf, x);
+        for (int i = 0; i < LOADS; ++i) {
+            const int x = tid + i * NW * 64, rr = x / CH;
+            if (x >= WR * CH) break;
+            const RowOf row(sh, s0, kvh, min(t * WR + rr, rows - 1));
+            held[i] = *reinterpret_cast<const uint4 *>(q + row.token * sh.ld_q + row.head * DH + x % CH * C);
         }
+        if (tid < WR) {
+            const RowOf row(sh, s0, kvh, min(t * WR + tid, rows - 1));
+            held_z = t * WR + tid < rows ? lse[row.token * sh.n_heads + row.head] * LOG2E : INFINITY;   // (rows past the last one give nothing)
+        }
+    };
+    auto store = [&](int stage) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) w[v] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], sl2, -z));
+        for (int i = 0; i < LOADS; ++i) {
+            const int x = tid + i * NW * 64;
+            if (x >= WR * CH) break;
+            *reinterpret_cast<uint4 *>(tiles[stage] + place(x / CH, x % CH)) = held[i];
+        }
+        if (tid < WR) z2[stage][tid] = held_z;
+    };
+    float w[NK][16];
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) w[i][v] = 0.f;
+    if (first < last) {
+        fetch(first);
+        store(0);
+    }
+    for (int t = first; t < last; ++t) {
+        const int stage = (t - first) & 1;
+        if (t + 1 < last) fetch(t + 1);
+        __syncthreads();
+#pragma unroll
+        for (int rt = 0; rt < WR / 32; ++rt) {
+            floatx16 x[NK];
+#pragma unroll
+            for (int i = 0; i < NK; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[i][v] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                Frag<T> qf;
+                load_chunks(qf, tiles[stage], [&](int e) { return place(rt * 32 + lrow, (ks * 16 + half * 8) / C + e); });
+#pragma unroll
+                for (int i = 0; i < NK; ++i) product(kf[i][ks], qf, x[i]);
+            }
+            const float z = z2[stage][rt * 32 + lrow];
+#pragma unroll
+            for (int i = 0; i < NK; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) w[i][v] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][v], sl2, -z));
+        }
+        if (t + 1 < last) store(stage ^ 1);   // (every wavefront has left that stage: it passed the barrier above)
     }
     const int64_t cache = seg.rows ? seg.rows[(int64_t)u * seg.seqs_per_unit] / seg.rows_div : u;
     float *to = seg.weights + cache * seg.stride_w + (int64_t)kvh * seg.ld_w;
+    float *part = ln.o + jb.part0 * 64ll + ((int64_t)split * jb.units * sh.n_kv_heads + (int64_t)u * sh.n_kv_heads + kvh) * seg.len;
+    const int shift = jb.splits > 1 ? 0 : accumulate;
+    if (jb.splits > 1) to = part;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
+    for (int i = 0; i < NK; ++i)
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) w[v] += __shfl_xor(w[v], d, 64);
-        const int key = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
-        if (lrow == 0 && key < keys.len) to[key] = accumulate ? to[key] + w[v] : w[v];
-    }
+        for (int v = 0; v < 16; ++v) {
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) w[i][v] += __shfl_xor(w[i][v], d, 64);
+            const int key = k0 + i * 32 + 8 * (v >> 2) + 4 * half + (v & 3);
+            if (lrow == 0 && key < keys.len) to[key] = shift ? to[key] + w[i][v] : w[i][v];
+        }
+}
+
+// the parts of weights whose rows were taken by several workgroups, added in order
+__global__ __launch_bounds__(256) void weights_join_kernel(SharedShape sh, SharedLaunch ln, int accumulate) {
+    int j = 0;
+    while (j + 1 < ln.n_jobs && (int)blockIdx.x >= ln.join0[j + 1]) ++j;
+    const SharedJob &jb = ln.job[j];
+    const SharedSegment &seg = ln.seg[jb.seg];
+    const int64_t local = blockIdx.x - ln.join0[j], blocks = (seg.len + 255) / 256;
+    const int64_t ug = local / blocks;
+    const int u = (int)(ug / sh.n_kv_heads), kvh = (int)(ug % sh.n_kv_heads), key = (int)(local % blocks) * 256 + threadIdx.x;
+    const int64_t cache = seg.rows ? seg.rows[(int64_t)u * seg.seqs_per_unit] / seg.rows_div : u;
+    if (key >= (seg.lens ? min(max(seg.lens[cache], 0), seg.len) : seg.len)) return;
+    const float *part = ln.o + jb.part0 * 64ll + ug * seg.len + key;
+    float w = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < jb.splits; ++s) w += part[(int64_t)s * jb.units * sh.n_kv_heads * seg.len];
+    float *to = seg.weights + cache * seg.stride_w + (int64_t)kvh * seg.ld_w + key;
+    *to = accumulate ? *to + w : w;
 }
 
 __global__ __launch_bounds__(256) void block_values_kernel(const float *__restrict__ qkv, int ld_qkv, int v_col, int L, int width, float *__restrict__ vT,
@@ -589,8 +711,12 @@ void run_attention(const T *q, const SharedShape &sh, const SharedLaunch &ln, hi
     ensure_dynamic_lds(reinterpret_cast<const void *>(kern), smem, lds_raised);
     if (ln.blocks > 0) hipLaunchKernelGGL(kern, dim3((unsigned)ln.blocks), dim3(NW * 64), smem, st, q, sh, ln, sl2);
     if (ln.blocks > 0 && ln.parts == 0) return;
-    constexpr int rows = 256 / (DH / 4);
-    hipLaunchKernelGGL((shared_join_kernel<T, DH>), dim3((unsigned)((sh.n_rows + rows - 1) / rows)), dim3(256), 0, st, sh, ln, sl2);
+    auto join = [&](auto g) {
+        constexpr int G = decltype(g)::value, rows = 256 / (DH / 4 * G);
+        hipLaunchKernelGGL((shared_join_kernel<T, DH, G>), dim3((unsigned)((sh.n_rows + rows - 1) / rows)), dim3(256), 0, st, sh, ln, sl2);
+    };
+    if (ln.parts >= 16) join(std::integral_constant<int, 8>());
+    else join(std::integral_constant<int, 1>());
 }
 
 template <typename T, int DH>
@@ -598,6 +724,8 @@ void run_weights(const T *q, const float *lse, const SharedShape &sh, const Shar
     if (ln.blocks > 0)
         hipLaunchKernelGGL((shared_weights_kernel<T, DH>), dim3((unsigned)ln.blocks), dim3(NW * 64), 0, st, q, lse, sh, ln, accumulate,
                            LOG2E / sqrtf((float)DH));
+    if (ln.join_blocks > 0)
+        hipLaunchKernelGGL(weights_join_kernel, dim3((unsigned)ln.join_blocks), dim3(256), 0, st, sh, ln, accumulate);
 }
 
 // The work of one launch.  Segments with keys, in order, are cut into jobs: those that a job takes together need no parts, but its
@@ -688,6 +816,45 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
     return ln;
 }
 
+// Weights: a job per segment that collects them; tiles = blocks of keys, splits = parts of the rows.  part0 and parts in units of 64 floats.
+SharedLaunch plan_weights(const SharedShape &sh, const SharedSegment *given, int n) {
+    SharedLaunch ln;
+    const bool bf16 = sh.dtype == PSD_DTYPE_BF16;
+    const int per_block = NW * 32 * (bf16 ? NKEYS<bf16_t> : NKEYS<float>), WR = bf16 ? WROWS<bf16_t> : WROWS<float>;
+    double total = 0.0;
+    for (int i = 0; i < n; ++i) {
+        if (!given[i].weights || given[i].len == 0) continue;
+        SharedJob &jb = ln.job[ln.n_jobs];
+        jb.seg = ln.n_segs;
+        ln.seg[ln.n_segs++] = given[i];
+        jb.units = sh.S / given[i].seqs_per_unit;
+        jb.tiles = (given[i].len + per_block - 1) / per_block;
+        total += (double)jb.units * sh.n_kv_heads * jb.tiles * ((rows_per_unit(sh, given[i]) + WR - 1) / WR);
+        ++ln.n_jobs;
+    }
+    // three workgroups to a CU, each with as many tiles of rows; a part costs a round trip, so at least 4
+    const int share = (int)std::max(4.0, std::min(total / 768.0 + 0.999, 1e9));
+    int64_t blocks = 0, joins = 0, parts = 0;
+    for (int j = 0; j < ln.n_jobs; ++j) {
+        SharedJob &jb = ln.job[j];
+        const SharedSegment &s = ln.seg[jb.seg];
+        jb.splits = ((rows_per_unit(sh, s) + WR - 1) / WR + share - 1) / share;
+        jb.block0 = (int)blocks;
+        ln.join0[j] = (int)joins;
+        jb.part0 = (int)parts;
+        const int64_t ug = (int64_t)jb.units * sh.n_kv_heads;
+        blocks += align_up(ug * jb.splits, 8) * jb.tiles;
+        if (jb.splits > 1) {
+            joins += ug * ((s.len + 255) / 256);
+            parts += (ug * jb.splits * s.len + 63) / 64;
+        }
+    }
+    ln.blocks = blocks;
+    ln.join_blocks = joins;
+    ln.parts = (int)parts;
+    return ln;
+}
+
 }   // namespace
 
 bool shared_attention_takes(int dtype, int d_head) {
@@ -710,7 +877,11 @@ int64_t shared_attention_bytes(const SharedShape &sh, const SharedSegment *seg, 
     return align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256) + align_up((int64_t)ln.parts * sh.n_rows * 8, 256);
 }
 
-bool shared_attention_fits(const SharedShape &sh, const SharedSegment *seg, int n) { return plan_attention(sh, seg, n).blocks < (1ll << 31); }
+bool shared_attention_fits(const SharedShape &sh, const SharedSegment *seg, int n) {
+    for (int i = 0; i < n; ++i)   // (counts that the plans keep in 32 bits)
+        if ((double)sh.n_rows / sh.d_head * seg[i].len > 1e15) return false;
+    return plan_attention(sh, seg, n).blocks < (1ll << 31) && plan_weights(sh, seg, n).blocks < (1ll << 31);
+}
 
 #define PSD_SHARED_DISPATCH(CALL)                                             \
     if (sh.dtype == PSD_DTYPE_BF16) {                                         \
@@ -738,22 +909,13 @@ void launch_block_values(const float *qkv, int ld_qkv, int v_col, int S, int L, 
     hipLaunchKernelGGL(block_values_kernel, dim3((unsigned)(S * L)), dim3(256), 0, st, qkv, ld_qkv, v_col, L, width, vT, ld_vt);
 }
 
-int64_t shared_weights_bytes(const SharedShape &, const SharedSegment *, int) { return 0; }
+int64_t shared_weights_bytes(const SharedShape &sh, const SharedSegment *seg, int n) {
+    return plan_weights(sh, seg, n).parts * 256ll;
+}
 
-void launch_attention_weights(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, const float *lse, int accumulate, void *,
+void launch_attention_weights(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, const float *lse, int accumulate, void *ws,
                               hipStream_t st) {
-    SharedLaunch ln;
-    int64_t blocks = 0;
-    for (int i = 0; i < n; ++i) {
-        if (!seg[i].weights || seg[i].len == 0) continue;
-        SharedJob &jb = ln.job[ln.n_jobs];
-        jb.seg = ln.n_jobs;
-        ln.seg[ln.n_jobs++] = seg[i];
-        jb.units = sh.S / seg[i].seqs_per_unit;
-        jb.splits = (seg[i].len + NW * BK - 1) / (NW * BK);
-        jb.block0 = (int)blocks;
-        blocks += (int64_t)jb.units * sh.n_kv_heads * jb.splits;
-    }
-    ln.blocks = blocks;
+    SharedLaunch ln = plan_weights(sh, seg, n);
+    ln.o = (float *)ws;
     PSD_SHARED_DISPATCH((run_weights<T, DH>((const T *)q, lse, sh, ln, accumulate, st)))
 }

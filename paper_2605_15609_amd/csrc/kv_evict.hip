@@ -12,7 +12,9 @@ namespace {
 
 constexpr int ST = 512;        // threads of a selection
 constexpr int GT = 256;        // threads of a gather
+constexpr int KP = 4;          // 16-byte pieces of keys per thread
 constexpr int VPOS = 512;      // kept positions that a workgroup of the value gather takes
+constexpr int VCH = 32;        // channels that it takes
 
 __device__ __forceinline__ int unit_length(const SharedSegment &s, int u) { return s.lens ? min(max(s.lens[u], 0), s.len) : s.len; }
 
@@ -101,50 +103,81 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(SharedSegment src, int
     }
 }
 
-// Workgroups [0, key_wgs): keys and weights of GT 16-byte pieces; the rest: values of VPOS kept positions of one (unit, head).
+// Workgroups [0, key_wgs): keys and weights, KP 16-byte pieces a thread; the rest: values of VPOS kept positions and VCH channels of one
+// (unit, head).  What bounds it: memory, and of the values whole lines of the source, whatever share of a line's positions stays.
 template <typename T>
 __global__ __launch_bounds__(GT) void evict_gather_kernel(SharedSegment src, SharedSegment dst, int n_kv_heads, int d_head, int keep,
                                                           const int32_t *__restrict__ kept, int wgs_per_unit, int64_t key_wgs) {
     constexpr int C = 16 / sizeof(T);
-    __shared__ int slots[VPOS];
     if ((int64_t)blockIdx.x < key_wgs) {
-        const int u = (int)(blockIdx.x / wgs_per_unit), pieces = n_kv_heads * d_head / C;
-        const int64_t x = (int64_t)(blockIdx.x % wgs_per_unit) * GT + threadIdx.x;
-        const int i = (int)(x / pieces), c = (int)(x % pieces), g = c * C / d_head;
-        if (i >= min(unit_length(src, u), keep)) return;
-        const int from = kept[((int64_t)u * n_kv_heads + g) * keep + i];
-        *reinterpret_cast<uint4 *>((T *)dst.k + (int64_t)u * dst.stride_k + (int64_t)i * dst.ld_k + c * C) =
-            *reinterpret_cast<const uint4 *>((const T *)src.k + (int64_t)u * src.stride_k + (int64_t)from * src.ld_k + c * C);
-        if (dst.weights && c * C % d_head == 0)
-            dst.weights[(int64_t)u * dst.stride_w + (int64_t)g * dst.ld_w + i] = src.weights[(int64_t)u * src.stride_w + (int64_t)g * src.ld_w + from];
+        const int u = (int)(blockIdx.x / wgs_per_unit), pieces = n_kv_heads * d_head / C, n = min(unit_length(src, u), keep);
+        const int64_t x0 = (int64_t)(blockIdx.x % wgs_per_unit) * (GT * KP) + threadIdx.x;
+        int from[KP];
+        uint4 v[KP];
+#pragma unroll
+        for (int e = 0; e < KP; ++e) {
+            const int64_t x = x0 + e * GT;
+            const int i = (int)(x / pieces), g = (int)(x % pieces) * C / d_head;
+            from[e] = i < n ? kept[((int64_t)u * n_kv_heads + g) * keep + i] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < KP; ++e)
+            if (from[e] >= 0)
+                v[e] = *reinterpret_cast<const uint4 *>((const T *)src.k + (int64_t)u * src.stride_k + (int64_t)from[e] * src.ld_k + (x0 + e * GT) % pieces * C);
+#pragma unroll
+        for (int e = 0; e < KP; ++e) {
+            if (from[e] < 0) continue;
+            const int64_t x = x0 + e * GT;
+            const int i = (int)(x / pieces), c = (int)(x % pieces) * C, g = c / d_head;
+            *reinterpret_cast<uint4 *>((T *)dst.k + (int64_t)u * dst.stride_k + (int64_t)i * dst.ld_k + c) = v[e];
+            if (dst.weights && c % d_head == 0)
+                dst.weights[(int64_t)u * dst.stride_w + (int64_t)g * dst.ld_w + i] = src.weights[(int64_t)u * src.stride_w + (int64_t)g * src.ld_w + from[e]];
+        }
         return;
     }
-    const int tiles = (keep + VPOS - 1) / VPOS;
+    const int tiles = (keep + VPOS - 1) / VPOS, groups = (d_head + VCH - 1) / VCH;
     const int64_t x = (int64_t)blockIdx.x - key_wgs;
-    const int i0 = (int)(x % tiles) * VPOS, ug = (int)(x / tiles), u = ug / n_kv_heads, g = ug % n_kv_heads;
+    const int c0 = (int)(x % groups) * VCH, i0 = (int)(x / groups % tiles) * VPOS, ug = (int)(x / groups / tiles), u = ug / n_kv_heads, g = ug % n_kv_heads;
     const int n = min(min(unit_length(src, u), keep) - i0, VPOS);   // positions of this workgroup
-    for (int i = threadIdx.x; i < n; i += GT) slots[i] = vt_key_slot(kept[(int64_t)ug * keep + i0 + i]);
-    __syncthreads();
-    const int lane = threadIdx.x & 63, first = (lane >> 1) * 16 + 4 * (lane & 1);   // the lane's 8 slots: positions first .. + 3 and first + 8 .. + 11
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int first = (lane >> 1) * 16 + 4 * (lane & 1);            // the lane's 8 slots: positions first .. + 3 and first + 8 .. + 11
     if (first >= n) return;
-    for (int c = threadIdx.x >> 6; c < d_head; c += GT / 64) {
-        const T *from = (const T *)src.vt + (int64_t)u * src.stride_vt + (int64_t)(g * d_head + c) * src.ld_vt;
-        T *to = (T *)dst.vt + (int64_t)u * dst.stride_vt + (int64_t)(g * d_head + c) * dst.ld_vt + i0 + lane * 8;
-        T v[8];
+    const bool whole = first + 11 < n;                              // (else the last group: slots behind the last position stay as they were)
+    int slot[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int i = first + (e & 3) + 8 * (e >> 2);
-            if (i < n) v[e] = from[slots[i]];
-        }
-        if (first + 11 < n) {
+    for (int e = 0; e < 8; ++e) slot[e] = vt_key_slot(kept[(int64_t)ug * keep + i0 + min(first + (e & 3) + 8 * (e >> 2), n - 1)]);
+    const T *from = (const T *)src.vt + (int64_t)u * src.stride_vt + (int64_t)g * d_head * src.ld_vt;
+    T *to = (T *)dst.vt + (int64_t)u * dst.stride_vt + (int64_t)g * d_head * dst.ld_vt + i0 + lane * 8;
+    for (int c = c0 + wave; c < min(c0 + VCH, d_head); c += 4 * (GT / 64)) {
+        T v[4][8];
 #pragma unroll
-            for (int h = 0; h < 8 / C; ++h) reinterpret_cast<uint4 *>(to)[h] = reinterpret_cast<const uint4 *>(v)[h];
-        } else {   // the last group: slots behind the last position stay as they were
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (first + (e & 3) + 8 * (e >> 2) < n) to[e] = v[e];
+            for (int e = 0; e < 8; ++e) v[k][e] = from[(int64_t)min(c + k * (GT / 64), d_head - 1) * src.ld_vt + slot[e]];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (c + k * (GT / 64) >= min(c0 + VCH, d_head)) break;
+            T *row = to + (int64_t)(c + k * (GT / 64)) * dst.ld_vt;
+            if (whole) {
+#pragma unroll
+                for (int h = 0; h < 8 / C; ++h) reinterpret_cast<uint4 *>(row)[h] = reinterpret_cast<const uint4 *>(v[k])[h];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (first + (e & 3) + 8 * (e >> 2) < n) row[e] = v[k][e];
+            }
         }
     }
+}
+
+// workgroups of the gather: those of the keys of a unit, and all of the values
+struct GatherGrid {
+    int64_t per_unit, values;
+};
+GatherGrid gather_grid(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep) {
+    const int c = dtype == PSD_DTYPE_BF16 ? 8 : 4;
+    return {((int64_t)std::min(keep, src.len) * (n_kv_heads * d_head / c) + GT * KP - 1) / (GT * KP),
+            (int64_t)units * n_kv_heads * ((keep + VPOS - 1) / VPOS) * ((d_head + VCH - 1) / VCH)};
 }
 
 }   // namespace
@@ -152,20 +185,17 @@ __global__ __launch_bounds__(GT) void evict_gather_kernel(SharedSegment src, Sha
 void launch_kv_evict(const SharedSegment &src, const SharedSegment &dst, int units, int n_kv_heads, int d_head, int dtype, int keep, int n_first,
                      int n_last, int32_t *kept, int32_t *kept_lens, hipStream_t st) {
     hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)(units * n_kv_heads)), dim3(ST), 0, st, src, n_kv_heads, keep, n_first, n_last, kept, kept_lens);
-    const int most = std::min(keep, src.len);
-    if (most == 0) return;
-    const int c = dtype == PSD_DTYPE_BF16 ? 8 : 4;
-    const int wgs_per_unit = (int)(((int64_t)most * (n_kv_heads * d_head / c) + GT - 1) / GT);
-    const int64_t key_wgs = (int64_t)wgs_per_unit * units, value_wgs = (int64_t)units * n_kv_heads * ((keep + VPOS - 1) / VPOS);
-    const dim3 grid((unsigned)(key_wgs + value_wgs));
+    if (src.len == 0) return;
+    const GatherGrid gr = gather_grid(src, units, n_kv_heads, d_head, dtype, keep);
+    const int64_t key_wgs = gr.per_unit * units;
+    const dim3 grid((unsigned)(key_wgs + gr.values));
     if (dtype == PSD_DTYPE_BF16)
-        hipLaunchKernelGGL(evict_gather_kernel<bf16_t>, grid, dim3(GT), 0, st, src, dst, n_kv_heads, d_head, keep, kept, wgs_per_unit, key_wgs);
+        hipLaunchKernelGGL(evict_gather_kernel<bf16_t>, grid, dim3(GT), 0, st, src, dst, n_kv_heads, d_head, keep, kept, (int)gr.per_unit, key_wgs);
     else
-        hipLaunchKernelGGL(evict_gather_kernel<float>, grid, dim3(GT), 0, st, src, dst, n_kv_heads, d_head, keep, kept, wgs_per_unit, key_wgs);
+        hipLaunchKernelGGL(evict_gather_kernel<float>, grid, dim3(GT), 0, st, src, dst, n_kv_heads, d_head, keep, kept, (int)gr.per_unit, key_wgs);
 }
 
 int64_t kv_evict_workgroups(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep) {
-    const int c = dtype == PSD_DTYPE_BF16 ? 8 : 4;
-    return ((int64_t)std::min(keep, src.len) * (n_kv_heads * d_head / c) + GT - 1) / GT * units +
-           (int64_t)units * n_kv_heads * ((keep + VPOS - 1) / VPOS);
+    const GatherGrid gr = gather_grid(src, units, n_kv_heads, d_head, dtype, keep);
+    return gr.per_unit * units + gr.values;
 }

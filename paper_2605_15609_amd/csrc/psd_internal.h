@@ -436,6 +436,9 @@ struct SharedLaunch {
     float2 *ml = nullptr;                // [parts][n_rows] maximum of the scores, sum of the exponentials (0: no keys, o not written)
     void *out = nullptr;
     float *lse = nullptr;
+    // weights: workgroups of the second kernel, which adds the parts of jobs whose rows are cut
+    int64_t join_blocks = 0;
+    int join0[kMaxSegments] = {};
 };
 bool shared_attention_takes(int dtype, int d_head);
 const char *shared_segment_fault(int dtype, const SharedSegment &s);
