@@ -770,6 +770,7 @@ class KvSegments:
             if (s.device, s.dtype, s.d_head, s.n_kv_heads) != (first.device, first.dtype, first.d_head, first.n_kv_heads):
                 raise PsdError("segments of different devices, types or heads")
         self.c = (_Segment * len(self.segments))(*[s.c for s in self.segments])
+        self.shapes: dict = {}      # (see _attention_shape)
         self.n, self.device, self.dtype, self.d_head, self.n_kv_heads = len(self.segments), first.device, first.dtype, first.d_head, first.n_kv_heads
 
 
@@ -783,6 +784,12 @@ def _rows(t: torch.Tensor, what: str) -> int:
 
 
 def _attention_shape(q: torch.Tensor, keys: KvSegments, out: Optional[torch.Tensor] = None) -> _AttentionShape:
+    """The shape of a call, checked.  A program makes the same call over and over: what was checked once for tensors of these shapes,
+    strides, types and devices is not checked again (it says nothing about their contents or addresses)."""
+    key = (q.shape, q.stride(), q.dtype, q.device) if out is None else (q.shape, q.stride(), q.dtype, q.device, out.shape, out.stride(), out.dtype, out.device)
+    found = keys.shapes.get(key)
+    if found is not None:
+        return found
     if q.dim() != 4 or q.dtype != keys.dtype or q.device != keys.device or q.shape[3] != keys.d_head:
         raise PsdError(f"q [S, L, heads, {keys.d_head}] {keys.dtype} on {keys.device}, not {q.dtype} {tuple(q.shape)} on {q.device}")
     S, L, H, d = q.shape
@@ -791,7 +798,11 @@ def _attention_shape(q: torch.Tensor, keys: KvSegments, out: Optional[torch.Tens
     for s in keys.segments:
         if s.seqs_per_unit < 1 or s.units * s.seqs_per_unit != S:
             raise PsdError(f"{s.units} units of {s.seqs_per_unit} sequences for a batch of {S}")
-    return _AttentionShape(S, L, H, keys.n_kv_heads, d, _DTYPES[q.dtype], _rows(q, "q"), H * d if out is None else _rows(out, "out"))
+    shape = _AttentionShape(S, L, H, keys.n_kv_heads, d, _DTYPES[q.dtype], _rows(q, "q"), H * d if out is None else _rows(out, "out"))
+    if len(keys.shapes) >= 64:
+        keys.shapes.clear()
+    keys.shapes[key] = shape
+    return shape
 
 
 def _check_lse(lse: torch.Tensor, q: torch.Tensor) -> None:
@@ -799,30 +810,37 @@ def _check_lse(lse: torch.Tensor, q: torch.Tensor) -> None:
         raise PsdError(f"lse: dense float32 {tuple(q.shape[:3])} on {q.device}, not {lse.dtype} {tuple(lse.shape)} on {lse.device}")
 
 
-def _bytes(n: int, device, given: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
-    if given is not None:
-        if given.device != device or not given.is_contiguous():
-            raise PsdError(f"a dense workspace on {device}, not on {given.device}")
-        return given
-    return torch.empty((n,), dtype=torch.uint8, device=device) if n else None
+def _workspace(need, device, given: Optional[torch.Tensor]):
+    """(address, bytes, the tensor that has to live until the call is enqueued) of a call's workspace, `given` or new."""
+    if given is None:
+        if need == 0:
+            return None, 0, None
+        given = torch.empty((need,), dtype=torch.uint8, device=device)
+    elif given.device != device or not given.is_contiguous():
+        raise PsdError(f"a dense workspace on {device}, not on {given.device}")
+    return given.data_ptr(), given.nbytes, given
 
 
 class _on_device:
-    """The stream of a tensor's device, whichever device is current."""
+    """The current stream of a tensor's device, whichever device is current."""
 
     def __init__(self, device):
         if device.type != "cuda":
             raise PsdError(f"tensors on a GPU, not on {device}")
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        self.device, self.guard = device, None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
     def __enter__(self):
         if self.guard is not None:
             self.guard.__enter__()
-        return _stream()
+        return torch.cuda.current_stream(self.device).cuda_stream if _raw_stream is None else _raw_stream(self.device.index)
 
     def __exit__(self, *what):
         if self.guard is not None:
             self.guard.__exit__(*what)
+
+
+# (the address alone: torch.cuda.current_stream makes an object for it, 2.9 of the 15 us that a small call took)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def psd_attention_workspace(q: torch.Tensor, keys: KvSegments) -> torch.Tensor:
@@ -848,13 +866,11 @@ def psd_attention_shared(q: torch.Tensor, keys: KvSegments, out: Optional[torch.
     shape = _attention_shape(q, keys, out)
     if lse is not None:
         _check_lse(lse, q)
-    if ws is None:
-        ws = _bytes(_check(lib.psd_attention_shared_bytes(C.byref(shape), keys.c, keys.n)), q.device)
-    else:
-        _bytes(0, q.device, ws)
     with _on_device(q.device) as stream:
-        _check(lib.psd_attention_shared(C.byref(shape), q.data_ptr(), keys.c, keys.n, out.data_ptr(), _ptr(lse), _ptr(ws),
-                                        0 if ws is None else ws.numel() * ws.element_size(), stream))
+        need = 0 if ws is not None else _check(lib.psd_attention_shared_bytes(C.byref(shape), keys.c, keys.n))
+        at, n, ws = _workspace(need, q.device, ws)
+        _check(lib.psd_attention_shared(C.byref(shape), q.data_ptr(), keys.c, keys.n, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                        at, n, stream))
     return out
 
 
@@ -865,11 +881,10 @@ def psd_attention_weights(q: torch.Tensor, keys: KvSegments, lse: torch.Tensor, 
     lib = load_library()
     shape = _attention_shape(q, keys)
     _check_lse(lse, q)
-    need = _check(lib.psd_attention_weights_bytes(C.byref(shape), keys.c, keys.n))
-    ws = _bytes(need, q.device, ws)
     with _on_device(q.device) as stream:
-        _check(lib.psd_attention_weights(C.byref(shape), q.data_ptr(), keys.c, keys.n, lse.data_ptr(), int(bool(accumulate)), _ptr(ws),
-                                         0 if ws is None else ws.numel() * ws.element_size(), stream))
+        need = 0 if ws is not None else _check(lib.psd_attention_weights_bytes(C.byref(shape), keys.c, keys.n))
+        at, n, ws = _workspace(need, q.device, ws)
+        _check(lib.psd_attention_weights(C.byref(shape), q.data_ptr(), keys.c, keys.n, lse.data_ptr(), int(bool(accumulate)), at, n, stream))
 
 
 def psd_kv_evict(src: KvSegment, dst: KvSegment, keep: int, first: int = 0, last: int = 0, kept: Optional[torch.Tensor] = None,

@@ -1084,7 +1084,6 @@ int32_t check_shared(const psd_attention_shape *a, const psd_kv_segment *segs, i
         above = per;
         CHECK(check_segment(segs[i], i, a->S / per, a->n_kv_heads, a->d_head, a->dtype, out + i));
     }
-    if (!shared_attention_fits(*sh, out, n)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
     return PSD_OK;
 }
 
@@ -1112,8 +1111,10 @@ int32_t psd_shared_struct_sizes(int32_t *out, int32_t n) {
 int64_t psd_attention_shared_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments) {
     SharedShape sh;
     SharedSegment seg[kMaxSegments];
+    SharedLaunch ln;
     CHECK(check_shared(shape, segments, n_segments, &sh, seg));
-    return shared_attention_bytes(sh, seg, n_segments);
+    if (!plan_attention_shared(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    return shared_attention_bytes(sh, ln);
 }
 
 int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments, void *out,
@@ -1123,10 +1124,12 @@ int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, co
     CHECK(check_shared(shape, segments, n_segments, &sh, seg));
     if (!q || !out) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL q / out");
     if (misaligned16(q) || misaligned16(out)) PSD_FAIL(PSD_ERR_SHAPE, "q and out must be 16-byte aligned");
-    const int64_t need = shared_attention_bytes(sh, seg, n_segments);
+    SharedLaunch ln;
+    if (!plan_attention_shared(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    const int64_t need = shared_attention_bytes(sh, ln);
     if (need > 0 && (!ws || ws_bytes < need)) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
     if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 255) != 0) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-    launch_attention_shared(q, sh, seg, n_segments, out, lse, ws, (hipStream_t)stream);
+    launch_attention_shared(q, sh, ln, out, lse, ws, (hipStream_t)stream);
     PSD_HIP(hipGetLastError());
     return PSD_OK;
 }
@@ -1134,8 +1137,10 @@ int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, co
 int64_t psd_attention_weights_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments) {
     SharedShape sh;
     SharedSegment seg[kMaxSegments];
+    SharedLaunch ln;
     CHECK(check_shared(shape, segments, n_segments, &sh, seg));
-    return shared_weights_bytes(sh, seg, n_segments);
+    if (!plan_attention_weights(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    return shared_weights_bytes(ln);
 }
 
 int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments,
@@ -1146,10 +1151,12 @@ int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, c
     if (!q || !lse) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL q / lse");
     if (misaligned16(q)) PSD_FAIL(PSD_ERR_SHAPE, "q must be 16-byte aligned");
     if (accumulate != 0 && accumulate != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "accumulate %d", accumulate);
-    const int64_t need = shared_weights_bytes(sh, seg, n_segments);
+    SharedLaunch ln;
+    if (!plan_attention_weights(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    const int64_t need = shared_weights_bytes(ln);
     if (need > 0 && (!ws || ws_bytes < need)) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
     if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 255) != 0) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-    launch_attention_weights(q, sh, seg, n_segments, lse, accumulate, ws, (hipStream_t)stream);
+    launch_attention_weights(q, sh, ln, lse, accumulate, ws, (hipStream_t)stream);
     PSD_HIP(hipGetLastError());
     return PSD_OK;
 }

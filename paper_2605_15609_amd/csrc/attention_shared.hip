@@ -11,6 +11,7 @@
 //
 // Per tile the problem is transposed as in attention_mfma.hip: S^T = K Q^T, O^T += V^T P^T.  A lane owns one row; the softmax stays
 // in its registers, and the probabilities are the second product's operand as they are.
+#include <algorithm>
 #include <type_traits>
 
 #include "psd_internal.h"
@@ -26,7 +27,8 @@ constexpr int TR = 32;    // rows of a tile where there are few
 constexpr int MT = 128;   // rows of a tile where there are many
 constexpr int BK = 32;    // keys that a wavefront takes at a time
 constexpr int NW = 4;     // wavefronts of a workgroup, which deal a tile's keys among themselves
-constexpr float SLACK = 8.f;   // (see many_rows)
+constexpr float SLACK = 8.f;      // (see many_rows)
+constexpr float NO_MAX = 1e38f;   // minus the reference of a row without a score yet: any score exceeds it, and -inf stays -inf
 constexpr float LOG2E = 1.4426950408889634f;
 
 // A row of 8 slots of T, as a lane of a 32x32 product holds it: bf16 in one 16-byte load, fp32 in two.
@@ -93,7 +95,14 @@ __device__ __forceinline__ void probabilities(const float *p, Frag<float> &f) {
     for (int e = 0; e < 8; ++e) f.v[e] = p[e];
 }
 
-// the keys that unit u (of the launch) sees, as device pointers of one KV head
+// unit u of a launch: which unit of the segment's memory it is, and how many keys that holds (a length outside the unit is cut to it)
+__device__ __forceinline__ int cache_of(const SharedSegment &s, int u) {
+    return s.rows ? __builtin_amdgcn_readfirstlane(s.rows[(int64_t)u * s.seqs_per_unit]) / s.rows_div : u;
+}
+__device__ __forceinline__ int unit_keys(const SharedSegment &s, int cache) {
+    return s.lens ? __builtin_amdgcn_readfirstlane(min(max(s.lens[cache], 0), s.len)) : s.len;
+}
+// its keys, as device pointers of one KV head
 template <typename T>
 struct Keys {
     const T *k, *vt;
@@ -101,11 +110,11 @@ struct Keys {
 };
 template <typename T>
 __device__ __forceinline__ Keys<T> keys_of(const SharedSegment &s, int u, int kvh, int d_head) {
-    const int64_t cache = s.rows ? s.rows[(int64_t)u * s.seqs_per_unit] / s.rows_div : u;
+    const int64_t cache = cache_of(s, u);
     Keys<T> r;
     r.k = (const T *)s.k + cache * s.stride_k + kvh * d_head;
     r.vt = (const T *)s.vt + cache * s.stride_vt + (int64_t)kvh * d_head * s.ld_vt;
-    r.len = s.lens ? min(max(s.lens[cache], 0), s.len) : s.len;   // (a length outside the unit is cut to it)
+    r.len = unit_keys(s, cache);
     return r;
 }
 
@@ -119,6 +128,20 @@ struct RowOf {
         head = kvh * group + r % group;
     }
 };
+
+// A job's workgroups are dealt to the XCDs in runs of equal length: (unit, KV head, part) by (unit, KV head, part), the tiles of one
+// behind one another, so that those that read the same keys meet in one L2.  False: a workgroup of the padding.
+struct Place {
+    int u, kvh, split, tile;
+};
+__device__ __forceinline__ bool place_of(const SharedJob &jb, int n_kv_heads, Place &p) {
+    const int n = jb.units * n_kv_heads * jb.splits * jb.tiles, run = (n + 7) / 8;
+    const int local = blockIdx.x - jb.block0, at = (local & 7) * run + (local >> 3);
+    if (at >= n) return false;
+    const int grp = at / jb.tiles;
+    p = {grp / jb.splits / n_kv_heads, grp / jb.splits % n_kv_heads, grp % jb.splits, at % jb.tiles};
+    return true;
+}
 
 // Where a row's result over the keys of one workgroup goes: a part that the join reads, or, where it is the only one, the output
 template <typename T, int DH>
@@ -153,10 +176,14 @@ struct PartOut {
     }
 };
 
-// The lane's partner in the other half of the wavefront
-__device__ __forceinline__ float other_half(float v) {
+// of a value and of the other half's
+__device__ __forceinline__ float both_max(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // Few rows: a tile of TR rows of a unit against a part of the unit's keys.  The wavefronts deal the keys, BK at a time, operands
@@ -181,19 +208,37 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc_o[ct][v] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
+    // Keys of the next step go out when the scores of this one are done, its values before them: a step is one round trip to memory
+    // where it would be two.  (Heads of 128 in fp32 have no registers for that; 32 keys of the 8B shape a wavefront: AHEAD_US.)
+    constexpr bool AHEAD = sizeof(T) * DH <= 256;
+    float m_run = -INFINITY, neg_m = NO_MAX, l_run = 0.f;
+    Frag<T> kf[KS], vf[BK / 16][CT];
+    auto load_keys = [&](int k0) {
+        const T *krow = keys.k + (int64_t)min(k0 + lrow, keys.len - 1) * seg.ld_k + half * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[ks].load(krow + ks * 16);
+    };
+    auto load_values = [&](int k0, int kg) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const int c = CT * 32 > DH ? min(lrow, DH - 1) : ct * 32 + lrow;
+            vf[kg][ct].load(keys.vt + (int64_t)c * seg.ld_vt + k0 + kg * 16 + half * 8);
+        }
+    };
+    if (AHEAD && first + wave < last) load_keys((first + wave) * BK);
     for (int st = first + wave; st < last; st += NW) {
         const int k0 = st * BK, left = keys.len - k0;
+        if constexpr (!AHEAD) load_keys(k0);
+        if constexpr (AHEAD) {
+            load_values(k0, 0);
+            load_values(left > 16 ? k0 : k0 - 16, 1);   // (a value row ends with the group of 16 that its last key is in)
+        }
         floatx16 x;
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[v] = 0.f;
-        const T *krow = keys.k + (int64_t)min(k0 + lrow, keys.len - 1) * seg.ld_k + half * 8;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            Frag<T> kf;
-            kf.load(krow + ks * 16);
-            product(kf, qf[ks], x);
-        }
+        for (int ks = 0; ks < KS; ++ks) product(kf[ks], qf[ks], x);
+        if (AHEAD && st + NW < last) load_keys((st + NW) * BK);
         // x[v] <-> key 8 (v / 4) + 4 half + v % 4 of the step
         if (left < BK) {
 #pragma unroll
@@ -203,39 +248,40 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
         float mx = x[0];
 #pragma unroll
         for (int v = 1; v < 16; ++v) mx = fmaxf(mx, x[v]);
-        mx = fmaxf(mx, other_half(mx));
-        const float m_new = fmaxf(m_run, mx);
-        const float m_s = m_new == -INFINITY ? 0.f : m_new * sl2;   // (scores of -inf alone: infinite keys)
-        const float alpha = __builtin_amdgcn_exp2f(__builtin_fmaf(m_run, sl2, -m_s));
-        float p[16], psum = 0.f;
+        mx = both_max(mx);
+        if (__any(__builtin_fmaf(mx, sl2, neg_m) > SLACK)) {   // (as in many_rows)
+            const float m_new = fmaxf(m_run, mx);
+            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * sl2);
+            l_run *= alpha;
+            m_run = m_new;
+            neg_m = m_new == -INFINITY ? NO_MAX : -m_new * sl2;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc_o[ct][v] *= alpha;
+        }
+        float p[16], psum[2] = {0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-            p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], sl2, -m_s));
-            psum += p[v];
+            p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], sl2, neg_m));
+            psum[v & 1] += p[v];
         }
-        l_run = l_run * alpha + psum;
-        m_run = m_new;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc_o[ct][v] *= alpha;
+        l_run += psum[0] + psum[1];
 #pragma unroll
         for (int kg = 0; kg < BK / 16; ++kg) {
-            if (kg * 16 >= left) break;   // (a value row ends with the group of 16 that its last key is in)
+            if (kg * 16 >= left) break;
             Frag<T> pf;
             probabilities(p + 8 * kg, pf);
+            if constexpr (!AHEAD) load_values(k0, kg);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                const int c = CT * 32 > DH ? min(lrow, DH - 1) : ct * 32 + lrow;
-                Frag<T> vf;
-                vf.load(keys.vt + (int64_t)c * seg.ld_vt + k0 + kg * 16 + half * 8);
                 // slots behind the last key hold anything: their probabilities are zero, but 0 x NaN is NaN
-                if (left < BK) vf.keep(left - kg * 16 - 4 * half);
-                product(vf, pf, acc_o[ct]);
+                if (left < BK) vf[kg][ct].keep(left - kg * 16 - 4 * half);
+                product(vf[kg][ct], pf, acc_o[ct]);
             }
         }
     }
-    l_run += __shfl_xor(l_run, 32, 64);   // the halves of a row hold disjoint keys
+    l_run = both_sum(l_run);   // the halves of a row hold disjoint keys
 
     float *mine = part + wave * (2 + NF) * 64 + lane;
     mine[0] = m_run;
@@ -279,8 +325,11 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
 // Many rows (bf16): a tile of 128 rows, 32 to a wavefront, walks tiles of 64 keys that pass through LDS, fetched a tile ahead by
 // loads that go to LDS directly (chunks of 16 bytes swizzled on the way, as in attention_mfma.hip).  The rows of the tile share the unit
 // of the job's first segment; of the others the tile walks every unit that one of its rows sees, and hides it from the rows that do not.
-struct Walk {   // the key tiles of a row tile, in order
-    int seg, u, u_last, k0, len;      // segment, unit, last unit that the tile's rows see, first key, keys of the unit
+// The keys of one unit are a run: whole tiles that all rows of a wavefront see go through a loop of their own, without masks.
+struct Run {
+    const bf16_t *k, *vt;             // at its first tile
+    int ld_k, ld_vt, keys, tiles;     // keys from there on, tiles of this workgroup
+    int seqs_per_unit, u;
 };
 
 template <int DH>
@@ -291,80 +340,71 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     constexpr int KG = KT / KRPI / NW, VG = DH / 8 / NW;     // load instructions per wavefront and tile
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
     const int group = sh.n_heads / sh.n_kv_heads, per_seq = sh.L * group;
-    const SharedSegment &top = ln.seg[jb.seg];
-    const int rows = top.seqs_per_unit * per_seq, r = tile * MT + wave * 32 + lrow;
-    const int s0 = u0 * top.seqs_per_unit;
+    const int rows = ln.seg[jb.seg].seqs_per_unit * per_seq, r = tile * MT + wave * 32 + lrow;
+    const int s0 = u0 * ln.seg[jb.seg].seqs_per_unit;
     const int s_first = s0 + tile * MT / per_seq, s_last = s0 + (min(tile * MT + MT, rows) - 1) / per_seq;
     const RowOf row(sh, s0, kvh, min(r, rows - 1));   // (rows past the last repeat it and store nothing)
-    const int my_seq = s0 + min(r, rows - 1) / per_seq;
+    const int my_seq = s0 + min(r, rows - 1) / per_seq, end_seg = jb.seg + jb.segs;
     const bool any_rows = tile * MT + wave * 32 < rows;
 
-    auto unit_len = [&](const SharedSegment &s, int u) {
-        if (!s.lens) return s.len;
-        const int64_t cache = s.rows ? s.rows[(int64_t)u * s.seqs_per_unit] / s.rows_div : u;
-        return __builtin_amdgcn_readfirstlane(min(max(s.lens[cache], 0), s.len));
-    };
     // this workgroup's share of the key tiles
     int n_tiles = 0;
-    for (int i = jb.seg; i < jb.seg + jb.segs; ++i)
-        for (int u = s_first / ln.seg[i].seqs_per_unit; u <= s_last / ln.seg[i].seqs_per_unit; ++u) n_tiles += (unit_len(ln.seg[i], u) + KT - 1) / KT;
-    const int first = (int)((int64_t)n_tiles * split / jb.splits), last = (int)((int64_t)n_tiles * (split + 1) / jb.splits);
-    Walk at;
-    auto enter = [&](int seg) {   // the first unit of a segment
-        at.seg = seg;
-        if (seg >= jb.seg + jb.segs) return;
-        at.u = s_first / ln.seg[seg].seqs_per_unit;
-        at.u_last = s_last / ln.seg[seg].seqs_per_unit;
-        at.k0 = 0;
-        at.len = unit_len(ln.seg[seg], at.u);
-    };
-    auto settle = [&]() {         // on to the next unit with keys left
-        while (at.seg < jb.seg + jb.segs && at.k0 >= at.len) {
-            if (at.u < at.u_last) {
-                ++at.u;
-                at.k0 = 0;
-                at.len = unit_len(ln.seg[at.seg], at.u);
-            } else {
-                enter(at.seg + 1);
-            }
-        }
-    };
-    enter(jb.seg);
-    settle();
-    for (int skip = first; skip > 0;) {
-        const int here = min(skip, (at.len - at.k0 + KT - 1) / KT);
-        at.k0 += here * KT;
-        skip -= here;
-        settle();
+    for (int i = jb.seg; i < end_seg; ++i) {
+        const SharedSegment &s = ln.seg[i];
+        for (int u = s_first / s.seqs_per_unit; u <= s_last / s.seqs_per_unit; ++u) n_tiles += (unit_keys(s, s.lens ? cache_of(s, u) : 0) + KT - 1) / KT;
     }
+    int skip = (int)((int64_t)n_tiles * split / jb.splits), budget = (int)((int64_t)n_tiles * (split + 1) / jb.splits) - skip;
+    int at_seg = jb.seg, at_u = s_first / ln.seg[jb.seg].seqs_per_unit;
+    auto next_run = [&](Run &run) {
+        while (budget > 0 && at_seg < end_seg) {
+            const SharedSegment &s = ln.seg[at_seg];
+            const int u = at_u;
+            if (at_u < s_last / s.seqs_per_unit) ++at_u;
+            else if (++at_seg < end_seg) at_u = s_first / ln.seg[at_seg].seqs_per_unit;
+            const Keys<bf16_t> k = keys_of<bf16_t>(s, u, kvh, DH);
+            const int tiles = (k.len + KT - 1) / KT;
+            if (skip >= tiles) {
+                skip -= tiles;
+                continue;
+            }
+            run.k = k.k + (int64_t)skip * KT * s.ld_k;
+            run.vt = k.vt + skip * KT;
+            run.ld_k = s.ld_k;
+            run.ld_vt = s.ld_vt;
+            run.keys = k.len - skip * KT;
+            run.tiles = min(tiles - skip, budget);
+            run.seqs_per_unit = s.seqs_per_unit;
+            run.u = u;
+            skip = 0;
+            budget -= run.tiles;
+            return true;
+        }
+        return false;
+    };
 
     bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
         qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(q + row.token * sh.ld_q + row.head * DH + ks * 16 + half * 8));
 
-    auto kkey = [](int x) { return DH == 128 ? (x & 15) : ((x >> 1) & 7); };   // swizzle keys, as in attention_mfma.hip
-    auto fetch = [&](int stage) {   // the tile `at` into a stage; what lies behind its keys is rejected by the descriptors or never used
-        const SharedSegment &s = ln.seg[at.seg];
-        const Keys<bf16_t> k = keys_of<bf16_t>(s, at.u, kvh, DH);
-        const int left = min(at.len - at.k0, KT), ld_k = s.ld_k, ld_vt = s.ld_vt;
-        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(k.k) + (int64_t)at.k0 * ld_k, 0,
-                                                                            ((left - 1) * ld_k + DH) * 2, 0x00020000);
-        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(k.vt) + at.k0, 0,
-                                                                            ((DH - 1) * ld_vt + (left + 15) / 16 * 16) * 2, 0x00020000);
+    // swizzle keys, as in attention_mfma.hip.  Those of the rows that a lane fetches do not depend on the instruction.
+    auto kkey = [](int x) { return DH == 128 ? (x & 15) : ((x >> 1) & 7); };
+    const int k_row = lane / KLPR, k_chunk = ((lane % KLPR) ^ kkey(wave * KRPI + k_row)) << 4;
+    const int v_row = lane >> 3, v_chunk = ((lane & 7) ^ (((wave * 8 + v_row) >> 1) & 7)) << 4;
+    auto fetch = [&](const Run &run, int i, int stage) {   // tile i; what lies behind its keys is rejected by the descriptors or never used
+        const int left = min(run.keys - i * KT, KT);
+        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(run.k) + (int64_t)i * KT * run.ld_k, 0,
+                                                                            ((left - 1) * run.ld_k + DH) * 2, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(run.vt) + i * KT, 0,
+                                                                            ((DH - 1) * run.ld_vt + (left + 15) / 16 * 16) * 2, 0x00020000);
         unsigned char *sk = lds + stage * STAGE + wave * 1024, *sv = sk + K_BYTES;
+        const int k_off = k_row * run.ld_k * 2 + k_chunk, v_off = v_row * run.ld_vt * 2 + v_chunk;
 #pragma unroll
-        for (int j = 0; j < KG; ++j) {
-            const int x = (j * NW + wave) * KRPI + lane / KLPR;
-            const int voff = (lane / KLPR) * ld_k * 2 + (((lane % KLPR) ^ kkey(x)) << 4);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void *)(sk + j * (NW * 1024)), 16, voff, (j * NW + wave) * KRPI * ld_k * 2, 0, 0);
-        }
+        for (int j = 0; j < KG; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void *)(sk + j * (NW * 1024)), 16, k_off, (j * NW + wave) * KRPI * run.ld_k * 2, 0, 0);
 #pragma unroll
-        for (int j = 0; j < VG; ++j) {
-            const int x = (j * NW + wave) * 8 + (lane >> 3);
-            const int voff = (lane >> 3) * ld_vt * 2 + (((lane & 7) ^ ((x >> 1) & 7)) << 4);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void *)(sv + j * (NW * 1024)), 16, voff, (j * NW + wave) * 8 * ld_vt * 2, 0, 0);
-        }
+        for (int j = 0; j < VG; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void *)(sv + j * (NW * 1024)), 16, v_off, (j * NW + wave) * 8 * run.ld_vt * 2, 0, 0);
     };
 
     floatx16 acc_o[CT];
@@ -372,94 +412,125 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     for (int i = 0; i < CT; ++i)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc_o[i][v] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, neg_m = NO_MAX, l_run = 0.f;   // neg_m: minus the reference of the exponentials
 
-    if (first < last) fetch(0);
-    for (int t = first; t < last; ++t) {
-        const int stage = (t - first) & 1;
-        const int left = at.len - at.k0, per = ln.seg[at.seg].seqs_per_unit;
-        const bool vis = my_seq / per == at.u;
-        // this tile has landed for every wavefront, and every wavefront is done with the stage that the next one goes to
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        at.k0 += KT;
-        settle();
-        if (t + 1 < last) fetch(stage ^ 1);
-        const uint64_t seen = __ballot(vis);
-        if (!any_rows || seen == 0) continue;
-        const unsigned char *sk = lds + stage * STAGE, *sv = sk + K_BYTES;
-        floatx16 x[2];
+    // the addresses of a lane's fragments within a stage
+    int k_at[KS], v_at[4];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+    for (int ks = 0; ks < KS; ++ks) k_at[ks] = lrow * KROW + (((ks * 2 + half) ^ kkey(lrow)) << 4);   // (32 rows further: the same key)
+#pragma unroll
+    for (int kg = 0; kg < 4; ++kg) v_at[kg] = K_BYTES + lrow * VROW + (((kg * 2 + half) ^ ((lrow >> 1) & 7)) << 4);
+
+    auto scores = [&](const unsigned char *st, floatx16 (&x)[2]) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int v = 0; v < 16; ++v) x[kt][v] = 0.f;
-            const int kr = kt * 32 + lrow;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    *reinterpret_cast<const bf16x8 *>(sk + kr * KROW + (((ks * 2 + half) ^ kkey(kr)) << 4)), qf[ks], x[kt], 0, 0, 0);
-        }
-        if (left < KT || seen != ~0ull) {
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (!vis || kt * 32 + 8 * (v >> 2) + 4 * half + (v & 3) >= left) x[kt][v] = -INFINITY;
-        }
+                x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(st + k_at[ks] + kt * 32 * KROW), qf[ks], x[kt], 0, 0, 0);
+    };
+    // The sums are kept relative to a running reference, raised to the maximum only where that has grown by more than 2^SLACK in a
+    // probability: bf16 and fp32 are as exact there, and the outputs are not touched in most tiles.
+    auto reference = [&](const floatx16 (&x)[2]) {
         float mx = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
         for (int v = 1; v < 16; ++v) mx = fmaxf(fmaxf(mx, x[0][v]), x[1][v]);
-        mx = fmaxf(mx, other_half(mx));
-        // The sums are kept relative to a running reference, raised to the maximum only where that has grown by more than 2^SLACK in a
-        // probability: bf16 and fp32 are as exact there, and the outputs are not touched in most tiles.
-        if (__any(mx * sl2 > m_run * sl2 + SLACK)) {
+        mx = both_max(mx);
+        if (__any(__builtin_fmaf(mx, sl2, neg_m) > SLACK)) {
             const float m_new = fmaxf(m_run, mx);
             const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * sl2);
             l_run *= alpha;
             m_run = m_new;
+            neg_m = m_new == -INFINITY ? NO_MAX : -m_new * sl2;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc_o[ct][v] *= alpha;
         }
-        const float m_s = m_run == -INFINITY ? 0.f : m_run * sl2;
-        bf16x8 pf[4];
-        float psum = 0.f;
+    };
+    auto exponentials = [&](const floatx16 (&x)[2], bf16x8 (&pf)[4]) {
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            float p[16];
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][v], sl2, -m_s));
-                psum += p[v];
+            for (int e = 0; e < 2; ++e) {
+                float p[8];
+#pragma unroll
+                for (int v = 0; v < 8; ++v) {
+                    p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][8 * e + v], sl2, neg_m));
+                    sum[v & 3] += p[v];
+                }
+                pf[kt * 2 + e] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]),
+                                                                       pack_bf16x2(p[6], p[7])));
             }
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                pf[kt * 2 + e] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(p[8 * e + 0], p[8 * e + 1]), pack_bf16x2(p[8 * e + 2], p[8 * e + 3]),
-                                                                       pack_bf16x2(p[8 * e + 4], p[8 * e + 5]), pack_bf16x2(p[8 * e + 6], p[8 * e + 7])));
-        }
-        l_run += psum;
-        auto values = [&](int kg, int ct) {
-            const int c = ct * 32 + lrow;
-            return *reinterpret_cast<const uint4 *>(sv + c * VROW + (((kg * 2 + half) ^ ((c >> 1) & 7)) << 4));
+        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+
+    Run run, next;
+    bool more = next_run(run);
+    int stage = 0;
+    if (more) fetch(run, 0, 0);
+    while (more) {
+        const bool after = next_run(next);
+        const bool vis = my_seq / run.seqs_per_unit == run.u;
+        const uint64_t seen = any_rows ? __ballot(vis) : 0;
+        const int whole = seen == ~0ull ? min(run.tiles, run.keys / KT) : 0;
+        int i = 0;
+        auto arrive = [&]() {   // tile i has landed for every wavefront, and every wavefront is done with the stage that the next one goes to
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (i + 1 < run.tiles) fetch(run, i + 1, stage ^ 1);
+            else if (after) fetch(next, 0, stage ^ 1);
         };
-        if (left >= KT && seen == ~0ull) {
+        for (; i < whole; ++i, stage ^= 1) {
+            arrive();
+            const unsigned char *st = lds + stage * STAGE;
+            floatx16 x[2];
+            scores(st, x);
+            // the values are under way while the exponentials are computed
+            uint4 vf[4][CT];
+#pragma unroll
+            for (int kg = 0; kg < 4; ++kg)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) vf[kg][ct] = *reinterpret_cast<const uint4 *>(st + v_at[kg] + ct * 32 * VROW);
+            asm volatile("" ::: "memory");
+            reference(x);
+            bf16x8 pf[4];
+            exponentials(x, pf);
 #pragma unroll
             for (int kg = 0; kg < 4; ++kg)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
-                    acc_o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(kg, ct)), pf[kg], acc_o[ct], 0, 0, 0);
-        } else {
-            // the last tile of a unit, or one that some rows do not see: 0 x NaN is NaN, so slots behind the last key are cleared and
-            // what a row does not see stays out of its sums
+                    acc_o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[kg][ct]), pf[kg], acc_o[ct], 0, 0, 0);
+        }
+        // the last tile of a unit, or one that some rows do not see: 0 x NaN is NaN, so slots behind the last key are cleared and what a row
+        // does not see stays out of its sums
+        for (; i < run.tiles; ++i, stage ^= 1) {
+            arrive();
+            if (seen == 0) continue;
+            const unsigned char *st = lds + stage * STAGE;
+            const int left = run.keys - i * KT;
+            floatx16 x[2];
+            scores(st, x);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (!vis || kt * 32 + 8 * (v >> 2) + 4 * half + (v & 3) >= left) x[kt][v] = -INFINITY;
+            reference(x);
+            bf16x8 pf[4];
+            exponentials(x, pf);
 #pragma unroll
             for (int kg = 0; kg < 4; ++kg) {
                 if (kg * 16 >= left) break;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     Frag<bf16_t> vf;
-                    vf.v = values(kg, ct);
+                    vf.v = *reinterpret_cast<const uint4 *>(st + v_at[kg] + ct * 32 * VROW);
                     vf.keep(left - kg * 16 - 4 * half);
                     const floatx16 sums = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf.v), pf[kg], acc_o[ct], 0, 0, 0);
 #pragma unroll
@@ -467,11 +538,13 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
                 }
             }
         }
+        run = next;
+        more = after;
     }
-    l_run += other_half(l_run);   // the halves of a row hold disjoint keys
+    l_run = both_sum(l_run);   // the halves of a row hold disjoint keys
     if (r >= rows) return;
     const PartOut<bf16_t, DH> to(sh, ln, jb.part0 + split, row);
-    if (half == 0) to.sums(m_run, l_run, m_run == -INFINITY ? 0.f : m_run * sl2);
+    if (half == 0) to.sums(m_run, l_run, -neg_m);
     const float f = to.factor(l_run);
     if (f == 0.f && !to.direct) return;
 #pragma unroll
@@ -495,58 +568,76 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
     int j = 0;
     while (j + 1 < ln.n_jobs && (int)blockIdx.x >= ln.job[j + 1].block0) ++j;
     const SharedJob &jb = ln.job[j];
-    // (unit, KV head, part) groups are dealt to the XCDs, all tiles of a group to one: they read the same keys
-    const int local = blockIdx.x - jb.block0, slot = local >> 3;
-    const int grp = slot / jb.tiles * 8 + (local & 7), tile = slot % jb.tiles;
-    if (grp >= jb.units * sh.n_kv_heads * jb.splits) return;
-    const int split = grp % jb.splits, kvh = grp / jb.splits % sh.n_kv_heads, u = grp / jb.splits / sh.n_kv_heads;
+    Place at;
+    if (!place_of(jb, sh.n_kv_heads, at)) return;
     if constexpr (sizeof(T) == 2) {
         if (jb.tiled) {
-            many_rows<DH>(q, sh, ln, jb, u, kvh, tile, split, sl2, lds);
+            many_rows<DH>(q, sh, ln, jb, at.u, at.kvh, at.tile, at.split, sl2, lds);
             return;
         }
     }
-    few_rows<T, DH>(q, sh, ln, jb, u, kvh, tile, split, sl2, reinterpret_cast<float *>(lds));
+    few_rows<T, DH>(q, sh, ln, jb, at.u, at.kvh, at.tile, at.split, sl2, reinterpret_cast<float *>(lds));
 }
 
-// The parts of a row joined: a thread takes 4 channels of every G-th part, and the G sums are added in order.  G = 8 where there are many
-// parts of few rows, each of which is a round trip to memory (896 rows of 74 parts: 44 -> JOIN_US us).
+// The parts of a row joined: a thread takes 4 channels of every G-th part, and the G sums, each relative to a maximum of its own, are
+// joined in order.  G = 8 where there are many parts of few rows: every load is a round trip to memory, so as many as possible are
+// under way at a time (896 rows of 60 parts: 21 us with one loop over all maxima in front, JOIN_US without).
 template <typename T, int DH, int G>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, SharedLaunch ln, float sl2) {
     constexpr int TPR = DH / 4, RPW = 256 / (TPR * G);   // threads per part, rows per workgroup
     static_assert(RPW >= 1, "a row's threads are one workgroup");
     __shared__ float4 sums[G > 1 ? 256 : 1];
-    __shared__ float lsum[G > 1 ? 256 : 1];
+    __shared__ float2 stats[G > 1 ? 256 : 1];
     const int64_t r = (int64_t)blockIdx.x * RPW + threadIdx.x / (TPR * G);
     const int g = threadIdx.x / TPR % G, c = threadIdx.x % TPR * 4;
     const bool live = r < sh.n_rows;
     const float2 *ml = ln.ml + (live ? r : 0);
     const float *op = ln.o + (live ? r : 0) * DH + c;
-    float m = -INFINITY;
-    for (int p = 0; p < ln.parts; ++p) m = fmaxf(m, ml[p * sh.n_rows].x);
-    const float m_s = m == -INFINITY ? 0.f : m * sl2;
-    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int p = g; p < ln.parts; p += G) {
-        const float2 s = ml[p * sh.n_rows];
-        const float4 v = *reinterpret_cast<const float4 *>(op + p * sh.n_rows * DH);
-        const bool none = s.y == 0.f;   // (values that were never written may be anything)
-        const float w = none ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(s.x, sl2, -m_s));
-        l += w * s.y;
-        o[0] += none ? 0.f : w * v.x, o[1] += none ? 0.f : w * v.y, o[2] += none ? 0.f : w * v.z, o[3] += none ? 0.f : w * v.w;
+    constexpr int B = 8;   // parts at a time
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = g; p0 < ln.parts; p0 += G * B) {
+        float2 s[B];
+        float4 v[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const int64_t at = (int64_t)min(p0 + i * G, ln.parts - 1) * sh.n_rows;
+            s[i] = ml[at];
+            v[i] = *reinterpret_cast<const float4 *>(op + at * DH);
+            if (p0 + i * G >= ln.parts) s[i] = make_float2(-INFINITY, 0.f);
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < B; ++i) top = fmaxf(top, s[i].x);
+        const float m_s = top == -INFINITY ? 0.f : top * sl2, a = __builtin_amdgcn_exp2f(__builtin_fmaf(m, sl2, -m_s));
+        l *= a, o[0] *= a, o[1] *= a, o[2] *= a, o[3] *= a;
+        m = top;
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const bool none = s[i].y == 0.f;   // (values that were never written may be anything)
+            const float w = none ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(s[i].x, sl2, -m_s));
+            l += w * s[i].y;
+            o[0] += none ? 0.f : w * v[i].x, o[1] += none ? 0.f : w * v[i].y, o[2] += none ? 0.f : w * v[i].z, o[3] += none ? 0.f : w * v[i].w;
+        }
     }
     if constexpr (G > 1) {
         sums[threadIdx.x] = make_float4(o[0], o[1], o[2], o[3]);
-        lsum[threadIdx.x] = l;
+        stats[threadIdx.x] = make_float2(m, l);
         __syncthreads();
         if (g > 0) return;
 #pragma unroll
-        for (int i = 1; i < G; ++i) {
+        for (int i = 1; i < G; ++i) m = fmaxf(m, stats[threadIdx.x + i * TPR].x);
+        const float ref = m == -INFINITY ? 0.f : m * sl2;
+        l = o[0] = o[1] = o[2] = o[3] = 0.f;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const float2 s = stats[threadIdx.x + i * TPR];
             const float4 v = sums[threadIdx.x + i * TPR];
-            l += lsum[threadIdx.x + i * TPR];
-            o[0] += v.x, o[1] += v.y, o[2] += v.z, o[3] += v.w;
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s.x, sl2, -ref));
+            l += w * s.y;
+            o[0] += w * v.x, o[1] += w * v.y, o[2] += w * v.z, o[3] += w * v.w;
         }
     }
+    const float m_s = m == -INFINITY ? 0.f : m * sl2;
     if (!live) return;
     const float inv = l == 0.f ? 0.f : 1.0f / l;   // (a row without keys: zeros)
     T *to = (T *)ln.out + r / sh.n_heads * sh.ld_out + r % sh.n_heads * DH + c;
@@ -576,11 +667,9 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__r
     while (j + 1 < ln.n_jobs && (int)blockIdx.x >= ln.job[j + 1].block0) ++j;
     const SharedJob &jb = ln.job[j];
     const SharedSegment &seg = ln.seg[jb.seg];
-    // (all key blocks of a unit, KV head and part read the same rows: one XCD)
-    const int local = blockIdx.x - jb.block0, slot = local >> 3;
-    const int grp = slot / jb.tiles * 8 + (local & 7), block = slot % jb.tiles;
-    if (grp >= jb.units * sh.n_kv_heads * jb.splits) return;
-    const int split = grp % jb.splits, kvh = grp / jb.splits % sh.n_kv_heads, u = grp / jb.splits / sh.n_kv_heads;
+    Place at;   // (tile: block of keys; all blocks of a unit, KV head and part read the same rows)
+    if (!place_of(jb, sh.n_kv_heads, at)) return;
+    const int u = at.u, kvh = at.kvh, split = at.split, block = at.tile;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lrow = lane & 31, half = lane >> 5;
     const Keys<T> keys = keys_of<T>(seg, u, kvh, DH);
     if (block * NW * KPW >= keys.len) return;
@@ -658,7 +747,7 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__r
         }
         if (t + 1 < last) store(stage ^ 1);   // (every wavefront has left that stage: it passed the barrier above)
     }
-    const int64_t cache = seg.rows ? seg.rows[(int64_t)u * seg.seqs_per_unit] / seg.rows_div : u;
+    const int64_t cache = cache_of(seg, u);
     float *to = seg.weights + cache * seg.stride_w + (int64_t)kvh * seg.ld_w;
     float *part = ln.o + jb.part0 * 64ll + ((int64_t)split * jb.units * sh.n_kv_heads + (int64_t)u * sh.n_kv_heads + kvh) * seg.len;
     const int shift = jb.splits > 1 ? 0 : accumulate;
@@ -683,8 +772,8 @@ __global__ __launch_bounds__(256) void weights_join_kernel(SharedShape sh, Share
     const int64_t local = blockIdx.x - ln.join0[j], blocks = (seg.len + 255) / 256;
     const int64_t ug = local / blocks;
     const int u = (int)(ug / sh.n_kv_heads), kvh = (int)(ug % sh.n_kv_heads), key = (int)(local % blocks) * 256 + threadIdx.x;
-    const int64_t cache = seg.rows ? seg.rows[(int64_t)u * seg.seqs_per_unit] / seg.rows_div : u;
-    if (key >= (seg.lens ? min(max(seg.lens[cache], 0), seg.len) : seg.len)) return;
+    const int64_t cache = cache_of(seg, u);
+    if (key >= unit_keys(seg, cache)) return;
     const float *part = ln.o + jb.part0 * 64ll + ug * seg.len + key;
     float w = 0.f;
 #pragma unroll 4
@@ -729,30 +818,26 @@ void run_weights(const T *q, const float *lse, const SharedShape &sh, const Shar
 }
 
 // The work of one launch.  Segments with keys, in order, are cut into jobs: those that a job takes together need no parts, but its
-// tiles walk the keys of every finer unit that they touch.
-struct JobCost {
-    double steps;     // (tile of rows, 64 keys) pairs, or what costs as much
-    int keys;         // of one tile of rows, in steps
-};
+// tiles walk the keys of every finer unit that they touch.  Then the keys of every job are cut so that the workgroups have about as
+// much to do each.  Times are in steps of a tile of MT rows against 64 keys with two workgroups on a CU (2.3 us with heads of 128):
+// ALONE where a workgroup has the CU to itself, FEW for TR rows against NW * BK keys, WG_FIXED what a workgroup costs besides, and what
+// the join costs, its launch and the parts' way through memory.
+constexpr double ALONE = 0.65, FEW = 0.6, WG_FIXED = 2.0, JOIN_FIXED = 1.5, STEP_SECONDS = 2.3e-6, PART_RATE = 6e12;
+constexpr int SLOTS = 512;
 int rows_per_unit(const SharedShape &sh, const SharedSegment &s) { return s.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads); }
 
-// segments [a, b] as tiles of MT rows; steps < 0: not possible
-JobCost tiled_cost(const SharedShape &sh, const SharedSegment *seg, int a, int b) {
+// key tiles of 64 that a tile of MT rows of segments [a, b] walks; 0: not possible
+int walked_tiles(const SharedShape &sh, const SharedSegment *seg, int a, int b) {
     const int64_t rows = rows_per_unit(sh, seg[a]);
     int64_t keys = 0;
     for (int i = a; i <= b; ++i) {
-        if (sh.dtype != PSD_DTYPE_BF16 || seg[i].ld_k >= 1 << 23 || seg[i].ld_vt >= 1 << 22) return {-1.0, 0};   // (32-bit offsets within a tile)
+        if (sh.dtype != PSD_DTYPE_BF16 || seg[i].ld_k >= 1 << 23 || seg[i].ld_vt >= 1 << 22) return 0;   // (32-bit offsets within a tile)
         const int64_t fine = rows_per_unit(sh, seg[i]);
         const int64_t touched = i == a ? 1 : std::min<int64_t>((std::min<int64_t>(rows, MT) + fine - 1) / fine + (MT % fine && fine % MT ? 1 : 0), rows / fine);
-        if (touched > 8) return {-1.0, 0};
+        if (touched > 8) return 0;
         keys += touched * ((seg[i].len + 63) / 64);
     }
-    if (keys > 1 << 30) return {-1.0, 0};
-    return {(double)(sh.S / seg[a].seqs_per_unit) * sh.n_kv_heads * ((rows + MT - 1) / MT) * (double)keys, (int)keys};
-}
-JobCost few_cost(const SharedShape &sh, const SharedSegment &s) {
-    const int64_t tiles = ((int64_t)rows_per_unit(sh, s) + TR - 1) / TR, keys = (s.len + NW * BK - 1) / (NW * BK);
-    return {(double)(sh.S / s.seqs_per_unit) * sh.n_kv_heads * tiles * (double)keys, (int)keys};
+    return keys > 1 << 30 ? 0 : (int)keys;
 }
 
 SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, int n_given) {
@@ -761,58 +846,70 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
         if (given[i].len > 0) ln.seg[ln.n_segs++] = given[i];
     const int n = ln.n_segs;
     if (n == 0) return ln;
-    // every way to cut the segments into runs (bit i of cut: a job ends with segment i); a part costs its way through memory: row bytes
-    // written and read, in steps of 4.7 ns
-    const double part_cost = (double)sh.n_rows * sh.d_head * 8 / 5e12 / 4.7e-9;
     double best = -1.0;
-    int best_cut = 0;
-    for (int cut = 0; cut < 1 << (n - 1); ++cut) {
-        double cost = 0.0;
-        int jobs = 0;
+    for (int cut = 0; cut < 1 << (n - 1); ++cut) {   // bit i: a job ends with segment i
+        SharedJob job[kMaxSegments] = {};
+        int keys[kMaxSegments], jobs = 0, most = 1;
+        int64_t rows[kMaxSegments];
         bool possible = true;
         for (int a = 0, b = 0; a < n && possible; a = b + 1, ++jobs) {
             b = a;
             while (b < n - 1 && !(cut >> b & 1)) ++b;
-            const JobCost t = tiled_cost(sh, ln.seg, a, b);
-            const bool few = a == b && (t.steps < 0 || rows_per_unit(sh, ln.seg[a]) <= TR);
-            if (!few && t.steps < 0) possible = false;
-            cost += few ? few_cost(sh, ln.seg[a]).steps : t.steps;
+            SharedJob &jb = job[jobs];
+            const int per_unit = rows_per_unit(sh, ln.seg[a]);
+            keys[jobs] = a == b && per_unit <= TR ? 0 : walked_tiles(sh, ln.seg, a, b);
+            jb.tiled = keys[jobs] > 0;
+            if (!jb.tiled && a < b) possible = false;
+            if (!jb.tiled) keys[jobs] = (ln.seg[a].len + NW * BK - 1) / (NW * BK);
+            jb.seg = a;
+            jb.segs = b - a + 1;
+            jb.units = sh.S / ln.seg[a].seqs_per_unit;
+            jb.tiles = (per_unit + (jb.tiled ? MT : TR) - 1) / (jb.tiled ? MT : TR);
+            rows[jobs] = (int64_t)jb.units * sh.n_kv_heads * jb.tiles;
+            most = std::max(most, keys[jobs]);
         }
-        cost += jobs > 1 ? jobs * part_cost : 0.0;
-        if (possible && (best < 0 || cost < best)) best = cost, best_cut = cut;
+        if (!possible) continue;
+        for (int pieces = 1; pieces <= most; pieces += std::max(1, pieces / 4)) {   // of the longest job
+            const double share = (double)most / pieces;
+            int64_t wgs = 0, parts = 0;
+            double longest = 0.0, work = 0.0;
+            int splits[kMaxSegments];
+            for (int j = 0; j < jobs; ++j) {
+                const double step = job[j].tiled ? 1.0 : FEW;
+                splits[j] = std::min(keys[j], std::max(1, (int)(keys[j] * step / share + 0.999)));
+                const double each = (keys[j] + splits[j] - 1) / splits[j] * step + WG_FIXED;
+                longest = std::max(longest, each);
+                work += each * rows[j] * splits[j];
+                wgs += rows[j] * splits[j];
+                parts += splits[j];
+            }
+            // one round lasts as long as its longest workgroup, many as long as the work
+            double cost = wgs <= SLOTS / 2 ? longest * ALONE : std::max(longest, work / SLOTS + (wgs > SLOTS ? longest / 2 : 0.0));
+            if (parts > 1) cost += JOIN_FIXED + parts * (double)sh.n_rows * sh.d_head * 8 / PART_RATE / STEP_SECONDS;
+            if (best >= 0 && cost >= best) continue;
+            best = cost;
+            ln.n_jobs = jobs;
+            ln.parts = 0;
+            ln.blocks = 0;
+            for (int j = 0; j < jobs; ++j) {
+                SharedJob &jb = ln.job[j];
+                jb = job[j];
+                jb.splits = splits[j];
+                jb.part0 = ln.parts;
+                ln.parts += jb.splits;
+                ln.blocks += align_up(rows[j] * jb.splits, 8);
+            }
+        }
     }
-    double total = 0.0;
-    int64_t row_tiles = 0;
-    int keys[kMaxSegments];
-    for (int a = 0, b = 0; a < n; a = b + 1) {
-        b = a;
-        while (b < n - 1 && !(best_cut >> b & 1)) ++b;
-        SharedJob &jb = ln.job[ln.n_jobs];
-        const JobCost t = tiled_cost(sh, ln.seg, a, b);
-        jb.seg = a;
-        jb.segs = b - a + 1;
-        jb.tiled = !(a == b && (t.steps < 0 || rows_per_unit(sh, ln.seg[a]) <= TR));
-        jb.units = sh.S / ln.seg[a].seqs_per_unit;
-        const int rows = rows_per_unit(sh, ln.seg[a]), per = jb.tiled ? MT : TR;
-        jb.tiles = (rows + per - 1) / per;
-        const JobCost c = jb.tiled ? t : few_cost(sh, ln.seg[a]);
-        keys[ln.n_jobs++] = c.keys;
-        total += c.steps;
-        row_tiles += (int64_t)jb.units * jb.tiles * sh.n_kv_heads;
-    }
-    // two workgroups to a CU, each with as much to do
-    const int share = std::max(2, (int)std::min(total / 512.0 + 0.999, 1e9));
-    int64_t blocks = 0;
+    // short workgroups first: the long ones take their places in turn
+    std::stable_sort(ln.job, ln.job + ln.n_jobs, [](const SharedJob &a, const SharedJob &b) { return a.tiled < b.tiled; });
+    int64_t block = 0;
     for (int j = 0; j < ln.n_jobs; ++j) {
         SharedJob &jb = ln.job[j];
-        jb.splits = std::max(1, (keys[j] + share - 1) / share);
-        jb.block0 = (int)blocks;   // (grids of 2^31 workgroups and more are refused)
-        jb.part0 = ln.parts;
-        ln.parts += jb.splits;
-        blocks += align_up((int64_t)jb.units * sh.n_kv_heads * jb.splits, 8) * jb.tiles;
+        jb.block0 = (int)block;   // (grids of 2^31 workgroups and more are refused)
+        block += align_up((int64_t)jb.units * sh.n_kv_heads * jb.splits * jb.tiles, 8);
     }
     if (ln.parts == 1) ln.parts = 0;
-    ln.blocks = blocks;
     return ln;
 }
 
@@ -843,7 +940,7 @@ SharedLaunch plan_weights(const SharedShape &sh, const SharedSegment *given, int
         ln.join0[j] = (int)joins;
         jb.part0 = (int)parts;
         const int64_t ug = (int64_t)jb.units * sh.n_kv_heads;
-        blocks += align_up(ug * jb.splits, 8) * jb.tiles;
+        blocks += align_up(ug * jb.splits * jb.tiles, 8);
         if (jb.splits > 1) {
             joins += ug * ((s.len + 255) / 256);
             parts += (ug * jb.splits * s.len + 63) / 64;
@@ -872,16 +969,22 @@ const char *shared_segment_fault(int dtype, const SharedSegment &s) {
     return nullptr;
 }
 
-int64_t shared_attention_bytes(const SharedShape &sh, const SharedSegment *seg, int n) {
-    const SharedLaunch ln = plan_attention(sh, seg, n);
+bool plan_attention_shared(const SharedShape &sh, const SharedSegment *seg, int n, SharedLaunch *out) {
+    for (int i = 0; i < n; ++i)   // (counts that the plans keep in 32 bits)
+        if ((double)sh.n_rows * seg[i].len > 1e15) return false;
+    *out = plan_attention(sh, seg, n);
+    return out->blocks < (1ll << 31);
+}
+int64_t shared_attention_bytes(const SharedShape &sh, const SharedLaunch &ln) {
     return align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256) + align_up((int64_t)ln.parts * sh.n_rows * 8, 256);
 }
-
-bool shared_attention_fits(const SharedShape &sh, const SharedSegment *seg, int n) {
-    for (int i = 0; i < n; ++i)   // (counts that the plans keep in 32 bits)
-        if ((double)sh.n_rows / sh.d_head * seg[i].len > 1e15) return false;
-    return plan_attention(sh, seg, n).blocks < (1ll << 31) && plan_weights(sh, seg, n).blocks < (1ll << 31);
+bool plan_attention_weights(const SharedShape &sh, const SharedSegment *seg, int n, SharedLaunch *out) {
+    for (int i = 0; i < n; ++i)
+        if ((double)sh.n_rows * seg[i].len > 1e15) return false;
+    *out = plan_weights(sh, seg, n);
+    return out->blocks < (1ll << 31) && out->join_blocks < (1ll << 31);
 }
+int64_t shared_weights_bytes(const SharedLaunch &ln) { return ln.parts * 256ll; }
 
 #define PSD_SHARED_DISPATCH(CALL)                                             \
     if (sh.dtype == PSD_DTYPE_BF16) {                                         \
@@ -896,8 +999,7 @@ bool shared_attention_fits(const SharedShape &sh, const SharedSegment *seg, int 
         else { constexpr int DH = 16; CALL; }                                 \
     }
 
-void launch_attention_shared(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, void *out, float *lse, void *ws, hipStream_t st) {
-    SharedLaunch ln = plan_attention(sh, seg, n);
+void launch_attention_shared(const void *q, const SharedShape &sh, SharedLaunch &ln, void *out, float *lse, void *ws, hipStream_t st) {
     ln.o = (float *)ws;
     ln.ml = (float2 *)((char *)ws + align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256));
     ln.out = out;
@@ -909,13 +1011,7 @@ void launch_block_values(const float *qkv, int ld_qkv, int v_col, int S, int L, 
     hipLaunchKernelGGL(block_values_kernel, dim3((unsigned)(S * L)), dim3(256), 0, st, qkv, ld_qkv, v_col, L, width, vT, ld_vt);
 }
 
-int64_t shared_weights_bytes(const SharedShape &sh, const SharedSegment *seg, int n) {
-    return plan_weights(sh, seg, n).parts * 256ll;
-}
-
-void launch_attention_weights(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, const float *lse, int accumulate, void *ws,
-                              hipStream_t st) {
-    SharedLaunch ln = plan_weights(sh, seg, n);
+void launch_attention_weights(const void *q, const SharedShape &sh, SharedLaunch &ln, const float *lse, int accumulate, void *ws, hipStream_t st) {
     ln.o = (float *)ws;
     PSD_SHARED_DISPATCH((run_weights<T, DH>((const T *)q, lse, sh, ln, accumulate, st)))
 }

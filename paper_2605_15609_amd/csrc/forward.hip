@@ -5,6 +5,12 @@
 // attention_ordered.hip, lm_head.hip (plain_kernels.hip for fp32 models and on the debug path).
 #include "psd_internal.h"
 
+#define CHECK(expr)                  \
+    do {                             \
+        int32_t rc_ = (expr);        \
+        if (rc_ != PSD_OK) return rc_; \
+    } while (0)
+
 // Row stride of the SwiGLU output [tokens, d_ffn]: 64 elements of padding.  With dense rows of 24 KB
 // (d_ffn = 12288) the row tiles of the down projection's activation operand all start in the same
 // cache channel and the fetches of a K-stage queue up behind each other (measured: 123 -> 93 us at
@@ -341,6 +347,17 @@ SharedShape shared_shape(const psd_model_config &c, int S, int R) {
     return {S, R, c.n_heads, c.n_kv_heads, c.d_head, c.dtype, qkv_row_stride(w + 2 * c.n_kv_heads * c.d_head), w, (int64_t)S * R * c.n_heads};
 }
 
+int32_t shared_attention(const SharedShape &sh, const SharedSegment *seg, int n, const void *qkv, void *o, float *lse, bool weighed, void *scratch,
+                         hipStream_t st) {
+    SharedLaunch ln;
+    if (!plan_attention_shared(sh, seg, n, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    launch_attention_shared(qkv, sh, ln, o, lse, scratch, st);
+    if (!weighed) return PSD_OK;
+    if (!plan_attention_weights(sh, seg, n, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    launch_attention_weights(qkv, sh, ln, lse, 1, scratch, st);
+    return PSD_OK;
+}
+
 // The same model call on block rows alone, for context-causal block attention: everything before the block is finished, its
 // keys and values sit in the sequence's KV cache (kv.len positions), and nothing after the block is visible.  S sequences of
 // R rows, one block of L.  With kv.append the rows' keys and values are stored behind the cache and become context; R may then
@@ -428,16 +445,14 @@ int32_t forward_cached_impl(psd_handle *h, const int32_t *tokens, const int32_t 
             if (kv.shared) {
                 SharedSegment seg[kMaxSegments];
                 const int n = shared_segments(c, kv, (int)li, seq_rows, S, all.len, nullptr, 0, nullptr, 0, seg);
-                launch_attention_shared(qkv, shared_shape(c, S, R), seg, n, o, nullptr, scratch, st);
+                CHECK(shared_attention(shared_shape(c, S, R), seg, n, qkv, o, nullptr, false, scratch, st));
             } else if (!Dispatch<T>::append_attention(h, qkv, ld_qkv, S, R, H, Hkv, dh, o, all, block_start, L, st))
                 launch_plain_attention<T>(qkv, ld_qkv, S, R, H, Hkv, dh, o, pre, L, st);
         } else if (kv.shared) {
             Dispatch<T>::rope_values(h, qkv, ld_qkv, S, R, block_start, H, Hkv, dh, vT, st);
             SharedSegment seg[kMaxSegments];
             const int n = shared_segments(c, kv, (int)li, seq_rows, S, kv.len, qkv + H * dh, ld_qkv, vT, R, seg);
-            const SharedShape sh = shared_shape(c, S, R);
-            launch_attention_shared(qkv, sh, seg, n, o, lse, scratch, st);
-            if (weighed) launch_attention_weights(qkv, sh, seg, n, lse, 1, scratch, st);
+            CHECK(shared_attention(shared_shape(c, S, R), seg, n, qkv, o, lse, weighed, scratch, st));
         } else if (!Dispatch<T>::block_attention(h, qkv, ld_qkv, S, R, block_start, H, Hkv, dh, o, pre, st)) {
             Dispatch<T>::rope_attention(h, qkv, ld_qkv, vT, S, R, block_start, H, Hkv, dh, o, pre, 0, st);
         }
@@ -487,7 +502,10 @@ int64_t shared_call_bytes(const psd_model_config &cfg, int S, int L, const KvCac
     const int n = shared_segments(cfg, kv, 0, nullptr, S, kv.append ? kv.len + L : kv.len, kv.append ? nullptr : &own, 0, nullptr, L, seg);
     const SharedShape sh = shared_shape(cfg, S, L);
     const bool weighed = !kv.append && (kv.prefix_weights || kv.cache_weights);
-    return (weighed ? align_up(sh.n_rows * 4, 256) : 0) + std::max(shared_attention_bytes(sh, seg, n), weighed ? shared_weights_bytes(sh, seg, n) : 0);
+    SharedLaunch ln;
+    int64_t most = plan_attention_shared(sh, seg, n, &ln) ? shared_attention_bytes(sh, ln) : 0;   // (a plan that fails refuses the call)
+    if (weighed && plan_attention_weights(sh, seg, n, &ln)) most = std::max(most, shared_weights_bytes(ln));
+    return (weighed ? align_up(sh.n_rows * 4, 256) : 0) + most;
 }
 
 int32_t run_debug_layer(psd_handle *h, int layer, float *hidden, int S, int N, int L, int stop_after, void *ws, int64_t ws_bytes,

@@ -442,15 +442,15 @@ struct SharedLaunch {
 };
 bool shared_attention_takes(int dtype, int d_head);
 const char *shared_segment_fault(int dtype, const SharedSegment &s);
-int64_t shared_attention_bytes(const SharedShape &sh, const SharedSegment *seg, int n);
-bool shared_attention_fits(const SharedShape &sh, const SharedSegment *seg, int n);   // (its grid)
-void launch_attention_shared(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, void *out, float *lse /* or NULL */, void *ws,
-                             hipStream_t st);
+// plans (false: more workgroups than a launch takes), the scratch that they need, and their launches
+bool plan_attention_shared(const SharedShape &sh, const SharedSegment *seg, int n, SharedLaunch *out);
+bool plan_attention_weights(const SharedShape &sh, const SharedSegment *seg, int n, SharedLaunch *out);
+int64_t shared_attention_bytes(const SharedShape &sh, const SharedLaunch &ln);
+int64_t shared_weights_bytes(const SharedLaunch &ln);
+void launch_attention_shared(const void *q, const SharedShape &sh, SharedLaunch &ln, void *out, float *lse /* or NULL */, void *ws, hipStream_t st);
+void launch_attention_weights(const void *q, const SharedShape &sh, SharedLaunch &ln, const float *lse, int accumulate, void *ws, hipStream_t st);
 // values of the L rows of every sequence of qkv [S * L, ld_qkv] (columns from v_col on) transposed, for fp32 models
 void launch_block_values(const float *qkv, int ld_qkv, int v_col, int S, int L, int width, float *vT, int ld_vt, hipStream_t st);
-int64_t shared_weights_bytes(const SharedShape &sh, const SharedSegment *seg, int n);
-void launch_attention_weights(const void *q, const SharedShape &sh, const SharedSegment *seg, int n, const float *lse, int accumulate, void *ws,
-                              hipStream_t st);
 // kv_evict.hip
 int64_t kv_evict_workgroups(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep);
 void launch_kv_evict(const SharedSegment &src, const SharedSegment &dst, int units, int n_kv_heads, int d_head, int dtype, int keep, int n_first,

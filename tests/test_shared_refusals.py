@@ -36,11 +36,11 @@ def ask(lib, sh, *segs):
 
 
 def test_the_shapes_that_are_taken(lib):
-    assert ask(lib, shape(), seg()) > 0
-    assert ask(lib, shape(), seg(), seg(seqs_per_unit=2), seg(seqs_per_unit=1)) > 0
+    assert ask(lib, shape(), seg()) >= 0
+    assert ask(lib, shape(), seg(len=5000, ld_vt=5008), seg(seqs_per_unit=2), seg(seqs_per_unit=1)) > 0
     assert ask(lib, shape(), seg(len=0, k=None, vt=None)) >= 0
     for d in (16, 32, 64, 128):
-        assert ask(lib, shape(dtype=0, d_head=d, ld_q=8 * d, ld_out=8 * d), seg(ld_k=4 * d)) > 0
+        assert ask(lib, shape(dtype=0, d_head=d, ld_q=8 * d, ld_out=8 * d), seg(ld_k=4 * d)) >= 0
     assert lib.psd_attention_weights_bytes(C.byref(shape()), (B._Segment * 1)(seg(weights=BASE, ld_w=50)), 1) >= 0
 
 
@@ -70,8 +70,10 @@ def test_order_and_number_of_segments(lib):
 
 
 def test_calls_check_pointers_and_workspace_before_anything_runs(lib):
-    s, one = shape(), (B._Segment * 1)(seg())
-    need = ask(lib, s, seg())
+    long = seg(len=5000, ld_vt=5008)
+    s, one = shape(), (B._Segment * 1)(long)
+    need = ask(lib, s, long)
+    assert need > 0
     ok = dict(q=BASE, out=BASE, ws=BASE, n=need)
 
     def call(**kw):
