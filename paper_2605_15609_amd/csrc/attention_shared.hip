@@ -344,7 +344,7 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     const int s0 = u0 * ln.seg[jb.seg].seqs_per_unit;
     const int s_first = s0 + tile * MT / per_seq, s_last = s0 + (min(tile * MT + MT, rows) - 1) / per_seq;
     const RowOf row(sh, s0, kvh, min(r, rows - 1));   // (rows past the last repeat it and store nothing)
-    const int my_seq = s0 + min(r, rows - 1) / per_seq, end_seg = jb.seg + jb.segs;
+    const int my_seq = s0 + (tile * MT + wave * 32) / per_seq, end_seg = jb.seg + jb.segs;   // (of all rows of the wavefront, where it matters)
     const bool any_rows = tile * MT + wave * 32 < rows;
 
     // this workgroup's share of the key tiles
@@ -475,29 +475,37 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     if (more) fetch(run, 0, 0);
     while (more) {
         const bool after = next_run(next);
-        const bool vis = my_seq / run.seqs_per_unit == run.u;
-        const uint64_t seen = any_rows ? __ballot(vis) : 0;
-        const int whole = seen == ~0ull ? min(run.tiles, run.keys / KT) : 0;
-        int i = 0;
-        auto arrive = [&]() {   // tile i has landed for every wavefront, and every wavefront is done with the stage that the next one goes to
+        const bool seen = any_rows && (jb.segs == 1 || my_seq / run.seqs_per_unit == run.u);
+        for (int i = 0; i < run.tiles; ++i, stage ^= 1) {
+            // this tile has landed for every wavefront, and every wavefront is done with the stage that the next one goes to
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (i + 1 < run.tiles) fetch(run, i + 1, stage ^ 1);
             else if (after) fetch(next, 0, stage ^ 1);
-        };
-        for (; i < whole; ++i, stage ^= 1) {
-            arrive();
+            if (!seen) continue;
             const unsigned char *st = lds + stage * STAGE;
+            const int left = run.keys - i * KT;
             floatx16 x[2];
             scores(st, x);
             // the values are under way while the exponentials are computed
-            uint4 vf[4][CT];
+            Frag<bf16_t> vf[4][CT];
 #pragma unroll
             for (int kg = 0; kg < 4; ++kg)
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) vf[kg][ct] = *reinterpret_cast<const uint4 *>(st + v_at[kg] + ct * 32 * VROW);
+                for (int ct = 0; ct < CT; ++ct) vf[kg][ct].v = *reinterpret_cast<const uint4 *>(st + v_at[kg] + ct * 32 * VROW);
             asm volatile("" ::: "memory");
+            if (left < KT) {   // the last tile of a unit.  Values behind the last key are cleared too: 0 x NaN is NaN
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (kt * 32 + 8 * (v >> 2) + 4 * half + (v & 3) >= left) x[kt][v] = -INFINITY;
+#pragma unroll
+                for (int kg = 0; kg < 4; ++kg)
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) vf[kg][ct].keep(left - kg * 16 - 4 * half);
+            }
             reference(x);
             bf16x8 pf[4];
             exponentials(x, pf);
@@ -505,38 +513,7 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
             for (int kg = 0; kg < 4; ++kg)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
-                    acc_o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[kg][ct]), pf[kg], acc_o[ct], 0, 0, 0);
-        }
-        // the last tile of a unit, or one that some rows do not see: 0 x NaN is NaN, so slots behind the last key are cleared and what a row
-        // does not see stays out of its sums
-        for (; i < run.tiles; ++i, stage ^= 1) {
-            arrive();
-            if (seen == 0) continue;
-            const unsigned char *st = lds + stage * STAGE;
-            const int left = run.keys - i * KT;
-            floatx16 x[2];
-            scores(st, x);
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (!vis || kt * 32 + 8 * (v >> 2) + 4 * half + (v & 3) >= left) x[kt][v] = -INFINITY;
-            reference(x);
-            bf16x8 pf[4];
-            exponentials(x, pf);
-#pragma unroll
-            for (int kg = 0; kg < 4; ++kg) {
-                if (kg * 16 >= left) break;
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    Frag<bf16_t> vf;
-                    vf.v = *reinterpret_cast<const uint4 *>(st + v_at[kg] + ct * 32 * VROW);
-                    vf.keep(left - kg * 16 - 4 * half);
-                    const floatx16 sums = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf.v), pf[kg], acc_o[ct], 0, 0, 0);
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) acc_o[ct][v] = vis ? sums[v] : acc_o[ct][v];
-                }
-            }
+                    acc_o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[kg][ct].v), pf[kg], acc_o[ct], 0, 0, 0);
         }
         run = next;
         more = after;
@@ -833,6 +810,7 @@ int walked_tiles(const SharedShape &sh, const SharedSegment *seg, int a, int b) 
     for (int i = a; i <= b; ++i) {
         if (sh.dtype != PSD_DTYPE_BF16 || seg[i].ld_k >= 1 << 23 || seg[i].ld_vt >= 1 << 22) return 0;   // (32-bit offsets within a tile)
         const int64_t fine = rows_per_unit(sh, seg[i]);
+        if (i > a && fine % 32) return 0;   // (see many_rows)
         const int64_t touched = i == a ? 1 : std::min<int64_t>((std::min<int64_t>(rows, MT) + fine - 1) / fine + (MT % fine && fine % MT ? 1 : 0), rows / fine);
         if (touched > 8) return 0;
         keys += touched * ((seg[i].len + 63) / 64);
