@@ -637,7 +637,8 @@ template <typename T, int DH>
 __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__restrict__ q, const float *__restrict__ lse, SharedShape sh, SharedLaunch ln,
                                                                     int accumulate, float sl2) {
     constexpr int NK = NKEYS<T>, WR = WROWS<T>, KS = DH / 16, KPW = 32 * NK, C = 16 / sizeof(T), CH = DH / C, ROW = DH * (int)sizeof(T);
-    constexpr int LOADS = WR * CH / (NW * 64) > 0 ? WR * CH / (NW * 64) : 1;       // 16-byte loads per thread and tile
+    constexpr int LOADS = (WR * CH + NW * 64 - 1) / (NW * 64), STEP = NW * 64 / CH;   // 16-byte loads per thread and tile, rows from one to the next
+    static_assert(WR % STEP == 0 || LOADS == 1, "a thread's loads are of one channel piece");
     __shared__ __align__(16) unsigned char tiles[2][WR * ROW];
     __shared__ float z2[2][WR];
     int j = 0;
@@ -665,29 +666,48 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__r
         constexpr int PER = ROW >= 256 ? 1 : 256 / ROW, MASK = CH >= 16 ? 15 : CH - 1;   // rows in 256 bytes of LDS
         return row * ROW + ((chunk ^ ((row / PER) & MASK)) << 4);
     };
+    // A thread's rows move on by WR a tile: WR / group tokens and WR % group heads, and a token more where the heads of one are through.
+    const int group = sh.n_heads / sh.n_kv_heads, tokens = WR / group, heads = WR % group;
+    const bool loads = WR * CH >= NW * 64 || tid < WR * CH;
+    const T *from[LOADS];
+    int head[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int r = first * WR + tid / CH + i * STEP;
+        head[i] = r % group;
+        from[i] = q + (s0 * sh.L + r / group) * sh.ld_q + (kvh * group + head[i]) * DH + tid % CH * C;
+    }
+    int z_head = (first * WR + tid) % group;
+    const float *z_from = lse + (s0 * sh.L + (first * WR + tid) / group) * sh.n_heads + kvh * group + z_head;
     uint4 held[LOADS];
     float held_z = 0.f;
     auto fetch = [&](int t) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int x = tid + i * NW * 64, rr = x / CH;
-            if (x >= WR * CH) break;
-            const RowOf row(sh, s0, kvh, min(t * WR + rr, rows - 1));
-            held[i] = *reinterpret_cast<const uint4 *>(q + row.token * sh.ld_q + row.head * DH + x % CH * C);
+            const bool there = loads && t * WR + tid / CH + i * STEP < rows;
+            held[i] = make_uint4(0, 0, 0, 0);
+            if (there) held[i] = *reinterpret_cast<const uint4 *>(from[i]);
+            from[i] += tokens * sh.ld_q + heads * DH;
+            head[i] += heads;
+            if (head[i] >= group) {
+                head[i] -= group;
+                from[i] += sh.ld_q - group * DH;
+            }
         }
-        if (tid < WR) {
-            const RowOf row(sh, s0, kvh, min(t * WR + tid, rows - 1));
-            held_z = t * WR + tid < rows ? lse[row.token * sh.n_heads + row.head] * LOG2E : INFINITY;   // (rows past the last one give nothing)
+        held_z = INFINITY;   // (rows past the last one give nothing)
+        if (tid < WR && t * WR + tid < rows) held_z = *z_from;
+        z_from += tokens * sh.n_heads + heads;
+        z_head += heads;
+        if (z_head >= group) {
+            z_head -= group;
+            z_from += sh.n_heads - group;
         }
     };
     auto store = [&](int stage) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int x = tid + i * NW * 64;
-            if (x >= WR * CH) break;
-            *reinterpret_cast<uint4 *>(tiles[stage] + place(x / CH, x % CH)) = held[i];
-        }
-        if (tid < WR) z2[stage][tid] = held_z;
+        for (int i = 0; i < LOADS; ++i)
+            if (loads) *reinterpret_cast<uint4 *>(tiles[stage] + place(tid / CH + i * STEP, tid % CH)) = held[i];
+        if (tid < WR) z2[stage][tid] = held_z * LOG2E;
     };
     float w[NK][16];
 #pragma unroll
@@ -727,17 +747,26 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__r
     const int64_t cache = cache_of(seg, u);
     float *to = seg.weights + cache * seg.stride_w + (int64_t)kvh * seg.ld_w;
     float *part = ln.o + jb.part0 * 64ll + ((int64_t)split * jb.units * sh.n_kv_heads + (int64_t)u * sh.n_kv_heads + kvh) * seg.len;
-    const int shift = jb.splits > 1 ? 0 : accumulate;
+    const bool shift = jb.splits == 1 && accumulate;   // (else the join adds)
     if (jb.splits > 1) to = part;
+    // The lanes of a half are added up: each step a lane hands one half of its keys to its partner and takes the partner's share of the
+    // others, so that lane x ends with the key of number x (with 16 keys, one step adds without handing over).
+    float a[NK * 16];
 #pragma unroll
     for (int i = 0; i < NK; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
+        for (int v = 0; v < 16; ++v) a[i * 16 + v] = w[i][v];
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) w[i][v] += __shfl_xor(w[i][v], d, 64);
-            const int key = k0 + i * 32 + 8 * (v >> 2) + 4 * half + (v & 3);
-            if (lrow == 0 && key < keys.len) to[key] = shift ? to[key] + w[i][v] : w[i][v];
+    for (int n = NK * 16, d = NK * 8; d > 0; d >>= 1, n >>= 1)
+#pragma unroll
+        for (int x = 0; x < n / 2; ++x) {
+            const bool upper = lane & d;
+            const float give = upper ? a[x] : a[x + n / 2], keep = upper ? a[x + n / 2] : a[x];
+            a[x] = keep + __shfl_xor(give, d, 64);
         }
+    if constexpr (NK == 1) a[0] += __shfl_xor(a[0], 16, 64);
+    const int x = lrow % (NK * 16), key = k0 + (x >> 4) * 32 + 8 * ((x & 15) >> 2) + 4 * half + (x & 3);
+    if (lrow < NK * 16 && key < keys.len) to[key] = shift ? to[key] + a[0] : a[0];
 }
 
 // the parts of weights whose rows were taken by several workgroups, added in order
