@@ -26,6 +26,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 constexpr int TR = 32;    // rows of a tile where there are few
 constexpr int MT = 128;   // rows of a tile where there are many
 constexpr int BK = 32;    // keys that a wavefront takes at a time
+constexpr int KT = 64;    // keys of a tile in LDS
 constexpr int NW = 4;     // wavefronts of a workgroup, which deal a tile's keys among themselves
 constexpr float SLACK = 8.f;      // (see many_rows)
 constexpr float NO_MAX = 1e38f;   // minus the reference of a row without a score yet: any score exceeds it, and -inf stays -inf
@@ -335,7 +336,7 @@ struct Run {
 template <int DH>
 __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const SharedShape &sh, const SharedLaunch &ln, const SharedJob &jb, int u0,
                                           int kvh, int tile, int split, float sl2, unsigned char *lds) {
-    constexpr int KT = 64, KROW = DH * 2, VROW = KT * 2, K_BYTES = KT * KROW, STAGE = K_BYTES + DH * VROW, CT = DH / 32, KS = DH / 16;
+    constexpr int KROW = DH * 2, VROW = KT * 2, K_BYTES = KT * KROW, STAGE = K_BYTES + DH * VROW, CT = DH / 32, KS = DH / 16;
     constexpr int KRPI = 1024 / KROW, KLPR = 64 / KRPI;      // key rows of a load instruction, lanes to a row
     constexpr int KG = KT / KRPI / NW, VG = DH / 8 / NW;     // load instructions per wavefront and tile
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
@@ -535,7 +536,7 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
 
 template <typename T, int DH>
 constexpr int attention_lds() {
-    constexpr int merge = NW * (2 + (DH + 31) / 32 * 16) * 64 * 4, ring = sizeof(T) == 2 ? 2 * (64 * DH * 2 + DH * 128) : 0;
+    constexpr int merge = NW * (2 + (DH + 31) / 32 * 16) * 64 * 4, ring = sizeof(T) == 2 ? 2 * (KT * DH * 2 + DH * KT * 2) : 0;
     return merge > ring ? merge : ring;
 }
 
@@ -832,18 +833,21 @@ constexpr double ALONE = 0.65, FEW = 0.6, WG_FIXED = 2.0, JOIN_FIXED = 1.5, STEP
 constexpr int SLOTS = 512;
 int rows_per_unit(const SharedShape &sh, const SharedSegment &s) { return s.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads); }
 
-// key tiles of 64 that a tile of MT rows of segments [a, b] walks; 0: not possible
-int walked_tiles(const SharedShape &sh, const SharedSegment *seg, int a, int b) {
+// key tiles of 64 that a tile of MT rows of segments [a, b] walks at most (0: not possible), and as a share of that on average: units of
+// lengths of their own are taken to be half full
+int walked_tiles(const SharedShape &sh, const SharedSegment *seg, int a, int b, double *full) {
     const int64_t rows = rows_per_unit(sh, seg[a]);
-    int64_t keys = 0;
+    int64_t keys = 0, half = 0;
     for (int i = a; i <= b; ++i) {
         if (sh.dtype != PSD_DTYPE_BF16 || seg[i].ld_k >= 1 << 23 || seg[i].ld_vt >= 1 << 22) return 0;   // (32-bit offsets within a tile)
         const int64_t fine = rows_per_unit(sh, seg[i]);
         if (i > a && fine % 32) return 0;   // (see many_rows)
         const int64_t touched = i == a ? 1 : std::min<int64_t>((std::min<int64_t>(rows, MT) + fine - 1) / fine + (MT % fine && fine % MT ? 1 : 0), rows / fine);
         if (touched > 8) return 0;
-        keys += touched * ((seg[i].len + 63) / 64);
+        keys += touched * ((seg[i].len + KT - 1) / KT);
+        if (seg[i].lens) half += touched * ((seg[i].len + KT - 1) / KT);
     }
+    *full = 1.0 - 0.5 * half / std::max<int64_t>(keys, 1);
     return keys > 1 << 30 ? 0 : (int)keys;
 }
 
@@ -857,6 +861,7 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
     for (int cut = 0; cut < 1 << (n - 1); ++cut) {   // bit i: a job ends with segment i
         SharedJob job[kMaxSegments] = {};
         int keys[kMaxSegments], jobs = 0, most = 1;
+        double full[kMaxSegments];
         int64_t rows[kMaxSegments];
         bool possible = true;
         for (int a = 0, b = 0; a < n && possible; a = b + 1, ++jobs) {
@@ -864,7 +869,8 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
             while (b < n - 1 && !(cut >> b & 1)) ++b;
             SharedJob &jb = job[jobs];
             const int per_unit = rows_per_unit(sh, ln.seg[a]);
-            keys[jobs] = a == b && per_unit <= TR ? 0 : walked_tiles(sh, ln.seg, a, b);
+            full[jobs] = ln.seg[a].lens ? 0.5 : 1.0;
+            keys[jobs] = a == b && per_unit <= TR ? 0 : walked_tiles(sh, ln.seg, a, b, full + jobs);
             jb.tiled = keys[jobs] > 0;
             if (!jb.tiled && a < b) possible = false;
             if (!jb.tiled) keys[jobs] = (ln.seg[a].len + NW * BK - 1) / (NW * BK);
@@ -886,7 +892,7 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
                 splits[j] = std::min(keys[j], std::max(1, (int)(keys[j] * step / share + 0.999)));
                 const double each = (keys[j] + splits[j] - 1) / splits[j] * step + WG_FIXED;
                 longest = std::max(longest, each);
-                work += each * rows[j] * splits[j];
+                work += (each - (1.0 - full[j]) * keys[j] / splits[j] * step) * rows[j] * splits[j];
                 wgs += rows[j] * splits[j];
                 parts += splits[j];
             }
