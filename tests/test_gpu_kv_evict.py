@@ -97,6 +97,17 @@ def test_without_weights_in_the_destination_and_long_units():
     run(make(FP, 1, 16, 2, 20011, seed=8, ties=512), 1, 16, 3001, 1, 1)
 
 
+@pytest.mark.parametrize("dtype,Hkv,dh,units,n,keep", [
+    *[(dtype, Hkv, dh, units, n, keep) for dtype, Hkv, dh, units in [(BF, 2, 64, 1), (BF, 1, 128, 3), (FP, 1, 64, 2)]
+      for n, keep in [(16000, 1000), (9000, 40), (9000, 200), (8193, 8000), (4097, 129), (2049, 513)]],
+    (BF, 4, 64, 70, 4097, 129), (BF, 4, 64, 70, 2049, 513), (FP, 4, 16, 64, 5000, 4500), (BF, 2, 16, 2, 32768, 600), (BF, 2, 16, 2, 32769, 9)])
+def test_kept_positions_near_and_far_apart(dtype, Hkv, dh, units, n, keep):
+    data = make(dtype, Hkv, dh, units, n, seed=n + keep)
+    if keep == 200:      # most of them in one place, the rest all over
+        data[2][:, :, 3000:3150] += 1.0
+    run(data, Hkv, dh, keep, 1, 3)
+
+
 def test_other_stream_and_graph():
     import paper_2605_15609_amd as psd
     k, vt, w, _ = make(BF, 4, 64, 3, 500, seed=9)
