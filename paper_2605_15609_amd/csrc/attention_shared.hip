@@ -348,31 +348,48 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     const int my_seq = s0 + (tile * MT + wave * 32) / per_seq, end_seg = jb.seg + jb.segs;   // (of all rows of the wavefront, where it matters)
     const bool any_rows = tile * MT + wave * 32 < rows;
 
-    // this workgroup's share of the key tiles
-    int n_tiles = 0;
-    for (int i = jb.seg; i < end_seg; ++i) {
-        const SharedSegment &s = ln.seg[i];
-        for (int u = s_first / s.seqs_per_unit; u <= s_last / s.seqs_per_unit; ++u) n_tiles += (unit_keys(s, s.lens ? cache_of(s, u) : 0) + KT - 1) / KT;
+    // Lane 16 i + j: of the job's segment i the j-th unit that the tile touches (at most 8, see walked_tiles), its place in memory and its
+    // keys.  One load for all of them: taken unit by unit, every one is a round trip to memory.
+    int lane_cache = 0, lane_keys = 0;
+    {
+        const int i = min(lane >> 4, jb.segs - 1);
+        const SharedSegment *s = &ln.seg[jb.seg];
+        const int *lens = s->lens, *rws = s->rows;
+        int spu = s->seqs_per_unit, most = s->len, div = s->rows_div;
+        for (int j = 1; j < jb.segs; ++j) {
+            const SharedSegment &o = ln.seg[jb.seg + j];
+            if (i == j) lens = o.lens, rws = o.rows, spu = o.seqs_per_unit, most = o.len, div = o.rows_div;
+        }
+        const int u = s_first / spu + (lane & 15);
+        if ((lane >> 4) < jb.segs && (int64_t)u * spu <= s_last) {
+            lane_cache = rws ? rws[(int64_t)u * spu] / div : u;
+            lane_keys = lens ? min(max(lens[lane_cache], 0), most) : most;
+        }
     }
+    // this workgroup's share of the key tiles
+    int n_tiles = (lane_keys + KT - 1) / KT;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) n_tiles += __shfl_xor(n_tiles, d, 64);
+    n_tiles = __builtin_amdgcn_readfirstlane(n_tiles);
     int skip = (int)((int64_t)n_tiles * split / jb.splits), budget = (int)((int64_t)n_tiles * (split + 1) / jb.splits) - skip;
-    int at_seg = jb.seg, at_u = s_first / ln.seg[jb.seg].seqs_per_unit;
+    int at_seg = jb.seg, at_u = 0;   // (counted from the first that the tile touches)
     auto next_run = [&](Run &run) {
         while (budget > 0 && at_seg < end_seg) {
             const SharedSegment &s = ln.seg[at_seg];
-            const int u = at_u;
-            if (at_u < s_last / s.seqs_per_unit) ++at_u;
-            else if (++at_seg < end_seg) at_u = s_first / ln.seg[at_seg].seqs_per_unit;
-            const Keys<bf16_t> k = keys_of<bf16_t>(s, u, kvh, DH);
-            const int tiles = (k.len + KT - 1) / KT;
+            const int u0 = s_first / s.seqs_per_unit, u = u0 + at_u, from = (at_seg - jb.seg) * 16 + at_u;
+            if (u < s_last / s.seqs_per_unit) ++at_u;
+            else ++at_seg, at_u = 0;
+            const int64_t cache = __builtin_amdgcn_readlane(lane_cache, from);
+            const int keys = __builtin_amdgcn_readlane(lane_keys, from), tiles = (keys + KT - 1) / KT;
             if (skip >= tiles) {
                 skip -= tiles;
                 continue;
             }
-            run.k = k.k + (int64_t)skip * KT * s.ld_k;
-            run.vt = k.vt + skip * KT;
+            run.k = (const bf16_t *)s.k + cache * s.stride_k + kvh * DH + (int64_t)skip * KT * s.ld_k;
+            run.vt = (const bf16_t *)s.vt + cache * s.stride_vt + (int64_t)kvh * DH * s.ld_vt + skip * KT;
             run.ld_k = s.ld_k;
             run.ld_vt = s.ld_vt;
-            run.keys = k.len - skip * KT;
+            run.keys = keys - skip * KT;
             run.tiles = min(tiles - skip, budget);
             run.seqs_per_unit = s.seqs_per_unit;
             run.u = u;
@@ -495,6 +512,14 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
             for (int kg = 0; kg < 4; ++kg)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) vf[kg][ct].v = *reinterpret_cast<const uint4 *>(st + v_at[kg] + ct * 32 * VROW);
+            // 6 fragments under way before the first product, then one for each (16 blocks of 32 rows over 1024 + 288 keys, 8B shape: 39.5 us
+            // where every product waits for its own read, 36 so)
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (int j = 0; j < 2 * KS; ++j) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
             asm volatile("" ::: "memory");
             if (left < KT) {   // the last tile of a unit.  Values behind the last key are cleared too: 0 x NaN is NaN
 #pragma unroll
