@@ -119,6 +119,24 @@ __device__ __forceinline__ Keys<T> keys_of(const SharedSegment &s, int u, int kv
     return r;
 }
 
+// A lane's unit: of the job's segment i the j-th from that of sequence s_first on, its place in memory and its keys; none where there is
+// no such segment, or the unit starts behind s_last.  One load for all that a workgroup needs: taken one by one, each is a round trip to memory.
+__device__ __forceinline__ void unit_of_lane(const SharedLaunch &ln, const SharedJob &jb, int i, int64_t s_first, int j, int64_t s_last, int &cache, int &keys) {
+    const SharedSegment *s = &ln.seg[jb.seg];
+    const int *lens = s->lens, *rows = s->rows;
+    int spu = s->seqs_per_unit, most = s->len, div = s->rows_div;
+    for (int n = 1; n < jb.segs; ++n) {
+        const SharedSegment &o = ln.seg[jb.seg + n];
+        if (i == n) lens = o.lens, rows = o.rows, spu = o.seqs_per_unit, most = o.len, div = o.rows_div;
+    }
+    const int u = (int)s_first / spu + j;
+    cache = keys = 0;
+    if (i < jb.segs && (int64_t)u * spu <= s_last) {
+        cache = rows ? rows[(int64_t)u * spu] / div : u;
+        keys = lens ? min(max(lens[cache], 0), most) : most;
+    }
+}
+
 // row r of a unit that starts at sequence s0: token row and query head
 struct RowOf {
     int64_t token;
@@ -187,19 +205,48 @@ __device__ __forceinline__ float both_sum(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Few rows: a tile of TR rows of a unit against a part of the unit's keys.  The wavefronts deal the keys, BK at a time, operands
-// straight from memory, and merge in LDS in wavefront order.
+// Few rows: a tile of TR rows of a unit of the job's last segment against a part of the keys that they see in the job's segments.  The
+// wavefronts deal the keys, BK at a time, operands straight from memory, and merge in LDS in wavefront order.  A job of several segments
+// reads the keys of the coarser ones once for every tile, which pays where one launch then does what two would (4 rows of 8 heads of 64
+// channels over 256 shared and 61 own keys: 11.4 us with parts and a join, 9.2 so).
 template <typename T, int DH>
 __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedShape &sh, const SharedLaunch &ln, const SharedJob &jb, int u, int kvh,
                                          int tile, int split, float sl2, float *part /* [wavefront][max, sum, NF values][64 lanes] */) {
     constexpr int KS = DH / 16, CT = (DH + 31) / 32, NF = CT * 16;   // contraction steps of the scores, channel subtiles, output values per lane
-    const SharedSegment &seg = ln.seg[jb.seg];
+    const int spu = ln.seg[jb.seg + jb.segs - 1].seqs_per_unit;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
-    const Keys<T> keys = keys_of<T>(seg, u, kvh, DH);
-    const int n_steps = (keys.len + BK - 1) / BK;
+    const int rows = spu * sh.L * (sh.n_heads / sh.n_kv_heads), r = tile * TR + lrow;
+    const RowOf row(sh, (int64_t)u * spu, kvh, min(r, rows - 1));   // (rows past the last repeat it and store nothing)
+    // lane i: the unit of the job's segment i that holds the rows (see many_rows)
+    int lane_cache, lane_keys;
+    unit_of_lane(ln, jb, lane, (int64_t)u * spu, 0, (int64_t)u * spu, lane_cache, lane_keys);
+    // a step: BK keys of one segment, from k0 on
+    struct Step {
+        const T *k, *vt;
+        int ld_k, ld_vt, k0, keys, seg, end;   // end: the first step behind the segment
+    };
+    int n_steps = 0;
+    for (int i = 0; i < jb.segs; ++i) n_steps += (__builtin_amdgcn_readlane(lane_keys, i) + BK - 1) / BK;
     const int first = (int)((int64_t)n_steps * split / jb.splits), last = (int)((int64_t)n_steps * (split + 1) / jb.splits);
-    const int rows = seg.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads), r = tile * TR + lrow;
-    const RowOf row(sh, (int64_t)u * seg.seqs_per_unit, kvh, min(r, rows - 1));   // (rows past the last repeat it and store nothing)
+    auto go = [&](Step &s, int st) {   // forward to step st
+        if (st >= s.end) {
+            int begin;
+            do {
+                begin = s.end;
+                s.keys = __builtin_amdgcn_readlane(lane_keys, ++s.seg);
+                s.end += (s.keys + BK - 1) / BK;
+            } while (st >= s.end);
+            const SharedSegment &seg = ln.seg[jb.seg + s.seg];
+            const int64_t cache = __builtin_amdgcn_readlane(lane_cache, s.seg);
+            s.k = (const T *)seg.k + cache * seg.stride_k + kvh * DH;
+            s.vt = (const T *)seg.vt + cache * seg.stride_vt + (int64_t)kvh * DH * seg.ld_vt;
+            s.ld_k = seg.ld_k;
+            s.ld_vt = seg.ld_vt;
+            s.k0 = (st - begin) * BK;
+            return;
+        }
+        s.k0 += NW * BK;
+    };
     Frag<T> qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks].load(q + row.token * sh.ld_q + row.head * DH + ks * 16 + half * 8);
@@ -214,32 +261,40 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
     constexpr bool AHEAD = sizeof(T) * DH <= 256;
     float m_run = -INFINITY, neg_m = NO_MAX, l_run = 0.f;
     Frag<T> kf[KS], vf[BK / 16][CT];
-    auto load_keys = [&](int k0) {
-        const T *krow = keys.k + (int64_t)min(k0 + lrow, keys.len - 1) * seg.ld_k + half * 8;
+    auto load_keys = [&](const Step &s) {
+        const T *krow = s.k + (int64_t)min(s.k0 + lrow, s.keys - 1) * s.ld_k + half * 8;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) kf[ks].load(krow + ks * 16);
     };
-    auto load_values = [&](int k0, int kg) {
+    auto load_values = [&](const Step &s, int k0, int kg) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             const int c = CT * 32 > DH ? min(lrow, DH - 1) : ct * 32 + lrow;
-            vf[kg][ct].load(keys.vt + (int64_t)c * seg.ld_vt + k0 + kg * 16 + half * 8);
+            vf[kg][ct].load(s.vt + (int64_t)c * s.ld_vt + k0 + kg * 16 + half * 8);
         }
     };
-    if (AHEAD && first + wave < last) load_keys((first + wave) * BK);
+    Step next = {nullptr, nullptr, 0, 0, 0, 0, -1, 0};
+    if (first + wave < last) {
+        go(next, first + wave);
+        if (AHEAD) load_keys(next);
+    }
     for (int st = first + wave; st < last; st += NW) {
-        const int k0 = st * BK, left = keys.len - k0;
-        if constexpr (!AHEAD) load_keys(k0);
+        const Step here = next;
+        const int k0 = here.k0, left = here.keys - k0;
+        if constexpr (!AHEAD) load_keys(here);
         if constexpr (AHEAD) {
-            load_values(k0, 0);
-            load_values(left > 16 ? k0 : k0 - 16, 1);   // (a value row ends with the group of 16 that its last key is in)
+            load_values(here, k0, 0);
+            load_values(here, left > 16 ? k0 : k0 - 16, 1);   // (a value row ends with the group of 16 that its last key is in)
         }
         floatx16 x;
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[v] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) product(kf[ks], qf[ks], x);
-        if (AHEAD && st + NW < last) load_keys((st + NW) * BK);
+        if (st + NW < last) {
+            go(next, st + NW);
+            if (AHEAD) load_keys(next);
+        }
         // x[v] <-> key 8 (v / 4) + 4 half + v % 4 of the step
         if (left < BK) {
 #pragma unroll
@@ -273,7 +328,7 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
             if (kg * 16 >= left) break;
             Frag<T> pf;
             probabilities(p + 8 * kg, pf);
-            if constexpr (!AHEAD) load_values(k0, kg);
+            if constexpr (!AHEAD) load_values(here, k0, kg);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 // slots behind the last key hold anything: their probabilities are zero, but 0 x NaN is NaN
@@ -348,24 +403,8 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     const int my_seq = s0 + (tile * MT + wave * 32) / per_seq, end_seg = jb.seg + jb.segs;   // (of all rows of the wavefront, where it matters)
     const bool any_rows = tile * MT + wave * 32 < rows;
 
-    // Lane 16 i + j: of the job's segment i the j-th unit that the tile touches (at most 8, see walked_tiles), its place in memory and its
-    // keys.  One load for all of them: taken unit by unit, every one is a round trip to memory.
-    int lane_cache = 0, lane_keys = 0;
-    {
-        const int i = min(lane >> 4, jb.segs - 1);
-        const SharedSegment *s = &ln.seg[jb.seg];
-        const int *lens = s->lens, *rws = s->rows;
-        int spu = s->seqs_per_unit, most = s->len, div = s->rows_div;
-        for (int j = 1; j < jb.segs; ++j) {
-            const SharedSegment &o = ln.seg[jb.seg + j];
-            if (i == j) lens = o.lens, rws = o.rows, spu = o.seqs_per_unit, most = o.len, div = o.rows_div;
-        }
-        const int u = s_first / spu + (lane & 15);
-        if ((lane >> 4) < jb.segs && (int64_t)u * spu <= s_last) {
-            lane_cache = rws ? rws[(int64_t)u * spu] / div : u;
-            lane_keys = lens ? min(max(lens[lane_cache], 0), most) : most;
-        }
-    }
+    int lane_cache, lane_keys;   // lane 16 i + j: of segment i the j-th unit that the tile touches (at most 8, see walked_tiles)
+    unit_of_lane(ln, jb, lane >> 4, s_first, lane & 15, s_last, lane_cache, lane_keys);
     // this workgroup's share of the key tiles
     int n_tiles = (lane_keys + KT - 1) / KT;
 #pragma unroll
@@ -852,9 +891,10 @@ void run_weights(const T *q, const float *lse, const SharedShape &sh, const Shar
 // The work of one launch.  Segments with keys, in order, are cut into jobs: those that a job takes together need no parts, but its
 // tiles walk the keys of every finer unit that they touch.  Then the keys of every job are cut so that the workgroups have about as
 // much to do each.  Times are in steps of a tile of MT rows against 64 keys with two workgroups on a CU (2.3 us with heads of 128):
-// ALONE where a workgroup has the CU to itself, FEW for TR rows against NW * BK keys, WG_FIXED what a workgroup costs besides, and what
+// ALONE where a workgroup has the CU to itself, FEW for TR rows against NW * BK keys of
+// 256 bytes (what a CU takes of them out of L2 bounds it; fp32: the products too), WG_FIXED what a workgroup costs besides, and what
 // the join costs, its launch and the parts' way through memory.
-constexpr double ALONE = 0.65, FEW = 0.6, WG_FIXED = 2.0, JOIN_FIXED = 1.5, STEP_SECONDS = 2.3e-6, PART_RATE = 6e12;
+constexpr double ALONE = 0.65, FEW = 1.5, FEW_FP32 = 2.0, WG_FIXED = 2.0, JOIN_FIXED = 1.5, STEP_SECONDS = 2.3e-6, PART_RATE = 6e12;
 constexpr int SLOTS = 512;
 int rows_per_unit(const SharedShape &sh, const SharedSegment &s) { return s.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads); }
 
@@ -882,8 +922,14 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
         if (given[i].len > 0) ln.seg[ln.n_segs++] = given[i];
     const int n = ln.n_segs;
     if (n == 0) return ln;
+    const double few = sh.dtype == PSD_DTYPE_BF16 ? FEW * sh.d_head / 128 : FEW_FP32 * sh.d_head / 64;
     double best = -1.0;
-    for (int cut = 0; cut < 1 << (n - 1); ++cut) {   // bit i: a job ends with segment i
+    // bit i of a cut: a job ends with segment i.  Jobs of more than one segment: tiles of MT rows of the first one's units, or (the second
+    // half of the choices, where the cut has such a job) of TR rows of the last one's, which read the keys of the coarser ones each for itself
+    for (int choice = 0; choice < 1 << n; ++choice) {
+        const int cut = choice & ((1 << (n - 1)) - 1);
+        const bool narrow = choice >> (n - 1);
+        if (narrow && cut == (1 << (n - 1)) - 1) continue;
         SharedJob job[kMaxSegments] = {};
         int keys[kMaxSegments], jobs = 0, most = 1;
         double full[kMaxSegments];
@@ -893,15 +939,24 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
             b = a;
             while (b < n - 1 && !(cut >> b & 1)) ++b;
             SharedJob &jb = job[jobs];
-            const int per_unit = rows_per_unit(sh, ln.seg[a]);
-            full[jobs] = ln.seg[a].lens ? 0.5 : 1.0;
-            keys[jobs] = a == b && per_unit <= TR ? 0 : walked_tiles(sh, ln.seg, a, b, full + jobs);
-            jb.tiled = keys[jobs] > 0;
-            if (!jb.tiled && a < b) possible = false;
-            if (!jb.tiled) keys[jobs] = (ln.seg[a].len + NW * BK - 1) / (NW * BK);
+            const int of = narrow ? b : a, per_unit = rows_per_unit(sh, ln.seg[of]);   // (whose units the job's tiles are cut from)
+            jb.tiled = a == b ? per_unit > TR : !narrow;
+            keys[jobs] = jb.tiled ? walked_tiles(sh, ln.seg, a, b, full + jobs) : 0;
+            if (keys[jobs] == 0 && a == b) jb.tiled = false;
+            if (!jb.tiled) {
+                int64_t steps = 0, half = 0;
+                for (int i = a; i <= b; ++i) {
+                    steps += (ln.seg[i].len + BK - 1) / BK;
+                    if (ln.seg[i].lens) half += (ln.seg[i].len + BK - 1) / BK;
+                }
+                full[jobs] = 1.0 - 0.5 * half / steps;
+                steps = (steps + NW - 1) / NW;
+                keys[jobs] = steps > 1 << 30 ? 0 : (int)steps;
+            }
+            if (keys[jobs] == 0) possible = false;
             jb.seg = a;
             jb.segs = b - a + 1;
-            jb.units = sh.S / ln.seg[a].seqs_per_unit;
+            jb.units = sh.S / ln.seg[of].seqs_per_unit;
             jb.tiles = (per_unit + (jb.tiled ? MT : TR) - 1) / (jb.tiled ? MT : TR);
             rows[jobs] = (int64_t)jb.units * sh.n_kv_heads * jb.tiles;
             most = std::max(most, keys[jobs]);
@@ -913,7 +968,7 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
             double longest = 0.0, work = 0.0;
             int splits[kMaxSegments];
             for (int j = 0; j < jobs; ++j) {
-                const double step = job[j].tiled ? 1.0 : FEW;
+                const double step = job[j].tiled ? 1.0 : few;
                 splits[j] = std::min(keys[j], std::max(1, (int)(keys[j] * step / share + 0.999)));
                 const double each = (keys[j] + splits[j] - 1) / splits[j] * step + WG_FIXED;
                 longest = std::max(longest, each);
