@@ -110,25 +110,10 @@ int32_t check_policy(const psd_policy *p) {
         if (rc_ != PSD_OK) return rc_; \
     } while (0)
 
-// Workspace of model calls with shared keys over up to S sequences, one or seqs_per_cache of them to a cache, and of the call that extends
-// the caches: how the attention is cut, and with it the scratch, depends on how many there are
-int64_t shared_workspace(const psd_model_config &cfg, int64_t S, int L, const KvCacheArg &kv, int seqs_per_cache) {
-    int64_t most = 0;
-    KvCacheArg a = kv;
-    for (int64_t n = 1; n <= S; ++n) {
-        const int64_t fwd = plan_forward(cfg, n, L, L).total;
-        for (int per : {1, seqs_per_cache}) {
-            if (n % per) continue;
-            a.seqs_per_cache = per;
-            a.append = false;
-            most = std::max(most, fwd + shared_call_bytes(cfg, (int)n, L, a));
-            if (per == 1) {
-                a.append = true;
-                most = std::max(most, fwd + shared_call_bytes(cfg, (int)n, L, a));
-            }
-        }
-    }
-    return most;
+// Workspace of model calls with shared keys over up to S sequences: how their attention is cut, and with it the scratch, differs from one
+// number of them to the next, so this is what any of them needs at most
+int64_t shared_workspace(const psd_model_config &cfg, int64_t S, int L, const KvCacheArg &kv) {
+    return plan_forward(cfg, S, L, L).total + shared_call_most(cfg, (int)S, L, kv);
 }
 
 struct DecodeScratch {
@@ -543,7 +528,7 @@ int32_t decode_impl(psd_handle *h, int32_t *tokens, int32_t B, int32_t N, int32_
     const bool dual = kv && kv->dual;  // approximate cache: the first model call runs over whole sequences and fills it
     const int plan_N = kv ? L : N;     // rows per sequence that a model call runs over
     int64_t fwd_bytes = plan_forward(h->cfg, (int64_t)B * K, plan_N, L).total;
-    if (kv && kv->shared) fwd_bytes = shared_workspace(h->cfg, B * K, L, *kv, K);
+    if (kv && kv->shared) fwd_bytes = shared_workspace(h->cfg, (int64_t)B * K, L, *kv);
     if (dual) fwd_bytes = std::max(fwd_bytes, plan_forward(h->cfg, B, N, L).total);
     const DecodeScratch sc = plan_decode(B, N, L, K);
     if (!ws || ws_bytes < fwd_bytes + sc.total)
@@ -1124,6 +1109,13 @@ int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, co
     CHECK(check_shared(shape, segments, n_segments, &sh, seg));
     if (!q || !out) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL q / out");
     if (misaligned16(q) || misaligned16(out)) PSD_FAIL(PSD_ERR_SHAPE, "q and out must be 16-byte aligned");
+    const int64_t esz = sh.dtype == PSD_DTYPE_BF16 ? 2 : 4, width = (int64_t)sh.n_heads * sh.d_head * esz, n_tokens = (int64_t)sh.S * sh.L;
+    const Extent from = extent(q, 1, 0, n_tokens, sh.ld_q, (int64_t)sh.n_heads * sh.d_head, esz);
+    const Extent to = extent(out, 1, 0, n_tokens, sh.ld_out, (int64_t)sh.n_heads * sh.d_head, esz);
+    if (from.meets(to)) {   // rows of equal stride may lie beside each other
+        const uintptr_t ld = (uintptr_t)(sh.ld_q * esz), apart = to.first >= from.first ? (to.first - from.first) % ld : ld - (from.first - to.first) % ld;
+        if (sh.ld_q != sh.ld_out || apart < (uintptr_t)width || apart + width > ld) PSD_FAIL(PSD_ERR_INVALID_ARG, "out overlaps q");
+    }
     SharedLaunch ln;
     if (!plan_attention_shared(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
     const int64_t need = shared_attention_bytes(sh, ln);
@@ -1243,7 +1235,7 @@ int64_t psd_shared_workspace_bytes(const psd_model_config *cfg, int32_t S, int32
     if (S < 1) PSD_FAIL(PSD_ERR_SHAPE, "batch %d", S);
     KvCacheArg a;
     CHECK(check_kv_shared(*cfg, kv, S, L, false, &a));
-    return shared_workspace(*cfg, S, L, a, a.seqs_per_cache);
+    return shared_workspace(*cfg, S, L, a);
 }
 
 int32_t psd_forward_confidence_shared(psd_handle *h, const int32_t *tokens, int32_t S, int32_t N, int32_t block_start, int32_t L,

@@ -896,6 +896,7 @@ void run_weights(const T *q, const float *lse, const SharedShape &sh, const Shar
 // the join costs, its launch and the parts' way through memory.
 constexpr double ALONE = 0.65, FEW = 1.5, FEW_FP32 = 2.0, WG_FIXED = 2.0, JOIN_FIXED = 1.5, STEP_SECONDS = 2.3e-6, PART_RATE = 6e12;
 constexpr int SLOTS = 512;
+constexpr int64_t MOST_PART_ROWS = 1 << 17;   // rows times parts, where segments are cut: 1024 tiles of 128 rows
 int rows_per_unit(const SharedShape &sh, const SharedSegment &s) { return s.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads); }
 
 // key tiles of 64 that a tile of MT rows of segments [a, b] walks at most (0: not possible), and as a share of that on average: units of
@@ -968,13 +969,19 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
             double longest = 0.0, work = 0.0;
             int splits[kMaxSegments];
             for (int j = 0; j < jobs; ++j) {
+                splits[j] = std::min(keys[j], std::max(1, (int)(keys[j] * (job[j].tiled ? 1.0 : few) / share + 0.999)));
+                parts += splits[j];
+            }
+            if (parts > jobs && parts * sh.n_rows > MOST_PART_ROWS) {   // (a part of every row and job is the least that there is)
+                for (int j = 0; j < jobs; ++j) splits[j] = 1;
+                parts = jobs;
+            }
+            for (int j = 0; j < jobs; ++j) {
                 const double step = job[j].tiled ? 1.0 : few;
-                splits[j] = std::min(keys[j], std::max(1, (int)(keys[j] * step / share + 0.999)));
                 const double each = (keys[j] + splits[j] - 1) / splits[j] * step + WG_FIXED;
                 longest = std::max(longest, each);
                 work += (each - (1.0 - full[j]) * keys[j] / splits[j] * step) * rows[j] * splits[j];
                 wgs += rows[j] * splits[j];
-                parts += splits[j];
             }
             // one round lasts as long as its longest workgroup, many as long as the work
             double cost = wgs <= SLOTS / 2 ? longest * ALONE : std::max(longest, work / SLOTS + (wgs > SLOTS ? longest / 2 : 0.0));
@@ -1071,6 +1078,13 @@ bool plan_attention_shared(const SharedShape &sh, const SharedSegment *seg, int 
 int64_t shared_attention_bytes(const SharedShape &sh, const SharedLaunch &ln) {
     return align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256) + align_up((int64_t)ln.parts * sh.n_rows * 8, 256);
 }
+// the most that any batch of 1 .. sh.S sequences over these segments needs, however they share them
+int64_t shared_attention_most(const SharedShape &sh, const SharedSegment *seg, int n) {
+    int64_t steps = 0;
+    for (int i = 0; i < n; ++i) steps += (seg[i].len + BK - 1) / BK;   // (no job is cut finer)
+    const int64_t rows = std::max(n * sh.n_rows, std::min(MOST_PART_ROWS, steps * sh.n_rows));
+    return align_up(rows * sh.d_head * 4, 256) + align_up(rows * 8, 256);
+}
 bool plan_attention_weights(const SharedShape &sh, const SharedSegment *seg, int n, SharedLaunch *out) {
     for (int i = 0; i < n; ++i)
         if ((double)sh.n_rows * seg[i].len > 1e15) return false;
@@ -1078,6 +1092,21 @@ bool plan_attention_weights(const SharedShape &sh, const SharedSegment *seg, int
     return out->blocks < (1ll << 31) && out->join_blocks < (1ll << 31);
 }
 int64_t shared_weights_bytes(const SharedLaunch &ln) { return ln.parts * 256ll; }
+
+// (parts cost one more than the workgroups that plan_weights asks for, and those are at most a quarter of the tiles of rows; seqs_per_unit 1
+// is the most units that a segment can have)
+int64_t shared_weights_most(const SharedShape &sh, const SharedSegment *seg, int n) {
+    const bool bf16 = sh.dtype == PSD_DTYPE_BF16;
+    const int64_t per_block = NW * 32 * (bf16 ? NKEYS<bf16_t> : NKEYS<float>), WR = bf16 ? WROWS<bf16_t> : WROWS<float>;
+    int64_t floats = 0;
+    for (int i = 0; i < n; ++i) {
+        if (!seg[i].weights || seg[i].len == 0) continue;
+        const int64_t ug = (int64_t)(sh.S / seg[i].seqs_per_unit) * sh.n_kv_heads;
+        const int64_t tiles = ug * ((seg[i].len + per_block - 1) / per_block) * ((rows_per_unit(sh, seg[i]) + WR - 1) / WR);
+        floats += per_block * std::min<int64_t>(tiles / 4 + 1, 800) + ug * seg[i].len + 64;
+    }
+    return floats * 4;
+}
 
 #define PSD_SHARED_DISPATCH(CALL)                                             \
     if (sh.dtype == PSD_DTYPE_BF16) {                                         \

@@ -508,6 +508,19 @@ int64_t shared_call_bytes(const psd_model_config &cfg, int S, int L, const KvCac
     return (weighed ? align_up(sh.n_rows * 4, 256) : 0) + most;
 }
 
+int64_t shared_call_most(const psd_model_config &cfg, int S, int L, const KvCacheArg &kv) {
+    SharedSegment seg[kMaxSegments];
+    static const char own = 0;
+    KvCacheArg a = kv;
+    a.seqs_per_cache = 1;
+    // (the cache's positions and the block apart need no less than the block behind them)
+    const int n = shared_segments(cfg, a, 0, nullptr, S, kv.len, &own, 0, nullptr, L, seg);
+    const SharedShape sh = shared_shape(cfg, S, L);
+    int64_t most = shared_attention_most(sh, seg, n);
+    if (!kv.prefix_weights && !kv.cache_weights) return most;
+    return align_up(sh.n_rows * 4, 256) + std::max(most, shared_weights_most(sh, seg, n));
+}
+
 int32_t run_debug_layer(psd_handle *h, int layer, float *hidden, int S, int N, int L, int stop_after, void *ws, int64_t ws_bytes,
                         hipStream_t st) {
     const ForwardPlan p = plan_forward(h->cfg, S, N, L);

@@ -240,6 +240,8 @@ struct KvCacheArg {
 };
 // scratch behind a cached forward's own workspace for the attention of a `shared` call over S sequences of L rows
 int64_t shared_call_bytes(const psd_model_config &cfg, int S, int L, const KvCacheArg &kv);
+// ... and the most that any call over up to S sequences needs, one or more of them to a cache, or the call that extends the caches
+int64_t shared_call_most(const psd_model_config &cfg, int S, int L, const KvCacheArg &kv);
 
 // ---------------------------------------------------------------- kernel launchers
 // elementwise.hip
@@ -447,6 +449,8 @@ bool plan_attention_shared(const SharedShape &sh, const SharedSegment *seg, int 
 bool plan_attention_weights(const SharedShape &sh, const SharedSegment *seg, int n, SharedLaunch *out);
 int64_t shared_attention_bytes(const SharedShape &sh, const SharedLaunch &ln);
 int64_t shared_weights_bytes(const SharedLaunch &ln);
+int64_t shared_attention_most(const SharedShape &sh, const SharedSegment *seg, int n);
+int64_t shared_weights_most(const SharedShape &sh, const SharedSegment *seg, int n);
 void launch_attention_shared(const void *q, const SharedShape &sh, SharedLaunch &ln, void *out, float *lse /* or NULL */, void *ws, hipStream_t st);
 void launch_attention_weights(const void *q, const SharedShape &sh, SharedLaunch &ln, const float *lse, int accumulate, void *ws, hipStream_t st);
 // values of the L rows of every sequence of qkv [S * L, ld_qkv] (columns from v_col on) transposed, for fp32 models

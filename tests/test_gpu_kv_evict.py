@@ -108,6 +108,15 @@ def test_kept_positions_near_and_far_apart(dtype, Hkv, dh, units, n, keep):
     run(data, Hkv, dh, keep, 1, 3)
 
 
+def test_units_without_any_position():
+    import paper_2605_15609_amd as psd
+    k, vt, w = torch.ones((3, 8, 128), dtype=BF, device=DEV), torch.ones((3, 128, 16), dtype=BF, device=DEV), torch.ones((3, 2, 8), device=DEV)
+    dst = [torch.full_like(t, 5.0) for t in (k, vt, w)]
+    lens = torch.full((3,), 7, dtype=torch.int32, device=DEV)
+    kept = psd.psd_kv_evict(psd.KvSegment(k, vt, 64, weights=w, length=0), psd.KvSegment(dst[0], dst[1], 64, weights=dst[2]), 4, 1, 1, kept_lens=lens)
+    assert (kept == -1).all() and (lens == 0).all() and all((t == 5.0).all() for t in dst)
+
+
 def test_other_stream_and_graph():
     import paper_2605_15609_amd as psd
     k, vt, w, _ = make(BF, 4, 64, 3, 500, seed=9)

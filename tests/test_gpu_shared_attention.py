@@ -179,6 +179,56 @@ def test_another_stream_and_a_replayed_graph():
         assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(ws, want_w)), i
 
 
+@pytest.mark.parametrize("shape", [(BF, 8, 8, 64, 4, 1), (BF, 28, 4, 128, 4, 32), (FP, 4, 2, 16, 2, 5)])
+def test_a_replayed_graph_follows_the_lengths_in_memory(shape):
+    import paper_2605_15609_amd as psd
+    dtype, H, Hkv, dh, S, L = shape
+    case = Case(dtype, H, Hkv, dh, S, L, [(S, 700, [700]), (1, 200, [200] * S)], seed=15)
+    q, keys, ws = case.device(DEV, (0, 1))
+    lens = [s.lens for s in keys.segments]
+    lse, out, work = torch.empty(case.q.shape[:3], device=DEV), torch.zeros_like(q), psd.psd_attention_workspace(q, keys)
+    work_w = torch.empty((256 + psd.psd_attention_weights_bytes(q, keys),), dtype=torch.uint8, device=DEV)
+
+    def step():
+        psd.psd_attention_shared(q, keys, out=out, lse=lse, ws=work)
+        psd.psd_attention_weights(q, keys, lse, accumulate=False, ws=work_w)
+    step()
+    torch.cuda.synchronize()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for a, b in ((700, 200), (0, 3), (65, 0), (0, 0), (699, 128)):
+        lens[0].fill_(a)
+        lens[1].copy_(torch.tensor([max(b - i, 0) for i in range(S)], dtype=torch.int32))
+        results = []
+        for run in (step, graph.replay):
+            for t in (out, lse, *ws):
+                t.fill_(5.0)
+            run()
+            torch.cuda.synchronize()
+            results.append([t.clone() for t in (out, lse, *ws)])
+        assert all(torch.equal(x, y) for x, y in zip(*results)), (a, b)
+        if a == 0 and b == 0:
+            assert (results[0][0] == 0).all() and torch.isneginf(results[0][1]).all() and (results[0][2] == 5.0).all()
+
+
+def test_calls_at_the_same_time_on_two_streams():
+    import paper_2605_15609_amd as psd
+    cases = [Case(BF, 28, 4, 128, 8, 32, [(8, 2000, None), (1, 300, None)], seed=16), Case(BF, 28, 4, 128, 8, 1, [(8, 5000, None), (1, 77, None)], seed=17)]
+    held = []
+    for case in cases:
+        q, keys, _ = case.device(DEV, ())
+        held.append((q, keys, psd.psd_attention_shared(q, keys), torch.empty_like(q), psd.psd_attention_workspace(q, keys), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, keys, _, out, work, stream in held:
+            with torch.cuda.stream(stream):
+                psd.psd_attention_shared(q, keys, out=out, ws=work)
+    torch.cuda.synchronize()
+    for _, _, want, out, _, _ in held:
+        assert torch.equal(out, want)
+
+
 def test_offsets_beyond_32_bits():
     import paper_2605_15609_amd as psd
     n, dh, ld_k, ld_vt = 2100, 128, 1 << 20, 1 << 24

@@ -74,7 +74,7 @@ def test_calls_check_pointers_and_workspace_before_anything_runs(lib):
     s, one = shape(), (B._Segment * 1)(long)
     need = ask(lib, s, long)
     assert need > 0
-    ok = dict(q=BASE, out=BASE, ws=BASE, n=need)
+    ok = dict(q=BASE, out=BASE + (1 << 20), ws=BASE, n=need)
 
     def call(**kw):
         a = dict(ok, **kw)
@@ -84,6 +84,45 @@ def test_calls_check_pointers_and_workspace_before_anything_runs(lib):
     assert lib.psd_attention_weights(C.byref(s), BASE, one, 1, None, 0, None, 0, None) < 0
     assert lib.psd_attention_weights(C.byref(s), None, one, 1, BASE, 0, None, 0, None) < 0
     assert lib.psd_attention_weights(C.byref(s), BASE, one, 1, BASE, 2, None, 0, None) < 0
+
+
+def test_an_output_on_its_queries_is_refused(lib):
+    one = (B._Segment * 1)(seg(len=5000, ld_vt=5008))
+
+    def call(q, out, ld_q, ld_out):     # (without a workspace: what is not refused for its addresses is refused for that)
+        assert lib.psd_attention_shared(C.byref(shape(ld_q=ld_q, ld_out=ld_out)), q, one, 1, out, None, None, 0, None) < 0
+        return b"overlaps" in lib.psd_last_error()
+    row = 512 * 2
+    assert call(BASE, BASE, 512, 512) and call(BASE, BASE + 16, 512, 512) and call(BASE + 7 * row, BASE, 512, 512)
+    assert call(BASE, BASE + row - 16, 2048, 2048) and call(BASE + row - 16, BASE, 2048, 2048) and call(BASE, BASE + row, 2048, 512)
+    assert not call(BASE, BASE + 8 * row, 512, 512) and not call(BASE + 8 * row, BASE, 512, 512)
+    assert not call(BASE, BASE + row, 2048, 2048) and not call(BASE + 3 * row, BASE, 2048, 2048)      # beside each other in the rows of one buffer
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,dtype", [(32, 32, 128, 1), (28, 4, 128, 1), (8, 8, 64, 1), (4, 4, 16, 0)])
+@pytest.mark.parametrize("prefix,length", [(0, 0), (0, 480), (1024, 288), (4096, 1024), (77, 0), (16000, 4000)])
+@pytest.mark.parametrize("L", [16, 32, 64])
+def test_the_workspace_of_model_calls_is_enough_for_fewer_sequences(lib, heads, kv_heads, d, dtype, prefix, length, L):
+    cfg = B._Config(2, heads * d, heads, kv_heads, d, 4 * heads * d, 5000, 4999, 1e-5, 0, dtype, 1.0, 32768, 1)
+    S, K, up = 24, 6, lambda n: (n + 63) // 64 * 64
+    kv = B._KvShared(BASE if prefix else None, BASE, BASE, BASE, prefix, prefix, max(length, 16), length, K, 0)
+    kv.prefix_weights = BASE if prefix else None
+    most = lib.psd_shared_workspace_bytes(C.byref(cfg), S, L, C.byref(kv)) - lib.psd_workspace_bytes(C.byref(cfg), S, L, L)
+    for n in range(1, S + 1):
+        for per in {1, K} if n % K == 0 else {1}:
+            w = kv_heads * d
+            sh = shape(S=n, L=L, n_heads=heads, n_kv_heads=kv_heads, d_head=d, dtype=dtype, ld_q=3 * heads * d, ld_out=heads * d)
+            block = seg(len=L, seqs_per_unit=1, ld_k=3 * heads * d, stride_k=L * 3 * heads * d, ld_vt=up(L), stride_vt=w * up(L))
+            first = [seg(len=prefix, seqs_per_unit=n, ld_k=w, ld_vt=up(prefix), weights=BASE, ld_w=prefix)] if prefix else []
+
+            def cache(keys):
+                return [seg(len=keys, seqs_per_unit=per, ld_k=w, ld_vt=up(keys), stride_k=keys * w, stride_vt=w * up(keys), weights=BASE, ld_w=keys,
+                            stride_w=kv_heads * keys)] if keys else []
+            sums = (n * L * heads * 4 + 255) // 256 * 256
+            for segs in (first + cache(length) + [block], first + cache(length + L)):
+                need = ask(lib, sh, *segs)
+                weights = lib.psd_attention_weights_bytes(C.byref(sh), (B._Segment * len(segs))(*segs), len(segs))
+                assert 0 <= need <= most and 0 <= weights and sums + max(need, weights if segs[-1] is block else 0) <= most, (n, per, need, weights, most)
 
 
 def evict(lib, src=None, dst=None, units=2, heads=4, d=64, dtype=1, keep=20, first=2, last=3, kept=BASE + (7 << 30)):
