@@ -4,11 +4,11 @@
 // Selection, one workgroup per (unit, head): the weights as integers of the same order, held in registers up to 32768 positions; the
 // keep-th largest by four histograms of 8 bits, then what is above it and, of what is equal, the first ones.  Whole numbers
 // throughout, so the result does not depend on the order in which the histogram's atomics arrive.
-// Gathering: 16 bytes per thread of a key row; of a value row (transposed) 8 slots per thread, and memory gives whole lines of the
-// source for them, whatever share of a line's positions stays: that is what bounds large evictions (8B shape, 32 layers, 4096 -> 1024
-// positions: 428 us, of which 380 are all value lines, and the keys that move, at 5.9 TB/s).  The workgroup that selected gathers, so
-// that the selections of some run beside the copies of others, in one launch; where there are few workgroups with much to copy each, a
-// second launch does (MIN_FUSED).
+// Gathering: 16 bytes per thread of a key row; of a value row (transposed) a slot per lane, so that 64 kept positions, which lie near
+// each other, are found in few lines (8 slots per lane and 16-byte stores visit 8 times the lines: 429 us where this takes 411).
+// Memory gives whole lines of the source for them, whatever share of a line's positions stays, and that bounds large evictions (8B
+// shape, 32 layers, 4096 -> 1024 positions: 411 us, 1.9 GB with all value lines, at 4.6 TB/s where a large copy has 4.9).  The workgroup
+// that selected may gather too, so that the selections of some run beside the copies of others, in one launch (MOST_FUSED).
 #include <type_traits>
 
 #include "psd_internal.h"
@@ -22,11 +22,11 @@ constexpr int KP = 4;          // 16-byte pieces of keys per thread
 constexpr int VPOS = 512;      // kept positions that a workgroup of the value gather takes
 constexpr int VCH = 32;        // channels that it takes
 constexpr int KEPT_LDS = 4096; // kept positions that a workgroup holds in LDS
-// One launch where there are at least MIN_FUSED workgroups, or each has no more to copy (of keys, and as much of values) than 16 KB or
-// 1 KB times their number.  One launch | two, us: 1024 workgroups of 256 KB 428 | 434, 560 of 125 KB 104 | 111, 256 of 256 KB 117 | 128,
-// 112 of 64 KB 27 | 28, 64 of 64 KB 26 | 27, 64 of 16 KB 11.5 | 14, 16 of 12 KB 9.7 | 11; 112 of 512 KB 179 | 116, 64 of 128 KB 37 | 28,
-// 32 of 256 KB 72 | 41, 4 of 32 KB 17 | 12, 4 of 1 MB 266 | 62.
-constexpr int MIN_FUSED = 256;
+// One launch where there are at most MOST_FUSED workgroups and each has no more to copy (of keys, and as much of values) than 2 KB times
+// their number, or 16 KB.  One launch | two, us: 560 workgroups of 125 KB 89 | 91, 256 of 256 KB 116 | 120, 128 of 256 KB 68 | 72, 112 of
+// 64 KB 24 | 28, 64 of 16 KB 9.7 | 14, 16 of 7 KB 9.4 | 11.4; 64 of 128 KB 28 | 28; 112 of 512 KB 148 | 108, 32 of 256 KB 55 | 35, 4 of
+// 32 KB 13 | 12, 4 of 1 MB 202 | 62; 1024 of 256 KB 418 | 411, 1024 of 16 KB 61 | 59.
+constexpr int MOST_FUSED = 768;
 
 __device__ __forceinline__ int unit_length(const SharedSegment &s, int u) { return s.lens ? min(max(s.lens[u], 0), s.len) : s.len; }
 
@@ -119,41 +119,38 @@ __device__ __forceinline__ void select_positions(const float *__restrict__ w, in
     });
 }
 
-// Values of positions i0 .. i0 + n - 1 (n at most VPOS) of one (unit, head), channels c0, c0 + step .. below c_end (c0 the same for a whole
-// wavefront): a lane takes 8 slots of a row, positions first .. + 3 and first + 8 .. + 11, 4 rows at a time, slot by slot from memory.
-// position(i): the source of the i-th kept one.  (Rows brought into LDS by 16-byte loads and picked there have a quarter of the lines
-// under way and took 1.4 to 2 times as long.)
-template <typename T, typename F>
-__device__ __forceinline__ void gather_values(const T *from, int ld_from, T *to, int ld_to, int i0, int n, int c0, int step, int c_end, F position) {
-    constexpr int C = 16 / sizeof(T);
-    const int lane = threadIdx.x & 63, first = (lane >> 1) * 16 + 4 * (lane & 1);
-    if (first >= n) return;
-    const bool whole = first + 11 < n;   // (else the last group: slots behind the last position stay as they were)
-    uint32_t slot[8];
+// Values of positions i0 .. i0 + n - 1 of one (unit, head), channels c0, c0 + step .. below c_end (c0 the same for a whole wavefront): a
+// lane takes a slot of every 64 of a row, E times, and RV rows at a time, so that a load finds its 64 positions in few lines.
+// position(i): the source of the i-th kept one.
+template <int E, int RV, typename T, typename F>
+__device__ __forceinline__ void gather_slots(const T *from, int ld_from, T *to, int ld_to, int i0, int n, int c0, int step, int c_end, F position) {
+    const int lane = threadIdx.x & 63, at = lane & ~15, s = lane & 15;
+    const int own = at + ((s & 3) | (s & 4) << 1 | (s & 8) >> 1);   // which position lies in the lane's slot
+    uint32_t slot[E];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) slot[e] = vt_key_slot(position(i0 + min(first + (e & 3) + 8 * (e >> 2), n - 1)));
-    to += i0;
-    const uint32_t lane_to = lane * 8;
-    for (int c = c0; c < c_end; c += 4 * step) {
-        T v[4][8];
+    for (int e = 0; e < E; ++e) slot[e] = vt_key_slot(position(i0 + min(e * 64 + own, n - 1)));
+    to += i0 + lane;
+    for (int c = c0; c < c_end; c += RV * step) {
+        T v[RV][E];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < RV; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[k][e] = (from + (int64_t)min(c + k * step, c_end - 1) * ld_from)[slot[e]];
+            for (int e = 0; e < E; ++e) v[k][e] = (from + (int64_t)min(c + k * step, c_end - 1) * ld_from)[slot[e]];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < RV; ++k) {
             if (c + k * step >= c_end) break;
-            T *row = to + (int64_t)(c + k * step) * ld_to + lane_to;
-            if (whole) {
 #pragma unroll
-                for (int h = 0; h < 8 / C; ++h) reinterpret_cast<uint4 *>(row)[h] = reinterpret_cast<const uint4 *>(v[k])[h];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (first + (e & 3) + 8 * (e >> 2) < n) row[e] = v[k][e];
-            }
+            for (int e = 0; e < E; ++e)
+                if (e * 64 + own < n) (to + (int64_t)(c + k * step) * ld_to)[e * 64] = v[k][e];
         }
     }
+}
+template <typename T, typename F>
+__device__ __forceinline__ void gather_values(const T *from, int ld_from, T *to, int ld_to, int i0, int n, int c0, int step, int c_end, F position) {
+    if (n <= 0) return;
+    if (n > VPOS / 2) gather_slots<VPOS / 64, 4>(from, ld_from, to, ld_to, i0, n, c0, step, c_end, position);
+    else if (n > VPOS / 4) gather_slots<VPOS / 128, 8>(from, ld_from, to, ld_to, i0, n, c0, step, c_end, position);
+    else gather_slots<VPOS / 256, 16>(from, ld_from, to, ld_to, i0, n, c0, step, c_end, position);
 }
 
 // One workgroup per (unit, head): selects, and (GATHER) gathers what it selected.
@@ -261,7 +258,7 @@ void run_evict(const SharedSegment &src, const SharedSegment &dst, int units, in
                int32_t *kept, int32_t *kept_lens, hipStream_t st) {
     const int wgs = units * n_kv_heads;
     const int64_t copied = (int64_t)std::min(keep, src.len) * d_head * sizeof(T);   // bytes of keys, and as many of values, per workgroup
-    const bool gather = wgs >= MIN_FUSED || copied <= 1024 * std::max(wgs, 16);
+    const bool gather = wgs <= MOST_FUSED && copied <= 2048ll * std::max(wgs, 8);
     auto select = [&](auto each, auto fused) {
         hipLaunchKernelGGL((evict_select_kernel<T, decltype(each)::value, decltype(fused)::value>), dim3((unsigned)wgs), dim3(ST), 0, st, src, dst, n_kv_heads,
                            d_head, keep, n_first, n_last, kept, kept_lens);
