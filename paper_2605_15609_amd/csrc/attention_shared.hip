@@ -9,6 +9,12 @@
 // rows that see it: the rows of a unit that read one KV head are stacked into tiles, whatever sequence or query head they belong
 // to, each tile walks the unit's keys (or, where there are few tiles, a part of them), and a second kernel joins a row's parts.
 //
+// What bounds it, with bf16 heads of 128: 128 drafts of 64 rows of the 8B shape over 4096 + 1024 + 64 keys take 670 us, 1.04 PFLOP/s (a
+// large library product has 1.22 here): the matrix cores are busy 57 % of a clock that power holds near 1.6 GHz, the rest goes to the
+// exponentials beside them (6 vector instructions a product).  32 single rows of the 7B shape over 32768 shared keys take 40 us, 34 of
+// them the attention (67 MB of keys and values, 2 TB/s): 13 tiles of keys a workgroup at 2 us each, a wait for other wavefronts or for
+// a tile in nearly half of it.  Small calls are one chain of round trips: about 8 us.
+//
 // Per tile the problem is transposed as in attention_mfma.hip: S^T = K Q^T, O^T += V^T P^T.  A lane owns one row; the softmax stays
 // in its registers, and the probabilities are the second product's operand as they are.
 #include <algorithm>
@@ -256,9 +262,10 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc_o[ct][v] = 0.f;
-    // Keys of the next step go out when the scores of this one are done, its values before them: a step is one round trip to memory
-    // where it would be two.  (Heads of 128 in fp32 have no registers for that; 32 keys of the 8B shape a wavefront: AHEAD_US.)
-    constexpr bool AHEAD = sizeof(T) * DH <= 256;
+    // bf16: keys of the next step go out when the scores of this one are done, its values before them: a step is one round trip to memory
+    // where it would be two (4 rows of 8 heads of 64 channels over 317 keys: 8.4 us, 9.2 without).  fp32 (slower
+    // products, twice the registers) gains nothing: 8.8 us and 8.6 without at 48 rows of 8 heads of 64 over 426 keys.
+    constexpr bool AHEAD = sizeof(T) == 2;
     float m_run = -INFINITY, neg_m = NO_MAX, l_run = 0.f;
     Frag<T> kf[KS], vf[BK / 16][CT];
     auto load_keys = [&](const Step &s) {
@@ -381,7 +388,10 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
 // Many rows (bf16): a tile of 128 rows, 32 to a wavefront, walks tiles of 64 keys that pass through LDS, fetched a tile ahead by
 // loads that go to LDS directly (chunks of 16 bytes swizzled on the way, as in attention_mfma.hip).  The rows of the tile share the unit
 // of the job's first segment; of the others the tile walks every unit that one of its rows sees, and hides it from the rows that do not.
-// The keys of one unit are a run: whole tiles that all rows of a wavefront see go through a loop of their own, without masks.
+// The keys of one unit are a run.  The rows of a wavefront see a run as a whole or not at all (walked_tiles), so a wavefront leaves out the
+// tiles that its rows do not see and masks only the last tile of a unit.
+// Tried and slower at 128 drafts of the 8B shape (where this took 745 us): 256 rows and 8 wavefronts, in step or half a tile apart 813 and
+// more; halves of a tile pipelined, the exponentials of one beside the products of two others, 786; three tiles under way 860.
 struct Run {
     const bf16_t *k, *vt;             // at its first tile
     int ld_k, ld_vt, keys, tiles;     // keys from there on, tiles of this workgroup
@@ -623,7 +633,7 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
 
 // The parts of a row joined: a thread takes 4 channels of every G-th part, and the G sums, each relative to a maximum of its own, are
 // joined in order.  G = 8 where there are many parts of few rows: every load is a round trip to memory, so as many as possible are
-// under way at a time (896 rows of 60 parts: 21 us with one loop over all maxima in front, JOIN_US without).
+// under way at a time (896 rows of 60 parts: 21 us with one loop over all maxima in front, 5.8 without).
 template <typename T, int DH, int G>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, SharedLaunch ln, float sl2) {
     constexpr int TPR = DH / 4, RPW = 256 / (TPR * G);   // threads per part, rows per workgroup
@@ -692,7 +702,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, Shared
 // walks the rows in tiles of WR that pass through LDS, fetched a tile ahead; a lane adds up what its row of every tile gives, and the
 // lanes are added at the end.  Where a unit has few keys and many rows, workgroups take a part of the rows each and a second kernel
 // adds the parts.  Every sum has an order that the shapes alone decide.
-// Bound: 64 exponentials a lane (a quarter of the rate) and as many additions and multiply-adds stand against 32 MFMAs a tile.
+// Bound: 64 exponentials a lane (a quarter of the rate) and as many additions and multiply-adds stand against 32 MFMAs a tile (16 x 64 rows
+// of the 7B shape over 2048 shared and up to 4001 own keys: 61 us, 0.33 PFLOP/s; the attention before it 100, its join 11).
 template <typename T>
 constexpr int NKEYS = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
