@@ -215,12 +215,14 @@ __device__ __forceinline__ float both_sum(float v) {
 // wavefronts deal the keys, BK at a time, operands straight from memory, and merge in LDS in wavefront order.  A job of several segments
 // reads the keys of the coarser ones once for every tile, which pays where one launch then does what two would (4 rows of 8 heads of 64
 // channels over 256 shared and 61 own keys: 11.4 us with parts and a join, 9.2 so).
-template <typename T, int DH>
+// W = 1: the workgroup's wavefronts have a unit each, where there are many units of few keys (184 single rows of the 8B shape, 4510 keys
+// shared and one their own: 83 us, 52 so; 300 single rows of 8 heads of 64, 800 shared and 120 own: 30, 24; up to 256 own: no difference).
+template <typename T, int DH, int W>
 __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedShape &sh, const SharedLaunch &ln, const SharedJob &jb, int u, int kvh,
                                          int tile, int split, float sl2, float *part /* [wavefront][max, sum, NF values][64 lanes] */) {
     constexpr int KS = DH / 16, CT = (DH + 31) / 32, NF = CT * 16;   // contraction steps of the scores, channel subtiles, output values per lane
     const int spu = ln.seg[jb.seg + jb.segs - 1].seqs_per_unit;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, lrow = lane & 31, half = lane >> 5;
     const int rows = spu * sh.L * (sh.n_heads / sh.n_kv_heads), r = tile * TR + lrow;
     const RowOf row(sh, (int64_t)u * spu, kvh, min(r, rows - 1));   // (rows past the last repeat it and store nothing)
     // lane i: the unit of the job's segment i that holds the rows (see many_rows)
@@ -251,7 +253,7 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
             s.k0 = (st - begin) * BK;
             return;
         }
-        s.k0 += NW * BK;
+        s.k0 += W * BK;
     };
     Frag<T> qf[KS];
 #pragma unroll
@@ -285,7 +287,7 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
         go(next, first + wave);
         if (AHEAD) load_keys(next);
     }
-    for (int st = first + wave; st < last; st += NW) {
+    for (int st = first + wave; st < last; st += W) {
         const Step here = next;
         const int k0 = here.k0, left = here.keys - k0;
         if constexpr (!AHEAD) load_keys(here);
@@ -298,8 +300,8 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
         for (int v = 0; v < 16; ++v) x[v] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) product(kf[ks], qf[ks], x);
-        if (st + NW < last) {
-            go(next, st + NW);
+        if (st + W < last) {
+            go(next, st + W);
             if (AHEAD) load_keys(next);
         }
         // x[v] <-> key 8 (v / 4) + 4 half + v % 4 of the step
@@ -346,6 +348,20 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
     }
     l_run = both_sum(l_run);   // the halves of a row hold disjoint keys
 
+    if constexpr (W == 1) {
+        if (r >= rows) return;
+        const PartOut<T, DH> to(sh, ln, jb.part0 + split, row);
+        if (half == 0) to.sums(m_run, l_run, -neg_m);
+        const float inv = to.factor(l_run);
+        if (inv == 0.f && !to.direct) return;
+#pragma unroll
+        for (int g = 0; g < NF / 4; ++g) {
+            const int c = (g >> 2) * 32 + 8 * (g & 3) + 4 * half;
+            const float o[4] = {acc_o[g >> 2][4 * (g & 3)], acc_o[g >> 2][4 * (g & 3) + 1], acc_o[g >> 2][4 * (g & 3) + 2], acc_o[g >> 2][4 * (g & 3) + 3]};
+            if (c < DH) to.values(c, o, inv);
+        }
+        return;
+    }
     float *mine = part + wave * (2 + NF) * 64 + lane;
     mine[0] = m_run;
     mine[64] = l_run;
@@ -620,6 +636,12 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
     int j = 0;
     while (j + 1 < ln.n_jobs && (int)blockIdx.x >= ln.job[j + 1].block0) ++j;
     const SharedJob &jb = ln.job[j];
+    if (jb.packed) {
+        const int n = jb.units * sh.n_kv_heads, run = ((n + NW - 1) / NW + 7) / 8, local = blockIdx.x - jb.block0;
+        const int of = __builtin_amdgcn_readfirstlane(((local & 7) * run + (local >> 3)) * NW + (threadIdx.x >> 6));
+        if (local >> 3 < run && of < n) few_rows<T, DH, 1>(q, sh, ln, jb, of / sh.n_kv_heads, of % sh.n_kv_heads, 0, 0, sl2, nullptr);
+        return;
+    }
     Place at;
     if (!place_of(jb, sh.n_kv_heads, at)) return;
     if constexpr (sizeof(T) == 2) {
@@ -628,7 +650,7 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
             return;
         }
     }
-    few_rows<T, DH>(q, sh, ln, jb, at.u, at.kvh, at.tile, at.split, sl2, reinterpret_cast<float *>(lds));
+    few_rows<T, DH, NW>(q, sh, ln, jb, at.u, at.kvh, at.tile, at.split, sl2, reinterpret_cast<float *>(lds));
 }
 
 // The parts of a row joined: a thread takes 4 channels of every G-th part, and the G sums, each relative to a maximum of its own, are
@@ -907,8 +929,14 @@ void run_weights(const T *q, const float *lse, const SharedShape &sh, const Shar
 // the join costs, its launch and the parts' way through memory.
 constexpr double ALONE = 0.65, FEW = 1.5, FEW_FP32 = 2.0, WG_FIXED = 2.0, JOIN_FIXED = 1.5, STEP_SECONDS = 2.3e-6, PART_RATE = 6e12;
 constexpr int SLOTS = 512;
+constexpr int PACKED_STEPS = 4;   // of BK keys: up to there a wavefront takes a unit by itself where there are more of them than SLOTS
 constexpr int64_t MOST_PART_ROWS = 1 << 17;   // rows times parts, where segments are cut: 1024 tiles of 128 rows
 int rows_per_unit(const SharedShape &sh, const SharedSegment &s) { return s.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads); }
+
+int64_t workgroups(const SharedJob &jb, int n_kv_heads, int splits) {
+    const int64_t n = (int64_t)jb.units * n_kv_heads;
+    return jb.packed ? (n + NW - 1) / NW : n * jb.tiles * splits;
+}
 
 // key tiles of 64 that a tile of MT rows of segments [a, b] walks at most (0: not possible), and as a share of that on average: units of
 // lengths of their own are taken to be half full
@@ -935,7 +963,7 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
     const int n = ln.n_segs;
     if (n == 0) return ln;
     const double few = sh.dtype == PSD_DTYPE_BF16 ? FEW * sh.d_head / 128 : FEW_FP32 * sh.d_head / 64;
-    double best = -1.0;
+    double best = -1.0, each_of[kMaxSegments] = {};
     // bit i of a cut: a job ends with segment i.  Jobs of more than one segment: tiles of MT rows of the first one's units, or (the second
     // half of the choices, where the cut has such a job) of TR rows of the last one's, which read the keys of the coarser ones each for itself
     for (int choice = 0; choice < 1 << n; ++choice) {
@@ -962,7 +990,8 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
                     if (ln.seg[i].lens) half += (ln.seg[i].len + BK - 1) / BK;
                 }
                 full[jobs] = 1.0 - 0.5 * half / steps;
-                steps = (steps + NW - 1) / NW;
+                jb.packed = steps <= PACKED_STEPS && per_unit <= TR && (int64_t)(sh.S / ln.seg[of].seqs_per_unit) * sh.n_kv_heads > SLOTS;
+                if (!jb.packed) steps = (steps + NW - 1) / NW;
                 keys[jobs] = steps > 1 << 30 ? 0 : (int)steps;
             }
             if (keys[jobs] == 0) possible = false;
@@ -970,17 +999,17 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
             jb.segs = b - a + 1;
             jb.units = sh.S / ln.seg[of].seqs_per_unit;
             jb.tiles = (per_unit + (jb.tiled ? MT : TR) - 1) / (jb.tiled ? MT : TR);
-            rows[jobs] = (int64_t)jb.units * sh.n_kv_heads * jb.tiles;
+            rows[jobs] = workgroups(jb, sh.n_kv_heads, 1);
             most = std::max(most, keys[jobs]);
         }
         if (!possible) continue;
-        for (int pieces = 1; pieces <= most; pieces += std::max(1, pieces / 4)) {   // of the longest job
+        for (int pieces = 1; pieces <= most; pieces += std::max(1, pieces / 8)) {   // of the longest job
             const double share = (double)most / pieces;
             int64_t wgs = 0, parts = 0;
-            double longest = 0.0, work = 0.0;
+            double longest = 0.0, work = 0.0, each[kMaxSegments];
             int splits[kMaxSegments];
             for (int j = 0; j < jobs; ++j) {
-                splits[j] = std::min(keys[j], std::max(1, (int)(keys[j] * (job[j].tiled ? 1.0 : few) / share + 0.999)));
+                splits[j] = job[j].packed ? 1 : std::min(keys[j], std::max(1, (int)(keys[j] * (job[j].tiled ? 1.0 : few) / share + 0.999)));
                 parts += splits[j];
             }
             if (parts > jobs && parts * sh.n_rows > MOST_PART_ROWS) {   // (a part of every row and job is the least that there is)
@@ -989,9 +1018,9 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
             }
             for (int j = 0; j < jobs; ++j) {
                 const double step = job[j].tiled ? 1.0 : few;
-                const double each = (keys[j] + splits[j] - 1) / splits[j] * step + WG_FIXED;
-                longest = std::max(longest, each);
-                work += (each - (1.0 - full[j]) * keys[j] / splits[j] * step) * rows[j] * splits[j];
+                each[j] = (keys[j] + splits[j] - 1) / splits[j] * step + WG_FIXED;
+                longest = std::max(longest, each[j]);
+                work += (each[j] - (1.0 - full[j]) * keys[j] / splits[j] * step) * rows[j] * splits[j];
                 wgs += rows[j] * splits[j];
             }
             // one round lasts as long as its longest workgroup, many as long as the work
@@ -1006,19 +1035,25 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
                 SharedJob &jb = ln.job[j];
                 jb = job[j];
                 jb.splits = splits[j];
+                each_of[j] = each[j];
                 jb.part0 = ln.parts;
                 ln.parts += jb.splits;
                 ln.blocks += align_up(rows[j] * jb.splits, 8);
             }
         }
     }
-    // short workgroups first: the long ones take their places in turn
-    std::stable_sort(ln.job, ln.job + ln.n_jobs, [](const SharedJob &a, const SharedJob &b) { return a.tiled < b.tiled; });
+    // long workgroups first, short ones fill what they leave (16 x 64 rows of the 7B shape over 2048 shared and up to 4001 own keys, with
+    // weights: 183 us in the order of the segments, 177 so)
+    for (int j = 1; j < ln.n_jobs; ++j)
+        for (int i = j; i > 0 && each_of[i] > each_of[i - 1]; --i) {
+            std::swap(each_of[i], each_of[i - 1]);
+            std::swap(ln.job[i], ln.job[i - 1]);
+        }
     int64_t block = 0;
     for (int j = 0; j < ln.n_jobs; ++j) {
         SharedJob &jb = ln.job[j];
         jb.block0 = (int)block;   // (grids of 2^31 workgroups and more are refused)
-        block += align_up((int64_t)jb.units * sh.n_kv_heads * jb.splits * jb.tiles, 8);
+        block += align_up(workgroups(jb, sh.n_kv_heads, jb.splits), 8);
     }
     if (ln.parts == 1) ln.parts = 0;
     return ln;

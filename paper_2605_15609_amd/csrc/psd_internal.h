@@ -424,10 +424,10 @@ struct SharedShape {
     int64_t ld_q, ld_out, n_rows;        // n_rows = S * L * n_heads
 };
 constexpr int kMaxSegments = PSD_MAX_SEGMENTS;
-// what one launch does: jobs behind one another in the grid.  A job's workgroups take a tile of rows of a unit of its first segment
-// against the keys of `segs` segments from `seg` on, or a part of them
+// what one launch does: jobs behind one another in the grid.  A job's workgroups take a tile of rows of a unit (tiled: of its first
+// segment, else of its last) against the keys of `segs` segments from `seg` on, or a part of them
 struct SharedJob {
-    int seg, segs, tiled, units, tiles, splits, block0, part0;
+    int seg, segs, tiled, packed, units, tiles, splits, block0, part0;   // packed: a unit and KV head to a wavefront
 };
 struct SharedLaunch {
     int n_jobs = 0, n_segs = 0, parts = 0;   // parts = 0: every row's one part goes straight to the output

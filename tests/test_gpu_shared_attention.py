@@ -70,6 +70,14 @@ def test_long_segments_are_cut_and_joined(dtype, H, Hkv, dh):
     check(Case(dtype, H, Hkv, dh, 4, 40, [(4, 1500, None), (2, 700, [3, 700]), (1, 40, None)], seed=6), weights=(0, 1))
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,dh,S,L", [(BF, 8, 8, 64, 70, 3), (BF, 28, 4, 128, 132, 1), (BF, 8, 8, 128, 66, 4), (FP, 8, 8, 32, 68, 2), (FP, 4, 4, 16, 131, 7)])
+def test_many_units_of_few_keys(dtype, H, Hkv, dh, S, L):
+    lens = [(37 * i) % 101 for i in range(S)]
+    check(Case(dtype, H, Hkv, dh, S, L, [(S, 150, None), (1, 100, lens), (1, 19, None)], seed=S), weights=(1,))
+    check(Case(dtype, H, Hkv, dh, S, L, [(1, 128, [128 - n for n in lens])], seed=S + 1), weights=(0,))
+    check(Case(dtype, H, Hkv, dh, S, L, [(1, 1, [i % 2 for i in range(S)])], seed=S + 2))
+
+
 def test_four_levels():
     check(Case(BF, 8, 2, 64, 8, 16, [(8, 130, None), (4, 65, [65, 10]), (2, 40, [1, 2, 40, 0]), (1, 16, None)], seed=7), weights=(0, 1, 2, 3))
 
