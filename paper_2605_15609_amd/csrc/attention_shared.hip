@@ -9,11 +9,11 @@
 // rows that see it: the rows of a unit that read one KV head are stacked into tiles, whatever sequence or query head they belong
 // to, each tile walks the unit's keys (or, where there are few tiles, a part of them), and a second kernel joins a row's parts.
 //
-// What bounds it, with bf16 heads of 128: 128 drafts of 64 rows of the 8B shape over 4096 + 1024 + 64 keys take 670 us, 1.04 PFLOP/s (a
-// large library product has 1.22 here): the matrix cores are busy 57 % of a clock that power holds near 1.6 GHz, the rest goes to the
-// exponentials beside them (6 vector instructions a product).  32 single rows of the 7B shape over 32768 shared keys take 40 us, 34 of
-// them the attention (67 MB of keys and values, 2 TB/s): 13 tiles of keys a workgroup at 2 us each, a wait for other wavefronts or for
-// a tile in nearly half of it.  Small calls are one chain of round trips: about 8 us.
+// What bounds it, with bf16 heads of 128: 128 drafts of 64 rows of the 8B shape over 4096 + 1024 + 64 keys take 680 us, 1.02 PFLOP/s (a
+// large library product has 1.22 here): the matrix cores are busy 57 % of a clock that power holds near 1.65 GHz, the rest goes to the
+// exponentials beside them (6 vector instructions a product).  32 single rows of the 7B shape over 32768 shared keys take 40 us, 32 of
+// them the attention (67 MB of keys and values): 11 tiles of keys a workgroup at 2.3 us each, a wait for other wavefronts or for a tile in
+// nearly half of it.  Small calls are one chain of round trips: about 8 us.
 //
 // Per tile the problem is transposed as in attention_mfma.hip: S^T = K Q^T, O^T += V^T P^T.  A lane owns one row; the softmax stays
 // in its registers, and the probabilities are the second product's operand as they are.
@@ -725,7 +725,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, Shared
 // lanes are added at the end.  Where a unit has few keys and many rows, workgroups take a part of the rows each and a second kernel
 // adds the parts.  Every sum has an order that the shapes alone decide.
 // Bound: 64 exponentials a lane (a quarter of the rate) and as many additions and multiply-adds stand against 32 MFMAs a tile (16 x 64 rows
-// of the 7B shape over 2048 shared and up to 4001 own keys: 61 us, 0.33 PFLOP/s; the attention before it 100, its join 11).
+// of the 7B shape over 2048 shared and up to 4001 own keys: 61 - 64 us, 0.33 PFLOP/s; the attention before it 96, its join 12).
 template <typename T>
 constexpr int NKEYS = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
