@@ -775,6 +775,8 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__r
         head[i] = r % group;
         from[i] = q + (s0 * sh.L + r / group) * sh.ld_q + (kvh * group + head[i]) * DH + tid % CH * C;
     }
+    // (rows past the last one: the unit's first, whose weight is taken away by an infinite z; zeros would make NaN of infinite keys)
+    const T *spare = q + s0 * sh.L * sh.ld_q + kvh * group * DH + tid % CH * C;
     int z_head = (first * WR + tid) % group;
     const float *z_from = lse + (s0 * sh.L + (first * WR + tid) / group) * sh.n_heads + kvh * group + z_head;
     uint4 held[LOADS];
@@ -782,9 +784,10 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__r
     auto fetch = [&](int t) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const bool there = loads && t * WR + tid / CH + i * STEP < rows;
+            const T *p = from[i];
+            if (t * WR + tid / CH + i * STEP >= rows) p = spare;
             held[i] = make_uint4(0, 0, 0, 0);
-            if (there) held[i] = *reinterpret_cast<const uint4 *>(from[i]);
+            if (loads) held[i] = *reinterpret_cast<const uint4 *>(p);
             from[i] += tokens * sh.ld_q + heads * DH;
             head[i] += heads;
             if (head[i] >= group) {
@@ -805,7 +808,8 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__r
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
             if (loads) *reinterpret_cast<uint4 *>(tiles[stage] + place(tid / CH + i * STEP, tid % CH)) = held[i];
-        if (tid < WR) z2[stage][tid] = held_z * LOG2E;
+        // (a row without a score above -inf gives nothing either)
+        if (tid < WR) z2[stage][tid] = held_z == -INFINITY ? INFINITY : held_z * LOG2E;
     };
     float w[NK][16];
 #pragma unroll

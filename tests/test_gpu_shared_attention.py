@@ -1,5 +1,7 @@
 """Attention over segments of keys that a batch shares, and the weights that the keys draw, against 64-bit references.  The bounds are
 derived in shared_common.Case.reference."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -185,6 +187,24 @@ def test_another_stream_and_a_replayed_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(ws, want_w)), i
+
+
+@pytest.mark.parametrize("dtype,n,L", [(BF, 1, 1), (BF, 130, 64), (FP, 40, 5)])
+def test_rows_that_score_minus_infinity_everywhere(dtype, n, L):
+    import paper_2605_15609_amd as psd
+    S, H, dh = 2, 4, 64
+    q = torch.rand((S, L, H, dh), generator=torch.Generator().manual_seed(n)).to(dtype).to(DEV) + 0.5
+    k, vt = torch.full((S, n, H * dh), -math.inf, dtype=dtype, device=DEV), torch.ones((S, H * dh, (n + 15) // 16 * 16), dtype=dtype, device=DEV)
+    k[1] = 1.0        # the second sequence's keys are ordinary ones
+    w, lse = torch.full((S, H, n), 0.25, device=DEV), torch.empty((S, L, H), device=DEV)
+    keys = psd.KvSegments([psd.KvSegment(k, vt, dh, weights=w)])
+    out = psd.psd_attention_shared(q, keys, lse=lse)
+    psd.psd_attention_weights(q, keys, lse)
+    torch.cuda.synchronize()
+    assert (out[0] == 0).all() and torch.isneginf(lse[0]).all() and (w[0] == 0.25).all()
+    # the same values everywhere, so out is a sum of n equal terms over their sum: n - 1 additions each and a division, half a step apiece
+    assert (out[1].double() - 1).abs().max() <= 2 * n * 2.0 ** -24 and torch.isfinite(lse[1]).all()
+    assert abs(float(w[1].double().sum()) - (0.25 * n + L) * H) < 1e-4 * n * L * H
 
 
 @pytest.mark.parametrize("shape", [(BF, 8, 8, 64, 4, 1), (BF, 28, 4, 128, 4, 32), (FP, 4, 2, 16, 2, 5)])
