@@ -1143,6 +1143,10 @@ int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, c
     if (!q || !lse) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL q / lse");
     if (misaligned16(q)) PSD_FAIL(PSD_ERR_SHAPE, "q must be 16-byte aligned");
     if (accumulate != 0 && accumulate != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "accumulate %d", accumulate);
+    for (int i = 0; i < n_segments; ++i)
+        for (int j = 0; j < i; ++j)
+            if (seg[i].weights && seg[i].weights == seg[j].weights && seg[i].len > 0 && seg[j].len > 0)
+                PSD_FAIL(PSD_ERR_INVALID_ARG, "segments %d and %d have the same weights", j, i);
     SharedLaunch ln;
     if (!plan_attention_weights(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
     const int64_t need = shared_weights_bytes(ln);

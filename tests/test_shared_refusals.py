@@ -125,6 +125,15 @@ def test_the_workspace_of_model_calls_is_enough_for_fewer_sequences(lib, heads, 
                 assert 0 <= need <= most and 0 <= weights and sums + max(need, weights if segs[-1] is block else 0) <= most, (n, per, need, weights, most)
 
 
+def test_weights_of_two_segments_in_one_place_are_refused(lib):
+    def call(second):      # (one that is not refused for its weights is refused for the missing lse)
+        two = (B._Segment * 2)(seg(weights=BASE, ld_w=50), seg(weights=second, ld_w=50, stride_w=200, seqs_per_unit=1))
+        return lib.psd_attention_weights(C.byref(shape()), BASE, two, 2, BASE, 0, None, -1, None) if second == BASE else \
+            lib.psd_attention_weights(C.byref(shape()), BASE, two, 2, None, 0, None, 0, None)
+    assert call(BASE) < 0 and b"same weights" in lib.psd_last_error()
+    assert call(BASE + (1 << 20)) < 0 and b"same weights" not in lib.psd_last_error()
+
+
 def evict(lib, src=None, dst=None, units=2, heads=4, d=64, dtype=1, keep=20, first=2, last=3, kept=BASE + (7 << 30)):
     base = dict(weights=BASE + (2 << 30), ld_w=50, stride_w=200, len=50)
     s = seg(**dict(base, **(src or {})))
