@@ -45,7 +45,6 @@ template <>
 struct Frag<bf16_t> {
     uint4 v;
     __device__ void load(const bf16_t *p) { v = *reinterpret_cast<const uint4 *>(p); }
-    __device__ void zero() { v = make_uint4(0, 0, 0, 0); }
     // keeps the slots of keys before `left`; the lane's slots are keys 0 - 3 and 8 - 11 (from its half on)
     __device__ void keep(int left) {
         const int hi = left - 8;
@@ -61,10 +60,6 @@ struct Frag<float> {
     __device__ void load(const float *p) {
         const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
         v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    }
-    __device__ void zero() {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
     }
     __device__ void keep(int left) {
 #pragma unroll
