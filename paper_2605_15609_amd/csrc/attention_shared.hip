@@ -929,6 +929,7 @@ void run_weights(const T *q, const float *lse, const SharedShape &sh, const Shar
 constexpr double ALONE = 0.65, FEW = 1.5, FEW_FP32 = 2.0, WG_FIXED = 2.0, JOIN_FIXED = 1.5, STEP_SECONDS = 2.3e-6, PART_RATE = 6e12;
 constexpr int SLOTS = 512;
 constexpr int PACKED_STEPS = 4;   // of BK keys: up to there a wavefront takes a unit by itself where there are more of them than SLOTS
+constexpr int MOST_TOUCHED = 8;   // units of a finer segment that the tiles of a walk may touch
 constexpr int64_t MOST_PART_ROWS = 1 << 17;   // rows times parts, where segments are cut: 1024 tiles of 128 rows
 int rows_per_unit(const SharedShape &sh, const SharedSegment &s) { return s.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads); }
 
@@ -947,7 +948,7 @@ int walked_tiles(const SharedShape &sh, const SharedSegment *seg, int a, int b, 
         const int64_t fine = rows_per_unit(sh, seg[i]);
         if (i > a && fine % 32) return 0;   // (see many_rows)
         const int64_t touched = i == a ? 1 : std::min<int64_t>((std::min<int64_t>(rows, MT) + fine - 1) / fine + (MT % fine && fine % MT ? 1 : 0), rows / fine);
-        if (touched > 8) return 0;
+        if (touched > MOST_TOUCHED) return 0;
         keys += touched * ((seg[i].len + KT - 1) / KT);
         if (seg[i].lens) half += touched * ((seg[i].len + KT - 1) / KT);
     }
@@ -1125,8 +1126,13 @@ int64_t shared_attention_bytes(const SharedShape &sh, const SharedLaunch &ln) {
 }
 // the most that any batch of 1 .. sh.S sequences over these segments needs, however they share them
 int64_t shared_attention_most(const SharedShape &sh, const SharedSegment *seg, int n) {
+    // No job has more parts than key tiles: those of a segment, or, of a finer segment in a walk, of every unit that a tile touches,
+    // of which there are no more than sequences.
     int64_t steps = 0;
-    for (int i = 0; i < n; ++i) steps += (seg[i].len + BK - 1) / BK;   // (no job is cut finer)
+    for (int i = 0; i < n; ++i) {
+        const int64_t walked = (int64_t)(i == 0 ? 1 : std::min(sh.S, MOST_TOUCHED)) * ((seg[i].len + KT - 1) / KT);
+        steps += std::max<int64_t>((seg[i].len + BK - 1) / BK, walked);
+    }
     const int64_t rows = std::max(n * sh.n_rows, std::min(MOST_PART_ROWS, steps * sh.n_rows));
     return align_up(rows * sh.d_head * 4, 256) + align_up(rows * 8, 256);
 }

@@ -309,3 +309,30 @@ def test_shared_calls_refuse():
     top1, conf = torch.empty((2, L), dtype=torch.int32, device=DEV), torch.empty((2, L), device=DEV)
     assert model.lib.psd_forward_confidence_shared(model.handle, d.data_ptr(), 2, 256, 96, L, C.byref(c), top1.data_ptr(), conf.data_ptr(), None,
                                                    small.data_ptr(), 4096, None) == -3
+
+
+@pytest.mark.parametrize("L,P,own,K", [(16, 96, 16, 3), (32, 96, 96, 4)])
+def test_one_request_whose_drafts_share_a_tile(L, P, own, K):
+    """Few heads: the rows of all drafts are one tile, which walks prefix, cache and every draft's block, cut into more parts than the
+    segments have steps of 32 keys."""
+    import paper_2605_15609_amd as psd
+    shape, tol = MODELS["gqa-bias-dh128"]
+    shape = _bc(shape)
+    t, start = _batch(shape, 1, P, own, L, 71)
+    N = t.shape[1]
+    host = inp.draw_model(shape, N)
+    model = psd.Model.from_host(host, DEV)
+    kv = _prefilled(psd, model, _dev(t), P, own, L, own + L)
+    rng = np.random.default_rng(6)
+    drafts = np.repeat(t, K, axis=0)
+    for i, row in enumerate(drafts):
+        masked = np.nonzero(row[start:start + L] == shape.mask_id)[0][:2 * i]
+        row[start + masked] = rng.integers(0, shape.vocab - 1, size=len(masked))
+    print(f"[shared model] one tile L={L} P={P} own={own} K={K}", flush=True)
+    top1, conf, logits = psd.psd_forward_confidence_shared(model, _dev(drafts), start, L, kv, seqs_per_cache=K, want_logits=True)
+    logits = logits.cpu().numpy().reshape(K, L, -1)
+    for i in range(K):
+        _check(shape, host, logits[i], top1[i].cpu().numpy(), conf[i].cpu().numpy(), drafts[i], start, L, tol, f"draft {i}")
+    d = _dev(t)
+    psd.psd_decode_block_shared(model, d, start, L, psd.Policy(0.9, 1), psd.chain_graph(K), kv)
+    assert not (d[:, start:start + L] == shape.mask_id).any()

@@ -191,3 +191,36 @@ def test_the_binding_refuses_tensors_that_the_library_would_misread(lib):
         psd.psd_kv_evict(ok, ok, 0)
     with pytest.raises(psd.PsdError):
         psd.psd_kv_evict(ok, ok, 5, kept=torch.zeros((2, 4, 6), dtype=torch.int32))
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,dtype", [(4, 4, 128, 1), (4, 2, 128, 1), (2, 1, 64, 1), (1, 1, 64, 1), (6, 2, 16, 0)])
+@pytest.mark.parametrize("K", [1, 2, 3, 4, 5, 8])
+def test_the_workspace_of_model_calls_is_enough_where_tiles_walk_several_units(lib, heads, kv_heads, d, dtype, K):
+    # few heads: a tile of rows holds several sequences and walks the caches of all of them, so its keys can be cut into more parts than
+    # the segments of one sequence have steps
+    cfg = B._Config(2, heads * d, heads, kv_heads, d, 4 * heads * d, 5000, 4999, 1e-5, 0, dtype, 1.0, 32768, 1)
+    w, up = kv_heads * d, lambda n: (n + 63) // 64 * 64
+    for L in (16, 32, 48, 64):
+        for prefix in (0, 16, 96, 500, 2000):
+            for length in (0, 16, 96, 128, 700):
+                for caches in (1, 2, 5):
+                    S = caches * K
+                    kv = B._KvShared(BASE if prefix else None, BASE, BASE if prefix else None, BASE, prefix, prefix, max(length, 16), length, K, 0)
+                    most = lib.psd_shared_workspace_bytes(C.byref(cfg), S, L, C.byref(kv))
+                    for n, per in {(S, K), (S, 1), (K, K), (caches, 1), (1, 1), (max(S - K, K), K)}:
+                        sh = shape(S=n, L=L, n_heads=heads, n_kv_heads=kv_heads, d_head=d, dtype=dtype, ld_q=3 * heads * d, ld_out=heads * d)
+                        block = seg(len=L, seqs_per_unit=1, ld_k=3 * heads * d, stride_k=L * 3 * heads * d, ld_vt=up(L), stride_vt=w * up(L))
+                        first = [seg(len=prefix, seqs_per_unit=n, ld_k=w, ld_vt=up(prefix), weights=BASE, ld_w=prefix)] if prefix else []
+
+                        def cache(keys):
+                            return [seg(len=keys, seqs_per_unit=per, ld_k=w, ld_vt=up(keys), stride_k=keys * w, stride_vt=w * up(keys), weights=BASE,
+                                        ld_w=keys, stride_w=kv_heads * keys)] if keys else []
+                        sums = (n * L * heads * 4 + 255) // 256 * 256
+                        rest = lib.psd_workspace_bytes(C.byref(cfg), n, L, L)
+                        for segs in [first + cache(length) + [block]] + ([first + cache(length + L)] if per == 1 else []):
+                            need = ask(lib, sh, *segs)
+                            assert need >= 0
+                            if segs[-1] is block:
+                                weights = lib.psd_attention_weights_bytes(C.byref(sh), (B._Segment * len(segs))(*segs), len(segs))
+                                need = sums + max(need, weights)
+                            assert rest + need <= most, (L, prefix, length, caches, n, per, rest + need - most)
