@@ -389,7 +389,8 @@ int32_t psd_shared_struct_sizes(int32_t *out, int32_t n);
  *   ld_out, may not overlap an input); lse device float [S*L, n_heads], ln of the sum of the exponentials of its scores, or NULL.  A row
  *   without a key (all lengths 0), or without a score above -inf, gets zeros and lse -inf, and draws no weight.  ws: device, 256-byte aligned, psd_attention_shared_bytes of the same
  *   shape and segments (which looks at shapes and len only, not at device memory); calls that overlap need one each.  Sums and statistics are
- *   fp32; with bf16 the probabilities are rounded to bf16 before they meet the values.
+ *   fp32; with bf16 the probabilities are rounded to bf16 before they meet the values.  How keys are cut follows shapes and lengths, so a row's
+ *   bits depend on those of its batch, but not on what other sequences hold.
  * psd_attention_weights: what each key drew: weights[u][g][j] = sum over the rows of the unit's sequences and the query heads of KV head g
  *   of exp(score - lse), lse from psd_attention_shared over all segments.  Segments without `weights` are skipped, no two may have the same; accumulate = 1
  *   adds to what is there, 0 overwrites.  Weights behind a unit's last key are left as they are.  ws likewise

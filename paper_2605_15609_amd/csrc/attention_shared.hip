@@ -309,12 +309,13 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
 #pragma unroll
         for (int v = 1; v < 16; ++v) mx = fmaxf(mx, x[v]);
         mx = both_max(mx);
-        if (__any(__builtin_fmaf(mx, sl2, neg_m) > SLACK)) {   // (as in many_rows)
-            const float m_new = fmaxf(m_run, mx);
-            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * sl2);
+        const float over = __builtin_fmaf(mx, sl2, neg_m);
+        if (__any(over > SLACK)) {   // (as in many_rows)
+            const bool raised = over > SLACK;
+            const float alpha = raised ? __builtin_amdgcn_exp2f((m_run - mx) * sl2) : 1.f;
             l_run *= alpha;
-            m_run = m_new;
-            neg_m = m_new == -INFINITY ? NO_MAX : -m_new * sl2;
+            m_run = raised ? mx : m_run;
+            neg_m = raised ? -mx * sl2 : neg_m;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -511,18 +512,20 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
                 x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(st + k_at[ks] + kt * 32 * KROW), qf[ks], x[kt], 0, 0, 0);
     };
     // The sums are kept relative to a running reference, raised to the maximum only where that has grown by more than 2^SLACK in a
-    // probability: bf16 and fp32 are as exact there, and the outputs are not touched in most tiles.
+    // probability: bf16 and fp32 are as exact there, and the outputs are not touched in most tiles.  A row that has not grown keeps its
+    // reference when others of the wavefront raise theirs (its factor is 1), so its bits do not depend on what other sequences hold.
     auto reference = [&](const floatx16 (&x)[2]) {
         float mx = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
         for (int v = 1; v < 16; ++v) mx = fmaxf(fmaxf(mx, x[0][v]), x[1][v]);
         mx = both_max(mx);
-        if (__any(__builtin_fmaf(mx, sl2, neg_m) > SLACK)) {
-            const float m_new = fmaxf(m_run, mx);
-            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * sl2);
+        const float over = __builtin_fmaf(mx, sl2, neg_m);
+        if (__any(over > SLACK)) {
+            const bool raised = over > SLACK;
+            const float alpha = raised ? __builtin_amdgcn_exp2f((m_run - mx) * sl2) : 1.f;
             l_run *= alpha;
-            m_run = m_new;
-            neg_m = m_new == -INFINITY ? NO_MAX : -m_new * sl2;
+            m_run = raised ? mx : m_run;
+            neg_m = raised ? -mx * sl2 : neg_m;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
