@@ -35,7 +35,7 @@ constexpr int BK = 32;    // keys that a wavefront takes at a time
 constexpr int KT = 64;    // keys of a tile in LDS
 constexpr int NW = 4;     // wavefronts of a workgroup, which deal a tile's keys among themselves
 constexpr float SLACK = 8.f;      // (see many_rows)
-constexpr float NO_MAX = 1e38f;   // minus the reference of a row without a score yet: any score exceeds it, and -inf stays -inf
+constexpr float FAR = 0x1p24f;    // (see many_rows)
 constexpr float LOG2E = 1.4426950408889634f;
 
 // A row of 8 slots of T, as a lane of a 32x32 product holds it: bf16 in one 16-byte load, fp32 in two.
@@ -177,12 +177,12 @@ struct PartOut {
         o = l.o + at * DH;
         out = (T *)l.out + row.token * sh.ld_out + row.head * DH;
     }
-    // m, l of the row, m_s = m in units of log2 (0 for -inf)
-    __device__ void sums(float m, float l, float m_s) const {
+    // maximum m (what l is relative to) and sum l of the row
+    __device__ void sums(float m, float l, float sl2) const {
         if (!direct) ln.ml[at] = make_float2(m, l);
-        else if (ln.lse) ln.lse[at] = log_sum(m_s, l);
+        else if (ln.lse) ln.lse[at] = log_sum(m, l, sl2);
     }
-    __device__ static float log_sum(float m_s, float l) { return l == 0.f ? -INFINITY : m_s / LOG2E + logf(l); }
+    __device__ static float log_sum(float m, float l, float sl2) { return l == 0.f ? -INFINITY : m * sl2 / LOG2E + logf(l); }
     // what values() multiplies by; 0 where there were no keys
     __device__ float factor(float l) const { return l == 0.f ? 0.f : direct ? 1.0f / l : 1.0f; }
     __device__ void values(int c, const float *v, float f) const {
@@ -263,7 +263,8 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
     // where it would be two (4 rows of 8 heads of 64 channels over 317 keys: 8.4 us, 9.2 without).  fp32 (slower
     // products, twice the registers) gains nothing: 8.8 us and 8.6 without at 48 rows of 8 heads of 64 over 426 keys.
     constexpr bool AHEAD = sizeof(T) == 2;
-    float m_run = -INFINITY, neg_m = NO_MAX, l_run = 0.f;
+    float m_run = -INFINITY, neg_m = 0.f, l_run = 0.f;   // (as in many_rows)
+    bool far = false;
     Frag<T> kf[KS], vf[BK / 16][CT];
     auto load_keys = [&](const Step &s) {
         const T *krow = s.k + (int64_t)min(s.k0 + lrow, s.keys - 1) * s.ld_k + half * 8;
@@ -309,22 +310,30 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
 #pragma unroll
         for (int v = 1; v < 16; ++v) mx = fmaxf(mx, x[v]);
         mx = both_max(mx);
-        const float over = __builtin_fmaf(mx, sl2, neg_m);
+        const float over = (mx - m_run) * sl2;   // (NaN where there is no score yet, which raises nothing)
         if (__any(over > SLACK)) {   // (as in many_rows)
             const bool raised = over > SLACK;
-            const float alpha = raised ? __builtin_amdgcn_exp2f((m_run - mx) * sl2) : 1.f;
+            const float alpha = raised ? __builtin_amdgcn_exp2f(-over) : 1.f;
             l_run *= alpha;
             m_run = raised ? mx : m_run;
             neg_m = raised ? -mx * sl2 : neg_m;
+            far = __any(fabsf(neg_m) > FAR);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc_o[ct][v] *= alpha;
         }
+        float shift = neg_m;
+        if (far) {
+            const float ref = fabsf(neg_m) > FAR ? m_run : 0.f;
+            if (fabsf(neg_m) > FAR) shift = 0.f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[v] -= ref;
+        }
         float p[16], psum[2] = {0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-            p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], sl2, neg_m));
+            p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], sl2, shift));
             psum[v & 1] += p[v];
         }
         l_run += psum[0] + psum[1];
@@ -347,7 +356,7 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
     if constexpr (W == 1) {
         if (r >= rows) return;
         const PartOut<T, DH> to(sh, ln, jb.part0 + split, row);
-        if (half == 0) to.sums(m_run, l_run, -neg_m);
+        if (half == 0) to.sums(m_run, l_run, sl2);
         const float inv = to.factor(l_run);
         if (inv == 0.f && !to.direct) return;
 #pragma unroll
@@ -372,15 +381,15 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
         scale[w] = part[w * (2 + NF) * 64 + lane];
         m_all = fmaxf(m_all, scale[w]);
     }
-    const float m_s = m_all == -INFINITY ? 0.f : m_all * sl2;
+    const float ref = m_all == -INFINITY ? 0.f : m_all;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-        scale[w] = __builtin_amdgcn_exp2f(__builtin_fmaf(scale[w], sl2, -m_s));
+        scale[w] = __builtin_amdgcn_exp2f((scale[w] - ref) * sl2);
         l_all += part[(w * (2 + NF) + 1) * 64 + lane] * scale[w];
     }
     if (r >= rows) return;
     const PartOut<T, DH> to(sh, ln, jb.part0 + split, row);
-    if (wave == 0 && half == 0) to.sums(m_all, l_all, m_s);
+    if (wave == 0 && half == 0) to.sums(m_all, l_all, sl2);
     const float inv = to.factor(l_all);
     if (inv == 0.f && !to.direct) return;   // (no keys: the join reads no values)
 #pragma unroll
@@ -491,7 +500,8 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     for (int i = 0; i < CT; ++i)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc_o[i][v] = 0.f;
-    float m_run = -INFINITY, neg_m = NO_MAX, l_run = 0.f;   // neg_m: minus the reference of the exponentials
+    float m_run = -INFINITY, neg_m = 0.f, l_run = 0.f;   // the reference of the exponentials, and minus it in units of log2 (0: no score yet)
+    bool far = false;                                    // a row of the wavefront has a reference beyond FAR
 
     // the addresses of a lane's fragments within a stage
     int k_at[KS], v_at[4];
@@ -514,25 +524,38 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     // The sums are kept relative to a running reference, raised to the maximum only where that has grown by more than 2^SLACK in a
     // probability: bf16 and fp32 are as exact there, and the outputs are not touched in most tiles.  A row that has not grown keeps its
     // reference when others of the wavefront raise theirs (its factor is 1), so its bits do not depend on what other sequences hold.
-    auto reference = [&](const floatx16 (&x)[2]) {
+    // Returns what the exponentials add to x sl2.  That is minus the reference in units of log2, rounded, which is off by up to half a unit where
+    // it reaches FAR and by any power of two beyond; there x is taken relative to the reference before it is scaled.
+    auto reference = [&](floatx16 (&x)[2]) {
         float mx = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
         for (int v = 1; v < 16; ++v) mx = fmaxf(fmaxf(mx, x[0][v]), x[1][v]);
         mx = both_max(mx);
-        const float over = __builtin_fmaf(mx, sl2, neg_m);
+        const float over = (mx - m_run) * sl2;   // (NaN where there is no score yet, which raises nothing)
         if (__any(over > SLACK)) {
             const bool raised = over > SLACK;
-            const float alpha = raised ? __builtin_amdgcn_exp2f((m_run - mx) * sl2) : 1.f;
+            const float alpha = raised ? __builtin_amdgcn_exp2f(-over) : 1.f;
             l_run *= alpha;
             m_run = raised ? mx : m_run;
             neg_m = raised ? -mx * sl2 : neg_m;
+            far = __any(fabsf(neg_m) > FAR);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc_o[ct][v] *= alpha;
         }
+        float shift = neg_m;
+        if (far) {
+            const float ref = fabsf(neg_m) > FAR ? m_run : 0.f;
+            if (fabsf(neg_m) > FAR) shift = 0.f;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[kt][v] -= ref;
+        }
+        return shift;
     };
-    auto exponentials = [&](const floatx16 (&x)[2], bf16x8 (&pf)[4]) {
+    auto exponentials = [&](const floatx16 (&x)[2], float shift, bf16x8 (&pf)[4]) {
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -541,7 +564,7 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
                 float p[8];
 #pragma unroll
                 for (int v = 0; v < 8; ++v) {
-                    p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][8 * e + v], sl2, neg_m));
+                    p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][8 * e + v], sl2, shift));
                     sum[v & 3] += p[v];
                 }
                 pf[kt * 2 + e] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]),
@@ -595,9 +618,9 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) vf[kg][ct].keep(left - kg * 16 - 4 * half);
             }
-            reference(x);
+            const float shift = reference(x);
             bf16x8 pf[4];
-            exponentials(x, pf);
+            exponentials(x, shift, pf);
 #pragma unroll
             for (int kg = 0; kg < 4; ++kg)
 #pragma unroll
@@ -610,7 +633,7 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     l_run = both_sum(l_run);   // the halves of a row hold disjoint keys
     if (r >= rows) return;
     const PartOut<bf16_t, DH> to(sh, ln, jb.part0 + split, row);
-    if (half == 0) to.sums(m_run, l_run, -neg_m);
+    if (half == 0) to.sums(m_run, l_run, sl2);
     const float f = to.factor(l_run);
     if (f == 0.f && !to.direct) return;
 #pragma unroll
@@ -680,13 +703,13 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, Shared
         float top = m;
 #pragma unroll
         for (int i = 0; i < B; ++i) top = fmaxf(top, s[i].x);
-        const float m_s = top == -INFINITY ? 0.f : top * sl2, a = __builtin_amdgcn_exp2f(__builtin_fmaf(m, sl2, -m_s));
+        const float ref = top == -INFINITY ? 0.f : top, a = __builtin_amdgcn_exp2f((m - ref) * sl2);
         l *= a, o[0] *= a, o[1] *= a, o[2] *= a, o[3] *= a;
         m = top;
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             const bool none = s[i].y == 0.f;   // (values that were never written may be anything)
-            const float w = none ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(s[i].x, sl2, -m_s));
+            const float w = none ? 0.f : __builtin_amdgcn_exp2f((s[i].x - ref) * sl2);
             l += w * s[i].y;
             o[0] += none ? 0.f : w * v[i].x, o[1] += none ? 0.f : w * v[i].y, o[2] += none ? 0.f : w * v[i].z, o[3] += none ? 0.f : w * v[i].w;
         }
@@ -698,24 +721,23 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, Shared
         if (g > 0) return;
 #pragma unroll
         for (int i = 1; i < G; ++i) m = fmaxf(m, stats[threadIdx.x + i * TPR].x);
-        const float ref = m == -INFINITY ? 0.f : m * sl2;
+        const float ref = m == -INFINITY ? 0.f : m;
         l = o[0] = o[1] = o[2] = o[3] = 0.f;
 #pragma unroll
         for (int i = 0; i < G; ++i) {
             const float2 s = stats[threadIdx.x + i * TPR];
             const float4 v = sums[threadIdx.x + i * TPR];
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s.x, sl2, -ref));
+            const float w = __builtin_amdgcn_exp2f((s.x - ref) * sl2);
             l += w * s.y;
             o[0] += w * v.x, o[1] += w * v.y, o[2] += w * v.z, o[3] += w * v.w;
         }
     }
-    const float m_s = m == -INFINITY ? 0.f : m * sl2;
     if (!live) return;
     const float inv = l == 0.f ? 0.f : 1.0f / l;   // (a row without keys: zeros)
     T *to = (T *)ln.out + r / sh.n_heads * sh.ld_out + r % sh.n_heads * DH + c;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
     else *reinterpret_cast<float4 *>(to) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-    if (ln.lse && c == 0) ln.lse[r] = PartOut<T, DH>::log_sum(m_s, l);
+    if (ln.lse && c == 0) ln.lse[r] = PartOut<T, DH>::log_sum(m, l, sl2);
 }
 
 // w[j] (+)= sum over the rows of the unit of exp(x_j - lse).  A wavefront keeps 32 NK keys in registers, a workgroup four times as many, and
