@@ -386,7 +386,7 @@ typedef struct {
 /* sizeof psd_kv_segment, psd_attention_shape and psd_kv_shared, as psd_struct_sizes gives those of the structures above. */
 int32_t psd_shared_struct_sizes(int32_t *out, int32_t n);
 /* psd_attention_shared: softmax(q k^T / sqrt(d_head)) v of every row over all keys of the units it sees.  out as q (row stride
- *   ld_out, may not overlap an input); lse device float [S*L, n_heads], ln of the sum of the exponentials of its scores, or NULL.  A row
+ *   ld_out); neither out nor lse may overlap an input or each other (columns of one buffer's rows may be q, keys and out); lse device float [S*L, n_heads], ln of the sum of the exponentials of its scores, or NULL.  A row
  *   without a key (all lengths 0), or without a score above -inf, gets zeros and lse -inf, and draws no weight.  ws: device, 256-byte aligned, psd_attention_shared_bytes of the same
  *   shape and segments (which looks at shapes and len only, not at device memory); calls that overlap need one each.  Sums and statistics are
  *   fp32; with bf16 the probabilities are rounded to bf16 before they meet the values.  How keys are cut follows shapes and lengths, so a row's

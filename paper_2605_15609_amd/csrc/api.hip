@@ -1074,6 +1074,43 @@ int32_t check_shared(const psd_attention_shape *a, const psd_kv_segment *segs, i
 
 bool misaligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
+// Memory of a call, in bytes: `units` times `rows` pieces of `width`
+struct Region {
+    uintptr_t first;
+    int64_t units, unit_stride, rows, row_stride, width;
+    int64_t unit_width() const { return (rows - 1) * row_stride + width; }
+    int64_t span() const { return units < 1 || rows < 1 || width < 1 ? 0 : (units - 1) * unit_stride + unit_width(); }
+};
+Region dense(const void *p, int64_t bytes) { return {reinterpret_cast<uintptr_t>(p), 1, 0, 1, 0, p ? bytes : 0}; }
+
+// [a, a + wa) and [b, b + wb), each repeated every p bytes, have no byte in common
+bool apart_modulo(uintptr_t a, int64_t wa, uintptr_t b, int64_t wb, int64_t p) {
+    if (p < 1 || wa > p || wb > p) return false;
+    const int64_t d = b >= a ? (int64_t)((b - a) % (uintptr_t)p) : (p - (int64_t)((a - b) % (uintptr_t)p)) % p;
+    return d >= wa && d + wb <= p;
+}
+
+// No byte in common: one lies behind the other, or they are columns of the same rows, or parts of the same units (what alternates in other ways
+// is taken to overlap)
+bool apart(const Region &a, const Region &b) {
+    const int64_t na = a.span(), nb = b.span();
+    if (na == 0 || nb == 0 || a.first + (uintptr_t)na <= b.first || b.first + (uintptr_t)nb <= a.first) return true;
+    auto row_period = [](const Region &r) {   // 0: no period
+        return r.units == 1 ? (r.rows == 1 ? -1 : r.row_stride) : r.rows == 1 ? r.unit_stride : r.row_stride > 0 && r.unit_stride % r.row_stride == 0 ? r.row_stride : 0;
+    };
+    auto same = [](int64_t x, int64_t y) { return x < 0 ? y : y < 0 || x == y ? x : 0; };   // (-1: a single piece, which fits any period)
+    return apart_modulo(a.first, a.width, b.first, b.width, same(row_period(a), row_period(b))) ||
+           apart_modulo(a.first, a.unit_width(), b.first, b.unit_width(), same(a.units > 1 ? a.unit_stride : -1, b.units > 1 ? b.unit_stride : -1));
+}
+
+Region keys_region(const SharedSegment &s, int64_t units, int64_t rows, int64_t width, int64_t esz) {
+    return {reinterpret_cast<uintptr_t>(s.k), units, s.stride_k * esz, rows, s.ld_k * esz, width * esz};
+}
+Region values_region(const SharedSegment &s, int64_t units, int64_t positions, int64_t width, int64_t esz) {
+    return {reinterpret_cast<uintptr_t>(s.vt), units, s.stride_vt * esz, positions > 0 ? width : 0, s.ld_vt * esz, (positions + 15) / 16 * 16 * esz};
+}
+Region lens_region(const SharedSegment &s, int64_t units) { return dense(s.lens, units * 4); }
+
 // [first, last) byte that a segment's units occupy
 struct Extent {
     uintptr_t first, last;
@@ -1109,12 +1146,15 @@ int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, co
     CHECK(check_shared(shape, segments, n_segments, &sh, seg));
     if (!q || !out) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL q / out");
     if (misaligned16(q) || misaligned16(out)) PSD_FAIL(PSD_ERR_SHAPE, "q and out must be 16-byte aligned");
-    const int64_t esz = sh.dtype == PSD_DTYPE_BF16 ? 2 : 4, width = (int64_t)sh.n_heads * sh.d_head * esz, n_tokens = (int64_t)sh.S * sh.L;
-    const Extent from = extent(q, 1, 0, n_tokens, sh.ld_q, (int64_t)sh.n_heads * sh.d_head, esz);
-    const Extent to = extent(out, 1, 0, n_tokens, sh.ld_out, (int64_t)sh.n_heads * sh.d_head, esz);
-    if (from.meets(to)) {   // rows of equal stride may lie beside each other
-        const uintptr_t ld = (uintptr_t)(sh.ld_q * esz), apart = to.first >= from.first ? (to.first - from.first) % ld : ld - (from.first - to.first) % ld;
-        if (sh.ld_q != sh.ld_out || apart < (uintptr_t)width || apart + width > ld) PSD_FAIL(PSD_ERR_INVALID_ARG, "out overlaps q");
+    const int64_t esz = sh.dtype == PSD_DTYPE_BF16 ? 2 : 4, row = (int64_t)sh.n_heads * sh.d_head * esz, n_tokens = (int64_t)sh.S * sh.L;
+    const Region from = {reinterpret_cast<uintptr_t>(q), 1, 0, n_tokens, sh.ld_q * esz, row}, sums = dense(lse, sh.n_rows * 4);
+    const Region to = {reinterpret_cast<uintptr_t>(out), 1, 0, n_tokens, sh.ld_out * esz, row};
+    if (!apart(from, to)) PSD_FAIL(PSD_ERR_INVALID_ARG, "out overlaps q");
+    if (!apart(from, sums) || !apart(to, sums)) PSD_FAIL(PSD_ERR_INVALID_ARG, "lse lies on q or out");
+    for (int i = 0; i < n_segments; ++i) {
+        const int64_t units = sh.S / seg[i].seqs_per_unit, w = (int64_t)sh.n_kv_heads * sh.d_head;
+        for (const Region &r : {keys_region(seg[i], units, seg[i].len, w, esz), values_region(seg[i], units, seg[i].len, w, esz), lens_region(seg[i], units)})
+            if (!apart(r, to) || !apart(r, sums)) PSD_FAIL(PSD_ERR_INVALID_ARG, "out or lse lies on the keys, values or lengths of segment %d", i);
     }
     SharedLaunch ln;
     if (!plan_attention_shared(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");

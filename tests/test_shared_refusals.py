@@ -224,3 +224,27 @@ def test_the_workspace_of_model_calls_is_enough_where_tiles_walk_several_units(l
                                 weights = lib.psd_attention_weights_bytes(C.byref(sh), (B._Segment * len(segs))(*segs), len(segs))
                                 need = sums + max(need, weights)
                             assert rest + need <= most, (L, prefix, length, caches, n, per, rest + need - most)
+
+
+def test_outputs_on_keys_values_lengths_or_each_other_are_refused(lib):
+    far = BASE + (1 << 35)
+
+    def call(out=far, lse=far + (1 << 20), ld_out=512, **kw):     # (without a workspace: what is not refused for its addresses is refused for that)
+        one = (B._Segment * 1)(seg(**dict(dict(len=5000, ld_vt=5008, stride_k=5000 * 256, stride_vt=256 * 5008, seqs_per_unit=2), **kw)))
+        assert lib.psd_attention_shared(C.byref(shape(ld_out=ld_out)), BASE + (1 << 34), one, 1, out, lse, None, 0, None) < 0
+        return b"lies on" in lib.psd_last_error()
+    keys, values = 2 * 5000 * 512, 2 * 256 * 5008 * 2
+    assert not call() and not call(lse=None)
+    for at in (BASE, BASE + keys - 16, BASE + (1 << 30), BASE + (1 << 30) + values - 64):
+        assert call(out=at) and call(lse=at)
+    assert not call(out=BASE + keys) and not call(out=BASE + (1 << 30) + values) and not call(lse=BASE - 4 * 2 * 8 * 4) and call(lse=BASE - 4 * 2 * 8 * 4 + 4)
+    assert call(lens=far) and call(lens=far + (1 << 20) + 4) and not call(lens=far - 8)
+    assert call(lse=far + 7 * 1024) and call(lse=far + 8 * 1024 - 4) and not call(lse=far + 8 * 1024) and not call(lse=far - 256)
+    assert call(lse=BASE + (1 << 34)) and call(lse=BASE + (1 << 34) + 8 * 1024 - 4)
+    # columns of one buffer: 256 keys, 512 outputs, 256 more; and the units of a cache whose keys end in front of its values
+    beside = dict(ld_k=1024, stride_k=5000 * 1024, ld_out=1024)
+    assert not call(out=BASE + 512, **beside) and call(out=BASE + 496, **beside) and not call(out=BASE + 1024, **beside) and call(out=BASE + 1040, **beside)
+    cache = dict(vt=BASE + keys // 2, stride_k=(keys + values) // 4, stride_vt=(keys + values) // 4)
+    assert not call(**cache) and call(out=BASE + keys, **cache) and not call(out=BASE + keys + values, **cache)
+    gap = dict(stride_k=5000 * 256 + 4096, stride_vt=256 * 5008 * 2)     # room for the outputs between two units
+    assert not call(out=BASE + keys // 2, **gap) and call(out=BASE + keys // 2 + 16, **gap)
