@@ -1109,6 +1109,9 @@ Region keys_region(const SharedSegment &s, int64_t units, int64_t rows, int64_t 
 Region values_region(const SharedSegment &s, int64_t units, int64_t positions, int64_t width, int64_t esz) {
     return {reinterpret_cast<uintptr_t>(s.vt), units, s.stride_vt * esz, positions > 0 ? width : 0, s.ld_vt * esz, (positions + 15) / 16 * 16 * esz};
 }
+Region weights_region(const SharedSegment &s, int64_t units, int64_t n_kv_heads, int64_t positions) {
+    return {reinterpret_cast<uintptr_t>(s.weights), units, s.stride_w * 4, s.weights ? n_kv_heads : 0, s.ld_w * 4ll, positions * 4};
+}
 Region lens_region(const SharedSegment &s, int64_t units) { return dense(s.lens, units * 4); }
 
 // [first, last) byte that a segment's units occupy
@@ -1183,10 +1186,21 @@ int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, c
     if (!q || !lse) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL q / lse");
     if (misaligned16(q)) PSD_FAIL(PSD_ERR_SHAPE, "q must be 16-byte aligned");
     if (accumulate != 0 && accumulate != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "accumulate %d", accumulate);
+    const int64_t esz = sh.dtype == PSD_DTYPE_BF16 ? 2 : 4, n_tokens = (int64_t)sh.S * sh.L;
+    const Region from = {reinterpret_cast<uintptr_t>(q), 1, 0, n_tokens, sh.ld_q * esz, (int64_t)sh.n_heads * sh.d_head * esz}, sums = dense(lse, sh.n_rows * 4);
+    auto weights = [&](int i) { return weights_region(seg[i], sh.S / seg[i].seqs_per_unit, sh.n_kv_heads, seg[i].len); };
     for (int i = 0; i < n_segments; ++i)
         for (int j = 0; j < i; ++j)
-            if (seg[i].weights && seg[i].weights == seg[j].weights && seg[i].len > 0 && seg[j].len > 0)
-                PSD_FAIL(PSD_ERR_INVALID_ARG, "segments %d and %d have the same weights", j, i);
+            if (!apart(weights(i), weights(j))) PSD_FAIL(PSD_ERR_INVALID_ARG, "segments %d and %d have the same weights, or some of them", j, i);
+    for (int i = 0; i < n_segments; ++i) {
+        const Region w = weights(i);
+        if (!apart(w, from) || !apart(w, sums)) PSD_FAIL(PSD_ERR_INVALID_ARG, "the weights of segment %d lie on q or lse", i);
+        for (int j = 0; j < n_segments; ++j) {
+            const int64_t units = sh.S / seg[j].seqs_per_unit;
+            if (!apart(w, keys_region(seg[j], units, seg[j].len, (int64_t)sh.n_kv_heads * sh.d_head, esz)) || !apart(w, lens_region(seg[j], units)))
+                PSD_FAIL(PSD_ERR_INVALID_ARG, "the weights of segment %d lie on keys or lengths of segment %d", i, j);
+        }
+    }
     SharedLaunch ln;
     if (!plan_attention_weights(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
     const int64_t need = shared_weights_bytes(ln);

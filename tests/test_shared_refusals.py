@@ -248,3 +248,31 @@ def test_outputs_on_keys_values_lengths_or_each_other_are_refused(lib):
     assert not call(**cache) and call(out=BASE + keys, **cache) and not call(out=BASE + keys + values, **cache)
     gap = dict(stride_k=5000 * 256 + 4096, stride_vt=256 * 5008 * 2)     # room for the outputs between two units
     assert not call(out=BASE + keys // 2, **gap) and call(out=BASE + keys // 2 + 16, **gap)
+
+
+def test_weights_that_share_memory_are_refused(lib):
+    W, Q = BASE + (1 << 36), BASE + (1 << 37)
+    far, Z, S, L = W + (1 << 20), Q + (1 << 30), 64, 64
+
+    def why(second=far, first=W, lse=Z, q=Q, prefix=dict(), cache=dict()):     # 50 shared keys, 64 caches of 40
+        two = (B._Segment * 2)(seg(**dict(dict(weights=first, ld_w=50, seqs_per_unit=S), **prefix)),
+                               seg(**dict(dict(weights=second, ld_w=40, stride_w=160, len=40, seqs_per_unit=1, k=BASE + (1 << 20)), **cache)))
+        sh = shape(S=S, L=L)
+        assert lib.psd_attention_weights_bytes(C.byref(sh), two, 2) > 0
+        # (without a workspace: what is not refused for its addresses is refused for that)
+        assert lib.psd_attention_weights(C.byref(sh), q, two, 2, lse, 0, None, 0, None) < 0
+        return lib.psd_last_error()
+    ok, shared = b"workspace of", b"same weights"
+    of_prefix, of_caches, sums = 4 * 50 * 4, 64 * 160 * 4, S * L * 8 * 4
+    assert ok in why() and ok in why(W + of_prefix) and ok in why(W - of_caches)
+    for second in (W, W + 4, W + of_prefix - 4, W - of_caches + 4):
+        assert shared in why(second)
+    # columns of one buffer: [heads, 50 + 40] of a single sequence would be taken, rows of 90 that share the last column are not
+    beside = dict(ld_w=90, stride_w=4 * 90)
+    assert ok in why(W + 200, prefix=dict(ld_w=90), cache=beside) and shared in why(W + 196, prefix=dict(ld_w=90), cache=beside)
+    for kw in (dict(lse=W), dict(lse=W + of_prefix - 4), dict(lse=far - sums + 4), dict(q=W), dict(q=far + of_caches - 16)):
+        assert b"lie on q or lse" in why(**kw)
+    assert ok in why(lse=W + of_prefix) and ok in why(lse=far - sums)
+    for kw in (dict(prefix=dict(lens=far)), dict(prefix=dict(k=far + 64)), dict(cache=dict(lens=W + 16)), dict(cache=dict(k=W))):
+        assert b"keys or lengths" in why(**kw)
+    assert ok in why(prefix=dict(vt=far))      # (values are not read)
