@@ -417,14 +417,14 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
  * tokens whatever the caches hold.  A prefix is filled by psd_kv_prefill with B = 1, a sequence's cache behind it by psd_kv_extend_shared.
  * Block-causal models: exact while nothing is evicted.  Bidirectional models: the caches of psd_forward_confidence_approx, whole or evicted.
  *   psd_forward_confidence_shared: as psd_forward_confidence_cached; sequence s uses cache s / seqs_per_cache.  What every cached
- *     position drew from the block rows, layer by layer, is added to prefix_weights / cache_weights (zero them first) where set.
+ *     position drew from the block rows, layer by layer, is added to prefix_weights / cache_weights (zero them first; they may share none) where set.
  *   psd_kv_extend_shared: one forward over the block rows of B sequences (seqs_per_cache 1), whose keys and values go to positions len ..
  *     len + L - 1 of their caches.  Block-causal models only; adds no weights.
  *   psd_decode_block_shared: psd_decode_block with such model calls; afterwards the block is appended as by psd_kv_extend_shared.
  * L a multiple of 16.  Workspace: psd_shared_workspace_bytes(cfg, S, L, kv), 256-byte aligned; for psd_decode_block_shared with S = B*K and
  * kv->seqs_per_cache = K there (1 in the call), plus psd_decode_scratch_bytes(B, N, L, K). */
 typedef struct {
-    const void *prefix;          /* device, one cache; may be NULL where prefix_len is 0 */
+    const void *prefix;          /* device, one cache, none of those that a block goes behind; may be NULL where prefix_len is 0 */
     void *cache;                 /* device, one per seqs_per_cache sequences; may be NULL where len is 0 and nothing is stored */
     float *prefix_weights;       /* device [n_layers][n_kv_heads][prefix_capacity], or NULL */
     float *cache_weights;        /* device [caches][n_layers][n_kv_heads][capacity], or NULL */

@@ -1286,6 +1286,20 @@ int32_t check_kv_shared(const psd_model_config &c, const psd_kv_shared *kv, int3
     return PSD_OK;
 }
 
+// the memory of a shared call over S sequences: weights are added to, and (append) caches written, while other workgroups read or add
+int32_t check_kv_shared_memory(const psd_model_config &c, const KvCacheArg &a, int32_t S, bool append) {
+    const int64_t esz = c.dtype == PSD_DTYPE_BF16 ? 2 : 4, caches = S / a.seqs_per_cache, rows = (int64_t)c.n_layers * c.n_kv_heads;
+    const Region prefix = dense(a.prefix, a.prefix_len > 0 ? kv_layout(c, a.prefix_capacity).per_seq * esz : 0);
+    const Region cache = dense(a.base, a.len > 0 || append ? caches * kv_layout(c, a.capacity).per_seq * esz : 0);
+    const Region of_prefix = dense(a.prefix_weights, a.prefix_len > 0 ? rows * a.prefix_capacity * 4 : 0);
+    const Region of_cache = dense(a.cache_weights, a.len > 0 ? caches * rows * a.capacity * 4 : 0);
+    if (!apart(of_prefix, of_cache)) PSD_FAIL(PSD_ERR_INVALID_ARG, "prefix and caches have the same weights, or some of them");
+    if (!apart(of_prefix, prefix) || !apart(of_prefix, cache) || !apart(of_cache, prefix) || !apart(of_cache, cache))
+        PSD_FAIL(PSD_ERR_INVALID_ARG, "weights lie on the prefix or the caches");
+    if (append && !apart(prefix, cache)) PSD_FAIL(PSD_ERR_INVALID_ARG, "a block cannot go behind caches that the prefix is one of");
+    return PSD_OK;
+}
+
 }   // namespace
 
 int64_t psd_shared_workspace_bytes(const psd_model_config *cfg, int32_t S, int32_t L, const psd_kv_shared *kv) {
@@ -1301,6 +1315,7 @@ int32_t psd_forward_confidence_shared(psd_handle *h, const int32_t *tokens, int3
     CHECK(check_block(h, S, N, block_start, L));
     KvCacheArg a;
     CHECK(check_kv_shared(h->cfg, kv, S, L, false, &a));
+    CHECK(check_kv_shared_memory(h->cfg, a, S, false));
     if (!tokens || (!logits && (!top1 || !conf))) PSD_FAIL(PSD_ERR_INVALID_ARG, "NULL tokens/top1/conf");
     hipStream_t st = (hipStream_t)stream;
     CHECK(run_forward_cached(h, tokens, nullptr, S, N, block_start, L, a, ws, ws_bytes, st));
@@ -1314,6 +1329,7 @@ int32_t psd_kv_extend_shared(psd_handle *h, const int32_t *tokens, int32_t B, in
     CHECK(check_block(h, B, N, block_start, L));
     KvCacheArg a;
     CHECK(check_kv_shared(h->cfg, kv, B, L, true, &a));
+    CHECK(check_kv_shared_memory(h->cfg, a, B, true));
     if (!tokens) PSD_FAIL(PSD_ERR_INVALID_ARG, "tokens is NULL");
     if (a.seqs_per_cache != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "extending needs one sequence per cache");
     a.append = true;
@@ -1325,6 +1341,7 @@ int32_t psd_decode_block_shared(psd_handle *h, int32_t *tokens, int32_t B, int32
     CHECK(check_block(h, B, N, block_start, L));
     KvCacheArg a;
     CHECK(check_kv_shared(h->cfg, kv, B, L, true, &a));
+    CHECK(check_kv_shared_memory(h->cfg, a, B, true));
     if (a.seqs_per_cache != 1) PSD_FAIL(PSD_ERR_INVALID_ARG, "decoding needs one sequence per cache");
     return decode_block_impl(h, tokens, B, N, block_start, L, policy, graph, stats, ws, ws_bytes, stream, &a);
 }

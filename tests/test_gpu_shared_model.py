@@ -336,3 +336,39 @@ def test_one_request_whose_drafts_share_a_tile(L, P, own, K):
     d = _dev(t)
     psd.psd_decode_block_shared(model, d, start, L, psd.Policy(0.9, 1), psd.chain_graph(K), kv)
     assert not (d[:, start:start + L] == shape.mask_id).any()
+
+
+def test_shared_calls_refuse_memory_that_they_would_add_to_twice():
+    import paper_2605_15609_amd as psd
+    shape = _bc(BF16["mha-dh64"])
+    L = 32
+    model = psd.Model.from_host(inp.draw_model(shape, 256), DEV)
+    d = torch.zeros((2, 256), dtype=torch.int32, device=DEV)
+    cache, prefix = psd.KvCache(model, 2, 96), psd.KvCache(model, 1, 64)
+    rows = (shape.n_layers, shape.n_kv_heads)
+    n_prefix, n_cache = rows[0] * rows[1] * 64, 2 * rows[0] * rows[1] * 96
+    buf = torch.zeros((n_prefix + n_cache,), device=DEV)
+
+    def kv(at_prefix, at_cache, **kw):
+        return psd.SharedKv(**dict(dict(prefix=prefix, prefix_len=64, cache=cache, length=32, prefix_weights=buf[at_prefix:at_prefix + n_prefix].view(1, *rows, 64),
+                                        cache_weights=buf[at_cache:at_cache + n_cache].view(2, *rows, 96)), **kw))
+    decode = (psd.Policy(), psd.chain_graph(2))
+    psd.psd_forward_confidence_shared(model, d, 96, L, kv(0, n_prefix))
+    psd.psd_forward_confidence_shared(model, d, 96, L, kv(n_cache, 0))
+    psd.psd_forward_confidence_shared(model, d, 96, L, kv(0, 0, length=0))       # (nothing cached, nothing to add to)
+    for bad in (kv(0, 0), kv(0, n_prefix - 1), kv(n_cache - 1, 0)):
+        with pytest.raises(psd.PsdError, match="same weights"):
+            psd.psd_forward_confidence_shared(model, d, 96, L, bad)
+        with pytest.raises(psd.PsdError, match="same weights"):
+            psd.psd_decode_block_shared(model, d, 96, L, *decode, bad)
+    on_keys = prefix.mem[:n_prefix * 4].view(torch.float32).view(1, *rows, 64)
+    with pytest.raises(psd.PsdError, match="weights lie on"):
+        psd.psd_forward_confidence_shared(model, d, 96, L, kv(0, n_prefix, prefix_weights=on_keys))
+    one = psd.KvCache(model, 1, 96)
+    for length in (0, 32, 64):
+        both = psd.SharedKv(prefix=one, prefix_len=64, cache=one, length=length)
+        with pytest.raises(psd.PsdError, match="the prefix is one of"):
+            psd.psd_kv_extend_shared(model, d[:1], 96, L, both)
+        with pytest.raises(psd.PsdError, match="the prefix is one of"):
+            psd.psd_decode_block_shared(model, d[:1], 96, L, *decode, both)
+    psd.psd_forward_confidence_shared(model, d[:1], 96, L, psd.SharedKv(prefix=one, prefix_len=64, cache=one, length=32))   # (read only)
