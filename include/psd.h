@@ -405,7 +405,7 @@ int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, c
  *   and the last n_last positions of a unit always (n_first + n_last <= keep), then by src->weights, descending, equal ones the
  *   lowest position first (both zeros are equal, NaN is below everything).  They go to dst in ascending order of their positions: keys, values and, where
  *   dst->weights is set, weights; a unit of at most `keep` positions is copied whole.  dst must hold min(keep, src->len) positions (its `len`), have
- *   lens NULL, and not overlap src; what lies behind the positions written is left as it is.  kept device int32 [units][n_kv_heads][keep]: the source position of
+ *   lens NULL, and not overlap src; its units lie behind one another, or beside each other in rows that hold all of them; what lies behind the positions written is left as it is.  kept device int32 [units][n_kv_heads][keep]: the source position of
  *   each, -1 behind the last; kept_lens device int32 [units] (or NULL): positions of each unit now.
  *   The layers of the caches of n sequences are n * n_layers units in a row.  d_head * element size a multiple of 16 bytes. */
 int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32_t units, int32_t n_kv_heads, int32_t d_head, int32_t dtype,

@@ -1231,6 +1231,12 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
         PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
     if (most > 0) {
         const int64_t w = (int64_t)n_kv_heads * d_head;
+        // units behind one another, or beside each other in rows that hold all of them
+        auto units_apart = [&](const Region &r) {
+            return r.units == 1 || r.unit_stride >= r.unit_width() || (r.unit_stride >= r.width && (r.units - 1) * r.unit_stride + r.width <= r.row_stride);
+        };
+        if (!units_apart(keys_region(to, units, most, w, esz)) || !units_apart(values_region(to, units, most, w, esz)))
+            PSD_FAIL(PSD_ERR_SHAPE, "the units of the destination lie on each other");
         const Extent in[] = {extent(src->k, units, src->stride_k, src->len, src->ld_k, w, esz),
                              extent(src->vt, units, src->stride_vt, w, src->ld_vt, src->ld_vt, esz),
                              extent(src->weights, units, src->stride_w, n_kv_heads, src->ld_w, src->len, 4)};
@@ -1242,7 +1248,6 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
         for (const Extent &a : in)
             for (const Extent &b : written)
                 if (a.meets(b)) PSD_FAIL(PSD_ERR_INVALID_ARG, "the destination overlaps the source");
-        if (units > 1 && (dst->stride_k < 1 || dst->stride_vt < 1)) PSD_FAIL(PSD_ERR_SHAPE, "the units of the destination lie on each other");
     }
     launch_kv_evict(from, to, units, n_kv_heads, d_head, dtype, keep, n_first, n_last, kept, kept_lens, (hipStream_t)stream);
     PSD_HIP(hipGetLastError());

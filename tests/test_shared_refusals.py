@@ -276,3 +276,15 @@ def test_weights_that_share_memory_are_refused(lib):
     for kw in (dict(prefix=dict(lens=far)), dict(prefix=dict(k=far + 64)), dict(cache=dict(lens=W + 16)), dict(cache=dict(k=W))):
         assert b"keys or lengths" in why(**kw)
     assert ok in why(prefix=dict(vt=far))      # (values are not read)
+
+
+def test_destination_units_that_lie_on_each_other_are_refused(lib):
+    def why(**dst):      # (what is not refused for its units is refused for `kept`, which lies on the source)
+        assert evict(lib, dst=dict(dict(stride_k=20 * 256, stride_vt=256 * 64), **dst), units=3, kept=BASE) < 0
+        return b"lie on each other" in lib.psd_last_error()
+    assert not why()
+    assert why(stride_k=0) and why(stride_k=19 * 256) and why(stride_k=20 * 256 - 8) and why(stride_k=8)
+    assert why(stride_vt=0) and why(stride_vt=255 * 64) and why(stride_vt=255 * 64 + 24) and not why(stride_vt=255 * 64 + 32)      # (20 positions: slots 0 - 31)
+    # beside each other: rows of three units
+    assert not why(stride_k=256, ld_k=768) and why(stride_k=256, ld_k=760) and why(stride_k=248, ld_k=768) and not why(stride_k=264, ld_k=784)
+    assert not why(stride_vt=64, ld_vt=192) and not why(stride_vt=32, ld_vt=96) and why(stride_vt=24, ld_vt=96) and why(stride_vt=40, ld_vt=96)
