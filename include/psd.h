@@ -407,6 +407,7 @@ int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, c
  *   dst->weights is set, weights; a unit of at most `keep` positions is copied whole.  dst must hold min(keep, src->len) positions (its `len`), have
  *   lens NULL, and not overlap src; its units lie behind one another, or beside each other in rows that hold all of them; what lies behind the positions written is left as it is.  kept device int32 [units][n_kv_heads][keep]: the source position of
  *   each, -1 behind the last; kept_lens device int32 [units] (or NULL): positions of each unit now.
+ *   Results share no memory with each other or with what is read, lens among it.
  *   The layers of the caches of n sequences are n * n_layers units in a row.  d_head * element size a multiple of 16 bytes. */
 int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32_t units, int32_t n_kv_heads, int32_t d_head, int32_t dtype,
                      int32_t keep, int32_t n_first, int32_t n_last, int32_t *kept, int32_t *kept_lens, void *stream);

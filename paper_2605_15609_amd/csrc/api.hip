@@ -1114,16 +1114,6 @@ Region weights_region(const SharedSegment &s, int64_t units, int64_t n_kv_heads,
 }
 Region lens_region(const SharedSegment &s, int64_t units) { return dense(s.lens, units * 4); }
 
-// [first, last) byte that a segment's units occupy
-struct Extent {
-    uintptr_t first, last;
-    bool meets(const Extent &o) const { return first < o.last && o.first < last; }
-};
-Extent extent(const void *p, int64_t units, int64_t stride, int64_t rows, int64_t ld, int64_t width, int64_t esz) {
-    const uintptr_t b = reinterpret_cast<uintptr_t>(p);
-    return {b, b + (uintptr_t)(((units - 1) * stride + (rows - 1) * ld + width) * esz)};
-}
-
 }   // namespace
 
 int32_t psd_shared_struct_sizes(int32_t *out, int32_t n) {
@@ -1229,25 +1219,22 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
     if (dst->len < most) PSD_FAIL(PSD_ERR_SHAPE, "a destination of %d positions for %d", dst->len, most);
     if (kv_evict_workgroups(from, units, n_kv_heads, d_head, dtype, keep) >= 1ll << 31 || (int64_t)units * n_kv_heads >= 1ll << 31)
         PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
-    if (most > 0) {
-        const int64_t w = (int64_t)n_kv_heads * d_head;
-        // units behind one another, or beside each other in rows that hold all of them
-        auto units_apart = [&](const Region &r) {
-            return r.units == 1 || r.unit_stride >= r.unit_width() || (r.unit_stride >= r.width && (r.units - 1) * r.unit_stride + r.width <= r.row_stride);
-        };
-        if (!units_apart(keys_region(to, units, most, w, esz)) || !units_apart(values_region(to, units, most, w, esz)))
+    // what is read, and what is written: `most` positions, value rows up to the group of 16 that the last one is in
+    const int64_t w = (int64_t)n_kv_heads * d_head;
+    const Region in[] = {keys_region(from, units, src->len, w, esz), values_region(from, units, src->len, w, esz),
+                         weights_region(from, units, n_kv_heads, src->len), lens_region(from, units)};
+    const Region written[] = {keys_region(to, units, most, w, esz), values_region(to, units, most, w, esz), weights_region(to, units, n_kv_heads, most),
+                              dense(kept, (int64_t)units * n_kv_heads * keep * 4), dense(kept_lens, (int64_t)units * 4)};
+    for (int i = 0; i < 2; ++i) {   // units behind one another, or beside each other in rows that hold all of them (check_segment looks at the weights)
+        const Region &r = written[i];
+        if (r.units > 1 && r.span() > 0 && r.unit_stride < r.unit_width() && (r.unit_stride < r.width || (r.units - 1) * r.unit_stride + r.width > r.row_stride))
             PSD_FAIL(PSD_ERR_SHAPE, "the units of the destination lie on each other");
-        const Extent in[] = {extent(src->k, units, src->stride_k, src->len, src->ld_k, w, esz),
-                             extent(src->vt, units, src->stride_vt, w, src->ld_vt, src->ld_vt, esz),
-                             extent(src->weights, units, src->stride_w, n_kv_heads, src->ld_w, src->len, 4)};
-        // (what is written: `most` positions, value rows up to the group of 16 that the last one is in)
-        const Extent written[] = {extent(dst->k, units, dst->stride_k, most, dst->ld_k, w, esz),
-                                  extent(dst->vt, units, dst->stride_vt, w, dst->ld_vt, (most + 15) / 16 * 16, esz),
-                                  dst->weights ? extent(dst->weights, units, dst->stride_w, n_kv_heads, dst->ld_w, most, 4) : Extent{0, 0},
-                                  extent(kept, 1, 0, 1, 0, (int64_t)units * n_kv_heads * keep, 4)};
-        for (const Extent &a : in)
-            for (const Extent &b : written)
-                if (a.meets(b)) PSD_FAIL(PSD_ERR_INVALID_ARG, "the destination overlaps the source");
+    }
+    for (int i = 0; i < 5; ++i) {
+        for (const Region &r : in)
+            if (!apart(r, written[i])) PSD_FAIL(PSD_ERR_INVALID_ARG, "the destination overlaps the source");
+        for (int j = 0; j < i; ++j)
+            if (!apart(written[i], written[j])) PSD_FAIL(PSD_ERR_INVALID_ARG, "results of the eviction overlap each other");
     }
     launch_kv_evict(from, to, units, n_kv_heads, d_head, dtype, keep, n_first, n_last, kept, kept_lens, (hipStream_t)stream);
     PSD_HIP(hipGetLastError());

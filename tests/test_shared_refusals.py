@@ -288,3 +288,19 @@ def test_destination_units_that_lie_on_each_other_are_refused(lib):
     # beside each other: rows of three units
     assert not why(stride_k=256, ld_k=768) and why(stride_k=256, ld_k=760) and why(stride_k=248, ld_k=768) and not why(stride_k=264, ld_k=784)
     assert not why(stride_vt=64, ld_vt=192) and not why(stride_vt=32, ld_vt=96) and why(stride_vt=24, ld_vt=96) and why(stride_vt=40, ld_vt=96)
+
+
+def test_evictions_whose_results_share_memory_are_refused(lib):
+    P, K, far = BASE + (7 << 30), BASE + (8 << 30), BASE + (9 << 30)
+
+    def why(kept=P, kept_lens=K, src=dict(), dst=dict(), units=2):      # (units of the destination that lie on each other are refused before anything else)
+        s = seg(**dict(dict(weights=BASE + (2 << 30), ld_w=50, stride_w=200, len=50, lens=far), **src))
+        t = seg(**dict(dict(k=BASE + (4 << 30), vt=BASE + (5 << 30), weights=BASE + (6 << 30), ld_w=50, stride_w=200, len=50), **dst))
+        assert lib.psd_kv_evict(C.byref(s), C.byref(t), units, 4, 64, 1, 20, 2, 3, kept, kept_lens, None) < 0
+        return lib.psd_last_error()
+    source, each = b"overlaps the source", b"overlap each other"
+    # lengths in place: other workgroups still read them
+    assert source in why(kept_lens=far) and source in why(kept_lens=far + 4) and source in why(kept=far - 4 * 2 * 4 * 20 + 4)
+    assert source in why(kept_lens=BASE) and source in why(kept_lens=BASE + (1 << 30)) and source in why(kept_lens=BASE + (2 << 30))
+    assert each in why(kept_lens=P) and each in why(kept_lens=P + 4 * 2 * 4 * 20 - 4) and each in why(kept=BASE + (5 << 30)) and each in why(kept=BASE + (6 << 30))
+    assert each in why(dst=dict(vt=BASE + (4 << 30))) and each in why(dst=dict(weights=BASE + (4 << 30))) and each in why(dst=dict(weights=P + 64))
