@@ -373,7 +373,7 @@ typedef struct {
     float *weights;              /* device: [units] stride_w apart, [n_kv_heads] ld_w apart, one per key; or NULL */
     int64_t stride_k, stride_vt, stride_w;
     int32_t ld_k, ld_vt, ld_w;
-    int32_t len;                 /* keys of a unit, or the most that any unit holds (0: the segment is skipped) */
+    int32_t len;                 /* keys of a unit, or the most that any unit holds (0: the segment is skipped); up to 2^30 */
     int32_t seqs_per_unit;       /* a multiple of the next segment's; that of the first divides S */
     int32_t reserved;            /* 0 */
 } psd_kv_segment;
@@ -401,7 +401,7 @@ int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, co
 int64_t psd_attention_weights_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments);
 int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments,
                               const float *lse, int32_t accumulate, void *ws, int64_t ws_bytes, void *stream);
-/* psd_kv_evict: of `units` units of src (seqs_per_unit is ignored) and every KV head the keep >= 1 positions with the largest weights: the first n_first
+/* psd_kv_evict: of `units` units of src (seqs_per_unit is ignored) and every KV head the `keep` (1 .. 2^30) positions with the largest weights: the first n_first
  *   and the last n_last positions of a unit always (n_first + n_last <= keep), then by src->weights, descending, equal ones the
  *   lowest position first (both zeros are equal, NaN is below everything).  They go to dst in ascending order of their positions: keys, values and, where
  *   dst->weights is set, weights; a unit of at most `keep` positions is copied whole.  dst must hold min(keep, src->len) positions (its `len`), have

@@ -1024,9 +1024,11 @@ int32_t psd_decode_block_cached(psd_handle *h, int32_t *tokens, int32_t B, int32
 
 namespace {
 
+constexpr int32_t kMostKeys = 1 << 30;   // positions of a unit, kept ones among them: the kernels count up to a workgroup's more in 32 bits
+
 int32_t check_segment(const psd_kv_segment &s, int i, int32_t units, int32_t n_kv_heads, int32_t d_head, int32_t dtype, SharedSegment *out) {
     if (s.reserved != 0) PSD_FAIL(PSD_ERR_INVALID_ARG, "segment %d: reserved is not 0", i);
-    if (s.len < 0) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: %d keys", i, s.len);
+    if (s.len < 0 || s.len > kMostKeys) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: %d keys", i, s.len);
     if (s.stride_k < 0 || s.stride_vt < 0 || s.stride_w < 0) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: negative stride", i);
     if (s.len > 0 && s.ld_k < n_kv_heads * d_head) PSD_FAIL(PSD_ERR_SHAPE, "segment %d: key rows of %d elements", i, s.ld_k);
     if (s.weights && s.len > 0 && (s.ld_w < s.len || (units > 1 && s.stride_w < (int64_t)(n_kv_heads - 1) * s.ld_w + s.len)))
@@ -1208,7 +1210,7 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
     const int64_t esz = dtype == PSD_DTYPE_BF16 ? 2 : 4;
     if (units < 1 || n_kv_heads < 1 || d_head < 1 || (int64_t)n_kv_heads * d_head >= 1 << 24) PSD_FAIL(PSD_ERR_SHAPE, "%d units of %d x %d", units, n_kv_heads, d_head);
     if (d_head * esz % 16) PSD_FAIL(PSD_ERR_UNSUPPORTED, "d_head %d: rows of a head are whole 16 bytes", d_head);
-    if (keep < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > keep)
+    if (keep < 1 || keep > kMostKeys || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > keep)
         PSD_FAIL(PSD_ERR_SHAPE, "keep %d with the first %d and the last %d", keep, n_first, n_last);
     SharedSegment from, to;
     CHECK(check_segment(*src, 0, units, n_kv_heads, d_head, dtype, &from));

@@ -304,3 +304,13 @@ def test_evictions_whose_results_share_memory_are_refused(lib):
     assert source in why(kept_lens=BASE) and source in why(kept_lens=BASE + (1 << 30)) and source in why(kept_lens=BASE + (2 << 30))
     assert each in why(kept_lens=P) and each in why(kept_lens=P + 4 * 2 * 4 * 20 - 4) and each in why(kept=BASE + (5 << 30)) and each in why(kept=BASE + (6 << 30))
     assert each in why(dst=dict(vt=BASE + (4 << 30))) and each in why(dst=dict(weights=BASE + (4 << 30))) and each in why(dst=dict(weights=P + 64))
+
+
+def test_counts_near_the_end_of_32_bits_are_refused(lib):
+    most = 1 << 30
+    for length, taken in ((most, True), (most + 1, False), (2 ** 31 - 16, False), (2 ** 31 - 1, False)):
+        long = seg(len=length, ld_vt=min(length + 15, 2 ** 31 - 1) // 16 * 16, ld_w=length, weights=BASE)
+        assert (ask(lib, shape(), long) > 0) == taken
+        assert (lib.psd_attention_weights_bytes(C.byref(shape()), (B._Segment * 1)(long), 1) >= 0) == taken
+    for keep in (most + 1, 2 ** 31 - 512, 2 ** 31 - 1):
+        assert evict(lib, keep=keep) < 0 and b"keep" in lib.psd_last_error()
