@@ -936,6 +936,14 @@ class SharedKv:
                          int(self.prefix_len), 0 if self.cache is None else self.cache.capacity, int(self.length), int(seqs_per_cache), 0)
 
 
+def _check_tokens(model: Model, tokens: torch.Tensor) -> torch.device:
+    """The device of the model, where its token rows have to be."""
+    device = model._tensors["tok_emb"].device      # (model.device may name no index)
+    if tokens.dim() != 2 or tokens.dtype != torch.int32 or not tokens.is_contiguous() or tokens.device != device:
+        raise PsdError(f"tokens: dense int32 [sequences, positions] on {device}, not {tokens.dtype} {tuple(tokens.shape)} {tokens.stride()} on {tokens.device}")
+    return device
+
+
 def _shared_ws(model: Model, S: int, L: int, kv: _KvShared, extra: int = 0):
     need = _check(model.lib.psd_shared_workspace_bytes(C.byref(model.cfg), S, L, C.byref(kv))) + extra
     return model.workspace(need), need
@@ -944,6 +952,7 @@ def _shared_ws(model: Model, S: int, L: int, kv: _KvShared, extra: int = 0):
 def psd_forward_confidence_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, kv: SharedKv, seqs_per_cache: int = 1,
                                   want_logits: bool = False):
     """tokens int32 [S, N]; the block rows against a prefix of the whole batch and their caches -> (top1 [S, L], conf [S, L][, logits])."""
+    _check_tokens(model, tokens)
     S, N = tokens.shape
     if seqs_per_cache < 1 or S % seqs_per_cache:
         raise PsdError(f"{S} sequences, {seqs_per_cache} to a cache")
@@ -960,6 +969,7 @@ def psd_forward_confidence_shared(model: Model, tokens: torch.Tensor, block_star
 def psd_kv_extend_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, kv: SharedKv) -> None:
     """The block of every sequence of tokens [B, N] behind the first kv.length positions of its cache (kv.length is then L more: the
     caller's to count)."""
+    _check_tokens(model, tokens)
     B, N = tokens.shape
     c = kv.c(model, B)
     ws, nb = _shared_ws(model, B, L, c)
@@ -969,6 +979,7 @@ def psd_kv_extend_shared(model: Model, tokens: torch.Tensor, block_start: int, L
 def psd_decode_block_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, policy: Policy, graph: Graph, kv: SharedKv,
                             stats: Optional[Sequence[Stats]] = None) -> List[Stats]:
     """psd_decode_block with shared model calls; the finished block is appended to the caches (kv.length is then L more)."""
+    _check_tokens(model, tokens)
     B, N = tokens.shape
     K = graph.K
     c = kv.c(model, B)

@@ -314,3 +314,21 @@ def test_counts_near_the_end_of_32_bits_are_refused(lib):
         assert (lib.psd_attention_weights_bytes(C.byref(shape()), (B._Segment * 1)(long), 1) >= 0) == taken
     for keep in (most + 1, 2 ** 31 - 512, 2 ** 31 - 1):
         assert evict(lib, keep=keep) < 0 and b"keep" in lib.psd_last_error()
+
+
+def _stub(lib):
+    """What the checks of the model calls look at, of a model whose weights are in host memory."""
+    import types
+    shape = types.SimpleNamespace(n_layers=2, n_kv_heads=2, n_heads=2, d_head=64, vocab=100, dtype="bf16")
+    return types.SimpleNamespace(shape=shape, lib=lib, handle=None, device=torch.device("cpu"), cfg=B._Config(), _tensors={"tok_emb": torch.zeros((1, 1), dtype=BF)})
+
+
+def test_token_rows_that_the_library_would_misread_are_refused(lib):
+    model, kv = _stub(lib), psd.SharedKv()
+    good = torch.zeros((2, 64), dtype=torch.int32)
+    for tokens in (good.long(), good.float(), good[0], good[None], torch.zeros((2, 128), dtype=torch.int32)[:, ::2], torch.zeros((64, 2), dtype=torch.int32).t(),
+                   good.to("meta")):
+        for call in (lambda: psd.psd_forward_confidence_shared(model, tokens, 0, 32, kv), lambda: psd.psd_kv_extend_shared(model, tokens, 0, 32, kv),
+                     lambda: psd.psd_decode_block_shared(model, tokens, 0, 32, psd.Policy(), psd.chain_graph(2), kv)):
+            with pytest.raises(psd.PsdError, match="tokens: dense int32"):
+                call()
