@@ -919,15 +919,16 @@ class SharedKv:
     cache_weights: Optional[torch.Tensor] = None
 
     def c(self, model: Model, n_caches: int, seqs_per_cache: int = 1) -> _KvShared:
+        device = _device_of(model)
         for what, cache, weights, n in (("prefix", self.prefix, self.prefix_weights, 1), ("cache", self.cache, self.cache_weights, n_caches)):
             if cache is not None and cache.n_seqs < n:
                 raise PsdError(f"{what}: {cache.n_seqs} sequences, {n} needed")
-            if cache is not None and (cache.model.shape, cache.mem.device) != (model.shape, model.device):
+            if cache is not None and (cache.model.shape, cache.mem.device) != (model.shape, device):
                 raise PsdError(f"{what}: the cache of another model or device")
             if weights is not None:
                 want = None if cache is None else (cache.n_seqs, model.shape.n_layers, model.shape.n_kv_heads, cache.capacity)
-                if tuple(weights.shape) != want or weights.dtype != torch.float32 or not weights.is_contiguous() or weights.device != model.device:
-                    raise PsdError(f"{what} weights: dense float32 {want} on {model.device}, not {weights.dtype} {tuple(weights.shape)} on {weights.device}")
+                if tuple(weights.shape) != want or weights.dtype != torch.float32 or not weights.is_contiguous() or weights.device != device:
+                    raise PsdError(f"{what} weights: dense float32 {want} on {device}, not {weights.dtype} {tuple(weights.shape)} on {weights.device}")
 
         def address(t):
             return None if t is None else t.data_ptr()
@@ -936,9 +937,14 @@ class SharedKv:
                          int(self.prefix_len), 0 if self.cache is None else self.cache.capacity, int(self.length), int(seqs_per_cache), 0)
 
 
+def _device_of(model: Model) -> torch.device:
+    """Where the weights are, with its index (model.device is what the caller named, "cuda" for one)."""
+    return model._tensors["tok_emb"].device
+
+
 def _check_tokens(model: Model, tokens: torch.Tensor) -> torch.device:
     """The device of the model, where its token rows have to be."""
-    device = model._tensors["tok_emb"].device      # (model.device may name no index)
+    device = _device_of(model)
     if tokens.dim() != 2 or tokens.dtype != torch.int32 or not tokens.is_contiguous() or tokens.device != device:
         raise PsdError(f"tokens: dense int32 [sequences, positions] on {device}, not {tokens.dtype} {tuple(tokens.shape)} {tokens.stride()} on {tokens.device}")
     return device

@@ -332,3 +332,18 @@ def test_token_rows_that_the_library_would_misread_are_refused(lib):
                      lambda: psd.psd_decode_block_shared(model, tokens, 0, 32, psd.Policy(), psd.chain_graph(2), kv)):
             with pytest.raises(psd.PsdError, match="tokens: dense int32"):
                 call()
+
+
+def test_caches_of_a_model_on_a_device_without_an_index(lib):
+    import types
+    model = _stub(lib)
+    model.device = torch.device("cuda")      # (its tensors, and those of its caches, name the device that this was: here the CPU)
+    s = model.shape
+    cache = types.SimpleNamespace(n_seqs=2, capacity=16, model=model, mem=torch.zeros(64, dtype=torch.uint8))
+    weights = torch.zeros((2, s.n_layers, s.n_kv_heads, 16))
+    assert psd.SharedKv(cache=cache, length=16, cache_weights=weights).c(model, 2).cache == cache.mem.data_ptr()
+    for bad in (dict(mem=torch.zeros(64, dtype=torch.uint8, device="meta")), dict(n_seqs=1), dict(model=types.SimpleNamespace(shape=types.SimpleNamespace()))):
+        with pytest.raises(psd.PsdError):
+            psd.SharedKv(cache=types.SimpleNamespace(**dict(vars(cache), **bad)), length=16).c(model, 2)
+    with pytest.raises(psd.PsdError):
+        psd.SharedKv(cache=cache, length=16, cache_weights=weights.to("meta")).c(model, 2)
