@@ -958,43 +958,43 @@ def _shared_ws(model: Model, S: int, L: int, kv: _KvShared, extra: int = 0):
 def psd_forward_confidence_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, kv: SharedKv, seqs_per_cache: int = 1,
                                   want_logits: bool = False):
     """tokens int32 [S, N]; the block rows against a prefix of the whole batch and their caches -> (top1 [S, L], conf [S, L][, logits])."""
-    _check_tokens(model, tokens)
-    S, N = tokens.shape
-    if seqs_per_cache < 1 or S % seqs_per_cache:
-        raise PsdError(f"{S} sequences, {seqs_per_cache} to a cache")
-    c = kv.c(model, S // seqs_per_cache, seqs_per_cache)
-    ws, nb = _shared_ws(model, S, L, c)
-    top1 = torch.empty((S, L), dtype=torch.int32, device=tokens.device)
-    conf = torch.empty((S, L), dtype=torch.float32, device=tokens.device)
-    logits = torch.empty((S * L, model.shape.vocab), dtype=torch.float32, device=tokens.device) if want_logits else None
-    _check(model.lib.psd_forward_confidence_shared(model.handle, _ptr(tokens), S, N, block_start, L, C.byref(c), _ptr(top1), _ptr(conf),
-                                                   _ptr(logits), _ptr(ws), nb, _stream()))
+    with _on_device(_check_tokens(model, tokens)) as stream:
+        S, N = tokens.shape
+        if seqs_per_cache < 1 or S % seqs_per_cache:
+            raise PsdError(f"{S} sequences, {seqs_per_cache} to a cache")
+        c = kv.c(model, S // seqs_per_cache, seqs_per_cache)
+        ws, nb = _shared_ws(model, S, L, c)
+        top1 = torch.empty((S, L), dtype=torch.int32, device=tokens.device)
+        conf = torch.empty((S, L), dtype=torch.float32, device=tokens.device)
+        logits = torch.empty((S * L, model.shape.vocab), dtype=torch.float32, device=tokens.device) if want_logits else None
+        _check(model.lib.psd_forward_confidence_shared(model.handle, _ptr(tokens), S, N, block_start, L, C.byref(c), _ptr(top1), _ptr(conf),
+                                                       _ptr(logits), _ptr(ws), nb, stream))
     return (top1, conf, logits) if want_logits else (top1, conf)
 
 
 def psd_kv_extend_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, kv: SharedKv) -> None:
     """The block of every sequence of tokens [B, N] behind the first kv.length positions of its cache (kv.length is then L more: the
     caller's to count)."""
-    _check_tokens(model, tokens)
-    B, N = tokens.shape
-    c = kv.c(model, B)
-    ws, nb = _shared_ws(model, B, L, c)
-    _check(model.lib.psd_kv_extend_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(c), _ptr(ws), nb, _stream()))
+    with _on_device(_check_tokens(model, tokens)) as stream:
+        B, N = tokens.shape
+        c = kv.c(model, B)
+        ws, nb = _shared_ws(model, B, L, c)
+        _check(model.lib.psd_kv_extend_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(c), _ptr(ws), nb, stream))
 
 
 def psd_decode_block_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, policy: Policy, graph: Graph, kv: SharedKv,
                             stats: Optional[Sequence[Stats]] = None) -> List[Stats]:
     """psd_decode_block with shared model calls; the finished block is appended to the caches (kv.length is then L more)."""
-    _check_tokens(model, tokens)
-    B, N = tokens.shape
-    K = graph.K
-    c = kv.c(model, B)
-    extra = _check(model.lib.psd_decode_scratch_bytes(B, N, L, K))
-    ws, nb = _shared_ws(model, B * K, L, kv.c(model, B, K), extra=extra)
-    cstats = (_Stats * B)()
-    g, pol = graph.c(), policy.c()
-    _check(model.lib.psd_decode_block_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(pol), C.byref(g), cstats, C.byref(c),
-                                             _ptr(ws), nb, _stream()))
+    with _on_device(_check_tokens(model, tokens)) as stream:
+        B, N = tokens.shape
+        K = graph.K
+        c = kv.c(model, B)
+        extra = _check(model.lib.psd_decode_scratch_bytes(B, N, L, K))
+        ws, nb = _shared_ws(model, B * K, L, kv.c(model, B, K), extra=extra)
+        cstats = (_Stats * B)()
+        g, pol = graph.c(), policy.c()
+        _check(model.lib.psd_decode_block_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(pol), C.byref(g), cstats, C.byref(c),
+                                                 _ptr(ws), nb, stream))
     return _add_stats(stats, cstats, B)
 
 

@@ -347,3 +347,25 @@ def test_caches_of_a_model_on_a_device_without_an_index(lib):
             psd.SharedKv(cache=types.SimpleNamespace(**dict(vars(cache), **bad)), length=16).c(model, 2)
     with pytest.raises(psd.PsdError):
         psd.SharedKv(cache=cache, length=16, cache_weights=weights.to("meta")).c(model, 2)
+
+
+def test_model_calls_run_on_the_stream_of_the_models_device(lib, monkeypatch):
+    # the current device is another one: the calls have to enter the model's, and take the stream that is current there
+    model, kv, seen = _stub(lib), psd.SharedKv(), []
+
+    class Entered:
+        def __init__(self, device):
+            seen.append(device)
+
+        def __enter__(self):
+            raise psd.PsdError("entered")
+
+        def __exit__(self, *what):
+            pass
+    monkeypatch.setattr(B, "_on_device", Entered)
+    tokens = torch.zeros((2, 64), dtype=torch.int32)
+    for call in (lambda: psd.psd_forward_confidence_shared(model, tokens, 0, 32, kv), lambda: psd.psd_kv_extend_shared(model, tokens, 0, 32, kv),
+                 lambda: psd.psd_decode_block_shared(model, tokens, 0, 32, psd.Policy(), psd.chain_graph(2), kv)):
+        with pytest.raises(psd.PsdError, match="entered"):
+            call()
+    assert seen == [torch.device("cpu")] * 3
