@@ -719,6 +719,14 @@ def psd_decode_block_approx(model: Model, tokens: torch.Tensor, block_start: int
 _DTYPES = {torch.bfloat16: 1, torch.float32: 0}
 
 
+def _int32(value, what: str) -> int:
+    """A count for a 32-bit argument (ctypes would cut what is larger)."""
+    n = int(value)
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise PsdError(f"{what} {n} is no 32-bit number")
+    return n
+
+
 class KvSegment:
     """Keys that the sequences of a batch attend to, one unit of them for every seqs_per_unit consecutive sequences.
 
@@ -752,10 +760,12 @@ class KvSegment:
         def address(t):
             return None if t is None or t.numel() == 0 else t.data_ptr()
         # (strides of dimensions of one entry mean nothing, and torch gives any)
+        ld_k, ld_vt = k.stride(1) if positions > 1 else width, vt.stride(1) if width > 1 else vt.shape[2]
+        ld_w = 0 if weights is None else weights.stride(1) if self.n_kv_heads > 1 else weights.shape[2]
         self.c = _Segment(address(k), address(vt), address(lens), address(weights), k.stride(0) if units > 1 else 0,
-                          vt.stride(0) if units > 1 else 0, 0 if weights is None or units == 1 else weights.stride(0),
-                          k.stride(1) if positions > 1 else width, vt.stride(1) if width > 1 else vt.shape[2],
-                          0 if weights is None else weights.stride(1) if self.n_kv_heads > 1 else weights.shape[2], n, self.seqs_per_unit, 0)
+                          vt.stride(0) if units > 1 else 0, 0 if weights is None or units == 1 else weights.stride(0), _int32(ld_k, "key row stride"),
+                          _int32(ld_vt, "value row stride"), _int32(ld_w, "weight row stride"), _int32(n, "length"),
+                          _int32(self.seqs_per_unit, "seqs_per_unit"), 0)
 
 
 class KvSegments:
@@ -798,6 +808,8 @@ def _attention_shape(q: torch.Tensor, keys: KvSegments, out: Optional[torch.Tens
     for s in keys.segments:
         if s.seqs_per_unit < 1 or s.units * s.seqs_per_unit != S:
             raise PsdError(f"{s.units} units of {s.seqs_per_unit} sequences for a batch of {S}")
+    if S * L * H >= 2 ** 31:
+        raise PsdError(f"{S} sequences of {L} rows of {H} heads are too many")
     shape = _AttentionShape(S, L, H, keys.n_kv_heads, d, _DTYPES[q.dtype], _rows(q, "q"), H * d if out is None else _rows(out, "out"))
     if len(keys.shapes) >= 64:
         keys.shapes.clear()
@@ -894,8 +906,8 @@ def psd_kv_evict(src: KvSegment, dst: KvSegment, keep: int, first: int = 0, last
     shape = (src.units, src.n_kv_heads, int(keep))
     if (dst.units, dst.n_kv_heads, dst.d_head, dst.dtype, dst.device) != (src.units, src.n_kv_heads, src.d_head, src.dtype, src.device):
         raise PsdError("source and destination differ in units, heads, type or device")
-    if keep < 1:
-        raise PsdError(f"keep {keep}")
+    if not 1 <= _int32(keep, "keep") or _int32(first, "first") < 0 or _int32(last, "last") < 0:
+        raise PsdError(f"keep {keep}, first {first}, last {last}")
     if kept is None:
         kept = torch.empty(shape, dtype=torch.int32, device=src.device)
     for name, t, want in (("kept", kept, shape), ("kept_lens", kept_lens, shape[:1])):
@@ -934,7 +946,8 @@ class SharedKv:
             return None if t is None else t.data_ptr()
         return _KvShared(None if self.prefix is None else self.prefix.mem.data_ptr(), None if self.cache is None else self.cache.mem.data_ptr(),
                          address(self.prefix_weights), address(self.cache_weights), 0 if self.prefix is None else self.prefix.capacity,
-                         int(self.prefix_len), 0 if self.cache is None else self.cache.capacity, int(self.length), int(seqs_per_cache), 0)
+                         _int32(self.prefix_len, "prefix_len"), 0 if self.cache is None else self.cache.capacity, _int32(self.length, "length"),
+                         _int32(seqs_per_cache, "seqs_per_cache"), 0)
 
 
 def _device_of(model: Model) -> torch.device:
@@ -967,7 +980,7 @@ def psd_forward_confidence_shared(model: Model, tokens: torch.Tensor, block_star
         top1 = torch.empty((S, L), dtype=torch.int32, device=tokens.device)
         conf = torch.empty((S, L), dtype=torch.float32, device=tokens.device)
         logits = torch.empty((S * L, model.shape.vocab), dtype=torch.float32, device=tokens.device) if want_logits else None
-        _check(model.lib.psd_forward_confidence_shared(model.handle, _ptr(tokens), S, N, block_start, L, C.byref(c), _ptr(top1), _ptr(conf),
+        _check(model.lib.psd_forward_confidence_shared(model.handle, _ptr(tokens), S, N, _int32(block_start, "block_start"), _int32(L, "L"), C.byref(c), _ptr(top1), _ptr(conf),
                                                        _ptr(logits), _ptr(ws), nb, stream))
     return (top1, conf, logits) if want_logits else (top1, conf)
 
@@ -979,7 +992,7 @@ def psd_kv_extend_shared(model: Model, tokens: torch.Tensor, block_start: int, L
         B, N = tokens.shape
         c = kv.c(model, B)
         ws, nb = _shared_ws(model, B, L, c)
-        _check(model.lib.psd_kv_extend_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(c), _ptr(ws), nb, stream))
+        _check(model.lib.psd_kv_extend_shared(model.handle, _ptr(tokens), B, N, _int32(block_start, "block_start"), _int32(L, "L"), C.byref(c), _ptr(ws), nb, stream))
 
 
 def psd_decode_block_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, policy: Policy, graph: Graph, kv: SharedKv,
@@ -993,8 +1006,8 @@ def psd_decode_block_shared(model: Model, tokens: torch.Tensor, block_start: int
         ws, nb = _shared_ws(model, B * K, L, kv.c(model, B, K), extra=extra)
         cstats = (_Stats * B)()
         g, pol = graph.c(), policy.c()
-        _check(model.lib.psd_decode_block_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(pol), C.byref(g), cstats, C.byref(c),
-                                                 _ptr(ws), nb, stream))
+        _check(model.lib.psd_decode_block_shared(model.handle, _ptr(tokens), B, N, _int32(block_start, "block_start"), _int32(L, "L"), C.byref(pol), C.byref(g),
+                                                 cstats, C.byref(c), _ptr(ws), nb, stream))
     return _add_stats(stats, cstats, B)
 
 

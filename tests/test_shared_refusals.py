@@ -369,3 +369,27 @@ def test_model_calls_run_on_the_stream_of_the_models_device(lib, monkeypatch):
         with pytest.raises(psd.PsdError, match="entered"):
             call()
     assert seen == [torch.device("cpu")] * 3
+
+
+def test_numbers_that_a_32_bit_argument_would_cut_are_refused(lib):
+    # (1 << 32 more than a number that is taken; strides of tensors without memory)
+    big = 1 << 32
+    k, vt = torch.zeros((2, 20, 256), dtype=BF), torch.zeros((2, 256, 32), dtype=BF)
+    with pytest.raises(psd.PsdError, match="32-bit"):
+        psd.KvSegment(k, vt, 64, seqs_per_unit=big + 2)
+    meta = torch.empty(1, dtype=BF, device="meta")
+    with pytest.raises(psd.PsdError, match="32-bit"):
+        psd.KvSegment(meta.as_strided((1, 20, 256), (0, big + 256, 1)), meta.as_strided((1, 256, 32), (0, 32, 1)), 64)
+    with pytest.raises(psd.PsdError, match="32-bit"):
+        psd.KvSegment(meta.as_strided((1, 20, 256), (0, 256, 1)), meta.as_strided((1, 256, 32), (0, big + 32, 1)), 64)
+    one = psd.KvSegment(meta.as_strided((1, 20, 256), (0, 256, 1)), meta.as_strided((1, 256, 32), (0, 32, 1)), 64, seqs_per_unit=1 << 30)
+    with pytest.raises(psd.PsdError, match="too many"):
+        psd.psd_attention_weights_bytes(meta.as_strided((1 << 30, 4, 8, 64), (2048, 512, 64, 1)), psd.KvSegments([one]))
+    ok = psd.KvSegment(k, vt, 64, weights=torch.zeros((2, 4, 20)))
+    for args in ((big + 5, 0, 0), (5, big, 0), (5, 0, big), (5, -1, 0), (5, 0, -1), (-big + 5, 0, 0)):
+        with pytest.raises(psd.PsdError) as why:
+            psd.psd_kv_evict(ok, ok, *args, kept=torch.zeros((2, 4, 5), dtype=torch.int32))
+        assert "on a GPU" not in str(why.value), args
+    for kv in (psd.SharedKv(prefix_len=big), psd.SharedKv(length=-big)):
+        with pytest.raises(psd.PsdError, match="32-bit"):
+            kv.c(_stub(lib), 1)
