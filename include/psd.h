@@ -398,6 +398,10 @@ int32_t psd_shared_struct_sizes(int32_t *out, int32_t n);
 int64_t psd_attention_shared_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments);
 int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments, void *out,
                              float *lse, void *ws, int64_t ws_bytes, void *stream);
+/* Debug: how psd_attention_shared splits its work.  For the first n_jobs jobs 7 numbers each: first segment (of those with keys), segments, form (0: up to 32 rows a
+ *   workgroup, 1: 128 rows, 2: a unit and KV head to a wavefront), units, tiles of rows of a unit and KV head, parts of the keys, and the
+ *   rows of a unit and KV head.  Returns the number of jobs. */
+int32_t psd_debug_attention_plan(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments, int32_t *jobs, int32_t n_jobs);
 int64_t psd_attention_weights_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments);
 int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments,
                               const float *lse, int32_t accumulate, void *ws, int64_t ws_bytes, void *stream);

@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass, field
-from typing import List, Optional, Sequence
+from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -171,6 +171,7 @@ def load_library():
         "psd_shared_struct_sizes": (i32, [C.POINTER(i32), i32]),
         "psd_attention_shared_bytes": (i64, [vp, vp, i32]),
         "psd_attention_shared": (i32, [vp, vp, vp, i32, vp, vp, vp, i64, vp]),
+        "psd_debug_attention_plan": (i32, [vp, vp, i32, C.POINTER(i32), i32]),
         "psd_attention_weights_bytes": (i64, [vp, vp, i32]),
         "psd_attention_weights": (i32, [vp, vp, vp, i32, vp, i32, vp, i64, vp]),
         "psd_shared_workspace_bytes": (i64, [C.POINTER(_Config), i32, i32, C.POINTER(_KvShared)]),
@@ -866,6 +867,13 @@ def psd_attention_weights_bytes(q: torch.Tensor, keys: KvSegments) -> int:
     """Bytes of workspace that psd_attention_weights needs for q and keys (possibly 0)."""
     shape = _attention_shape(q, keys)
     return int(_check(load_library().psd_attention_weights_bytes(C.byref(shape), keys.c, keys.n)))
+
+
+def attention_plan(q: torch.Tensor, keys: KvSegments) -> List[Tuple[int, ...]]:
+    """psd_debug_attention_plan: (first segment, segments, form, units, tiles, parts, rows of a unit and KV head) of every job."""
+    shape, jobs = _attention_shape(q, keys), (C.c_int32 * 28)()
+    n = _check(load_library().psd_debug_attention_plan(C.byref(shape), keys.c, keys.n, jobs, 4))
+    return [tuple(jobs[7 * i:7 * i + 7]) for i in range(n)]
 
 
 def psd_attention_shared(q: torch.Tensor, keys: KvSegments, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,

@@ -1161,6 +1161,21 @@ int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, co
     return PSD_OK;
 }
 
+int32_t psd_debug_attention_plan(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments, int32_t *jobs, int32_t n_jobs) {
+    SharedShape sh;
+    SharedSegment seg[kMaxSegments];
+    SharedLaunch ln;
+    CHECK(check_shared(shape, segments, n_segments, &sh, seg));
+    if (!plan_attention_shared(sh, seg, n_segments, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
+    for (int32_t i = 0; jobs && i < n_jobs && i < ln.n_jobs; ++i) {
+        const SharedJob &jb = ln.job[i];
+        const int32_t rows = sh.S / jb.units * sh.L * (sh.n_heads / sh.n_kv_heads);
+        const int32_t what[7] = {jb.seg, jb.segs, jb.packed ? 2 : jb.tiled, jb.units, jb.tiles, jb.splits, rows};
+        std::copy(what, what + 7, jobs + 7 * i);
+    }
+    return ln.n_jobs;
+}
+
 int64_t psd_attention_weights_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments) {
     SharedShape sh;
     SharedSegment seg[kMaxSegments];
