@@ -13,7 +13,7 @@ import torch
 
 import psd_inputs as inp
 from oracle import psd_oracle as orc
-from tests.shared_common import kept_positions
+from tests.shared_common import kept_positions, slots
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -372,3 +372,127 @@ def test_shared_calls_refuse_memory_that_they_would_add_to_twice():
         with pytest.raises(psd.PsdError, match="the prefix is one of"):
             psd.psd_decode_block_shared(model, d[:1], 96, L, *decode, both)
     psd.psd_forward_confidence_shared(model, d[:1], 96, L, psd.SharedKv(prefix=one, prefix_len=64, cache=one, length=32))   # (read only)
+
+
+def _block_behind(host, t, start, L, frozen):
+    """Oracle: logits of the block rows behind `frozen` ((keys, values) of every layer), and the rows' own (keys, values)."""
+    cos, sin = np.asarray(host.rope_cos[start:start + L], dtype=np.float64), np.asarray(host.rope_sin[start:start + L], dtype=np.float64)
+    h, own = np.asarray(host.tok_emb, dtype=np.float64)[t[start:start + L]], []
+    for lw, kv in zip(host.layers, frozen):
+        h = orc.layer_forward(h, lw, host.shape, cos, sin, None, None, own, kv)
+    y = orc.rmsnorm(h, np.asarray(host.final_norm, dtype=np.float64), host.shape.rms_eps)
+    return host.shape.logit_scale * (y @ np.asarray(host.lm_head, dtype=np.float64).T), own
+
+
+def _evicted(shape, seed, L, P, own, keep, first, last):
+    """Two requests whose caches of `own` positions were cut to `keep`: (psd, host, model, tokens, start, SharedKv, oracle's entries of each)."""
+    import paper_2605_15609_amd as psd
+    B = 2
+    t, start = _batch(shape, B, P, own, L, seed, blocks_behind=1)
+    host = inp.draw_model(shape, t.shape[1])
+    model = psd.Model.from_host(host, DEV)
+    kv = _prefilled(psd, model, _dev(t), P, own, L, own + L)
+    kv.cache_weights = kv.cache.new_weights()
+    psd.psd_forward_confidence_shared(model, _dev(t), start, L, kv)
+    small = psd.KvCache(model, B, keep + 2 * L)
+    kept = psd.psd_kv_evict(kv.cache.segment(own, kv.cache_weights), small.segment(keep + 2 * L), keep, first, last)
+    kept = kept.cpu().numpy().reshape(B, shape.n_layers, shape.n_kv_heads, keep)
+    frozen = []
+    for b in range(B):
+        seen = []
+        orc.forward_hidden(host, t[b], None, L, seen)
+        frozen.append([tuple(np.concatenate([x[:P], np.stack([x[P + kept[b, li, g], g] for g in range(shape.n_kv_heads)], 1)]) for x in kv_)
+                       for li, kv_ in enumerate(seen)])
+    return psd, host, model, t, start, psd.SharedKv(prefix=kv.prefix, prefix_len=P, cache=small, length=keep), frozen
+
+
+@pytest.mark.parametrize("name", list(MODELS))
+@pytest.mark.parametrize("L,keep", [(16, 41), (32, 40), (16, 63)])
+def test_a_block_goes_behind_a_length_that_is_no_multiple_of_16(name, L, keep):
+    """Eviction leaves any length.  The block behind it, its keys and values in the cache, and the block after that, against the oracle's
+    forward over the entries that stayed."""
+    shape, tol = MODELS[name]
+    shape = _bc(shape)
+    psd, host, model, t, start, kv, frozen = _evicted(shape, 81, L, 48 if L == 16 else 64, 64, keep, 4, 8)
+    B, w = 2, shape.n_kv_heads * shape.d_head
+    print(f"[shared model] {name} L={L} behind {keep}", flush=True)
+
+    def block(at, behind):
+        top1, conf, logits = psd.psd_forward_confidence_shared(model, _dev(t), at, L, kv, want_logits=True)
+        logits, rows = logits.cpu().numpy().reshape(B, L, -1), []
+        for b in range(B):
+            z, own = _block_behind(host, t[b], at, L, behind[b])
+            _against(z, logits[b], top1[b].cpu().numpy(), conf[b].cpu().numpy(), t[b], shape.mask_id, at, L, tol, f"{name} sequence {b} at {at}")
+            rows.append(own)
+        return rows
+    block(start, frozen)
+    t[:, start:start + L] = np.stack([inp.draw_prompt(shape.vocab, L, 90 + b) for b in range(B)])
+    before = kv.cache.segment(keep + 2 * L)
+    k_before, vt_before = before.k.clone(), before.vt.clone()
+    psd.psd_kv_extend_shared(model, _dev(t), start, L, kv)
+    kv.length += L
+    rows = block(start + L, [[(np.concatenate([k, r[0]]), np.concatenate([v, r[1]])) for (k, v), r in zip(frozen[b], _block_behind(host, t[b], start, L, frozen[b])[1])]
+                             for b in range(B)])
+    # what was written, and what was not
+    after = kv.cache.segment(keep + 2 * L)
+    k, vt = after.k.float().cpu().numpy(), after.vt.float().cpu().numpy()
+    at = np.arange(keep, keep + L)
+    slot = slots(keep + L).numpy()[at]
+    other = np.ones(vt.shape[2], dtype=bool)
+    other[slot] = False
+    assert torch.equal(after.k[:, :keep], k_before[:, :keep]) and torch.equal(after.k[:, keep + L:], k_before[:, keep + L:])
+    assert torch.equal(after.vt[:, :, torch.from_numpy(other)], vt_before[:, :, torch.from_numpy(other)])
+    # The first layer's, element by element: the norm's output, the projection and its rotation are rounded to the model's type (u each, two
+    # channels meet in a rotation), sums of d_model products are fp32
+    u, d = (0.0 if shape.dtype == "fp32" else 2.0 ** -8), shape.d_model
+    rel = u + (d + 16) * 2.0 ** -24
+    for b in range(B):
+        a = orc.rmsnorm(np.asarray(host.tok_emb, dtype=np.float64)[t[b, start:start + L]], np.asarray(host.layers[0]["attn_norm"], dtype=np.float64), shape.rms_eps)
+        want = _block_behind(host, t[b], start, L, frozen[b])[1][0]
+        size_k, size_v = (np.abs(a) @ np.abs(np.asarray(host.layers[0][m], dtype=np.float64)).T for m in ("wk", "wv"))
+        if host.layers[0].get("bk") is not None:
+            size_k, size_v = size_k + np.abs(host.layers[0]["bk"]), size_v + np.abs(host.layers[0]["bv"])
+        size_k = size_k.reshape(L, shape.n_kv_heads, 2, shape.d_head // 2).sum(2)      # (the two channels of a rotation are half a head apart)
+        size_k = np.concatenate([size_k, size_k], -1).reshape(L, w)
+        got_k, got_v = k[b * shape.n_layers, at], vt[b * shape.n_layers][:, slot].T
+        assert (np.abs(got_k - want[0].reshape(L, w)) <= 3.1 * rel * size_k).all() and (np.abs(got_v - want[1].reshape(L, w)) <= 2.1 * rel * size_v).all(), b
+
+
+@pytest.mark.parametrize("graph_kind", ["chain", "lattice"])
+def test_requests_decoded_together_behind_evicted_caches(graph_kind):
+    """fp32, two blocks each: together, one at a time, and the oracle's decode over the entries that stayed give the same tokens."""
+    from tests.gpu_common import oracle_graph
+    shape, L = _bc(FP32, logit_scale=6.0), 16
+    psd, host, model, t, start, kv, frozen = _evicted(shape, 82, L, 32, 64, 37, 4, 16)
+    t[:, start:] = shape.mask_id
+    graph = psd.chain_graph(3) if graph_kind == "chain" else psd.lattice_graph(2)
+    policy, oracle_policy = psd.Policy(0.5, 1), orc.Policy(0.5, 1)
+    singles, per_seq = [], kv.cache.segment(37).k.shape[0] // 2
+    for b in range(2):
+        one = psd.KvCache(model, 1, kv.cache.capacity)
+        a, c = kv.cache.segment(37), one.segment(37)
+        c.k.copy_(a.k[b * per_seq:(b + 1) * per_seq])
+        c.vt.copy_(a.vt[b * per_seq:(b + 1) * per_seq])
+        singles.append(psd.SharedKv(prefix=kv.prefix, prefix_len=kv.prefix_len, cache=one, length=37))
+    together, alone = _dev(t), [_dev(t[b:b + 1]) for b in range(2)]
+    want = [t[b].copy() for b in range(2)]
+    for n in range(2):
+        at = start + n * L
+        psd.psd_decode_block_shared(model, together, at, L, policy, graph, kv)
+        kv.length += L
+        for b in range(2):
+            psd.psd_decode_block_shared(model, alone[b], at, L, policy, graph, singles[b])
+            singles[b].length += L
+            entries = frozen[b]
+
+            def confidence(tokens, block_start, length):
+                z, _ = _block_behind(host, np.asarray(tokens), block_start, length, entries)
+                x, c = orc.top1_confidence(z, shape.mask_id)
+                blk = np.asarray(tokens)[block_start:block_start + length]
+                return np.where(blk == shape.mask_id, x, blk).astype(np.int32), np.where(blk == shape.mask_id, c, -1.0).astype(np.float32)
+            want[b], _ = orc.decode_block(confidence, want[b], at, L, oracle_policy, oracle_graph(graph), shape.mask_id)
+            own = _block_behind(host, want[b], at, L, entries)[1]
+            frozen[b] = [(np.concatenate([k, r[0]]), np.concatenate([v, r[1]])) for (k, v), r in zip(entries, own)]
+    for b in range(2):
+        got = together[b].cpu().numpy()
+        assert (got == alone[b][0].cpu().numpy()).all() and (got == want[b]).all(), b
