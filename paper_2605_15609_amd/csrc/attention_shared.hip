@@ -582,7 +582,7 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
         const bool seen = any_rows && (jb.segs == 1 || my_seq / run.seqs_per_unit == run.u);
         for (int i = 0; i < run.tiles; ++i, stage ^= 1) {
             // this tile has landed for every wavefront, and every wavefront is done with the stage that the next one goes to
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (i + 1 < run.tiles) fetch(run, i + 1, stage ^ 1);
