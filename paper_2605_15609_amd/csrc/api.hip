@@ -1234,7 +1234,7 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
     if (dst->lens) PSD_FAIL(PSD_ERR_INVALID_ARG, "the destination has lengths of its own");
     const int32_t most = std::min(keep, src->len);
     if (dst->len < most) PSD_FAIL(PSD_ERR_SHAPE, "a destination of %d positions for %d", dst->len, most);
-    if (kv_evict_workgroups(from, units, n_kv_heads, d_head, dtype, keep) >= 1ll << 31 || (int64_t)units * n_kv_heads >= 1ll << 31)
+    if (!kv_evict_launchable(from, units, n_kv_heads, d_head, dtype, keep))
         PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
     // what is read, and what is written: `most` positions, value rows up to the group of 16 that the last one is in
     const int64_t w = (int64_t)n_kv_heads * d_head;

@@ -917,6 +917,14 @@ __global__ __launch_bounds__(256) void block_values_kernel(const float *__restri
     for (int c = threadIdx.x; c < width; c += 256) vT[(s * width + c) * ld_vt + vt_key_slot(i)] = qkv[(int64_t)blockIdx.x * ld_qkv + v_col + c];
 }
 
+// the join of a launch: lanes of parts to a row (G of its kernel), workgroups
+constexpr int MANY_PARTS = 8;
+bool many_parts(const SharedLaunch &ln) { return ln.parts >= 16; }
+int64_t join_workgroups(const SharedShape &sh, const SharedLaunch &ln) {
+    const int rows = 256 / (sh.d_head / 4 * (many_parts(ln) ? MANY_PARTS : 1));
+    return (sh.n_rows + rows - 1) / rows;
+}
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 template <typename T, int DH>
@@ -928,12 +936,9 @@ void run_attention(const T *q, const SharedShape &sh, const SharedLaunch &ln, hi
     ensure_dynamic_lds(reinterpret_cast<const void *>(kern), smem, lds_raised);
     if (ln.blocks > 0) hipLaunchKernelGGL(kern, dim3((unsigned)ln.blocks), dim3(NW * 64), smem, st, q, sh, ln, sl2);
     if (ln.blocks > 0 && ln.parts == 0) return;
-    auto join = [&](auto g) {
-        constexpr int G = decltype(g)::value, rows = 256 / (DH / 4 * G);
-        hipLaunchKernelGGL((shared_join_kernel<T, DH, G>), dim3((unsigned)((sh.n_rows + rows - 1) / rows)), dim3(256), 0, st, sh, ln, sl2);
-    };
-    if (ln.parts >= 16) join(std::integral_constant<int, 8>());
-    else join(std::integral_constant<int, 1>());
+    const dim3 grid((unsigned)join_workgroups(sh, ln));
+    if (many_parts(ln)) hipLaunchKernelGGL((shared_join_kernel<T, DH, MANY_PARTS>), grid, dim3(256), 0, st, sh, ln, sl2);
+    else hipLaunchKernelGGL((shared_join_kernel<T, DH, 1>), grid, dim3(256), 0, st, sh, ln, sl2);
 }
 
 template <typename T, int DH>
@@ -1077,7 +1082,7 @@ SharedLaunch plan_attention(const SharedShape &sh, const SharedSegment *given, i
     int64_t block = 0;
     for (int j = 0; j < ln.n_jobs; ++j) {
         SharedJob &jb = ln.job[j];
-        jb.block0 = (int)block;   // (grids of 2^31 workgroups and more are refused)
+        jb.block0 = (int)block;   // (grids of 2^24 workgroups and more are refused)
         block += align_up(workgroups(jb, sh.n_kv_heads, jb.splits), 8);
     }
     if (ln.parts == 1) ln.parts = 0;
@@ -1144,7 +1149,7 @@ bool plan_attention_shared(const SharedShape &sh, const SharedSegment *seg, int 
     for (int i = 0; i < n; ++i)   // (counts that the plans keep in 32 bits)
         if ((double)sh.n_rows * seg[i].len > 1e15) return false;
     *out = plan_attention(sh, seg, n);
-    return out->blocks < (1ll << 31);
+    return launchable(out->blocks, NW * 64) && ((out->blocks > 0 && out->parts == 0) || launchable(join_workgroups(sh, *out), 256));
 }
 int64_t shared_attention_bytes(const SharedShape &sh, const SharedLaunch &ln) {
     return align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256) + align_up((int64_t)ln.parts * sh.n_rows * 8, 256);
@@ -1165,7 +1170,7 @@ bool plan_attention_weights(const SharedShape &sh, const SharedSegment *seg, int
     for (int i = 0; i < n; ++i)
         if ((double)sh.n_rows * seg[i].len > 1e15) return false;
     *out = plan_weights(sh, seg, n);
-    return out->blocks < (1ll << 31) && out->join_blocks < (1ll << 31);
+    return launchable(out->blocks, NW * 64) && launchable(out->join_blocks, 256);
 }
 int64_t shared_weights_bytes(const SharedLaunch &ln) { return ln.parts * 256ll; }
 

@@ -550,6 +550,7 @@ int32_t run_forward_cached(psd_handle *h, const int32_t *tokens, const int32_t *
     if (kv.shared && ws_bytes < p.total + shared_call_bytes(h->cfg, S, R, kv))
         PSD_FAIL(PSD_ERR_WORKSPACE, "workspace of %lld bytes, a forward over %d x %d rows with shared keys needs %lld", (long long)ws_bytes, S, R,
                  (long long)(p.total + shared_call_bytes(h->cfg, S, R, kv)));
+    if (kv.shared && !launchable((int64_t)S * R, 256)) PSD_FAIL(PSD_ERR_SHAPE, "%d x %d rows are more than a launch takes", S, R);
     if (kv.shared && R > L) PSD_FAIL(PSD_ERR_INVALID_ARG, "%d rows per sequence in blocks of %d", R, L);
     if (!kv.dual && !kv.shared && kv.len != block_start)
         PSD_FAIL(PSD_ERR_SHAPE, "the cache holds %d positions, the block starts at %d", kv.len, block_start);

@@ -290,7 +290,7 @@ void launch_kv_evict(const SharedSegment &src, const SharedSegment &dst, int uni
     else run_evict<float>(src, dst, units, n_kv_heads, d_head, dtype, keep, n_first, n_last, kept, kept_lens, st);
 }
 
-int64_t kv_evict_workgroups(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep) {
+bool kv_evict_launchable(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep) {
     const GatherGrid gr = gather_grid(src, units, n_kv_heads, d_head, dtype, keep);
-    return gr.per_unit * units + gr.values;
+    return launchable((int64_t)units * n_kv_heads, ST) && launchable(gr.per_unit * units + gr.values, GT);
 }

@@ -424,6 +424,8 @@ struct SharedShape {
     int64_t ld_q, ld_out, n_rows;        // n_rows = S * L * n_heads
 };
 constexpr int kMaxSegments = PSD_MAX_SEGMENTS;
+// A launch holds fewer than 2^32 threads: above, only the lower 32 bits of their number are run, and no error says so.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups * threads < 1ll << 32; }
 // what one launch does: jobs behind one another in the grid.  A job's workgroups take a tile of rows of a unit (tiled: of its first
 // segment, else of its last) against the keys of `segs` segments from `seg` on, or a part of them
 struct SharedJob {
@@ -456,7 +458,7 @@ void launch_attention_weights(const void *q, const SharedShape &sh, SharedLaunch
 // values of the L rows of every sequence of qkv [S * L, ld_qkv] (columns from v_col on) transposed, for fp32 models
 void launch_block_values(const float *qkv, int ld_qkv, int v_col, int S, int L, int width, float *vT, int ld_vt, hipStream_t st);
 // kv_evict.hip
-int64_t kv_evict_workgroups(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep);
+bool kv_evict_launchable(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep);
 void launch_kv_evict(const SharedSegment &src, const SharedSegment &dst, int units, int n_kv_heads, int d_head, int dtype, int keep, int n_first,
                      int n_last, int32_t *kept, int32_t *kept_lens, hipStream_t st);
 // lm_head.hip (bf16): LM-head fused with the online top-1 / sum-exp reduction

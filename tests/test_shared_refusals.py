@@ -311,7 +311,7 @@ def test_counts_near_the_end_of_32_bits_are_refused(lib):
     for length, taken in ((most, True), (most + 1, False), (2 ** 31 - 16, False), (2 ** 31 - 1, False)):
         long = seg(len=length, ld_vt=min(length + 15, 2 ** 31 - 1) // 16 * 16, ld_w=length, weights=BASE)
         assert (ask(lib, shape(), long) > 0) == taken
-        assert (lib.psd_attention_weights_bytes(C.byref(shape()), (B._Segment * 1)(long), 1) >= 0) == taken
+        assert (lib.psd_attention_weights_bytes(C.byref(shape(n_heads=2, n_kv_heads=2)), (B._Segment * 1)(long), 1) >= 0) == taken
     for keep in (most + 1, 2 ** 31 - 512, 2 ** 31 - 1):
         assert evict(lib, keep=keep) < 0 and b"keep" in lib.psd_last_error()
 
@@ -393,3 +393,25 @@ def test_numbers_that_a_32_bit_argument_would_cut_are_refused(lib):
     for kv in (psd.SharedKv(prefix_len=big), psd.SharedKv(length=-big)):
         with pytest.raises(psd.PsdError, match="32-bit"):
             kv.c(_stub(lib), 1)
+
+
+def test_launches_of_2_to_the_32_threads_are_refused(lib):
+    # workgroups of 256: 2^24 of them; what is planned onto fewer is taken
+    def plan(S, heads, n, ld_vt, per=1, L=1):
+        s = seg(len=n, seqs_per_unit=per, ld_k=heads * 64, ld_vt=ld_vt, stride_k=n * heads * 64, stride_vt=heads * 64 * ld_vt, weights=BASE, ld_w=n, stride_w=heads * n)
+        sh = shape(S=S, L=L, n_heads=heads, n_kv_heads=heads, ld_q=heads * 64, ld_out=heads * 64)
+        return ask(lib, sh, s), lib.psd_attention_weights_bytes(C.byref(sh), (B._Segment * 1)(s), 1)
+    attention, weights = plan((1 << 21) - 1, 8, 200, 208)        # a unit and KV head to a workgroup
+    assert attention >= 0 and weights >= 0
+    assert plan((1 << 20) - 1, 8, 500, 512)[1] >= 0 and plan(1 << 20, 8, 500, 512)[1] < 0      # two blocks of keys to a unit
+    for S in (1 << 21, (1 << 21) + 1, 1 << 22):
+        attention, weights = plan(S, 8, 200, 208)
+        assert attention < 0 and weights < 0 and b"more workgroups" in lib.psd_last_error()
+    assert plan(1 << 21, 8, 100, 112)[0] >= 0 and plan(1 << 23, 8, 100, 112)[0] < 0      # a unit and KV head to a wavefront
+    # no keys: zeros by the kernel that joins parts, 16 rows of 64 channels a workgroup
+    empty = seg(len=0, seqs_per_unit=1)
+    assert ask(lib, shape(S=(1 << 24) - 1), empty) >= 0 and ask(lib, shape(S=1 << 24), empty) < 0
+    # eviction: 512 threads select for a unit and KV head
+    for units, heads in ((1 << 21, 4), (1 << 22, 4), (1 << 23, 1)):
+        assert evict(lib, units=units, heads=heads, kept=BASE) < 0 and b"more workgroups" in lib.psd_last_error()
+    assert evict(lib, units=(1 << 20) - 1, heads=4, kept=BASE) < 0 and b"more workgroups" not in lib.psd_last_error()
