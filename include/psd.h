@@ -392,7 +392,8 @@ int32_t psd_shared_struct_sizes(int32_t *out, int32_t n);
  *   fp32; with bf16 the probabilities are rounded to bf16 before they meet the values.  How keys are cut follows shapes and lengths, so a row's
  *   bits depend on those of its batch, but not on what other sequences hold.
  * psd_attention_weights: what each key drew: weights[u][g][j] = sum over the rows of the unit's sequences and the query heads of KV head g
- *   of exp(score - lse), lse from psd_attention_shared over all segments.  Segments without `weights` are skipped, no two may share any; accumulate = 1
+ *   of exp(score - lse), lse from psd_attention_shared over all segments (a float: a row's weights are off by a factor within |lse| 2^-22, and
+ *   where that says nothing any more, beyond 2^23, each is at least between 0 and 1).  Segments without `weights` are skipped, no two may share any; accumulate = 1
  *   adds to what is there, 0 overwrites.  Weights behind a unit's last key are left as they are.  ws likewise
  *   (psd_attention_weights_bytes; may be NULL where that is 0). */
 int64_t psd_attention_shared_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments);

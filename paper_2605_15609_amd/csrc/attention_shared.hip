@@ -859,6 +859,17 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_weights_kernel(const T *__r
                 for (int i = 0; i < NK; ++i) product(kf[i][ks], qf, x[i]);
             }
             const float z = z2[stage][rt * 32 + lrow];
+            // Beyond FAR the rounding of lse is more than an exponential spans: what would exceed a probability of 1 counts as 1
+            if (__any(fabsf(z) > FAR && fabsf(z) < INFINITY)) {
+#pragma unroll
+                for (int i = 0; i < NK; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float e = __builtin_fmaf(x[i][v], sl2, -z);
+                        w[i][v] += __builtin_amdgcn_exp2f(fabsf(z) > FAR && e > 0.f ? 0.f : e);
+                    }
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < NK; ++i)
 #pragma unroll

@@ -104,3 +104,28 @@ def test_keys_of_the_lowest_value_draw_nothing(dtype, H, Hkv, dh, S, L, n):
     near(lse, ref["lse"], ref["lse_tol"], "lse")
     near(ws[0][..., :n], ref["w"][0], ref["w_tol"][0], "weights")
     assert (ws[1][..., :45] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,dh,S,L,n", FORMS)
+@pytest.mark.parametrize("a,b", [(2.0 ** 20, 2.0 ** 20), (2.0 ** 20, -2.0 ** 20), (1.0, LOWEST), (1.0, -LOWEST)])
+def test_rows_of_huge_scores_give_no_more_than_one_each(dtype, H, Hkv, dh, S, L, n, a, b):
+    """The last sequence's scores are all huge, and equal: it adds between 0 and its number of rows to a key of its own, and leaves those of
+    the others alone."""
+    import paper_2605_15609_amd as psd
+    if abs(b) == 1.0:
+        b *= torch.finfo(dtype).max
+    print(f"[rows] {dtype} H={H}/{Hkv} dh={dh} S={S} L={L} n={n} a={a:.3g} b={b:.3g}", flush=True)
+    case = Case(dtype, H, Hkv, dh, S, L, [(1, n, None)], seed=25)
+    want = case.reference()
+    case.q[-1].zero_()
+    case.q[-1, ..., 0] = a
+    seg = case.segments[0]
+    seg["k"][-1].zero_()
+    seg["k"][-1, :, ::dh] = b
+    q, keys, ws = case.device(DEV, (0,))
+    lse = torch.empty(case.q.shape[:3], device=DEV)
+    psd.psd_attention_shared(q, keys, lse=lse)
+    psd.psd_attention_weights(q, keys, lse, accumulate=False)
+    got = ws[0][..., :n]
+    assert torch.isfinite(got).all() and (got[-1] >= 0).all() and (got[-1] <= L * (H // Hkv)).all()
+    near(got[:-1], want["w"][0][:-1], want["w_tol"][0][:-1], "weights")
