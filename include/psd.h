@@ -418,6 +418,8 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
                      int32_t keep, int32_t n_first, int32_t n_last, int32_t *kept, int32_t *kept_lens, void *stream);
 
 /* Model calls whose block rows attend to a prefix that the whole batch shares, then to the cache of their sequence, then to their block.
+ * All caches hold the same number of positions, all layers and heads of a cache too; caches that were cut to lengths of their own
+ * (psd_kv_evict with lens) are for psd_attention_shared.
  * Both caches are laid out like the exact one (psd_kv_cache_bytes(cfg, capacity) per sequence; the prefix is one), and their positions
  * count as they lie: rotary positions are in the keys, so a cache may have gaps (psd_kv_evict), and the block's rows sit at positions block_start .. of
  * tokens whatever the caches hold.  A prefix is filled by psd_kv_prefill with B = 1, a sequence's cache behind it by psd_kv_extend_shared.

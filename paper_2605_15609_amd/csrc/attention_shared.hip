@@ -9,9 +9,9 @@
 // rows that see it: the rows of a unit that read one KV head are stacked into tiles, whatever sequence or query head they belong
 // to, each tile walks the unit's keys (or, where there are few tiles, a part of them), and a second kernel joins a row's parts.
 //
-// What bounds it, with bf16 heads of 128: 128 drafts of 64 rows of the 8B shape over 4096 + 1024 + 64 keys take 680 us, 1.02 PFLOP/s (a
-// large library product has 1.22 here): the matrix cores are busy 57 % of a clock that power holds near 1.65 GHz, the rest goes to the
-// exponentials beside them (6 vector instructions a product).  32 single rows of the 7B shape over 32768 shared keys take 40 us, 32 of
+// What bounds it, with bf16 heads of 128: 128 drafts of 64 rows of the 8B shape over 4096 + 1024 + 64 keys take 650 - 670 us, 1.04 - 1.07
+// PFLOP/s (on this card a loop of the same instructions without loads has 1.55, a library product of 8192 cubed 1.22): the matrix cores are
+// busy 59 % of a clock that power holds near 1.65 GHz, the rest goes to the exponentials beside them (6 vector instructions a product).  32 single rows of the 7B shape over 32768 shared keys take 40 us, 32 of
 // them the attention (67 MB of keys and values): 11 tiles of keys a workgroup at 2.3 us each, a wait for other wavefronts or for a tile in
 // nearly half of it.  Small calls are one chain of round trips: about 8 us.
 //
@@ -744,8 +744,10 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, Shared
 // walks the rows in tiles of WR that pass through LDS, fetched a tile ahead; a lane adds up what its row of every tile gives, and the
 // lanes are added at the end.  Where a unit has few keys and many rows, workgroups take a part of the rows each and a second kernel
 // adds the parts.  Every sum has an order that the shapes alone decide.
-// Bound: 64 exponentials a lane (a quarter of the rate) and as many additions and multiply-adds stand against 32 MFMAs a tile (16 x 64 rows
-// of the 7B shape over 2048 shared and up to 4001 own keys: 61 - 64 us, 0.33 PFLOP/s; the attention before it 96, its join 12).
+// 16 x 64 rows of the 7B shape over 2048 shared and up to 4001 own keys take 60 - 64 us, 0.33 PFLOP/s (the attention before it 92 - 96, its
+// join 12).  The exponentials, 64 a lane and tile at a quarter of the rate, are some 20 us of that.  The rest is the shape of the launch: of 1280
+// workgroups, of which a CU holds two (248 registers), those whose block lies behind a unit's last key leave at once, and each of the others
+// loads its 64 KB of keys, with nothing beside it, for some seven tiles of rows.
 template <typename T>
 constexpr int NKEYS = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
@@ -1116,7 +1118,8 @@ SharedLaunch plan_weights(const SharedShape &sh, const SharedSegment *given, int
         total += (double)jb.units * sh.n_kv_heads * jb.tiles * ((rows_per_unit(sh, given[i]) + WR - 1) / WR);
         ++ln.n_jobs;
     }
-    // three workgroups to a CU, each with as many tiles of rows; a part costs a round trip, so at least 4
+    // About 768 workgroups with as many tiles of rows each, if every unit is full: one and a half rounds of the two that a CU holds.  A part costs
+    // a round trip, so at least 4 tiles.
     const int share = (int)std::max(4.0, std::min(total / 768.0 + 0.999, 1e9));
     int64_t blocks = 0, joins = 0, parts = 0;
     for (int j = 0; j < ln.n_jobs; ++j) {

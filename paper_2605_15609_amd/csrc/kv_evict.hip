@@ -8,7 +8,8 @@
 // each other, are found in few lines (8 slots per lane and 16-byte stores visit 8 times the lines: 429 us where this takes 411).
 // Memory gives whole lines of the source for them, whatever share of a line's positions stays, and that bounds large evictions (8B
 // shape, 32 layers, 4096 -> 1024 positions: 411 us, 1.9 GB with all value lines, at 4.6 TB/s where a large copy has 4.9).  The workgroup
-// that selected may gather too, so that the selections of some run beside the copies of others, in one launch (MOST_FUSED).
+// that selected may gather too (MOST_FUSED), which saves a launch and the list's way through memory.  That many workgroups are on the card at
+// once, three to a CU (up to 16 positions a lane; one above), so all of them select first and copy then.
 #include <type_traits>
 
 #include "psd_internal.h"
