@@ -979,6 +979,7 @@ def _shared_ws(model: Model, S: int, L: int, kv: _KvShared, extra: int = 0):
 def psd_forward_confidence_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, kv: SharedKv, seqs_per_cache: int = 1,
                                   want_logits: bool = False):
     """tokens int32 [S, N]; the block rows against a prefix of the whole batch and their caches -> (top1 [S, L], conf [S, L][, logits])."""
+    block_start, L = _int32(block_start, "block_start"), _int32(L, "L")
     with _on_device(_check_tokens(model, tokens)) as stream:
         S, N = tokens.shape
         if seqs_per_cache < 1 or S % seqs_per_cache:
@@ -988,7 +989,7 @@ def psd_forward_confidence_shared(model: Model, tokens: torch.Tensor, block_star
         top1 = torch.empty((S, L), dtype=torch.int32, device=tokens.device)
         conf = torch.empty((S, L), dtype=torch.float32, device=tokens.device)
         logits = torch.empty((S * L, model.shape.vocab), dtype=torch.float32, device=tokens.device) if want_logits else None
-        _check(model.lib.psd_forward_confidence_shared(model.handle, _ptr(tokens), S, N, _int32(block_start, "block_start"), _int32(L, "L"), C.byref(c), _ptr(top1), _ptr(conf),
+        _check(model.lib.psd_forward_confidence_shared(model.handle, _ptr(tokens), S, N, block_start, L, C.byref(c), _ptr(top1), _ptr(conf),
                                                        _ptr(logits), _ptr(ws), nb, stream))
     return (top1, conf, logits) if want_logits else (top1, conf)
 
@@ -996,16 +997,18 @@ def psd_forward_confidence_shared(model: Model, tokens: torch.Tensor, block_star
 def psd_kv_extend_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, kv: SharedKv) -> None:
     """The block of every sequence of tokens [B, N] behind the first kv.length positions of its cache (kv.length is then L more: the
     caller's to count)."""
+    block_start, L = _int32(block_start, "block_start"), _int32(L, "L")
     with _on_device(_check_tokens(model, tokens)) as stream:
         B, N = tokens.shape
         c = kv.c(model, B)
         ws, nb = _shared_ws(model, B, L, c)
-        _check(model.lib.psd_kv_extend_shared(model.handle, _ptr(tokens), B, N, _int32(block_start, "block_start"), _int32(L, "L"), C.byref(c), _ptr(ws), nb, stream))
+        _check(model.lib.psd_kv_extend_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(c), _ptr(ws), nb, stream))
 
 
 def psd_decode_block_shared(model: Model, tokens: torch.Tensor, block_start: int, L: int, policy: Policy, graph: Graph, kv: SharedKv,
                             stats: Optional[Sequence[Stats]] = None) -> List[Stats]:
     """psd_decode_block with shared model calls; the finished block is appended to the caches (kv.length is then L more)."""
+    block_start, L = _int32(block_start, "block_start"), _int32(L, "L")
     with _on_device(_check_tokens(model, tokens)) as stream:
         B, N = tokens.shape
         K = graph.K
@@ -1014,7 +1017,7 @@ def psd_decode_block_shared(model: Model, tokens: torch.Tensor, block_start: int
         ws, nb = _shared_ws(model, B * K, L, kv.c(model, B, K), extra=extra)
         cstats = (_Stats * B)()
         g, pol = graph.c(), policy.c()
-        _check(model.lib.psd_decode_block_shared(model.handle, _ptr(tokens), B, N, _int32(block_start, "block_start"), _int32(L, "L"), C.byref(pol), C.byref(g),
+        _check(model.lib.psd_decode_block_shared(model.handle, _ptr(tokens), B, N, block_start, L, C.byref(pol), C.byref(g),
                                                  cstats, C.byref(c), _ptr(ws), nb, stream))
     return _add_stats(stats, cstats, B)
 

@@ -390,6 +390,13 @@ def test_numbers_that_a_32_bit_argument_would_cut_are_refused(lib):
         with pytest.raises(psd.PsdError) as why:
             psd.psd_kv_evict(ok, ok, *args, kept=torch.zeros((2, 4, 5), dtype=torch.int32))
         assert "on a GPU" not in str(why.value), args
+    tokens = torch.zeros((2, 64), dtype=torch.int32)
+    for at, length in ((big, 32), (0, big + 32), (-big, 32)):
+        for call in (lambda: psd.psd_forward_confidence_shared(_stub(lib), tokens, at, length, psd.SharedKv()),
+                     lambda: psd.psd_kv_extend_shared(_stub(lib), tokens, at, length, psd.SharedKv()),
+                     lambda: psd.psd_decode_block_shared(_stub(lib), tokens, at, length, psd.Policy(), psd.chain_graph(2), psd.SharedKv())):
+            with pytest.raises(psd.PsdError, match="32-bit"):
+                call()
     for kv in (psd.SharedKv(prefix_len=big), psd.SharedKv(length=-big)):
         with pytest.raises(psd.PsdError, match="32-bit"):
             kv.c(_stub(lib), 1)
