@@ -386,22 +386,22 @@ typedef struct {
 /* sizeof psd_kv_segment, psd_attention_shape and psd_kv_shared, as psd_struct_sizes gives those of the structures above. */
 int32_t psd_shared_struct_sizes(int32_t *out, int32_t n);
 /* psd_attention_shared: softmax(q k^T / sqrt(d_head)) v of every row over all keys of the units it sees.  out as q (row stride
- *   ld_out); neither out nor lse may overlap an input or each other (columns of one buffer's rows may be q, keys and out); lse device float [S*L, n_heads], ln of the sum of the exponentials of its scores, or NULL.  A row
- *   without a key (all lengths 0), or without a score above -inf, gets zeros and lse -inf, and draws no weight.  ws: device, 256-byte aligned, psd_attention_shared_bytes of the same
- *   shape and segments (which looks at shapes and len only, not at device memory); calls that overlap need one each.  Sums and statistics are
- *   fp32; with bf16 the probabilities are rounded to bf16 before they meet the values.  How keys are cut follows shapes and lengths, so a row's
+ *   ld_out); lse device float [S*L, n_heads], ln of the sum of the exponentials of its scores, or NULL.  Neither may overlap an input or the
+ *   other (q, keys and out may be columns of one buffer's rows).  A row without a key (all lengths 0), or without a score above -inf, gets
+ *   zeros and lse -inf, and draws no weight.  ws: device, 256-byte aligned, psd_attention_shared_bytes of the same shape and segments (which
+ *   looks at shapes and len only, not at device memory); calls that overlap need one each.  Sums and statistics are fp32; with bf16 the probabilities are rounded to bf16 before they meet the values.  How keys are cut follows shapes and lengths, so a row's
  *   bits depend on those of its batch, but not on what other sequences hold.
  * psd_attention_weights: what each key drew: weights[u][g][j] = sum over the rows of the unit's sequences and the query heads of KV head g
- *   of exp(score - lse), lse from psd_attention_shared over all segments (a float: a row's weights are off by a factor within |lse| 2^-22, and
- *   where that says nothing any more, beyond 2^23, each is at least between 0 and 1).  Segments without `weights` are skipped, no two may share any; accumulate = 1
+ *   of exp(score - lse), lse from psd_attention_shared over all segments (a float: a row's weights are off by a factor within |lse| 2^-21, and
+ *   where that says nothing any more, beyond |lse| = 2^24, each is at least between 0 and 1).  Segments without `weights` are skipped, no two may share any; accumulate = 1
  *   adds to what is there, 0 overwrites.  Weights behind a unit's last key are left as they are.  ws likewise
  *   (psd_attention_weights_bytes; may be NULL where that is 0). */
 int64_t psd_attention_shared_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments);
 int32_t psd_attention_shared(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments, void *out,
                              float *lse, void *ws, int64_t ws_bytes, void *stream);
-/* Debug: how psd_attention_shared splits its work.  For the first n_jobs jobs 7 numbers each: first segment (of those with keys), segments, form (0: up to 32 rows a
- *   workgroup, 1: 128 rows, 2: a unit and KV head to a wavefront), units, tiles of rows of a unit and KV head, parts of the keys, and the
- *   rows of a unit and KV head.  Returns the number of jobs. */
+/* Debug: how psd_attention_shared splits its work.  For the first n_jobs jobs 7 numbers each: first segment (of those with keys), segments,
+ *   form (0: up to 32 rows a workgroup, 1: 128 rows, 2: a unit and KV head to a wavefront), units, tiles of rows of a unit and KV head, parts
+ *   of the keys, and the rows of a unit and KV head.  Returns the number of jobs. */
 int32_t psd_debug_attention_plan(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments, int32_t *jobs, int32_t n_jobs);
 int64_t psd_attention_weights_bytes(const psd_attention_shape *shape, const psd_kv_segment *segments, int32_t n_segments);
 int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, const psd_kv_segment *segments, int32_t n_segments,
@@ -410,8 +410,8 @@ int32_t psd_attention_weights(const psd_attention_shape *shape, const void *q, c
  *   and the last n_last positions of a unit always (n_first + n_last <= keep), then by src->weights, descending, equal ones the
  *   lowest position first (both zeros are equal, NaN is below everything).  They go to dst in ascending order of their positions: keys, values and, where
  *   dst->weights is set, weights; a unit of at most `keep` positions is copied whole.  dst must hold min(keep, src->len) positions (its `len`), have
- *   lens NULL, and not overlap src; its units lie behind one another, or beside each other in rows that hold all of them; what lies behind the positions written is left as it is.  kept device int32 [units][n_kv_heads][keep]: the source position of
- *   each, -1 behind the last; kept_lens device int32 [units] (or NULL): positions of each unit now.
+ *   lens NULL, and not overlap src; its units lie behind one another, or beside each other in rows that hold all of them; what lies behind
+ *   the positions written is left as it is.  kept device int32 [units][n_kv_heads][keep]: the source position of each, -1 behind the last; kept_lens device int32 [units] (or NULL): positions of each unit now.
  *   Results share no memory with each other or with what is read, lens among it.
  *   The layers of the caches of n sequences are n * n_layers units in a row.  d_head * element size a multiple of 16 bytes. */
 int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32_t units, int32_t n_kv_heads, int32_t d_head, int32_t dtype,

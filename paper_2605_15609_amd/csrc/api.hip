@@ -1098,7 +1098,9 @@ bool apart(const Region &a, const Region &b) {
     const int64_t na = a.span(), nb = b.span();
     if (na == 0 || nb == 0 || a.first + (uintptr_t)na <= b.first || b.first + (uintptr_t)nb <= a.first) return true;
     auto row_period = [](const Region &r) {   // 0: no period
-        return r.units == 1 ? (r.rows == 1 ? -1 : r.row_stride) : r.rows == 1 ? r.unit_stride : r.row_stride > 0 && r.unit_stride % r.row_stride == 0 ? r.row_stride : 0;
+        if (r.units == 1) return r.rows == 1 ? (int64_t)-1 : r.row_stride;
+        if (r.rows == 1) return r.unit_stride;
+        return r.row_stride > 0 && r.unit_stride % r.row_stride == 0 ? r.row_stride : 0;
     };
     auto same = [](int64_t x, int64_t y) { return x < 0 ? y : y < 0 || x == y ? x : 0; };   // (-1: a single piece, which fits any period)
     return apart_modulo(a.first, a.width, b.first, b.width, same(row_period(a), row_period(b))) ||
@@ -1242,7 +1244,7 @@ int32_t psd_kv_evict(const psd_kv_segment *src, const psd_kv_segment *dst, int32
                          weights_region(from, units, n_kv_heads, src->len), lens_region(from, units)};
     const Region written[] = {keys_region(to, units, most, w, esz), values_region(to, units, most, w, esz), weights_region(to, units, n_kv_heads, most),
                               dense(kept, (int64_t)units * n_kv_heads * keep * 4), dense(kept_lens, (int64_t)units * 4)};
-    for (int i = 0; i < 2; ++i) {   // units behind one another, or beside each other in rows that hold all of them (check_segment looks at the weights)
+    for (int i = 0; i < 2; ++i) {   // units behind one another, or beside each other in rows that hold all of them (the weights: check_segment)
         const Region &r = written[i];
         if (r.units > 1 && r.span() > 0 && r.unit_stride < r.unit_width() && (r.unit_stride < r.width || (r.units - 1) * r.unit_stride + r.width > r.row_stride))
             PSD_FAIL(PSD_ERR_SHAPE, "the units of the destination lie on each other");

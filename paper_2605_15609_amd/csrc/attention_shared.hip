@@ -9,11 +9,12 @@
 // rows that see it: the rows of a unit that read one KV head are stacked into tiles, whatever sequence or query head they belong
 // to, each tile walks the unit's keys (or, where there are few tiles, a part of them), and a second kernel joins a row's parts.
 //
-// What bounds it, with bf16 heads of 128: 128 drafts of 64 rows of the 8B shape over 4096 + 1024 + 64 keys take 650 - 670 us, 1.04 - 1.07
-// PFLOP/s (on this card a loop of the same instructions without loads has 1.55, a library product of 8192 cubed 1.22): the matrix cores are
-// busy 59 % of a clock that power holds near 1.65 GHz, the rest goes to the exponentials beside them (6 vector instructions a product).  32 single rows of the 7B shape over 32768 shared keys take 40 us, 32 of
-// them the attention (67 MB of keys and values): 11 tiles of keys a workgroup at 2.3 us each, a wait for other wavefronts or for a tile in
-// nearly half of it.  Small calls are one chain of round trips: about 8 us.
+// What bounds it, with bf16 heads of 128: 128 drafts of 64 rows of the 8B shape over 4096 + 1024 + 64 keys take 650 - 670 us, 1.04 -
+// 1.07 PFLOP/s (on this card a loop of the same instructions without loads has 1.55, a library product of 8192 cubed 1.22): the matrix
+// cores are busy 59 % of a clock that power holds near 1.65 GHz, the rest goes to the exponentials beside them (6 vector instructions a
+// product).  32 single rows of the 7B shape over 32768 shared keys take 40 us, 32 of them the attention (67 MB of keys and values): 11
+// tiles of keys a workgroup at 2.3 us each, a wait for other wavefronts or for a tile in nearly half of it.  Small calls are one chain
+// of round trips: about 8 us.
 //
 // Per tile the problem is transposed as in attention_mfma.hip: S^T = K Q^T, O^T += V^T P^T.  A lane owns one row; the softmax stays
 // in its registers, and the probabilities are the second product's operand as they are.
@@ -524,8 +525,9 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     // The sums are kept relative to a running reference, raised to the maximum only where that has grown by more than 2^SLACK in a
     // probability: bf16 and fp32 are as exact there, and the outputs are not touched in most tiles.  A row that has not grown keeps its
     // reference when others of the wavefront raise theirs (its factor is 1), so its bits do not depend on what other sequences hold.
-    // Returns what the exponentials add to x sl2.  That is minus the reference in units of log2, rounded, which is off by up to half a unit where
-    // it reaches FAR and by any power of two beyond; there x is taken relative to the reference before it is scaled.
+    // Returns what the exponentials add to x sl2.  That is minus the reference in units of log2, rounded: off by up to half a unit up to FAR,
+    // which is a factor of all of the row's terms, but beyond FAR by more than they span; there x is taken relative to the reference before it
+    // is scaled.
     auto reference = [&](floatx16 (&x)[2]) {
         float mx = fmaxf(x[0][0], x[1][0]);
 #pragma unroll

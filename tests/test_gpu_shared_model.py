@@ -13,7 +13,7 @@ import torch
 
 import psd_inputs as inp
 from oracle import psd_oracle as orc
-from tests.shared_common import kept_positions, slots
+from tests.shared_common import kept_positions
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -411,6 +411,7 @@ def _evicted(shape, seed, L, P, own, keep, first, last):
 def test_a_block_goes_behind_a_length_that_is_no_multiple_of_16(name, L, keep):
     """Eviction leaves any length.  The block behind it, its keys and values in the cache, and the block after that, against the oracle's
     forward over the entries that stayed."""
+    from tests.shared_common import slots
     shape, tol = MODELS[name]
     shape = _bc(shape)
     psd, host, model, t, start, kv, frozen = _evicted(shape, 81, L, 48 if L == 16 else 64, 64, keep, 4, 8)
