@@ -449,6 +449,96 @@ int32_t psd_decode_block_shared(psd_handle *h, int32_t *tokens, int32_t B, int32
                                 const psd_policy *policy, const psd_graph *graph, psd_stats *stats, const psd_kv_shared *kv, void *ws,
                                 int64_t ws_bytes, void *stream);
 
+/* ---- Head norms with rotary positions, and caches in 8 bits ---------------------------------------
+ * What stands between the rows of a QKV projection and attention over a cache of half the size: psd_rotary turns queries and keys,
+ * psd_kv8_store puts keys and values into the cache, psd_attention_kv8 attends to it and to the rows that are not in it yet, psd_kv8_load reads
+ * it back.  These calls take no handle; they run on the current HIP device.
+ *
+ * psd_rotary: every head of the n_heads query heads and n_kv_heads key heads (0: no keys) of n_tokens rows,
+ *     y = x / sqrt(mean x^2 + eps) * gain                                   (q_gain, k_gain: device float [d_head]; NULL: x as it is)
+ *     (y_a, y_b) <- factor * (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position * frequency of the pair,
+ *   for the pairs a, b = j, j + rotated / 2 or, interleaved, 2j, 2j + 1 of its first `rotated` channels.  Heads of a row lie one behind the
+ *   other, rows ld_* elements apart.  Everything is computed in fp32 and rounded once; an angle is position * frequency in 64 bits, with
+ *   whole turns taken away before it is rounded.  frequencies: device double [rotated / 2], radians a position; positions: device int32 [n_tokens], or
+ *   NULL: row i stands at first + i % rows_per_seq.  q_out / k_out may be q / k with the same row stride (in place); else no output may
+ *   overlap an input or the other output (all may be columns of one buffer's rows).
+ * psd_rotary_frequencies: theta^(-2j / rotated), host double [rotated / 2], plain or scaled for contexts `stretch` times as long as a model was
+ *   trained for: PSD_ROTARY_LINEAR divides all by stretch; PSD_ROTARY_BASE uses theta * stretch^(rotated / (rotated - 2)), which keeps the
+ *   fastest and divides the slowest by stretch; PSD_ROTARY_PARTS divides those that turn less than `slow` times over `trained` positions by stretch, keeps
+ *   those that turn more than `fast` times, goes linearly between, and has a factor of 0.1 ln(stretch) + 1 (else *factor is 1; it may be NULL). */
+#define PSD_MAX_ROTARY_HEAD 256
+#define PSD_ROTARY_PLAIN 0
+#define PSD_ROTARY_LINEAR 1
+#define PSD_ROTARY_BASE 2
+#define PSD_ROTARY_PARTS 3
+typedef struct {
+    double theta, stretch, trained, slow, fast;   /* stretch >= 1; the last three: PSD_ROTARY_PARTS */
+    int32_t kind;                                 /* PSD_ROTARY_* */
+    int32_t reserved;                             /* 0 */
+} psd_rotary_scaling;
+typedef struct {
+    int64_t n_tokens, ld_q, ld_k, ld_q_out, ld_k_out;   /* row strides in elements */
+    int32_t n_heads, n_kv_heads, d_head;                /* d_head: even, up to PSD_MAX_ROTARY_HEAD */
+    int32_t rotated, interleaved;                       /* channels that are turned (even); 0 / 1 */
+    int32_t first, rows_per_seq;                        /* where positions is NULL */
+    int32_t dtype;
+    float   factor, eps;
+    int32_t reserved;                                   /* 0 */
+} psd_rotary_shape;
+int32_t psd_rotary_frequencies(const psd_rotary_scaling *scaling, int32_t rotated, double *frequencies, double *factor);
+int32_t psd_rotary(const psd_rotary_shape *shape, const void *q, const void *k, const double *frequencies, const int32_t *positions,
+                   const float *q_gain, const float *k_gain, void *q_out, void *k_out, void *stream);
+
+/* A cache in 8 bits: units (requests, or their layers) of `capacity` positions, a multiple of 32 and of `block`.  A unit has, for each KV head one
+ * behind the other,
+ *   codes   [capacity / 32] tiles of 32 * d_head bytes of keys, [d_head / 16][32 positions][16 channels], then as many of values,
+ *           [d_head / w][2][w channels][16], w = min(32, d_head), part h of 2 with positions 8 b + 4 h + j at 4 b + j (b, j: 0 .. 3);
+ *   scales  [capacity / block] pairs of floats: of the block's keys, of its values (not negative).
+ * A code stands for code * scale: a whole number -127 .. 127 (PSD_KV8_INT8) or a float of 4 bits of exponent and 3 of mantissa, bias 7, up to 448
+ * (PSD_KV8_E4M3).  What lies behind a unit's length is never used.  Nothing has to be zeroed.
+ * psd_kv8_store: n rows of each unit (row i of unit u: k + (u * n + i) * ld_k, heads one behind the other; v likewise) go to positions first + i or, where
+ *   starts is set (device int32 [units]), starts[u] + i; counts (device int32 [units], or NULL): only the first counts[u] (cut to 0 .. n).
+ *   Rows that would lie outside the cache are left out.  A block's scale is the largest magnitude in its new rows over the largest code (127, 448),
+ *   rounded to fp32, or what it was where positions in front of the new ones need more; codes are the nearest to x / scale, ties to even.  Where a
+ *   block's scale grows, what it held in front of the new rows is rounded again to that.  What it held behind them stands for nothing any more.  A block with an
+ *   infinity or NaN among its new rows reads as NaN until it is begun anew.  The lengths are the caller's (cache->lens is not written).
+ *   Units may not overlap.  d_head 16, 32, 64 or 128 in either dtype; rows 16-byte aligned.
+ * psd_kv8_load: positions first .. first + n - 1 of each unit to rows k, v (as in psd_kv8_store), code * scale rounded to dtype once; rows at or behind a
+ *   unit's length are left as they are. */
+#define PSD_KV8_INT8 0
+#define PSD_KV8_E4M3 1
+typedef struct {
+    void *codes;                 /* device, 16-byte aligned */
+    float *scales;               /* device, 8-byte aligned */
+    const int32_t *lens;         /* device int32, positions of every unit (cut to 0 .. len), or NULL: each unit holds len */
+    int64_t stride_codes;        /* from unit to unit: bytes, a multiple of 16 */
+    int64_t stride_scales;       /* floats, even */
+    int32_t capacity;            /* positions of a unit, up to 2^30 */
+    int32_t len;                 /* positions that a unit holds, or the most that any does */
+    int32_t block;               /* positions to a scale: 16, 32, 64 or 128 */
+    int32_t format;              /* PSD_KV8_* */
+    int32_t n_kv_heads, d_head;
+    int32_t seqs_per_unit;       /* attention: sequences u * seqs_per_unit .. + seqs_per_unit - 1 see unit u */
+    int32_t reserved;            /* 0 */
+} psd_kv8_cache;
+/* sizeof psd_rotary_shape, psd_rotary_scaling and psd_kv8_cache, as psd_struct_sizes gives those of the structures above. */
+int32_t psd_kv8_struct_sizes(int32_t *out, int32_t n);
+int32_t psd_kv8_store(const psd_kv8_cache *cache, int32_t units, const void *k, const void *v, int64_t ld_k, int64_t ld_v, int32_t dtype, int32_t n,
+                      int32_t first, const int32_t *starts, const int32_t *counts, void *stream);
+int32_t psd_kv8_load(const psd_kv8_cache *cache, int32_t units, int32_t first, int32_t n, void *k, void *v, int64_t ld_k, int64_t ld_v,
+                     int32_t dtype, void *stream);
+/* psd_attention_kv8: softmax(q k^T / sqrt(d_head)) v of every row over all positions of its sequence's unit and, where k and v are set, the L rows of its
+ *   own sequence (row i of sequence s: k + (s*L + i) * ld_k, in the dtype of the call, 16-byte aligned rows), which are not in the cache: a block attends
+ *   to all of itself.  Shape, out, lse and rows without a key as for psd_attention_shared (S a multiple of cache->seqs_per_unit; cache->len may be
+ *   0, then codes and scales may be NULL with capacity 0).  Codes are used as they are: a key's scale multiplies its score, a value's its probability, which with
+ *   bf16 is rounded after that.  Sums and statistics are fp32.  ws: device, 256-byte aligned, psd_attention_kv8_bytes of the same shape and cache (own_rows: 1
+ *   where k is set; it does not look at device memory); calls that overlap need one each.
+ * psd_debug_attention_kv8_plan: form (0: tiles of 32 rows, 1: of 128), tiles of rows of a unit and KV head, parts of the keys, keys of a part. */
+int64_t psd_attention_kv8_bytes(const psd_attention_shape *shape, const psd_kv8_cache *cache, int32_t own_rows);
+int32_t psd_attention_kv8(const psd_attention_shape *shape, const void *q, const psd_kv8_cache *cache, const void *k, const void *v, int64_t ld_k,
+                          int64_t ld_v, void *out, float *lse, void *ws, int64_t ws_bytes, void *stream);
+int32_t psd_debug_attention_kv8_plan(const psd_attention_shape *shape, const psd_kv8_cache *cache, int32_t own_rows, int32_t *plan);
+
 /* ---- Approximate KV cache for fully bidirectional models -----------------------------------------
  * Sec. 3.2 stage 3 notes that KV-cache sharing can cut redundant computation; with bidirectional
  * attention any cache is an approximation, and the paper fixes no scheme.  The one offered here is the

@@ -89,6 +89,24 @@ class _DebugLayout(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+class _RotaryScaling(C.Structure):
+    _fields_ = [("theta", C.c_double), ("stretch", C.c_double), ("trained", C.c_double), ("slow", C.c_double), ("fast", C.c_double),
+                ("kind", C.c_int32), ("reserved", C.c_int32)]
+
+
+class _RotaryShape(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64), ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_q_out", C.c_int64), ("ld_k_out", C.c_int64),
+                ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("rotated", C.c_int32), ("interleaved", C.c_int32),
+                ("first", C.c_int32), ("rows_per_seq", C.c_int32), ("dtype", C.c_int32), ("factor", C.c_float), ("eps", C.c_float),
+                ("reserved", C.c_int32)]
+
+
+class _Kv8Cache(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("lens", C.c_void_p), ("stride_codes", C.c_int64), ("stride_scales", C.c_int64),
+                ("capacity", C.c_int32), ("len", C.c_int32), ("block", C.c_int32), ("format", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("d_head", C.c_int32), ("seqs_per_unit", C.c_int32), ("reserved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -180,6 +198,14 @@ def load_library():
         "psd_decode_block_shared": (i32, [vp, vp, i32, i32, i32, i32, C.POINTER(_Policy), C.POINTER(_Graph), C.POINTER(_Stats),
                                           C.POINTER(_KvShared), vp, i64, vp]),
         "psd_kv_evict": (i32, [vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp]),
+        "psd_kv8_struct_sizes": (i32, [C.POINTER(i32), i32]),
+        "psd_rotary_frequencies": (i32, [C.POINTER(_RotaryScaling), i32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
+        "psd_rotary": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "psd_kv8_store": (i32, [vp, i32, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp]),
+        "psd_kv8_load": (i32, [vp, i32, i32, i32, vp, vp, i64, i64, i32, vp]),
+        "psd_attention_kv8_bytes": (i64, [vp, vp, i32]),
+        "psd_attention_kv8": (i32, [vp, vp, vp, vp, vp, i64, i64, vp, vp, vp, i64, vp]),
+        "psd_debug_attention_kv8_plan": (i32, [vp, vp, i32, C.POINTER(i32)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -193,6 +219,10 @@ def load_library():
     theirs = (i32 * len(mine))()
     if lib.psd_shared_struct_sizes(theirs, len(mine)) != len(mine) or list(theirs) != mine:
         raise PsdError(f"binding and libpsd.so disagree on the segment layouts: {mine} vs {list(theirs)} (rebuild the library)")
+    mine = [C.sizeof(t) for t in (_RotaryShape, _RotaryScaling, _Kv8Cache)]
+    theirs = (i32 * len(mine))()
+    if lib.psd_kv8_struct_sizes(theirs, len(mine)) != len(mine) or list(theirs) != mine:
+        raise PsdError(f"binding and libpsd.so disagree on the layouts of 8-bit caches: {mine} vs {list(theirs)} (rebuild the library)")
     _lib = lib
     return lib
 
@@ -925,6 +955,220 @@ def psd_kv_evict(src: KvSegment, dst: KvSegment, keep: int, first: int = 0, last
         _check(load_library().psd_kv_evict(C.byref(src.c), C.byref(dst.c), src.units, src.n_kv_heads, src.d_head, _DTYPES[src.dtype], int(keep),
                                            int(first), int(last), kept.data_ptr(), _ptr(kept_lens), stream))
     return kept
+
+
+_ROTARY_KINDS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+_KV8_FORMATS = {"int8": 0, "e4m3": 1}
+
+
+def rotary_frequencies(rotated: int, theta: float, kind: str = "plain", stretch: float = 1.0, trained: float = 0.0, slow: float = 1.0,
+                       fast: float = 32.0) -> Tuple[torch.Tensor, float]:
+    """psd_rotary_frequencies: (float64 [rotated / 2] on the CPU, the factor for psd_rotary) of theta^(-2j / rotated), plain or scaled for contexts
+    `stretch` times as long ("linear", "base", "parts" with the trained length and the turns over it below / above which a frequency is
+    stretched / kept)."""
+    if kind not in _ROTARY_KINDS:
+        raise PsdError(f"scaling {kind!r}, not one of {sorted(_ROTARY_KINDS)}")
+    n = _int32(rotated, "rotated")
+    out, factor = torch.empty((max(0, min(n, 1 << 16)) // 2,), dtype=torch.float64), C.c_double(1.0)
+    scaling = _RotaryScaling(float(theta), float(stretch), float(trained), float(slow), float(fast), _ROTARY_KINDS[kind], 0)
+    _check(load_library().psd_rotary_frequencies(C.byref(scaling), n, C.cast(out.data_ptr(), C.POINTER(C.c_double)), C.byref(factor)))
+    return out, factor.value
+
+
+def _dense_on(t: torch.Tensor, what: str, dtype, shape, device) -> None:
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise PsdError(f"{what}: dense {dtype} {tuple(shape)} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def psd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Tensor, positions: Optional[torch.Tensor] = None, first: int = 0,
+               interleaved: bool = False, factor: float = 1.0, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
+               eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None
+               ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """q [S, L, n_heads, d_head] and k [S, L, n_kv_heads, d_head] (or None), normed where there are gains (float32 [d_head]), their first
+    2 * len(frequencies) channels (float64) turned by positions int32 [S, L] (None: first + row) -> (q_out, k_out), new or given; q_out = q
+    and k_out = k work in place."""
+    if q.dim() != 4 or q.dtype not in _DTYPES or (k is not None and (k.dim() != 4 or k.dtype != q.dtype or k.device != q.device
+                                                                     or (k.shape[0], k.shape[1], k.shape[3]) != (q.shape[0], q.shape[1], q.shape[3]))):
+        raise PsdError(f"q [S, L, heads, d] and k [S, L, KV heads, d], bf16 or fp32, not {q.dtype} {tuple(q.shape)} and "
+                       f"{None if k is None else (k.dtype, tuple(k.shape), k.device)}")
+    if k is None and (k_gain is not None or k_out is not None):
+        raise PsdError("a gain or an output of no keys")
+    S, L, H, d = q.shape
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    for name, t, like in (("q_out", q_out, q), ("k_out", k_out, k)):
+        if t is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+            raise PsdError(f"{name}: {like.dtype} {tuple(like.shape)} on {like.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if frequencies.dim() != 1:
+        raise PsdError(f"frequencies: float64 [pairs], not {tuple(frequencies.shape)}")
+    _dense_on(frequencies, "frequencies", torch.float64, frequencies.shape, q.device)
+    if positions is not None:
+        _dense_on(positions, "positions", torch.int32, (S, L), q.device)
+    for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
+        if t is not None:
+            _dense_on(t, name, torch.float32, (d,), q.device)
+    shape = _RotaryShape(S * L, _rows(q, "q"), 0 if k is None else _rows(k, "k"), _rows(q_out, "q_out"), 0 if k is None else _rows(k_out, "k_out"),
+                         _int32(H, "heads"), 0 if k is None else _int32(k.shape[2], "KV heads"), _int32(d, "d_head"), _int32(2 * frequencies.numel(), "rotated"),
+                         int(bool(interleaved)), _int32(first, "first"), _int32(L, "rows"), _DTYPES[q.dtype], float(factor), float(eps), 0)
+    with _on_device(q.device) as stream:
+        _check(load_library().psd_rotary(C.byref(shape), q.data_ptr(), None if k is None else k.data_ptr(), frequencies.data_ptr(),
+                                         None if positions is None else positions.data_ptr(), None if q_gain is None else q_gain.data_ptr(),
+                                         None if k_gain is None else k_gain.data_ptr(), q_out.data_ptr(), None if k is None else k_out.data_ptr(), stream))
+    return q_out, k_out
+
+
+class Kv8Cache:
+    """Keys and values in 8 bits with a scale for every block of positions and KV head.
+
+    codes uint8 [units, n_kv_heads, positions / 32, 2, 32 * d_head] and scales float32 [units, n_kv_heads, positions / block, 2], each unit dense
+    (include/psd.h has the order of the codes); format "int8" or "e4m3".  The first `length` positions (default: all) of a unit are held, or lens[unit]
+    of them (int32 [units], what is outside 0 .. length is cut); seqs_per_unit consecutive sequences attend to a unit."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, d_head: int, format: str = "int8", length: Optional[int] = None,
+                 lens: Optional[torch.Tensor] = None, seqs_per_unit: int = 1):
+        if format not in _KV8_FORMATS:
+            raise PsdError(f"format {format!r}, not one of {sorted(_KV8_FORMATS)}")
+        if codes.dim() != 5 or codes.dtype != torch.uint8 or d_head < 1 or tuple(codes.shape[3:]) != (2, 32 * d_head) or scales.dim() != 4 \
+                or scales.dtype != torch.float32 or scales.shape[:2] != codes.shape[:2] or scales.shape[3] != 2 \
+                or not codes[:1].is_contiguous() or not scales[:1].is_contiguous():
+            raise PsdError(f"codes uint8 [units, heads, positions / 32, 2, {32 * d_head}] and scales float32 [units, heads, blocks, 2], dense, not "
+                           f"{codes.dtype} {tuple(codes.shape)} {codes.stride()} and {scales.dtype} {tuple(scales.shape)} {scales.stride()}")
+        units, heads, tiles = codes.shape[:3]
+        positions, blocks = 32 * tiles, scales.shape[2]
+        block = positions // blocks if blocks else 32
+        if block * blocks != positions:
+            raise PsdError(f"{blocks} scales for {positions} positions")
+        n = positions if length is None else int(length)
+        if not 0 <= n <= positions:
+            raise PsdError(f"{n} positions of {positions}")
+        if lens is not None:
+            _dense_on(lens, "lens", torch.int32, (units,), codes.device)
+        if scales.device != codes.device:
+            raise PsdError(f"a cache on {codes.device} and {scales.device}")
+        self.codes, self.scales, self.lens, self.format = codes, scales, lens, format
+        self.units, self.n_kv_heads, self.d_head, self.capacity, self.block, self.length = units, heads, int(d_head), positions, block, n
+        self.seqs_per_unit, self.device = int(seqs_per_unit), codes.device
+        def address(t):
+            return None if t is None or t.numel() == 0 else t.data_ptr()
+        self.c = _Kv8Cache(address(codes), address(scales), address(lens), codes.stride(0) if units > 1 else 0, scales.stride(0) if units > 1 else 0,
+                           _int32(positions, "positions"), _int32(n, "length"), _int32(block, "block"), _KV8_FORMATS[format],
+                           _int32(heads, "KV heads"), _int32(d_head, "d_head"), _int32(self.seqs_per_unit, "seqs_per_unit"), 0)
+        self.shapes: dict = {}      # (see _kv8_shape)
+
+    @classmethod
+    def empty(cls, units: int, n_kv_heads: int, d_head: int, positions: int, block: int = 32, format: str = "int8", device="cuda:0",
+              lens: Optional[torch.Tensor] = None, seqs_per_unit: int = 1) -> "Kv8Cache":
+        """A cache of at least `positions` positions, not written yet."""
+        if block not in (16, 32, 64, 128) or min(units, n_kv_heads, d_head) < 1 or positions < 0:
+            raise PsdError(f"{units} units of {n_kv_heads} x {d_head}, {positions} positions, {block} to a scale (16, 32, 64, 128)")
+        n = -(-positions // max(block, 32)) * max(block, 32)
+        return cls(torch.empty((units, n_kv_heads, n // 32, 2, 32 * d_head), dtype=torch.uint8, device=device),
+                   torch.empty((units, n_kv_heads, n // block, 2), dtype=torch.float32, device=device), d_head, format, None, lens, seqs_per_unit)
+
+    def rows(self, k: torch.Tensor, v: torch.Tensor) -> Tuple[int, int, int]:
+        """(rows of a unit, row stride of k, of v) of [units, n, n_kv_heads, d_head], checked."""
+        want = (self.units, self.n_kv_heads, self.d_head)
+        for name, t in (("k", k), ("v", v)):
+            if t.dim() != 4 or t.dtype not in _DTYPES or t.dtype != k.dtype or (t.shape[0], t.shape[2], t.shape[3]) != want or t.shape != k.shape \
+                    or t.device != self.device:
+                raise PsdError(f"{name}: [{want[0]}, n, {want[1]}, {want[2]}] bf16 or fp32 on {self.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+        return _int32(k.shape[1], "rows"), _rows(k, "k"), _rows(v, "v")
+
+
+def psd_kv8_store(cache: Kv8Cache, k: torch.Tensor, v: torch.Tensor, first: int = 0, starts: Optional[torch.Tensor] = None,
+                  counts: Optional[torch.Tensor] = None) -> None:
+    """Rows k, v [units, n, n_kv_heads, d_head] into the cache, at positions first .. of every unit or from starts int32 [units] on; counts
+    int32 [units]: only the first of a unit's rows.  cache.lens is left as it is."""
+    n, ld_k, ld_v = cache.rows(k, v)
+    for name, t in (("starts", starts), ("counts", counts)):
+        if t is not None:
+            _dense_on(t, name, torch.int32, (cache.units,), cache.device)
+    with _on_device(cache.device) as stream:
+        _check(load_library().psd_kv8_store(C.byref(cache.c), _int32(cache.units, "units"), k.data_ptr(), v.data_ptr(), ld_k, ld_v, _DTYPES[k.dtype], n,
+                                            _int32(first, "first"), None if starts is None else starts.data_ptr(), None if counts is None else counts.data_ptr(),
+                                            stream))
+
+
+def psd_kv8_load(cache: Kv8Cache, first: int = 0, n: Optional[int] = None, dtype=torch.bfloat16, k_out: Optional[torch.Tensor] = None,
+                 v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """What positions first .. first + n - 1 (default: up to cache.length) of every unit stand for -> k, v [units, n, n_kv_heads, d_head], new (of dtype, zero behind
+    a unit's length) or given (left as they are there)."""
+    n = max(cache.length - _int32(first, "first"), 0) if n is None else _int32(n, "n")
+    if (k_out is None) != (v_out is None):
+        raise PsdError("k_out and v_out, or neither")
+    if k_out is None:
+        if n < 0 or dtype not in _DTYPES:
+            raise PsdError(f"{n} positions as {dtype}")
+        k_out, v_out = (torch.zeros((cache.units, n, cache.n_kv_heads, cache.d_head), dtype=dtype, device=cache.device) for _ in range(2))
+    rows, ld_k, ld_v = cache.rows(k_out, v_out)
+    if rows != n:
+        raise PsdError(f"{rows} rows for {n} positions")
+    with _on_device(cache.device) as stream:
+        _check(load_library().psd_kv8_load(C.byref(cache.c), _int32(cache.units, "units"), _int32(first, "first"), n, k_out.data_ptr(), v_out.data_ptr(), ld_k,
+                                           ld_v, _DTYPES[k_out.dtype], stream))
+    return k_out, v_out
+
+
+def _kv8_shape(q: torch.Tensor, cache: Kv8Cache, k: Optional[torch.Tensor], v: Optional[torch.Tensor], out: Optional[torch.Tensor]):
+    """(shape, row strides of k and v) of a call, checked once for tensors of these shapes, strides, types and devices (as _attention_shape)."""
+    key = tuple(None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in (q, k, v, out))
+    found = cache.shapes.get(key)
+    if found is not None:
+        return found
+    if q.dim() != 4 or q.dtype not in _DTYPES or q.device != cache.device or q.shape[3] != cache.d_head:
+        raise PsdError(f"q [S, L, heads, {cache.d_head}] bf16 or fp32 on {cache.device}, not {q.dtype} {tuple(q.shape)} on {q.device}")
+    S, L, H, d = q.shape
+    if (k is None) != (v is None):
+        raise PsdError("keys and values of the rows' own blocks, or neither")
+    for name, t in (("k", k), ("v", v)):
+        if t is not None and (t.dtype != q.dtype or t.device != q.device or tuple(t.shape) != (S, L, cache.n_kv_heads, d)):
+            raise PsdError(f"{name}: {q.dtype} {(S, L, cache.n_kv_heads, d)} on {q.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != q.device):
+        raise PsdError(f"out like q, not {out.dtype} {tuple(out.shape)} on {out.device}")
+    if cache.seqs_per_unit < 1 or cache.units * cache.seqs_per_unit != S:
+        raise PsdError(f"{cache.units} units of {cache.seqs_per_unit} sequences for a batch of {S}")
+    if S * L * H >= 2 ** 31:
+        raise PsdError(f"{S} sequences of {L} rows of {H} heads are too many")
+    shape = _AttentionShape(S, L, H, cache.n_kv_heads, d, _DTYPES[q.dtype], _rows(q, "q"), H * d if out is None else _rows(out, "out"))
+    found = (shape, 0 if k is None else _rows(k, "k"), 0 if v is None else _rows(v, "v"))
+    if len(cache.shapes) >= 64:
+        cache.shapes.clear()
+    cache.shapes[key] = found
+    return found
+
+
+def psd_attention_kv8_workspace(q: torch.Tensor, cache: Kv8Cache, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """What psd_attention_kv8 needs for q and cache, to be kept and passed on as ws."""
+    shape = _kv8_shape(q, cache, k, v, None)[0]
+    need = _check(load_library().psd_attention_kv8_bytes(C.byref(shape), C.byref(cache.c), int(k is not None)))
+    return torch.empty((max(256, need),), dtype=torch.uint8, device=q.device)
+
+
+def attention_kv8_plan(q: torch.Tensor, cache: Kv8Cache, own_rows: bool = False) -> Tuple[int, ...]:
+    """psd_debug_attention_kv8_plan: (form, tiles of rows of a unit and KV head, parts of the keys, keys of a part)."""
+    plan = (C.c_int32 * 4)()
+    _check(load_library().psd_debug_attention_kv8_plan(C.byref(_kv8_shape(q, cache, None, None, None)[0]), C.byref(cache.c), int(bool(own_rows)), plan))
+    return tuple(plan)
+
+
+def psd_attention_kv8(q: torch.Tensor, cache: Kv8Cache, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of q [S, L, n_heads, d_head] over the cache and, where given, the rows k, v [S, L, n_kv_heads, d_head] of each sequence's own
+    block -> out like q; lse fp32 [S, L, n_heads] receives the log of each row's sum of exponentials."""
+    lib = load_library()
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    shape, ld_k, ld_v = _kv8_shape(q, cache, k, v, out)
+    if lse is not None:
+        _check_lse(lse, q)
+    with _on_device(q.device) as stream:
+        need = 0 if ws is not None else _check(lib.psd_attention_kv8_bytes(C.byref(shape), C.byref(cache.c), int(k is not None)))
+        at, n, ws = _workspace(need, q.device, ws)
+        _check(lib.psd_attention_kv8(C.byref(shape), q.data_ptr(), C.byref(cache.c), None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
+                                     ld_k, ld_v, out.data_ptr(), None if lse is None else lse.data_ptr(), at, n, stream))
+    return out
 
 
 @dataclass

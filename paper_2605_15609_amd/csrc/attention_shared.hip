@@ -23,11 +23,10 @@
 
 #include "psd_internal.h"
 #include "device_types.h"
+#include "attention_parts.h"
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int TR = 32;    // rows of a tile where there are few
@@ -37,37 +36,6 @@ constexpr int KT = 64;    // keys of a tile in LDS
 constexpr int NW = 4;     // wavefronts of a workgroup, which deal a tile's keys among themselves
 constexpr float SLACK = 8.f;      // (see many_rows)
 constexpr float FAR = 0x1p24f;    // (see many_rows)
-constexpr float LOG2E = 1.4426950408889634f;
-
-// A row of 8 slots of T, as a lane of a 32x32 product holds it: bf16 in one 16-byte load, fp32 in two.
-template <typename T>
-struct Frag;
-template <>
-struct Frag<bf16_t> {
-    uint4 v;
-    __device__ void load(const bf16_t *p) { v = *reinterpret_cast<const uint4 *>(p); }
-    // keeps the slots of keys before `left`; the lane's slots are keys 0 - 3 and 8 - 11 (from its half on)
-    __device__ void keep(int left) {
-        const int hi = left - 8;
-        v.x &= left >= 2 ? 0xffffffffu : left == 1 ? 0x0000ffffu : 0u;
-        v.y &= left >= 4 ? 0xffffffffu : left == 3 ? 0x0000ffffu : 0u;
-        v.z &= hi >= 2 ? 0xffffffffu : hi == 1 ? 0x0000ffffu : 0u;
-        v.w &= hi >= 4 ? 0xffffffffu : hi == 3 ? 0x0000ffffu : 0u;
-    }
-};
-template <>
-struct Frag<float> {
-    float v[8];
-    __device__ void load(const float *p) {
-        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    }
-    __device__ void keep(int left) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if ((i >= 4 ? i + 4 : i) >= left) v[i] = 0.f;
-    }
-};
 
 // a Frag out of LDS, chunk by chunk of 16 bytes
 template <typename F>
@@ -78,24 +46,6 @@ template <typename F>
 __device__ __forceinline__ void load_chunks(Frag<float> &f, const unsigned char *lds, F at) {
     const float4 a = *reinterpret_cast<const float4 *>(lds + at(0)), b = *reinterpret_cast<const float4 *>(lds + at(1));
     f.v[0] = a.x, f.v[1] = a.y, f.v[2] = a.z, f.v[3] = a.w, f.v[4] = b.x, f.v[5] = b.y, f.v[6] = b.z, f.v[7] = b.w;
-}
-
-// acc += A B over 16 contraction slots, 8 in each half of the wavefront
-__device__ __forceinline__ void product(const Frag<bf16_t> &a, const Frag<bf16_t> &b, floatx16 &acc) {
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), acc, 0, 0, 0);
-}
-__device__ __forceinline__ void product(const Frag<float> &a, const Frag<float> &b, floatx16 &acc) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], acc, 0, 0, 0);
-}
-// The probabilities of 16 keys as the second product takes them.  bf16: rounded to 8 bits of mantissa, as the other attention
-// kernels of the bf16 path do (their sum l is taken from the unrounded ones); fp32: as they are.
-__device__ __forceinline__ void probabilities(const float *p, Frag<bf16_t> &f) {
-    f.v = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-}
-__device__ __forceinline__ void probabilities(const float *p, Frag<float> &f) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = p[e];
 }
 
 // unit u of a launch: which unit of the segment's memory it is, and how many keys that holds (a length outside the unit is cut to it)
@@ -139,17 +89,6 @@ __device__ __forceinline__ void unit_of_lane(const SharedLaunch &ln, const Share
     }
 }
 
-// row r of a unit that starts at sequence s0: token row and query head
-struct RowOf {
-    int64_t token;
-    int head;
-    __device__ RowOf(const SharedShape &sh, int64_t s0, int kvh, int r) {
-        const int group = sh.n_heads / sh.n_kv_heads;
-        token = s0 * sh.L + r / group;
-        head = kvh * group + r % group;
-    }
-};
-
 // A job's workgroups are dealt to the XCDs in runs of equal length: (unit, KV head, part) by (unit, KV head, part), the tiles of one
 // behind one another, so that those that read the same keys meet in one L2.  False: a workgroup of the padding.
 struct Place {
@@ -162,49 +101,6 @@ __device__ __forceinline__ bool place_of(const SharedJob &jb, int n_kv_heads, Pl
     const int grp = at / jb.tiles;
     p = {grp / jb.splits / n_kv_heads, grp / jb.splits % n_kv_heads, grp % jb.splits, at % jb.tiles};
     return true;
-}
-
-// Where a row's result over the keys of one workgroup goes: a part that the join reads, or, where it is the only one, the output
-template <typename T, int DH>
-struct PartOut {
-    const SharedLaunch &ln;
-    const bool direct;
-    int64_t at;      // of the row in [parts][n_rows], or among the rows
-    float *o;
-    T *out;
-    __device__ PartOut(const SharedShape &sh, const SharedLaunch &l, int part, const RowOf &row) : ln(l), direct(l.parts == 0) {
-        const int64_t r = row.token * sh.n_heads + row.head;
-        at = direct ? r : part * sh.n_rows + r;
-        o = l.o + at * DH;
-        out = (T *)l.out + row.token * sh.ld_out + row.head * DH;
-    }
-    // maximum m (what l is relative to) and sum l of the row
-    __device__ void sums(float m, float l, float sl2) const {
-        if (!direct) ln.ml[at] = make_float2(m, l);
-        else if (ln.lse) ln.lse[at] = log_sum(m, l, sl2);
-    }
-    __device__ static float log_sum(float m, float l, float sl2) { return l == 0.f ? -INFINITY : m * sl2 / LOG2E + logf(l); }
-    // what values() multiplies by; 0 where there were no keys
-    __device__ float factor(float l) const { return l == 0.f ? 0.f : direct ? 1.0f / l : 1.0f; }
-    __device__ void values(int c, const float *v, float f) const {
-        if (!direct) {
-            *reinterpret_cast<float4 *>(o + c) = make_float4(v[0], v[1], v[2], v[3]);
-        } else if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<uint2 *>(out + c) = make_uint2(pack_bf16x2(v[0] * f, v[1] * f), pack_bf16x2(v[2] * f, v[3] * f));
-        } else {
-            *reinterpret_cast<float4 *>(out + c) = make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-        }
-    }
-};
-
-// of a value and of the other half's
-__device__ __forceinline__ float both_max(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float both_sum(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // Few rows: a tile of TR rows of a unit of the job's last segment against a part of the keys that they see in the job's segments.  The
@@ -680,7 +576,7 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_attention_kernel(const T *_
 // joined in order.  G = 8 where there are many parts of few rows: every load is a round trip to memory, so as many as possible are
 // under way at a time (896 rows of 60 parts: 21 us with one loop over all maxima in front, 5.8 without).
 template <typename T, int DH, int G>
-__global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, SharedLaunch ln, float sl2) {
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedShape sh, AttentionParts ln, float sl2) {
     constexpr int TPR = DH / 4, RPW = 256 / (TPR * G);   // threads per part, rows per workgroup
     static_assert(RPW >= 1, "a row's threads are one workgroup");
     __shared__ float4 sums[G > 1 ? 256 : 1];
@@ -934,10 +830,16 @@ __global__ __launch_bounds__(256) void block_values_kernel(const float *__restri
 
 // the join of a launch: lanes of parts to a row (G of its kernel), workgroups
 constexpr int MANY_PARTS = 8;
-bool many_parts(const SharedLaunch &ln) { return ln.parts >= 16; }
-int64_t join_workgroups(const SharedShape &sh, const SharedLaunch &ln) {
+bool many_parts(const AttentionParts &ln) { return ln.parts >= 16; }
+int64_t join_workgroups(const SharedShape &sh, const AttentionParts &ln) {
     const int rows = 256 / (sh.d_head / 4 * (many_parts(ln) ? MANY_PARTS : 1));
     return (sh.n_rows + rows - 1) / rows;
+}
+template <typename T, int DH>
+void run_join(const SharedShape &sh, const AttentionParts &ln, float sl2, hipStream_t st) {
+    const dim3 grid((unsigned)join_workgroups(sh, ln));
+    if (many_parts(ln)) hipLaunchKernelGGL((shared_join_kernel<T, DH, MANY_PARTS>), grid, dim3(256), 0, st, sh, ln, sl2);
+    else hipLaunchKernelGGL((shared_join_kernel<T, DH, 1>), grid, dim3(256), 0, st, sh, ln, sl2);
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -951,9 +853,7 @@ void run_attention(const T *q, const SharedShape &sh, const SharedLaunch &ln, hi
     ensure_dynamic_lds(reinterpret_cast<const void *>(kern), smem, lds_raised);
     if (ln.blocks > 0) hipLaunchKernelGGL(kern, dim3((unsigned)ln.blocks), dim3(NW * 64), smem, st, q, sh, ln, sl2);
     if (ln.blocks > 0 && ln.parts == 0) return;
-    const dim3 grid((unsigned)join_workgroups(sh, ln));
-    if (many_parts(ln)) hipLaunchKernelGGL((shared_join_kernel<T, DH, MANY_PARTS>), grid, dim3(256), 0, st, sh, ln, sl2);
-    else hipLaunchKernelGGL((shared_join_kernel<T, DH, 1>), grid, dim3(256), 0, st, sh, ln, sl2);
+    run_join<T, DH>(sh, ln, sl2, st);
 }
 
 template <typename T, int DH>
@@ -1167,9 +1067,10 @@ bool plan_attention_shared(const SharedShape &sh, const SharedSegment *seg, int 
     *out = plan_attention(sh, seg, n);
     return launchable(out->blocks, NW * 64) && ((out->blocks > 0 && out->parts == 0) || launchable(join_workgroups(sh, *out), 256));
 }
-int64_t shared_attention_bytes(const SharedShape &sh, const SharedLaunch &ln) {
+int64_t attention_parts_bytes(const SharedShape &sh, const AttentionParts &ln) {
     return align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256) + align_up((int64_t)ln.parts * sh.n_rows * 8, 256);
 }
+int64_t shared_attention_bytes(const SharedShape &sh, const SharedLaunch &ln) { return attention_parts_bytes(sh, ln); }
 // the most that any batch of 1 .. sh.S sequences over these segments needs, however they share them
 int64_t shared_attention_most(const SharedShape &sh, const SharedSegment *seg, int n) {
     // No job has more parts than key tiles: those of a segment, or, of a finer segment in a walk, of every unit that a tile touches,
@@ -1218,11 +1119,18 @@ int64_t shared_weights_most(const SharedShape &sh, const SharedSegment *seg, int
         else { constexpr int DH = 16; CALL; }                                 \
     }
 
-void launch_attention_shared(const void *q, const SharedShape &sh, SharedLaunch &ln, void *out, float *lse, void *ws, hipStream_t st) {
+void place_attention_parts(const SharedShape &sh, AttentionParts &ln, void *out, float *lse, void *ws) {
     ln.o = (float *)ws;
     ln.ml = (float2 *)((char *)ws + align_up((int64_t)ln.parts * sh.n_rows * sh.d_head * 4, 256));
     ln.out = out;
     ln.lse = lse;
+}
+bool attention_join_launchable(const SharedShape &sh, const AttentionParts &ln) { return launchable(join_workgroups(sh, ln), 256); }
+void launch_attention_join(const SharedShape &sh, const AttentionParts &ln, float score_log2, hipStream_t st) {
+    PSD_SHARED_DISPATCH((run_join<T, DH>(sh, ln, score_log2, st)))
+}
+void launch_attention_shared(const void *q, const SharedShape &sh, SharedLaunch &ln, void *out, float *lse, void *ws, hipStream_t st) {
+    place_attention_parts(sh, ln, out, lse, ws);
     PSD_SHARED_DISPATCH((run_attention<T, DH>((const T *)q, sh, ln, st)))
 }
 

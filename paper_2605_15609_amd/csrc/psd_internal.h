@@ -431,19 +431,28 @@ inline bool launchable(int64_t workgroups, int threads) { return workgroups * th
 struct SharedJob {
     int seg, segs, tiled, packed, units, tiles, splits, block0, part0;   // packed: a unit and KV head to a wavefront
 };
-struct SharedLaunch {
-    int n_jobs = 0, n_segs = 0, parts = 0;   // parts = 0: every row's one part goes straight to the output
-    int64_t blocks = 0;
-    SharedJob job[kMaxSegments] = {};
-    SharedSegment seg[kMaxSegments];
+// where the results of an attention launch go: to the output, or, as parts over a part of the keys each, to scratch that a join reads
+struct AttentionParts {
+    int parts = 0;                       // 0: every row's one part goes straight to the output
     float *o = nullptr;                  // [parts][n_rows][d_head] sums relative to the part's maximum
     float2 *ml = nullptr;                // [parts][n_rows] maximum of the scores, sum of the exponentials (0: no keys, o not written)
     void *out = nullptr;
     float *lse = nullptr;
+};
+struct SharedLaunch : AttentionParts {
+    int n_jobs = 0, n_segs = 0;
+    int64_t blocks = 0;
+    SharedJob job[kMaxSegments] = {};
+    SharedSegment seg[kMaxSegments];
     // weights: workgroups of the second kernel, which adds the parts of jobs whose rows are cut
     int64_t join_blocks = 0;
     int join0[kMaxSegments] = {};
 };
+// scratch of the parts, their place in it, and the join of every row's parts (maxima times score_log2 are in units of log 2)
+int64_t attention_parts_bytes(const SharedShape &sh, const AttentionParts &ln);
+void place_attention_parts(const SharedShape &sh, AttentionParts &ln, void *out, float *lse, void *ws);
+bool attention_join_launchable(const SharedShape &sh, const AttentionParts &ln);
+void launch_attention_join(const SharedShape &sh, const AttentionParts &ln, float score_log2, hipStream_t st);
 bool shared_attention_takes(int dtype, int d_head);
 const char *shared_segment_fault(int dtype, const SharedSegment &s);
 // plans (false: more workgroups than a launch takes), the scratch that they need, and their launches
@@ -461,6 +470,53 @@ void launch_block_values(const float *qkv, int ld_qkv, int v_col, int S, int L, 
 bool kv_evict_launchable(const SharedSegment &src, int units, int n_kv_heads, int d_head, int dtype, int keep);
 void launch_kv_evict(const SharedSegment &src, const SharedSegment &dst, int units, int n_kv_heads, int d_head, int dtype, int keep, int n_first,
                      int n_last, int32_t *kept, int32_t *kept_lens, hipStream_t st);
+// rotary.hip: norms of heads and rotation by positions (psd_rotary)
+struct RotaryRows {
+    const void *in = nullptr;
+    void *out = nullptr;
+    const float *gain = nullptr;         // NULL: not normed
+    int64_t ld_in = 0, ld_out = 0;
+    int heads = 0;
+};
+struct Rotary {
+    RotaryRows rows[2];                  // queries, keys
+    const double *frequencies = nullptr;
+    const int32_t *positions = nullptr;  // NULL: first + row % rows_per_seq
+    int64_t n_tokens = 0;
+    int d_head = 0, rotated = 0, interleaved = 0, first = 0, rows_per_seq = 1, dtype = 0;
+    float factor = 1.f, eps = 0.f;
+};
+bool rotary_launchable(const Rotary &r);
+void launch_rotary(const Rotary &r, hipStream_t st);
+// caches in 8 bits (psd_kv8_cache)
+constexpr int KV8_TILE = 32;             // positions whose codes lie together
+struct Kv8 {
+    uint8_t *codes = nullptr;            // units of [n_kv_heads][capacity / 32][2][32 * d_head]
+    float2 *scales = nullptr;            // units of [n_kv_heads][capacity / block] (key, value)
+    const int32_t *lens = nullptr;       // device, one per unit; NULL: every unit holds len
+    int64_t stride_codes = 0, stride_scales = 0;   // bytes, pairs
+    int capacity = 0, len = 0, block_shift = 5, format = 0, n_kv_heads = 1, d_head = 64, seqs_per_unit = 1;
+};
+// rows of a token by unit: row i of unit u is u * n + i
+struct Kv8Rows {
+    void *k = nullptr, *v = nullptr;
+    int64_t ld_k = 0, ld_v = 0;
+    int n = 0, first = 0, dtype = 0;
+};
+// kv8.hip
+bool kv8_store_launchable(const Kv8 &c, int units, int n);
+void launch_kv8_store(const Kv8 &c, int units, const Kv8Rows &rows, const int32_t *starts, const int32_t *counts, hipStream_t st);
+bool kv8_load_launchable(const Kv8 &c, int units, int n);
+void launch_kv8_load(const Kv8 &c, int units, const Kv8Rows &rows, hipStream_t st);
+// attention_kv8.hip
+struct Kv8Launch : AttentionParts {
+    Kv8 cache;
+    const void *k = nullptr, *v = nullptr;   // rows of the sequences' own blocks, which are not in the cache (NULL: none)
+    int64_t ld_k = 0, ld_v = 0;
+    int units = 0, tiled = 0, tiles = 0, splits = 1, chunk = 0;   // tiles of rows of a unit and KV head, parts of `chunk` keys
+};
+bool plan_attention_kv8(const SharedShape &sh, const Kv8 &cache, bool own_rows, Kv8Launch *out);
+void launch_attention_kv8(const void *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st);
 // lm_head.hip (bf16): LM-head fused with the online top-1 / sum-exp reduction
 int64_t head_partial_bytes(int rows, int V);
 // fragment-order copies: [ceil(R/32)][K/16][64 lanes][8 bf16]
