@@ -975,6 +975,10 @@ def rotary_frequencies(rotated: int, theta: float, kind: str = "plain", stretch:
     return out, factor.value
 
 
+def _layout(t: Optional[torch.Tensor]):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.device)
+
+
 def _dense_on(t: torch.Tensor, what: str, dtype, shape, device) -> None:
     if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
         raise PsdError(f"{what}: dense {dtype} {tuple(shape)} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -987,6 +991,28 @@ def psd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Te
     """q [S, L, n_heads, d_head] and k [S, L, n_kv_heads, d_head] (or None), normed where there are gains (float32 [d_head]), their first
     2 * len(frequencies) channels (float64) turned by positions int32 [S, L] (None: first + row) -> (q_out, k_out), new or given; q_out = q
     and k_out = k work in place."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    shape = _rotary_shape(q, k, frequencies, positions, first, interleaved, factor, q_gain, k_gain, eps, q_out, k_out)
+    with _on_device(q.device) as stream:
+        _check(load_library().psd_rotary(C.byref(shape), q.data_ptr(), None if k is None else k.data_ptr(), frequencies.data_ptr(),
+                                         None if positions is None else positions.data_ptr(), None if q_gain is None else q_gain.data_ptr(),
+                                         None if k_gain is None else k_gain.data_ptr(), q_out.data_ptr(), None if k is None else k_out.data_ptr(), stream))
+    return q_out, k_out
+
+
+_rotary_shapes: dict = {}
+
+
+def _rotary_shape(q, k, frequencies, positions, first, interleaved, factor, q_gain, k_gain, eps, q_out, k_out) -> _RotaryShape:
+    """The shape of a call, checked once for tensors of these shapes, strides, types and devices (as _attention_shape)."""
+    key = (first, interleaved, factor, eps, _layout(q), _layout(k), _layout(frequencies), _layout(positions), _layout(q_gain), _layout(k_gain), _layout(q_out),
+           _layout(k_out))
+    found = _rotary_shapes.get(key)
+    if found is not None:
+        return found
     if q.dim() != 4 or q.dtype not in _DTYPES or (k is not None and (k.dim() != 4 or k.dtype != q.dtype or k.device != q.device
                                                                      or (k.shape[0], k.shape[1], k.shape[3]) != (q.shape[0], q.shape[1], q.shape[3]))):
         raise PsdError(f"q [S, L, heads, d] and k [S, L, KV heads, d], bf16 or fp32, not {q.dtype} {tuple(q.shape)} and "
@@ -994,10 +1020,6 @@ def psd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Te
     if k is None and (k_gain is not None or k_out is not None):
         raise PsdError("a gain or an output of no keys")
     S, L, H, d = q.shape
-    if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
     for name, t, like in (("q_out", q_out, q), ("k_out", k_out, k)):
         if t is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
             raise PsdError(f"{name}: {like.dtype} {tuple(like.shape)} on {like.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -1012,11 +1034,10 @@ def psd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], frequencies: torch.Te
     shape = _RotaryShape(S * L, _rows(q, "q"), 0 if k is None else _rows(k, "k"), _rows(q_out, "q_out"), 0 if k is None else _rows(k_out, "k_out"),
                          _int32(H, "heads"), 0 if k is None else _int32(k.shape[2], "KV heads"), _int32(d, "d_head"), _int32(2 * frequencies.numel(), "rotated"),
                          int(bool(interleaved)), _int32(first, "first"), _int32(L, "rows"), _DTYPES[q.dtype], float(factor), float(eps), 0)
-    with _on_device(q.device) as stream:
-        _check(load_library().psd_rotary(C.byref(shape), q.data_ptr(), None if k is None else k.data_ptr(), frequencies.data_ptr(),
-                                         None if positions is None else positions.data_ptr(), None if q_gain is None else q_gain.data_ptr(),
-                                         None if k_gain is None else k_gain.data_ptr(), q_out.data_ptr(), None if k is None else k_out.data_ptr(), stream))
-    return q_out, k_out
+    if len(_rotary_shapes) >= 256:
+        _rotary_shapes.clear()
+    _rotary_shapes[key] = shape
+    return shape
 
 
 class Kv8Cache:
@@ -1055,7 +1076,7 @@ class Kv8Cache:
         self.c = _Kv8Cache(address(codes), address(scales), address(lens), codes.stride(0) if units > 1 else 0, scales.stride(0) if units > 1 else 0,
                            _int32(positions, "positions"), _int32(n, "length"), _int32(block, "block"), _KV8_FORMATS[format],
                            _int32(heads, "KV heads"), _int32(d_head, "d_head"), _int32(self.seqs_per_unit, "seqs_per_unit"), 0)
-        self.shapes: dict = {}      # (see _kv8_shape)
+        self.shapes: dict = {}      # (see rows and _kv8_shape)
 
     @classmethod
     def empty(cls, units: int, n_kv_heads: int, d_head: int, positions: int, block: int = 32, format: str = "int8", device="cuda:0",
@@ -1067,28 +1088,40 @@ class Kv8Cache:
         return cls(torch.empty((units, n_kv_heads, n // 32, 2, 32 * d_head), dtype=torch.uint8, device=device),
                    torch.empty((units, n_kv_heads, n // block, 2), dtype=torch.float32, device=device), d_head, format, None, lens, seqs_per_unit)
 
-    def rows(self, k: torch.Tensor, v: torch.Tensor) -> Tuple[int, int, int]:
-        """(rows of a unit, row stride of k, of v) of [units, n, n_kv_heads, d_head], checked."""
+    def rows(self, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None,
+             counts: Optional[torch.Tensor] = None) -> Tuple[int, int, int, int]:
+        """(rows of a unit, row stride of k, of v, dtype) of [units, n, n_kv_heads, d_head] and what goes with them, checked once for tensors of
+        these shapes, strides, types and devices (as _attention_shape)."""
+        key = ("rows", _layout(k), _layout(v), _layout(starts), _layout(counts))
+        found = self.shapes.get(key)
+        if found is not None:
+            return found
         want = (self.units, self.n_kv_heads, self.d_head)
         for name, t in (("k", k), ("v", v)):
             if t.dim() != 4 or t.dtype not in _DTYPES or t.dtype != k.dtype or (t.shape[0], t.shape[2], t.shape[3]) != want or t.shape != k.shape \
                     or t.device != self.device:
                 raise PsdError(f"{name}: [{want[0]}, n, {want[1]}, {want[2]}] bf16 or fp32 on {self.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-        return _int32(k.shape[1], "rows"), _rows(k, "k"), _rows(v, "v")
+        for name, t in (("starts", starts), ("counts", counts)):
+            if t is not None:
+                _dense_on(t, name, torch.int32, (self.units,), self.device)
+        _int32(self.units, "units")
+        return self.remember(key, (_int32(k.shape[1], "rows"), _rows(k, "k"), _rows(v, "v"), _DTYPES[k.dtype]))
+
+    def remember(self, key, found):
+        if len(self.shapes) >= 64:
+            self.shapes.clear()
+        self.shapes[key] = found
+        return found
 
 
 def psd_kv8_store(cache: Kv8Cache, k: torch.Tensor, v: torch.Tensor, first: int = 0, starts: Optional[torch.Tensor] = None,
                   counts: Optional[torch.Tensor] = None) -> None:
     """Rows k, v [units, n, n_kv_heads, d_head] into the cache, at positions first .. of every unit or from starts int32 [units] on; counts
     int32 [units]: only the first of a unit's rows.  cache.lens is left as it is."""
-    n, ld_k, ld_v = cache.rows(k, v)
-    for name, t in (("starts", starts), ("counts", counts)):
-        if t is not None:
-            _dense_on(t, name, torch.int32, (cache.units,), cache.device)
+    n, ld_k, ld_v, dtype = cache.rows(k, v, starts, counts)
     with _on_device(cache.device) as stream:
-        _check(load_library().psd_kv8_store(C.byref(cache.c), _int32(cache.units, "units"), k.data_ptr(), v.data_ptr(), ld_k, ld_v, _DTYPES[k.dtype], n,
-                                            _int32(first, "first"), None if starts is None else starts.data_ptr(), None if counts is None else counts.data_ptr(),
-                                            stream))
+        _check(load_library().psd_kv8_store(C.byref(cache.c), cache.units, k.data_ptr(), v.data_ptr(), ld_k, ld_v, dtype, n, _int32(first, "first"),
+                                            None if starts is None else starts.data_ptr(), None if counts is None else counts.data_ptr(), stream))
 
 
 def psd_kv8_load(cache: Kv8Cache, first: int = 0, n: Optional[int] = None, dtype=torch.bfloat16, k_out: Optional[torch.Tensor] = None,
@@ -1102,18 +1135,17 @@ def psd_kv8_load(cache: Kv8Cache, first: int = 0, n: Optional[int] = None, dtype
         if n < 0 or dtype not in _DTYPES:
             raise PsdError(f"{n} positions as {dtype}")
         k_out, v_out = (torch.zeros((cache.units, n, cache.n_kv_heads, cache.d_head), dtype=dtype, device=cache.device) for _ in range(2))
-    rows, ld_k, ld_v = cache.rows(k_out, v_out)
+    rows, ld_k, ld_v, kind = cache.rows(k_out, v_out)
     if rows != n:
         raise PsdError(f"{rows} rows for {n} positions")
     with _on_device(cache.device) as stream:
-        _check(load_library().psd_kv8_load(C.byref(cache.c), _int32(cache.units, "units"), _int32(first, "first"), n, k_out.data_ptr(), v_out.data_ptr(), ld_k,
-                                           ld_v, _DTYPES[k_out.dtype], stream))
+        _check(load_library().psd_kv8_load(C.byref(cache.c), cache.units, _int32(first, "first"), n, k_out.data_ptr(), v_out.data_ptr(), ld_k, ld_v, kind, stream))
     return k_out, v_out
 
 
 def _kv8_shape(q: torch.Tensor, cache: Kv8Cache, k: Optional[torch.Tensor], v: Optional[torch.Tensor], out: Optional[torch.Tensor]):
     """(shape, row strides of k and v) of a call, checked once for tensors of these shapes, strides, types and devices (as _attention_shape)."""
-    key = tuple(None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in (q, k, v, out))
+    key = (_layout(q), _layout(k), _layout(v), _layout(out))
     found = cache.shapes.get(key)
     if found is not None:
         return found
@@ -1132,11 +1164,7 @@ def _kv8_shape(q: torch.Tensor, cache: Kv8Cache, k: Optional[torch.Tensor], v: O
     if S * L * H >= 2 ** 31:
         raise PsdError(f"{S} sequences of {L} rows of {H} heads are too many")
     shape = _AttentionShape(S, L, H, cache.n_kv_heads, d, _DTYPES[q.dtype], _rows(q, "q"), H * d if out is None else _rows(out, "out"))
-    found = (shape, 0 if k is None else _rows(k, "k"), 0 if v is None else _rows(v, "v"))
-    if len(cache.shapes) >= 64:
-        cache.shapes.clear()
-    cache.shapes[key] = found
-    return found
+    return cache.remember(key, (shape, 0 if k is None else _rows(k, "k"), 0 if v is None else _rows(v, "v")))
 
 
 def psd_attention_kv8_workspace(q: torch.Tensor, cache: Kv8Cache, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -3,8 +3,7 @@
 // A block of positions and a KV head have one scale for their keys and one for their values,
 //     s = max(what the block's kept positions have, fl(largest magnitude of the new rows / M)),   code = RN(x / s),   value = code * s,
 // M = 127 (whole numbers) or 448 (floats of 4 and 3 bits), RN to the nearest code, ties to even.  Where s grows, kept codes are rounded again:
-// RN(code * s_kept / s).  The quotients are exact before they are rounded, so a code does not depend on how the division is done: one in
-// fp32 decides where it is further from a border between two codes than it can be off, one in 64 bits where it is not.
+// RN(code * s_kept / s).  The quotients are exact before they are rounded, so a code does not depend on how the division is done.
 //
 // Bound: memory (rows read once, codes written once); a single token a chain of round trips in one launch.
 #include "psd_internal.h"
@@ -14,116 +13,249 @@ namespace {
 
 constexpr int THREADS = 256;
 
-// RN to a code, as its byte
-template <int FORMAT>
-__device__ __forceinline__ uint32_t code_of(double y) {
-    if constexpr (FORMAT == PSD_KV8_INT8) {
-        return (uint32_t)(int)fmin(fmax(rint(y), -127.0), 127.0) & 0xffu;
-    } else {
-        int e;
-        (void)frexp(y, &e);
-        const int step = (e < -5 ? -5 : e) - 4;                               // of the codes around y: 2^step
-        const double r = fmin(fabs(rint(ldexp(y, -step))), ldexp(448.0, -step));   // 0 .. 16 steps
-        const int n = (int)r;
-        // n steps above 2^(step + 3) or, below the smallest normal number, above 0
-        const uint32_t bits = n < 8 ? n : ((uint32_t)(step + 9) << 3) + n;
-        return bits | (y < 0.0 ? 0x80u : 0u);
-    }
-}
 template <int FORMAT>
 __device__ __forceinline__ float number_of(uint32_t code) {
     if constexpr (FORMAT == PSD_KV8_INT8) return (float)(int8_t)code;
     else return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
 }
-
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, float (&x)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(u[i] << 16);
-            x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-        }
+// four numbers that codes stand for, as their bytes
+template <int FORMAT>
+__device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float d) {
+    if constexpr (FORMAT == PSD_KV8_INT8) {
+        const uint32_t lo = __builtin_amdgcn_perm((uint32_t)(int)b, (uint32_t)(int)a, 0x0c0c0400u), hi = __builtin_amdgcn_perm((uint32_t)(int)d, (uint32_t)(int)c, 0x0c0c0400u);
+        return lo | hi << 16;
     } else {
-        const float4 v = *reinterpret_cast<const float4 *>(p), w = *reinterpret_cast<const float4 *>(p + 4);
-        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w, x[4] = w.x, x[5] = w.y, x[6] = w.z, x[7] = w.w;
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
     }
 }
 
-// A workgroup stores what the rows of a unit put into one block of a KV head, keys or values.  Codes are put together in LDS, as they lie in the
-// cache (whole tiles, of a block of 16 positions half of one).
-template <typename T, int FORMAT>
-__global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows, const int32_t *starts, const int32_t *counts, int blocks) {
-    extern __shared__ __align__(16) uint8_t tile[];
-    __shared__ float tops[THREADS / 64];
-    const int d = c.d_head, block = 1 << c.block_shift;
-    int64_t at = blockIdx.x;
-    const int which = (int)(at & 1);
-    at >>= 1;
-    const int b = (int)(at % blocks);
-    at /= blocks;
-    const int head = (int)(at % c.n_kv_heads);
-    const int64_t u = at / c.n_kv_heads;
+// RN(x / s) to a code, x / s at most M (1 + 2^-23).  t = x * fl(1 / s) is off by 2^-23 of itself, so the nearest code v to t is the right one or next to
+// it; x - v s tells which, and in fp32 it is exact: v has 8 bits at most and x is v s or more than half a step away, so the difference is a
+// multiple of 2^-25 steps and hardly more than half a step.  (Scales below 2^-100, where it might not be, are lifted with x.)
+template <int FORMAT>
+struct Rounding {
+    float s, inv, lift;
+    __device__ explicit Rounding(float scale) {
+        lift = scale < 0x1p-100f ? 0x1p64f : 1.f;
+        s = scale * lift;
+        inv = 1.0f / s;
+    }
+    // power of two that the codes around t are apart
+    static __device__ __forceinline__ float step_of(float t) {
+        return FORMAT == PSD_KV8_INT8 ? 1.f : fmaxf(__uint_as_float(__float_as_uint(t) & 0x7f800000u), 0x1p-6f) * 0.125f;
+    }
+    // x + low (what x itself was rounded off by: both 0 or x the larger)
+    __device__ __forceinline__ float exact(float x, float low) const {
+        const float t = x * inv, step = step_of(t), per = FORMAT == PSD_KV8_INT8 ? 1.f : __uint_as_float(0x7f000000u - __float_as_uint(step));
+        const float n = rintf(t * per), v = n * step, rest = __builtin_fmaf(-v, s, x), half = 0.5f * step * s;
+        const float over = (fabsf(rest) - half) + (rest < 0.f ? -low : low);
+        return over > 0.f || (over == 0.f && ((int)n & 1)) ? v + copysignf(step, rest) : v;
+    }
+    // four of them as bytes
+    __device__ __forceinline__ uint32_t careful(const float (&x)[4]) const {
+        return pack_codes<FORMAT>(exact(x[0] * lift, 0.f), exact(x[1] * lift, 0.f), exact(x[2] * lift, 0.f), exact(x[3] * lift, 0.f));
+    }
+    // the same where no t is next to a border or on it and nothing is lifted; else `again` is set
+    __device__ __forceinline__ uint32_t quick(const float (&x)[4], bool &again) const {
+        float t[4], v[4];
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] = x[i] * inv;
+        if constexpr (FORMAT == PSD_KV8_INT8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = rintf(t[i]);
+            word = pack_codes<FORMAT>(v[0], v[1], v[2], v[3]);
+        } else {
+            word = pack_codes<FORMAT>(t[0], t[1], t[2], t[3]);
+            v[0] = __builtin_amdgcn_cvt_f32_fp8((int)word, 0), v[1] = __builtin_amdgcn_cvt_f32_fp8((int)word, 1);
+            v[2] = __builtin_amdgcn_cvt_f32_fp8((int)word, 2), v[3] = __builtin_amdgcn_cvt_f32_fp8((int)word, 3);
+        }
+        const float half = 0.5f * s;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) again |= !(fabsf(__builtin_fmaf(-v[i], s, x[i])) < (FORMAT == PSD_KV8_INT8 ? half : step_of(t[i]) * half));
+        return word;
+    }
+    // kept codes under a scale of `had` rounded again, the first n of four
+    __device__ __forceinline__ uint32_t regrown(uint32_t codes, float had, int n) const {
+        float v[4];
+        had *= lift;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float code = number_of<FORMAT>(codes >> (8 * i) & 0xff), x = code * had;
+            v[i] = exact(x, __builtin_fmaf(code, had, -x));
+        }
+        const uint32_t first = n >= 4 ? ~0u : (1u << (8 * max(n, 0))) - 1;
+        return (codes & ~first) | (pack_codes<FORMAT>(v[0], v[1], v[2], v[3]) & first);
+    }
+};
+
+// Codes of a tile in LDS: rows of 4 words -- of values the 16 positions of a half and channel, of keys 16 channels of a position -- 5 words apart, so that
+// neither the pieces that threads put there nor the rows meet in few banks.
+__device__ __forceinline__ int value_word(int h, int c, int b, int d) { return (h * (d + 4) + c) * 5 + b; }
+__device__ __forceinline__ int key_word(int position, int c, int d) { return ((c >> 4) * KV8_TILE + position) * 5 + (c >> 2 & 3); }
+constexpr int tile_words(int d) { return (2 * d + 8) * 5; }
+// the row that the i-th 16 bytes of a tile are
+__device__ __forceinline__ int row_word(int i, int which, int d) {
+    const int w = min(d, 32), ws = d < 32 ? 4 : 5;
+    return which ? value_word(i >> ws & 1, (i >> (ws + 1) << ws) + (i & (w - 1)), 0, d) : i * 5;
+}
+
+// Task i of units x heads x parts x (keys, values), of which there are fewer than 2^24 (what a launch holds)
+struct Task {
+    bool there;
+    int which, part, head, unit;
+    __device__ Task(uint32_t i, uint32_t tasks, uint32_t parts, uint32_t heads) {
+        there = i < tasks;
+        i = there ? i : 0;
+        which = i & 1;
+        i >>= 1;
+        part = i % parts;
+        i /= parts;
+        head = i % heads;
+        unit = i / heads;
+    }
+};
+
+// A task is what the rows of a unit put into one block of a KV head, keys or values; d_head threads take one, tile by tile, a thread 4 positions of 8
+// channels.  Their codes are words of a position's channels (keys) or of a channel's positions (values), put together in LDS and written as they
+// lie in the cache.
+template <typename T, int FORMAT, int NB>
+__global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows, const int32_t *starts, const int32_t *counts, uint32_t blocks, uint32_t tasks) {
+    extern __shared__ __align__(16) uint32_t words[];   // [tasks][NB][tile_words]
+    __shared__ uint32_t tops[THREADS / 64];
+    const int ds = __ffs(c.d_head) - 1, d = 1 << ds, block = 1 << c.block_shift, mine = threadIdx.x >> ds, t = threadIdx.x & (d - 1);
+    const Task of(blockIdx.x * (THREADS >> ds) + mine, tasks, blocks, c.n_kv_heads);
+    const int which = of.which, b = of.part, head = of.head;
+    const int64_t u = of.unit;
     const int64_t start = starts ? starts[u] : rows.first, count = counts ? min(max(counts[u], 0), rows.n) : rows.n;
     const int64_t end = min(start + count, (int64_t)c.capacity);
     // the b-th block that the unit's rows touch
     const int64_t p0 = ((max(start, (int64_t)0) >> c.block_shift) + b) << c.block_shift;
-    const int lo = (int)(max(start, p0) - p0), hi = (int)min(end - p0, (int64_t)block);
-    if (p0 >= end || lo >= hi) return;
-    const T *x = (const T *)(which ? rows.v : rows.k) + (u * rows.n + (p0 - start)) * (which ? rows.ld_v : rows.ld_k) + (int64_t)head * d;   // of position p0
+    const int lo = (int)(max(start, p0) - p0), hi = (int)max(min(end - p0, (int64_t)block), (int64_t)-1);
+    const bool live = of.there && lo < hi;
     const int64_t ld = which ? rows.ld_v : rows.ld_k;
-    const int pieces = d >> 3, n = (hi - lo) * pieces;
-    float top = 0.f;
-    bool bad = false;
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-        float v[8];
-        load8(x + (lo + i / pieces) * ld + i % pieces * 8, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            bad |= !(fabsf(v[e]) < INFINITY);
-            top = fmaxf(top, fabsf(v[e]));
-        }
-    }
-    if (bad) top = INFINITY;
-    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-    // codes that stay, and those behind the rows: as they are
-    const bool partial = lo > 0 || hi < block;
-    const int row0 = (int)(p0 & (KV8_TILE - 1)), tiles = max(block / KV8_TILE, 1);
+    const T *x = (const T *)(which ? rows.v : rows.k) + (u * rows.n + (p0 - start)) * ld + (int64_t)head * d;   // of position p0
+    const int row0 = (int)(p0 & (KV8_TILE - 1));   // of the block in its first tile
     uint8_t *codes = c.codes + u * c.stride_codes + ((int64_t)head * (c.capacity / KV8_TILE) + p0 / KV8_TILE) * (64 * d) + which * (32 * d);
-    if (partial)
-        for (int i = threadIdx.x; i < tiles * 2 * d; i += THREADS)
-            *reinterpret_cast<uint4 *>(tile + i * 16) = *reinterpret_cast<const uint4 *>(codes + (int64_t)(i / (2 * d)) * (64 * d) + i % (2 * d) * 16);
     float *scale = &c.scales[u * c.stride_scales + (int64_t)head * (c.capacity >> c.block_shift) + (p0 >> c.block_shift)].x + which;
-    const float had = lo > 0 ? *scale : 0.f;   // (a block that begins with a new row starts afresh)
-    __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const float need = top / kv8_most(FORMAT);
-    const bool finite = need < INFINITY && had < INFINITY;   // (else nothing that the block holds can be told: all of it reads as NaN)
-    const float s = finite ? fmaxf(had, need) : NAN;
-    auto place = [&](int p, int ch) { return (row0 + p) / KV8_TILE * (32 * d) + (which ? kv8_value_at((row0 + p) % KV8_TILE, ch, d) : kv8_key_at((row0 + p) % KV8_TILE, ch)); };
-    if (finite && had > 0.f && s > had)
-        for (int i = threadIdx.x; i < lo * d; i += THREADS) {
-            uint8_t *q = tile + place(i / d, i % d);
-            *q = (uint8_t)code_of<FORMAT>((double)number_of<FORMAT>(*q) * (double)had / (double)s);
-        }
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-        const int p = lo + i / pieces, ch = i % pieces * 8;
-        float v[8];
-        load8(x + p * ld + ch, v);
+    uint32_t *lds = words + mine * NB * tile_words(d);
+    const int rg = t >> (ds - 3), c8 = (t & ((d >> 3) - 1)) * 8;   // the thread's positions 4 rg .. and channels c8 ..
+    const bool partial = live && (lo > 0 || hi < block);
+
+    alignas(16) T raw[NB][4][8];
+    uint32_t top = 0;
+    float had = 0.f;
+    if (live) {
+        if (lo > 0) had = *scale;   // (a block that begins with a new row starts afresh)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) tile[place(p, ch + e)] = (uint8_t)(finite && s > 0.f ? code_of<FORMAT>((double)v[e] / (double)s) : 0u);
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {   // (positions without a new row repeat one that has)
+                const T *from = x + min(max(n * KV8_TILE - row0 + 4 * rg + j, lo), hi - 1) * ld + c8;
+                if constexpr (sizeof(T) == 2) {
+                    *reinterpret_cast<uint4 *>(raw[n][j]) = *reinterpret_cast<const uint4 *>(from);
+                } else {
+                    *reinterpret_cast<float4 *>(raw[n][j]) = *reinterpret_cast<const float4 *>(from);
+                    *reinterpret_cast<float4 *>(raw[n][j] + 4) = *reinterpret_cast<const float4 *>(from + 4);
+                }
+            }
+        if (partial)   // (codes that stay, and those behind the rows)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int i = t + d * k;
+                    const uint4 old = *reinterpret_cast<const uint4 *>(codes + (int64_t)n * (64 * d) + i * 16);
+                    uint32_t *to = lds + n * tile_words(d) + row_word(i, which, d);
+                    to[0] = old.x, to[1] = old.y, to[2] = old.z, to[3] = old.w;
+                }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(to_float(raw[n][j][e])) & 0x7fffffffu);   // (infinities and NaN are above all numbers)
     }
-    if (threadIdx.x == 0) *scale = s;
+    for (int s = min(d, 64) >> 1; s > 0; s >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s, 64));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
-    // Blocks of 16 share the 16 bytes of a value's positions: 8 bytes are one block's alone.
-    for (int i = threadIdx.x; i < tiles * 4 * d; i += THREADS) {
-        const int in_tile = i % (4 * d) * 8;
-        if (block < KV8_TILE && (which ? in_tile & 8 : in_tile >> 4 & 16) != (which ? row0 >> 1 : row0)) continue;
-        *reinterpret_cast<uint2 *>(codes + (int64_t)(i / (4 * d)) * (64 * d) + in_tile) = *reinterpret_cast<const uint2 *>(tile + i * 8);
+    if (d == 128) top = max(tops[mine * 2], tops[mine * 2 + 1]);
+    const float need = __uint_as_float(top) / kv8_most(FORMAT);
+    const bool finite = top < 0x7f800000u && had < INFINITY;   // (else nothing that the block holds can be told: all of it reads as NaN)
+    const float s = finite ? fmaxf(had, need) : NAN;
+    const bool grown = finite && had > 0.f && s > had, some = finite && s > 0.f;
+    if (live) {
+        const Rounding<FORMAT> round(some ? s : 1.f);
+        auto put = [&](int n, auto numbers, auto place) {   // the 8 words of the thread in tile n
+            uint32_t code[8];
+            bool again = round.lift != 1.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float v[4];
+                numbers(i, v);
+                code[i] = round.quick(v, again);
+            }
+            if (__any(again)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float v[4];
+                    numbers(i, v);
+                    code[i] = round.careful(v);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) place(i, some ? code[i] : 0u);
+        };
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            uint32_t *to = lds + n * tile_words(d);
+            const int p = n * KV8_TILE - row0 + 4 * rg;   // of the thread's first position in the block
+            // a word whose bytes in `fresh` are new: of what it held in front of them `kept` bytes stay
+            auto merge = [&](uint32_t *word, uint32_t code, uint32_t fresh, int kept) {
+                if (fresh == 0xffffffffu) {
+                    *word = code;
+                } else if (partial && p >= 0 && p < block) {
+                    uint32_t old = *word;
+                    if (grown) old = round.regrown(old, had, kept);
+                    *word = (old & ~fresh) | (code & fresh);
+                }
+            };
+            if (which) {
+                uint32_t fresh = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) fresh |= p + j >= lo && p + j < hi ? 0xffu << (8 * j) : 0u;
+                put(n, [&](int i, float (&v)[4]) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = to_float(raw[n][j][i]);
+                }, [&](int i, uint32_t code) { merge(to + value_word(rg & 1, c8 + i, rg >> 1, d), code, fresh, lo - p); });
+            } else {
+                put(n, [&](int i, float (&v)[4]) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = to_float(raw[n][i >> 1][4 * (i & 1) + e]);
+                }, [&](int i, uint32_t code) {
+                    const int j = i >> 1;
+                    merge(to + key_word(4 * rg + j, c8 + 4 * (i & 1), d), code, p + j >= lo && p + j < hi ? 0xffffffffu : 0u, p + j < lo ? 4 : 0);
+                });
+            }
+        }
+        if (t == 0) *scale = s;
     }
+    __syncthreads();
+    if (!live) return;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = t + d * k;
+            const uint32_t *from = lds + n * tile_words(d) + row_word(i, which, d);
+            uint8_t *to = codes + (int64_t)n * (64 * d) + i * 16;
+            if (block == KV8_TILE / 2) {   // half of a tile's positions are another block's: rows of keys, 8 bytes of a row of values
+                if (which) *reinterpret_cast<uint2 *>(to + (row0 >> 1)) = make_uint2(from[row0 >> 3], from[(row0 >> 3) + 1]);
+                else if ((i & 16) == row0) *reinterpret_cast<uint4 *>(to) = make_uint4(from[0], from[1], from[2], from[3]);
+            } else {
+                *reinterpret_cast<uint4 *>(to) = make_uint4(from[0], from[1], from[2], from[3]);
+            }
+        }
 }
 
 // code * s to T: exact before it is rounded.  In fp32 the product is rounded already; bf16 takes it with the last bit set where something was cut off
@@ -139,30 +271,57 @@ __device__ __forceinline__ T value_of(float code, float s) {
     return from_float<T>(p);
 }
 
-// A workgroup loads the positions of one tile of a unit and KV head, keys or values.
+// A task is one tile of a unit and KV head, keys or values, and d_head threads: codes into LDS as they lie in memory, and a thread takes 4
+// positions of 8 channels out of it.
 template <typename T, int FORMAT>
-__global__ __launch_bounds__(THREADS) void kv8_load_kernel(Kv8 c, Kv8Rows rows, int tiles) {
-    extern __shared__ __align__(16) uint8_t tile[];
-    const int d = c.d_head;
-    int64_t at = blockIdx.x;
-    const int which = (int)(at & 1);
-    at >>= 1;
-    const int t = rows.first / KV8_TILE + (int)(at % tiles);
-    at /= tiles;
-    const int head = (int)(at % c.n_kv_heads);
-    const int64_t u = at / c.n_kv_heads;
-    const int lo = max(rows.first - t * KV8_TILE, 0), hi = min(min(rows.first + rows.n, kv8_keys(c, (int)u)) - t * KV8_TILE, KV8_TILE);
-    if (lo >= hi) return;
-    const uint8_t *codes = c.codes + u * c.stride_codes + ((int64_t)head * (c.capacity / KV8_TILE) + t) * (64 * d) + which * (32 * d);
-    for (int i = threadIdx.x; i < 2 * d; i += THREADS) *reinterpret_cast<uint4 *>(tile + i * 16) = *reinterpret_cast<const uint4 *>(codes + i * 16);
-    __syncthreads();
-    const float *scales = &c.scales[u * c.stride_scales + (int64_t)head * (c.capacity >> c.block_shift)].x + which;
+__global__ __launch_bounds__(THREADS) void kv8_load_kernel(Kv8 c, Kv8Rows rows, uint32_t tiles, uint32_t tasks) {
+    extern __shared__ __align__(16) uint32_t words[];   // [tasks][tile_words]
+    const int ds = __ffs(c.d_head) - 1, d = 1 << ds, mine = threadIdx.x >> ds, t = threadIdx.x & (d - 1);
+    const Task of(blockIdx.x * (THREADS >> ds) + mine, tasks, tiles, c.n_kv_heads);
+    const int which = of.which, tile = rows.first / KV8_TILE + of.part, head = of.head;
+    const int64_t u = of.unit;
+    const int lo = max(rows.first - tile * KV8_TILE, 0), hi = min(min(rows.first + rows.n, kv8_keys(c, (int)u)) - tile * KV8_TILE, KV8_TILE);
+    const bool live = of.there && lo < hi;
+    uint32_t *lds = words + mine * tile_words(d);
+    const int rg = t >> (ds - 3), c8 = (t & ((d >> 3) - 1)) * 8;
     const int64_t ld = which ? rows.ld_v : rows.ld_k;
-    T *out = (T *)(which ? rows.v : rows.k) + (u * rows.n + ((int64_t)t * KV8_TILE - rows.first)) * ld + (int64_t)head * d;   // of the tile's position 0
-    for (int i = threadIdx.x; i < (hi - lo) * d; i += THREADS) {
-        const int p = lo + i / d, ch = i % d;
-        const float s = scales[2 * (int64_t)((t * KV8_TILE + p) >> c.block_shift)];
-        out[p * ld + ch] = value_of<T>(number_of<FORMAT>(tile[which ? kv8_value_at(p, ch, d) : kv8_key_at(p, ch)]), s);
+    T *out = (T *)(which ? rows.v : rows.k) + (u * rows.n + ((int64_t)tile * KV8_TILE - rows.first)) * ld + (int64_t)head * d + c8;   // of the tile's position 0
+    float s = 0.f;
+    if (live) {
+        const uint8_t *codes = c.codes + u * c.stride_codes + ((int64_t)head * (c.capacity / KV8_TILE) + tile) * (64 * d) + which * (32 * d);
+        // (4 positions are of one block)
+        s = (&c.scales[u * c.stride_scales + (int64_t)head * (c.capacity >> c.block_shift) + ((tile * KV8_TILE + 4 * rg) >> c.block_shift)].x)[which];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = t + d * k;
+            const uint4 v = *reinterpret_cast<const uint4 *>(codes + i * 16);
+            uint32_t *to = lds + row_word(i, which, d);
+            to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
+        }
+    }
+    __syncthreads();
+    if (!live) return;
+    uint32_t w[8];   // keys: 2 words of each position; values: one of each channel
+    if (which) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = lds[value_word(rg & 1, c8 + e, rg >> 1, d)];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t *from = lds + key_word(4 * rg + j, c8, d);
+            w[2 * j] = from[0], w[2 * j + 1] = from[1];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int p = 4 * rg + j;
+        if (p < lo || p >= hi) continue;
+        alignas(16) T v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = value_of<T>(number_of<FORMAT>((which ? w[e] >> (8 * j) : w[2 * j + (e >> 2)] >> (8 * (e & 3))) & 0xffu), s);
+        T *to = out + p * ld;
+        *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(v);
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(to + 4) = *reinterpret_cast<const uint4 *>(v + 4);
     }
 }
 
@@ -187,14 +346,23 @@ bool kv8_load_launchable(const Kv8 &c, int units, int n) { return (double)units 
 
 void launch_kv8_store(const Kv8 &c, int units, const Kv8Rows &rows, const int32_t *starts, const int32_t *counts, hipStream_t st) {
     if (rows.n < 1) return;
-    const int blocks = store_blocks(c, rows.n), smem = std::max(1 << c.block_shift, KV8_TILE) * c.d_head;
-    const dim3 grid((unsigned)((int64_t)units * c.n_kv_heads * blocks * 2));
-    PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_store_kernel<T, F>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks))
+    const int blocks = store_blocks(c, rows.n), per = THREADS / c.d_head, nb = std::max((1 << c.block_shift) / KV8_TILE, 1);
+    const uint32_t tasks = (uint32_t)(units * c.n_kv_heads * blocks * 2);
+    const int smem = per * nb * tile_words(c.d_head) * 4;
+    const dim3 grid((unsigned)((tasks + per - 1) / per));
+    if (nb == 1) {
+        PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_store_kernel<T, F, 1>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks))
+    } else if (nb == 2) {
+        PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_store_kernel<T, F, 2>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks))
+    } else {
+        PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_store_kernel<T, F, 4>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks))
+    }
 }
 
 void launch_kv8_load(const Kv8 &c, int units, const Kv8Rows &rows, hipStream_t st) {
     if (rows.n < 1) return;
-    const int tiles = load_tiles(rows.first, rows.n), smem = KV8_TILE * c.d_head;
-    const dim3 grid((unsigned)((int64_t)units * c.n_kv_heads * tiles * 2));
-    PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_load_kernel<T, F>), grid, dim3(THREADS), smem, st, c, rows, tiles))
+    const int tiles = load_tiles(rows.first, rows.n), per = THREADS / c.d_head;
+    const uint32_t tasks = (uint32_t)(units * c.n_kv_heads * tiles * 2);
+    const dim3 grid((unsigned)((tasks + per - 1) / per));
+    PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_load_kernel<T, F>), grid, dim3(THREADS), per * tile_words(c.d_head) * 4, st, c, rows, tiles, tasks))
 }
