@@ -7,6 +7,8 @@
 //
 // Per tile the problem is transposed as in the other attention kernels: S^T = K Q^T, O^T += V^T P^T.  A lane owns one row; the cache holds
 // codes in the order of the products' fragments (kv8_device.h), so a lane's 16 bytes are two fragments once they are converted.
+#include <math.h>
+
 #include <algorithm>
 
 #include "psd_internal.h"
@@ -22,13 +24,13 @@ constexpr int NW = 4;     // wavefronts of a workgroup
 constexpr float SLACK = 8.f;      // the reference of a row's exponentials is raised where its maximum has grown by more (in units of log 2)
 constexpr float FAR = 0x1p24f;    // references beyond it (see Softmax)
 
-// 16 codes: the first 8 into a, the last 8 into b
+// 8 codes, and 16: the first 8 into a, the last 8 into b
 template <int FORMAT>
-__device__ __forceinline__ void convert(const uint4 c, Frag<bf16_t> &a, Frag<bf16_t> &b) {
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    uint32_t r[8];
+__device__ __forceinline__ uint4 convert(uint32_t c0, uint32_t c1) {
+    const uint32_t w[2] = {c0, c1};
+    uint32_t r[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
         if constexpr (FORMAT == PSD_KV8_INT8) {
             r[2 * i] = pack_bf16x2((float)(int8_t)w[i], (float)(int8_t)(w[i] >> 8));
             r[2 * i + 1] = pack_bf16x2((float)(int8_t)(w[i] >> 16), (float)((int32_t)w[i] >> 24));
@@ -37,8 +39,12 @@ __device__ __forceinline__ void convert(const uint4 c, Frag<bf16_t> &a, Frag<bf1
             r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, true));
         }
     }
-    a.v = make_uint4(r[0], r[1], r[2], r[3]);
-    b.v = make_uint4(r[4], r[5], r[6], r[7]);
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+template <int FORMAT>
+__device__ __forceinline__ void convert(const uint4 c, Frag<bf16_t> &a, Frag<bf16_t> &b) {
+    a.v = convert<FORMAT>(c.x, c.y);
+    b.v = convert<FORMAT>(c.z, c.w);
 }
 template <int FORMAT>
 __device__ __forceinline__ void convert(const uint4 c, Frag<float> &a, Frag<float> &b) {
@@ -79,10 +85,9 @@ struct Softmax {
     float m = -INFINITY, neg = 0.f, l = 0.f;   // reference (-inf: no score yet), what is added to scores, sum
     bool far = false;                          // a row of the wavefront has a reference beyond FAR
 
-    // Scores of NT groups of 32 positions (x[t][v] <-> position 32 t + 8 (v / 4) + 4 half + v % 4) into probabilities times value scales, 8 at a time as
-    // the second product takes them.
-    template <typename T, int NT, int CT>
-    __device__ __forceinline__ void step(floatx16 (&x)[NT], const Scale (&s)[2 * NT], floatx16 (&acc)[CT], Frag<T> (&p)[2 * NT]) {
+    // x: scores of NT groups of 32 positions (x[t][v] <-> position 32 t + 8 (v / 4) + 4 half + v % 4), as sums over the codes.  Raises the reference.
+    template <int NT, int CT>
+    __device__ __forceinline__ void reference(floatx16 (&x)[NT], const Scale (&s)[2 * NT], floatx16 (&acc)[CT]) {
         float mx = -INFINITY;
 #pragma unroll
         for (int g = 0; g < 2 * NT; ++g) {
@@ -106,29 +111,44 @@ struct Softmax {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[ct][v] *= alpha;
         }
+    }
+    // (the last words of reference(): scores scaled and rounded, scales of 1)
+    template <int NT>
+    __device__ __forceinline__ void scale_far(floatx16 (&x)[NT], Scale (&s)[2 * NT]) const {
+        if (!far) return;
+#pragma unroll
+        for (int g = 0; g < 2 * NT; ++g) {
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                float scaled = x[g >> 1][8 * (g & 1) + v] * s[g].k;
+                asm volatile("" : "+v"(scaled));   // (rounded: contracted into what follows it would not be)
+                x[g >> 1][8 * (g & 1) + v] = scaled;
+            }
+            s[g].k = 1.f;
+        }
+    }
+    // Scores into probabilities times value scales, 8 at a time as the second product takes them.
+    template <typename T, int NT>
+    __device__ __forceinline__ void weights(const floatx16 (&x)[NT], const Scale (&s)[2 * NT], Frag<T> (&p)[2 * NT]) {
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int g = 0; g < 2 * NT; ++g) {
-            float by = s[g].k;
-            if (far) {
-#pragma unroll
-                for (int v = 0; v < 8; ++v) {
-                    float scaled = x[g >> 1][8 * (g & 1) + v] * by;
-                    asm volatile("" : "+v"(scaled));   // (rounded: contracted into what follows it would not be)
-                    x[g >> 1][8 * (g & 1) + v] = scaled;
-                }
-                by = 1.f;
-            }
             float e[8];
 #pragma unroll
             for (int v = 0; v < 8; ++v) {
-                e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g >> 1][8 * (g & 1) + v], by, neg));
+                e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g >> 1][8 * (g & 1) + v], s[g].k, neg));
                 sum[v & 1] += e[v];
                 e[v] *= s[g].v;
             }
             probabilities(e, p[g]);
         }
         l += sum[0] + sum[1];
+    }
+    template <typename T, int NT, int CT>
+    __device__ __forceinline__ void step(floatx16 (&x)[NT], Scale (&s)[2 * NT], floatx16 (&acc)[CT], Frag<T> (&p)[2 * NT]) {
+        reference(x, s, acc);
+        scale_far(x, s);
+        weights(x, s, p);
     }
 };
 
@@ -169,14 +189,55 @@ __device__ __forceinline__ int channel_of(int ks, int half) {
     return DH < 32 ? half * 8 : (ks >> 1) * 32 + half * 16 + (ks & 1) * 8;
 }
 
+// Value rows of a sequence's own block lie position by position, and the second product wants 4 positions of a channel together.  bf16: 32 rows pass
+// through LDS, 64 bytes apart more than they are long (the four positions of a read meet all banks), and come back transposed; fp32: element by element.
+template <typename T, int DH>
+constexpr int own_lds() {
+    return sizeof(T) == 2 ? 32 * (DH * 2 + 64) : 0;
+}
+template <int DH>
+struct OwnValues {
+    static constexpr int ROW = DH * 2 + 64, LPR = DH / 8, RPI = 64 / LPR, N = 32 / RPI;   // bytes of a row, lanes to a row, rows a load
+    uint4 v[N];
+    __device__ __forceinline__ void load(const bf16_t *at, int64_t ld, int left) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int j = i * RPI + lane / LPR;
+            v[i] = *reinterpret_cast<const uint4 *>(at + min(j, left - 1) * ld + lane % LPR * 8);
+            if (j >= left) v[i] = make_uint4(0, 0, 0, 0);   // (their probabilities are 0, but 0 x NaN is NaN)
+        }
+    }
+    __device__ __forceinline__ void put(unsigned char *lds) const {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<uint4 *>(lds + (i * RPI + lane / LPR) * ROW + lane % LPR * 16) = v[i];
+    }
+    // positions 16 kg + 8 b + 4 half + (0 .. 3), channel 32 ct + lane % 32: every 16 lanes read 4 rows of 16 channels
+    static __device__ __forceinline__ void read(const unsigned char *lds, int kg, int ct, Frag<bf16_t> &f) {
+        typedef short short4_t __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) short4_t lds_short4;
+        const int lane = threadIdx.x & 63, row = 16 * kg + 4 * (lane >> 5) + (lane >> 2 & 3), c = 32 * ct + (lane & 16) + 4 * (lane & 3);
+        const unsigned char *at = lds + row * ROW + c * 2;
+        const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)at));
+        const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(at + 8 * ROW)));
+        f.v = make_uint4(a.x, a.y, b.x, b.y);
+    }
+};
+
 // 32 rows at most of a sequence's own block, from row k0 of sequence s on: keys and values as the projection leaves them.  mixed: the wavefront
-// has rows of other sequences, which see nothing of it.
-template <typename T, int DH, int CT>
-__device__ __forceinline__ void own_step(const SharedShape &sh, const Kv8Launch &ln, int kvh, int64_t s, int k0, bool mixed, bool sees, float sl2, const Frag<T> (&qf)[DH / 16],
-                                         Softmax &soft, floatx16 (&acc)[CT]) {
+// has rows of other sequences, which see nothing of it.  lds: own_lds bytes of the wavefront's.
+template <typename T, int DH, int CT, typename Q>
+__device__ __forceinline__ void own_step(const SharedShape &sh, const Kv8Launch &ln, int kvh, int64_t s, int k0, bool mixed, bool sees, float sl2, const Q &query,
+                                         Softmax &soft, floatx16 (&acc)[CT], unsigned char *lds) {
     const int lane = threadIdx.x & 63, lrow = lane & 31, half = lane >> 5, left = min(sh.L - k0, 32);
     const T *k = (const T *)ln.k + (s * sh.L + k0 + min(lrow, left - 1)) * ln.ld_k + kvh * DH;
     const T *v = (const T *)ln.v + (s * sh.L + k0) * ln.ld_v + kvh * DH;
+    if constexpr (sizeof(T) == 2) {
+        OwnValues<DH> rows;
+        rows.load(v, ln.ld_v, left);
+        rows.put(lds);
+    }
     floatx16 x[1];
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[0][i] = 0.f;
@@ -184,69 +245,66 @@ __device__ __forceinline__ void own_step(const SharedShape &sh, const Kv8Launch 
     for (int ks = 0; ks < DH / 16; ++ks) {
         Frag<T> kf;
         kf.load(k + channel_of<DH>(ks, half));
-        product(kf, qf[ks], x[0]);
+        product(kf, query(ks), x[0]);
     }
-    // a lane's channel of 8 positions, one by one: they lie in rows of their own
-    Frag<T> vf[2][CT];
-#pragma unroll
-    for (int kg = 0; kg < 2; ++kg)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            const T *at = v + (CT * 32 > DH ? min(lrow, DH - 1) : ct * 32 + lrow);
-            T e[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int j = kg * 16 + 8 * (i >> 2) + 4 * half + (i & 3);
-                e[i] = at[(int64_t)min(j, left - 1) * ln.ld_v];
-                if (j >= left) e[i] = from_float<T>(0.f);
-            }
-            if constexpr (sizeof(T) == 2) {
-                vf[kg][ct].v = make_uint4(e[0].bits | (uint32_t)e[1].bits << 16, e[2].bits | (uint32_t)e[3].bits << 16, e[4].bits | (uint32_t)e[5].bits << 16,
-                                          e[6].bits | (uint32_t)e[7].bits << 16);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) vf[kg][ct].v[i] = e[i];
-            }
-        }
 #pragma unroll
     for (int i = 0; i < 16; ++i)
         if (8 * (i >> 2) + 4 * half + (i & 3) >= left || !sees) x[0][i] = -INFINITY;
-    const Scale scale[2] = {{sl2, 1.f}, {sl2, 1.f}};
+    Scale scale[2] = {{sl2, 1.f}, {sl2, 1.f}};
     Frag<T> p[2];
     soft.step(x, scale, acc, p);
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int kg = 0; kg < 2; ++kg)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
+            Frag<T> vf;
+            if constexpr (sizeof(T) == 2) {
+                OwnValues<DH>::read(lds, kg, ct, vf);
+            } else {
+                const T *at = v + (CT * 32 > DH ? min(lrow, DH - 1) : ct * 32 + lrow);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int j = kg * 16 + 8 * (i >> 2) + 4 * half + (i & 3);
+                    vf.v[i] = at[(int64_t)min(j, left - 1) * ln.ld_v];
+                    if (j >= left) vf.v[i] = 0.f;
+                }
+            }
             if (!mixed) {
-                product(vf[kg][ct], p[kg], acc[ct]);
+                product(vf, p[kg], acc[ct]);
             } else {   // (rows that do not see the block: their probabilities are 0, but its values may be anything)
                 floatx16 sum = acc[ct];
-                product(vf[kg][ct], p[kg], sum);
+                product(vf, p[kg], sum);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[ct][i] = sees ? sum[i] : acc[ct][i];
             }
         }
+    asm volatile("" ::: "memory");
 }
 
 // A tile of up to 32 rows of a unit and KV head (r_first ..) against the own blocks of their sequences, every W-th step from `first` on
-template <typename T, int DH, int CT>
+template <typename T, int DH, int CT, typename Q>
 __device__ __forceinline__ void own_blocks(const SharedShape &sh, const Kv8Launch &ln, int u, int kvh, int r_first, int rows, int64_t token, int first, int W, float sl2,
-                                           const Frag<T> (&qf)[DH / 16], Softmax &soft, floatx16 (&acc)[CT]) {
+                                           const Q &query, Softmax &soft, floatx16 (&acc)[CT], unsigned char *lds) {
     const int per_seq = sh.L * (sh.n_heads / sh.n_kv_heads), n = (sh.L + 31) / 32;
     const int a = r_first / per_seq, b = (min(r_first + 32, rows) - 1) / per_seq;
     const int mine = (int)(token / sh.L);
     for (int i = first; i < (b - a + 1) * n; i += W) {
         const int s = u * ln.cache.seqs_per_unit + a + i / n;
-        own_step<T, DH, CT>(sh, ln, kvh, s, i % n * 32, a != b, mine == s, sl2, qf, soft, acc);
+        own_step<T, DH, CT>(sh, ln, kvh, s, i % n * 32, a != b, mine == s, sl2, query, soft, acc, lds);
     }
 }
 
 // Few rows: a tile of TR rows against a part of its unit's keys, and the last part against their own blocks too.  The wavefronts deal the keys, 32 at
 // a time, codes straight from memory a step ahead, and merge in LDS in wavefront order.
+template <typename T, int DH>
+constexpr int few_rows_lds() {
+    constexpr int merge = NW * (2 + (DH + 31) / 32 * 16) * 64 * 4, own = NW * own_lds<T, DH>();
+    return merge > own ? merge : own;
+}
 template <typename T, int DH, int FORMAT>
 __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedShape &sh, const Kv8Launch &ln, int u, int kvh, int tile, int split, float sl2,
-                                         float *part /* [wavefront][max, sum, NF values][64 lanes] */) {
+                                         unsigned char *lds /* own values of every wavefront, then [wavefront][max, sum, NF values][64 lanes] */) {
     constexpr int KS = DH / 16, CT = (DH + 31) / 32, NF = CT * 16, KL = DH < 32 ? 1 : DH / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
     const int spu = ln.cache.seqs_per_unit, rows = spu * sh.L * (sh.n_heads / sh.n_kv_heads), r = tile * TR + lrow;
@@ -324,9 +382,13 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
             product(b, p[1], acc[ct]);
         }
     }
-    if (ln.k && split == ln.splits - 1) own_blocks<T, DH, CT>(sh, ln, u, kvh, tile * TR, rows, row.token, (wave - steps) & (NW - 1), NW, sl2, qf, soft, acc);
+    if (ln.k && split == ln.splits - 1)
+        own_blocks<T, DH, CT>(sh, ln, u, kvh, tile * TR, rows, row.token, (wave - steps) & (NW - 1), NW, sl2, [&](int ks) { return qf[ks]; }, soft, acc,
+                              lds + wave * own_lds<T, DH>());
     const float l_run = both_sum(soft.l);   // the halves of a row hold disjoint keys
 
+    __syncthreads();
+    float *part = reinterpret_cast<float *>(lds);
     float *mine = part + wave * (2 + NF) * 64 + lane;
     mine[0] = soft.m;
     mine[64] = l_run;
@@ -366,17 +428,18 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
     }
 }
 
-// Many rows (bf16): a tile of 128 rows, 32 to a wavefront, walks stages of 64 keys.  Each wavefront fetches a quarter of a stage's codes a stage ahead,
-// converts them once for all four and puts them into LDS as the fragments that they are: lane by lane, so neither side has a bank conflict.
+// Many rows (bf16): a tile of 128 rows, 32 to a wavefront, walks stages of 64 keys.  Each wavefront fetches a quarter of a stage's codes, converts it once
+// for all four and puts it into LDS as the fragments that it is: lane by lane, so neither side has a bank conflict.
+// Vector instructions (exponentials, conversions) take longer than the matrix instructions beside them, so the two are kept apart by a stage: the scores of
+// the next stage are computed beside the exponentials of this one, and its codes converted beside this one's second product.
 template <int DH, int FORMAT>
 __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const SharedShape &sh, const Kv8Launch &ln, int u, int kvh, int tile, int split, float sl2,
                                           unsigned char *lds) {
-    constexpr int KS = DH / 16, CT = DH / 32, LOADS = 2 * CT / NW, STAGE = KT * DH * 4;   // loads of keys, and of values, a wavefront; bytes of a stage
+    constexpr int KS = DH / 16, CT = DH / 32, LOADS = 2 * CT / NW, HALF = KT * DH * 2;   // loads of keys, and of values, a wavefront; bytes of a stage's keys
     static_assert(2 * CT % NW == 0, "the wavefronts take equal shares of a stage");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lrow = lane & 31, half = lane >> 5;
     const int spu = ln.cache.seqs_per_unit, rows = spu * sh.L * (sh.n_heads / sh.n_kv_heads), r_first = tile * MT + wave * 32, r = r_first + lrow;
-    const RowOf row(sh, (int64_t)u * spu, kvh, min(r, rows - 1));
-    const bool any_rows = r_first < rows;
+    const RowOf row(sh, (int64_t)u * spu, kvh, min(r, rows - 1));   // (rows past the last repeat it and store nothing)
     const Head head(ln.cache, u, kvh);
     const int begin = (int)min((int64_t)split * ln.chunk, (int64_t)head.keys), end = (int)min((int64_t)begin + ln.chunk, (int64_t)head.keys);
     const int t0 = begin / KV8_TILE, stages = (end - begin + KT - 1) / KT, t_last = (end - 1) / KV8_TILE;
@@ -391,40 +454,36 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
     Softmax soft;
     uint4 kc[LOADS], vc[LOADS];
     float2 sc;
-    auto load = [&](int st) {   // (a tile behind the part's last is that one again: its positions are hidden)
+    unsigned char *mine = lds + lane * 16;
+    // (a tile behind the part's last is that one again: its positions are hidden, and stages behind the last are never used)
+    auto load = [&](uint4 (&to)[LOADS], int st, int which) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int n = wave * LOADS + i;
-            const uint8_t *at = head.codes + (int64_t)min(t0 + 2 * st + n / CT, t_last) * (64 * DH) + n % CT * 1024 + lane * 16;
-            kc[i] = *reinterpret_cast<const uint4 *>(at);
-            vc[i] = *reinterpret_cast<const uint4 *>(at + 32 * DH);
+            to[i] = *reinterpret_cast<const uint4 *>(head.codes + (int64_t)min(t0 + 2 * st + n / CT, t_last) * (64 * DH) + which * (32 * DH) + n % CT * 1024 + lane * 16);
         }
-        sc = head.scale(t0 + 2 * st, lane & 3);
     };
-    if (stages > 0) load(0);
-    for (int st = 0; st < stages; ++st) {
-        unsigned char *at = lds + (st & 1) * STAGE + lane * 16;
-        const int left = end - begin - st * KT;
+    // keys: fragment (tile, step) at tile * KS + step, two a load; values: (tile, channels, 16 positions), likewise
+    auto put = [&](const uint4 (&from)[LOADS], int st, int which) {
+        unsigned char *at = mine + which * (2 * HALF) + (st & 1) * HALF;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int n = wave * LOADS + i;   // keys: fragment (tile, step) at tile * KS + step, two a load; values: (tile, channels, 16 positions) behind them
+            const int n = wave * LOADS + i;
             Frag<bf16_t> a, b;
-            convert<FORMAT>(kc[i], a, b);
+            convert<FORMAT>(from[i], a, b);
             *reinterpret_cast<uint4 *>(at + (2 * n) * 1024) = a.v;
             *reinterpret_cast<uint4 *>(at + (2 * n + 1) * 1024) = b.v;
-            convert<FORMAT>(left < KT ? keep(vc[i], left - n / CT * 32 - 4 * half) : vc[i], a, b);
-            *reinterpret_cast<uint4 *>(at + (2 * KS + 2 * n) * 1024) = a.v;
-            *reinterpret_cast<uint4 *>(at + (2 * KS + 2 * n + 1) * 1024) = b.v;
         }
-        Scale scale[4];
+    };
+    auto hide_values = [&](int st) {   // in the codes that have been loaded for stage st
+        const int left = end - begin - st * KT;
+        if (FORMAT == PSD_KV8_E4M3 && left < KT) {   // (whole numbers are no NaN)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            scale[g] = {__int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.x), g)) * sl2, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), g))};
-        if (st + 1 < stages) load(st + 1);
-        // The stage is whole.  (The one before it is read until this point, the next goes to where that was.)
-        __syncthreads();
-        if (!any_rows) continue;
-        floatx16 x[2];
+            for (int i = 0; i < LOADS; ++i) vc[i] = keep(vc[i], left - (wave * LOADS + i) / CT * 32 - 4 * half);
+        }
+    };
+    auto scores = [&](floatx16 (&x)[2], int st) {
+        const unsigned char *at = mine + (st & 1) * HALF;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -437,19 +496,100 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
                 kf.v = *reinterpret_cast<const uint4 *>(at + (kt * KS + ks) * 1024);
                 product(kf, qf[ks], x[kt]);
             }
-        if (left < KT) hide(x, scale, left, half);
-        Frag<bf16_t> p[4];
-        soft.step(x, scale, acc, p);
+    };
+    // what the wavefront put into LDS has arrived, and so has everybody's
+    auto meet = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // Stage st, whose scores are in x.  In LDS: keys of st + 1 and values of st; in registers: codes of the keys of st + 2 and of the values of st + 1.  They go
+    // where the keys of st and the values of st - 1 were, which all wavefronts have read in front of the last meeting.
+    // The order is laid out by hand, in pieces that the compiler keeps apart: two products each, whose fragments were read a piece ahead, beside a part of
+    // the exponentials or the conversion of one fragment.
+    auto stage = [&](int st, floatx16 (&x)[2], floatx16 (&next)[2]) {
+        const unsigned char *ak = mine + ((st + 1) & 1) * HALF, *av = mine + 2 * HALF + (st & 1) * HALF;
+        unsigned char *pk = mine + (st & 1) * HALF, *pv = mine + 2 * HALF + ((st + 1) & 1) * HALF;
+        Frag<bf16_t> f[2][2];
+        auto read = [&](Frag<bf16_t> (&to)[2], const unsigned char *at, int a, int b) {
+            to[0].v = *reinterpret_cast<const uint4 *>(at + a * 1024);
+            to[1].v = *reinterpret_cast<const uint4 *>(at + b * 1024);
+        };
+        read(f[0], ak, 0, KS);
+        Scale scale[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g)
+            scale[g] = {__int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.x), g)) * sl2, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), g))};
+        sc = head.scale(t0 + 2 * (st + 1), lane & 3);
+        const int left = end - begin - st * KT;
+        if (left < KT) hide(x, scale, left, half);
+        hide_values(st + 1);
+        soft.reference(x, scale, acc);
+        soft.scale_far(x, scale);
+        Frag<bf16_t> p[4];
+        float e[32], sum[2] = {0.f, 0.f};
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                Frag<bf16_t> vf;
-                vf.v = *reinterpret_cast<const uint4 *>(at + (2 * KS + ((g >> 1) * CT + ct) * 2 + (g & 1)) * 1024);
-                product(vf, p[g], acc[ct]);
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) next[kt][v] = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            if (ks + 1 < KS) read(f[(ks + 1) & 1], ak, ks + 1, KS + ks + 1);
+            else read(f[(ks + 1) & 1], av, 0, 2);   // (value_at(0), value_at(1))
+            product(f[ks & 1][0], qf[ks], next[0]);
+            product(f[ks & 1][1], qf[ks], next[1]);
+            constexpr int N = 32 / KS;
+#pragma unroll
+            for (int i = ks * N; i < ks * N + N; ++i) {
+                e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 4][i & 15], scale[i >> 3].k, soft.neg));
+                sum[i & 1] += e[i];
+                e[i] *= scale[i >> 3].v;
+                if ((i & 7) == 7) probabilities(e + i - 7, p[i >> 3]);
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        soft.l += sum[0] + sum[1];
+        // product j of the values: 16 positions g = j / CT, channels j % CT, whose fragment is the one at 2 (g / 2 CT + j % CT) + g % 2
+        auto value_at = [](int j) { return ((j / CT >> 1) * CT + j % CT) * 2 + (j / CT & 1); };
+#pragma unroll
+        for (int j = 0; j < 4 * CT; j += 2) {
+            const int i = j / 2, of = i / 2 % LOADS, n = wave * LOADS + of;   // fragment i of the next stages': keys first
+            Frag<bf16_t>(&now)[2] = f[(KS + i) & 1];
+            if (j + 2 < 4 * CT) read(f[(KS + i + 1) & 1], av, value_at(j + 2), value_at(j + 3));
+            product(now[0], p[j / CT], acc[j % CT]);
+            product(now[1], p[(j + 1) / CT], acc[(j + 1) % CT]);
+            const bool keys = i < 2 * LOADS;
+            const uint4 c = keys ? kc[of] : vc[of];
+            *reinterpret_cast<uint4 *>((keys ? pk : pv) + (2 * n + (i & 1)) * 1024) = i & 1 ? convert<FORMAT>(c.z, c.w) : convert<FORMAT>(c.x, c.y);
+            if (i == 2 * LOADS - 1) load(kc, st + 3, 0);
+            if (i == 4 * LOADS - 1) load(vc, st + 2, 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        meet();
+    };
+    if (stages > 0) {
+        floatx16 x[2], y[2];
+        load(kc, 0, 0);
+        load(vc, 0, 1);
+        sc = head.scale(t0, lane & 3);
+        put(kc, 0, 0);
+        load(kc, 1, 0);
+        hide_values(0);
+        put(vc, 0, 1);
+        load(vc, 1, 1);
+        put(kc, 1, 0);
+        load(kc, 2, 0);
+        meet();
+        scores(x, 0);
+        meet();
+        for (int st = 0; st < stages; st += 2) {
+            stage(st, x, y);
+            if (st + 1 < stages) stage(st + 1, y, x);
+        }
     }
-    if (ln.k && split == ln.splits - 1 && any_rows) own_blocks<bf16_t, DH, CT>(sh, ln, u, kvh, r_first, rows, row.token, 0, 1, sl2, qf, soft, acc);
+    if (ln.k && split == ln.splits - 1 && r_first < rows) 
+        own_blocks<bf16_t, DH, CT>(sh, ln, u, kvh, r_first, rows, row.token, 0, 1, sl2, [&](int ks) { return qf[ks]; }, soft, acc, lds + wave * own_lds<bf16_t, DH>());
     const float l_run = both_sum(soft.l);
     if (r >= rows) return;
     const PartOut<bf16_t, DH> to(sh, ln, split, row);
@@ -465,44 +605,78 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
         }
 }
 
-template <typename T, int DH>
+template <typename T, int DH, bool MANY>
 constexpr int attention_lds() {
-    constexpr int merge = NW * (2 + (DH + 31) / 32 * 16) * 64 * 4, stages = sizeof(T) == 2 ? 2 * KT * DH * 4 : 0;
-    return merge > stages ? merge : stages;
+    return MANY ? 2 * KT * DH * 4 : few_rows_lds<T, DH>();
 }
 
 // Workgroups are dealt to the XCDs in runs of equal length, the tiles of one unit, KV head and part behind one another, so that those that read the same
 // keys meet in one L2.
-template <typename T, int DH, int FORMAT>
+template <typename T, int DH, int FORMAT, bool MANY>
 __global__ __launch_bounds__(NW * 64, 2) void attention_kv8_kernel(const T *__restrict__ q, SharedShape sh, Kv8Launch ln, float sl2) {
     extern __shared__ __align__(16) unsigned char lds[];
     const int n = ln.units * sh.n_kv_heads * ln.splits * ln.tiles, run = (n + 7) / 8;
     const int at = (blockIdx.x & 7) * run + (blockIdx.x >> 3);
     if (at >= n) return;
     const int tile = at % ln.tiles, split = at / ln.tiles % ln.splits, kvh = at / ln.tiles / ln.splits % sh.n_kv_heads, u = at / ln.tiles / ln.splits / sh.n_kv_heads;
-    if constexpr (sizeof(T) == 2) {
-        if (ln.tiled) {
-            many_rows<DH, FORMAT>(q, sh, ln, u, kvh, tile, split, sl2, lds);
-            return;
-        }
-    }
-    few_rows<T, DH, FORMAT>(q, sh, ln, u, kvh, tile, split, sl2, reinterpret_cast<float *>(lds));
+    if constexpr (MANY) many_rows<DH, FORMAT>(q, sh, ln, u, kvh, tile, split, sl2, lds);
+    else few_rows<T, DH, FORMAT>(q, sh, ln, u, kvh, tile, split, sl2, lds);
 }
 
 int64_t workgroups(const SharedShape &sh, const Kv8Launch &ln) { return (int64_t)ln.units * sh.n_kv_heads * ln.splits * ln.tiles; }
 
-template <typename T, int DH, int FORMAT>
+template <typename T, int DH, int FORMAT, bool MANY>
 void run(const T *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st) {
-    constexpr int smem = attention_lds<T, DH>();
-    auto kern = attention_kv8_kernel<T, DH, FORMAT>;
+    constexpr int smem = attention_lds<T, DH, MANY>();
+    auto kern = attention_kv8_kernel<T, DH, FORMAT, MANY>;
     static std::atomic<uint64_t> lds_raised{0};   // one per instantiation
     ensure_dynamic_lds(reinterpret_cast<const void *>(kern), smem, lds_raised);
     hipLaunchKernelGGL(kern, dim3((unsigned)align_up(workgroups(sh, ln), 8)), dim3(NW * 64), smem, st, q, sh, ln, LOG2E / sqrtf((float)DH));
 }
 template <typename T, int DH>
 void run(const T *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st) {
-    if (ln.cache.format == PSD_KV8_INT8) run<T, DH, PSD_KV8_INT8>(q, sh, ln, st);
-    else run<T, DH, PSD_KV8_E4M3>(q, sh, ln, st);
+    const bool int8 = ln.cache.format == PSD_KV8_INT8;
+    if constexpr (sizeof(T) == 2) {
+        if (ln.tiled) {
+            if (int8) run<T, DH, PSD_KV8_INT8, true>(q, sh, ln, st);
+            else run<T, DH, PSD_KV8_E4M3, true>(q, sh, ln, st);
+            return;
+        }
+    }
+    if (int8) run<T, DH, PSD_KV8_INT8, false>(q, sh, ln, st);
+    else run<T, DH, PSD_KV8_E4M3, false>(q, sh, ln, st);
+}
+
+// Both forms and every number of parts priced, in us (what the sizes below took on this card, heads of 128 unless it says otherwise):
+//   a workgroup alone on a CU  few rows: 0.93 for 128 keys (32768 keys of 4 requests, 16 workgroups), 0.55 with heads of 64, 2.7 in fp32 with heads of 64;
+//                              many rows: 1.36 for 64 keys (2000 keys, 8 drafts of 64 rows)
+//   two and more               few rows: 0.88 a workgroup, 0.75 with e4m3, whose conversion is shorter (one unit of 512 rows a KV head; 4 of 1344); many rows: 1.25
+//   fixed                      4.5 for the call, 2 or 5 for a workgroup, 4 for the join
+//   memory                     5.7 TB/s (32 caches of 16384 keys: 94 us)
+// and units of lengths of their own, which are taken to be about half full, by how long the last of them runs.
+struct Price {
+    double us;
+    int tiles, splits, each;
+};
+Price price(const SharedShape &sh, const Kv8 &c, bool own_rows, bool many, int units) {
+    const bool fp32 = sh.dtype == PSD_DTYPE_FP32;
+    const int64_t rows = (int64_t)c.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads);
+    const int rows_of_tile = many ? MT : TR, keys = many ? KT : KV8_TILE * NW, steps = (int)((c.len + (int64_t)keys - 1) / keys);
+    const double size = sh.d_head / 128.0, step = fp32 ? 5.4 * size : many ? 1.36 * size : 0.93 * pow(size, 0.75);
+    const double shared = fp32 ? step : many ? 1.25 * size : (c.format == PSD_KV8_E4M3 ? 0.75 : 0.88) * pow(size, 0.75);
+    const double fixed = many ? 5.0 : 2.0, full = c.lens ? 0.55 : 1.0;
+    const double own = own_rows ? (sh.L + 31) / 32 * (many ? 0.7 : 0.35) * step : 0.0;
+    const double memory = (double)units * sh.n_kv_heads * c.len * sh.d_head * 2 * full / 5.7e6, join_part = (double)sh.n_rows * sh.d_head * 8 / 4e6;
+    Price best = {-1.0, (int)((rows + rows_of_tile - 1) / rows_of_tile), 1, std::max(steps, 1)};
+    const double base = (double)units * sh.n_kv_heads * best.tiles;
+    // (up to as many parts as give the CUs eight workgroups each, no more than 256 MB of them but for one, every eighth of many: this is host time of every call)
+    for (int n = 1; n <= std::max(1, steps) && (n == 1 || (base * n <= 2048.0 && (double)n * sh.n_rows * sh.d_head * 4 <= 256e6)); n += 1 + n / 8) {
+        const int each = std::max((steps + n - 1) / n, 1), splits = std::max((steps + each - 1) / each, 1);
+        const double work = base * splits * ((each * shared * full) + fixed * 0.8) / 256.0, alone = each * step + fixed;
+        const double us = 4.5 + std::max(std::max(alone, work), memory) + (c.lens ? 0.3 * each * step : 0.0) + own + (splits > 1 ? 4.0 + splits * join_part : 0.0);
+        if (best.us < 0.0 || us < best.us) best.us = us, best.splits = splits, best.each = each;
+    }
+    return best;
 }
 
 }   // namespace
@@ -511,19 +685,18 @@ bool plan_attention_kv8(const SharedShape &sh, const Kv8 &cache, bool own_rows, 
     Kv8Launch ln;
     ln.cache = cache;
     ln.units = sh.S / cache.seqs_per_unit;
-    const int64_t rows = (int64_t)cache.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads);
-    ln.tiled = sh.dtype == PSD_DTYPE_BF16 && rows >= 64;
-    const int rows_of_tile = ln.tiled ? MT : TR, step = ln.tiled ? KT : KV8_TILE * NW;
-    ln.tiles = (int)((rows + rows_of_tile - 1) / rows_of_tile);
-    const double base = (double)ln.units * sh.n_kv_heads * ln.tiles;
-    const int steps = (cache.len + step - 1) / step;
-    const int want = (int)std::max(1.0, std::min(std::ceil(512.0 / base), steps / 4.0));
-    const int each = std::max(1, (steps + want - 1) / want);
-    ln.chunk = each * step;
-    ln.splits = std::max(1, (steps + each - 1) / each);
+    Price p = price(sh, cache, own_rows, false, ln.units);
+    if (sh.dtype == PSD_DTYPE_BF16) {
+        const Price many = price(sh, cache, own_rows, true, ln.units);
+        if (many.us < p.us) p = many, ln.tiled = 1;
+    }
+    ln.tiles = p.tiles;
+    ln.splits = p.splits;
+    ln.chunk = p.each * (ln.tiled ? KT : KV8_TILE * NW);
     ln.parts = ln.splits > 1 ? ln.splits : 0;
     *out = ln;
-    return base * ln.splits < 0x1p31 && launchable(align_up(workgroups(sh, ln), 8), NW * 64) && (ln.parts == 0 || attention_join_launchable(sh, ln));
+    return (double)ln.units * sh.n_kv_heads * ln.tiles * ln.splits < 0x1p31 && launchable(align_up(workgroups(sh, ln), 8), NW * 64) &&
+           (ln.parts == 0 || attention_join_launchable(sh, ln));
 }
 
 void launch_attention_kv8(const void *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st) {
