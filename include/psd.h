@@ -533,11 +533,14 @@ int32_t psd_kv8_load(const psd_kv8_cache *cache, int32_t units, int32_t first, i
  *   0, then codes and scales may be NULL with capacity 0).  Codes are used as they are: a key's scale multiplies its score, a value's its probability, which with
  *   bf16 is rounded after that.  Sums and statistics are fp32.  ws: device, 256-byte aligned, psd_attention_kv8_bytes of the same shape and cache (own_rows: 1
  *   where k is set; it does not look at device memory); calls that overlap need one each.
- * psd_debug_attention_kv8_plan: form (0: tiles of 32 rows, 1: of 128), tiles of rows of a unit and KV head, parts of the keys, keys of a part. */
+ * psd_debug_attention_kv8_plan: form (0: tiles of 32 rows, 1: of 128), tiles of rows of a unit and KV head, parts of the keys, keys of a part.
+ * psd_debug_force_attention_kv8: the form (-1: by price; fp32 has form 0 only) and the parts (0: by price; cut to what there is) of the calls that
+ *   follow, workspaces included.  Process-wide. */
 int64_t psd_attention_kv8_bytes(const psd_attention_shape *shape, const psd_kv8_cache *cache, int32_t own_rows);
 int32_t psd_attention_kv8(const psd_attention_shape *shape, const void *q, const psd_kv8_cache *cache, const void *k, const void *v, int64_t ld_k,
                           int64_t ld_v, void *out, float *lse, void *ws, int64_t ws_bytes, void *stream);
 int32_t psd_debug_attention_kv8_plan(const psd_attention_shape *shape, const psd_kv8_cache *cache, int32_t own_rows, int32_t *plan);
+int32_t psd_debug_force_attention_kv8(int32_t form, int32_t parts);
 
 /* ---- Approximate KV cache for fully bidirectional models -----------------------------------------
  * Sec. 3.2 stage 3 notes that KV-cache sharing can cut redundant computation; with bidirectional

@@ -205,6 +205,7 @@ def load_library():
         "psd_kv8_load": (i32, [vp, i32, i32, i32, vp, vp, i64, i64, i32, vp]),
         "psd_attention_kv8_bytes": (i64, [vp, vp, i32]),
         "psd_attention_kv8": (i32, [vp, vp, vp, vp, vp, i64, i64, vp, vp, vp, i64, vp]),
+        "psd_debug_force_attention_kv8": (i32, [i32, i32]),
         "psd_debug_attention_kv8_plan": (i32, [vp, vp, i32, C.POINTER(i32)]),
     }
     for name, (res, args) in sig.items():

@@ -270,6 +270,12 @@ int32_t psd_debug_attention_kv8_plan(const psd_attention_shape *shape, const psd
     return PSD_OK;
 }
 
+int32_t psd_debug_force_attention_kv8(int32_t form, int32_t parts) {
+    if (form < -1 || form > 1 || parts < 0) PSD_FAIL(PSD_ERR_INVALID_ARG, "form %d, %d parts", form, parts);
+    force_attention_kv8(form, parts);
+    return PSD_OK;
+}
+
 int32_t psd_attention_kv8(const psd_attention_shape *shape, const void *q, const psd_kv8_cache *cache, const void *k, const void *v, int64_t ld_k, int64_t ld_v, void *out,
                           float *lse, void *ws, int64_t ws_bytes, void *stream) {
     SharedShape sh;

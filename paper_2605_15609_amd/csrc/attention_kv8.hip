@@ -654,6 +654,8 @@ void run(const T *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st)
 //   fixed                      4.5 for the call, 2 or 5 for a workgroup, 4 for the join
 //   memory                     5.7 TB/s (32 caches of 16384 keys: 94 us)
 // and units of lengths of their own, which are taken to be about half full, by how long the last of them runs.
+std::atomic<int> forced_form{-1}, forced_parts{0};
+
 struct Price {
     double us;
     int tiles, splits, each;
@@ -670,6 +672,12 @@ Price price(const SharedShape &sh, const Kv8 &c, bool own_rows, bool many, int u
     Price best = {-1.0, (int)((rows + rows_of_tile - 1) / rows_of_tile), 1, std::max(steps, 1)};
     const double base = (double)units * sh.n_kv_heads * best.tiles;
     // (up to as many parts as give the CUs eight workgroups each, no more than 256 MB of them but for one, every eighth of many: this is host time of every call)
+    if (const int parts = std::min(forced_parts.load(), std::max(steps, 1))) {
+        best.each = (steps + parts - 1) / parts;
+        best.splits = std::max(1, (steps + std::max(best.each, 1) - 1) / std::max(best.each, 1));
+        best.us = 0.0;
+        return best;
+    }
     for (int n = 1; n <= std::max(1, steps) && (n == 1 || (base * n <= 2048.0 && (double)n * sh.n_rows * sh.d_head * 4 <= 256e6)); n += 1 + n / 8) {
         const int each = std::max((steps + n - 1) / n, 1), splits = std::max((steps + each - 1) / each, 1);
         const double work = base * splits * ((each * shared * full) + fixed * 0.8) / 256.0, alone = each * step + fixed;
@@ -681,18 +689,24 @@ Price price(const SharedShape &sh, const Kv8 &c, bool own_rows, bool many, int u
 
 }   // namespace
 
+void force_attention_kv8(int form, int parts) {
+    forced_form = form;
+    forced_parts = parts;
+}
+
 bool plan_attention_kv8(const SharedShape &sh, const Kv8 &cache, bool own_rows, Kv8Launch *out) {
     Kv8Launch ln;
     ln.cache = cache;
     ln.units = sh.S / cache.seqs_per_unit;
     Price p = price(sh, cache, own_rows, false, ln.units);
-    if (sh.dtype == PSD_DTYPE_BF16) {
+    const int form = forced_form;
+    if (sh.dtype == PSD_DTYPE_BF16 && form != 0) {
         const Price many = price(sh, cache, own_rows, true, ln.units);
-        if (many.us < p.us) p = many, ln.tiled = 1;
+        if (form == 1 || many.us < p.us) p = many, ln.tiled = 1;
     }
     ln.tiles = p.tiles;
     ln.splits = p.splits;
-    ln.chunk = p.each * (ln.tiled ? KT : KV8_TILE * NW);
+    ln.chunk = std::max(p.each, 1) * (ln.tiled ? KT : KV8_TILE * NW);
     ln.parts = ln.splits > 1 ? ln.splits : 0;
     *out = ln;
     return (double)ln.units * sh.n_kv_heads * ln.tiles * ln.splits < 0x1p31 && launchable(align_up(workgroups(sh, ln), 8), NW * 64) &&

@@ -515,6 +515,7 @@ struct Kv8Launch : AttentionParts {
     int64_t ld_k = 0, ld_v = 0;
     int units = 0, tiled = 0, tiles = 0, splits = 1, chunk = 0;   // tiles of rows of a unit and KV head, parts of `chunk` keys
 };
+void force_attention_kv8(int form, int parts);   // debug, process-wide
 bool plan_attention_kv8(const SharedShape &sh, const Kv8 &cache, bool own_rows, Kv8Launch *out);
 void launch_attention_kv8(const void *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st);
 // lm_head.hip (bf16): LM-head fused with the online top-1 / sum-exp reduction

@@ -138,6 +138,14 @@ def test_token_by_token_is_the_same_as_rules_say():
 
 
 # ----------------------------------------------------------------------------------------------------------- attention
+@pytest.fixture
+def forced():
+    """Forces the form and the parts of the calls of a test."""
+    lib = psd.load_library()
+    yield lambda form, parts=0: B._check(lib.psd_debug_force_attention_kv8(form, parts))
+    lib.psd_debug_force_attention_kv8(-1, 0)
+
+
 def run_attention(dtype, H, Hkv, d, S, L, per, positions, block, fmt, lens, own, pad=0, seed=0, scale=1.5):
     g = torch.Generator().manual_seed(seed)
     q = (scale * torch.randn((S, L, H, d), generator=g)).to(dtype)
@@ -171,18 +179,18 @@ def run_attention(dtype, H, Hkv, d, S, L, per, positions, block, fmt, lens, own,
     (F32, 4, 2, 32, 4, 3, 2, 65, 32, [65, 1], True, 0),
     (F32, 8, 8, 64, 3, 16, 1, 410, 64, [410, 3, 64], True, 0),
     (F32, 2, 1, 128, 2, 64, 1, 900, 32, None, True, 0)])                    # parts in fp32
-def test_attention_against_64_bits(fmt, dtype, H, Hkv, d, S, L, per, positions, block, lens, own, pad):
-    run_attention(dtype, H, Hkv, d, S, L, per, positions, block, fmt, lens, own, pad, seed=positions + L)
+def test_attention_against_64_bits(forced, fmt, dtype, H, Hkv, d, S, L, per, positions, block, lens, own, pad):
+    for form in (-1, 0, 1) if dtype == BF else (-1,):
+        for parts in (0, 3) if form >= 0 else (0,):
+            forced(form, parts)
+            plan = run_attention(dtype, H, Hkv, d, S, L, per, positions, block, fmt, lens, own, pad, seed=positions + L)
+            assert form < 0 or plan[0] == form
+            assert parts == 0 or plan[2] == min(parts, -(-(positions or 1) // (64 if form else 128))) or plan[2] == 2
 
 
-def test_the_forms_are_what_they_are_said_to_be():
-    assert run_attention(BF, 28, 4, 128, 2, 1, 1, 5000, 32, "int8", None, True)[0] == 0
-    few = run_attention(BF, 2, 2, 64, 1, 1, 1, 8192, 32, "int8", None, True)
-    many = run_attention(BF, 8, 1, 64, 1, 64, 1, 8192, 32, "e4m3", None, True)
-    assert few[0] == 0 and few[2] > 1 and many[0] == 1 and many[2] > 1
-
-
-def test_a_unit_without_a_position_gives_zeros():
+@pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
+def test_a_unit_without_a_position_gives_zeros(forced, form, parts):
+    forced(form, parts)
     host = Cache(2, 2, 64, 64, 32, "int8", lens=[0, 64])
     q = torch.randn((2, 3, 4, 64)).to(BF).to(DEV)
     lse = torch.empty((2, 3, 4), device=DEV)
@@ -194,8 +202,10 @@ def test_a_unit_without_a_position_gives_zeros():
 
 
 @pytest.mark.parametrize("L,group", [(1, 1), (5, 3), (16, 2), (64, 4)])
-def test_a_draft_without_a_value_leaves_the_others_alone(L, group):
+@pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
+def test_a_draft_without_a_value_leaves_the_others_alone(forced, form, parts, L, group):
     """Sequences that share a cache: NaN in one's own block reaches none of the others, whatever tile their rows share."""
+    forced(form, parts)
     S, H, Hkv, d = 6, group, 1, 64
     g = torch.Generator().manual_seed(L)
     q, host = torch.randn((S, L, H, d), generator=g).to(BF).to(DEV), Cache(2, Hkv, d, 45, 32, "e4m3")
@@ -212,7 +222,9 @@ def test_a_draft_without_a_value_leaves_the_others_alone(L, group):
         assert torch.isnan(got[1]).all() and not torch.isfinite(got[4][..., 7]).any() and torch.isfinite(got[4][..., 8]).all()
 
 
-def test_a_cache_block_without_a_value_reaches_who_sees_it():
+@pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
+def test_a_cache_block_without_a_value_reaches_who_sees_it(forced, form, parts):
+    forced(form, parts)
     host = Cache(2, 1, 64, 100, 32, "int8")
     host.scales[1, 0, 1, 0] = np.nan
     q = torch.randn((2, 2, 2, 64)).to(BF).to(DEV)
@@ -222,8 +234,10 @@ def test_a_cache_block_without_a_value_reaches_who_sees_it():
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 @pytest.mark.parametrize("L", [4, 64])
-def test_scores_of_any_size(fmt, L):
+@pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
+def test_scores_of_any_size(forced, form, parts, fmt, L):
     """Keys of the same code at scales that make scores up to 2^30: the largest ones share the weight, none of the sums overflows."""
+    forced(form, parts)
     d, n = 64, 160
     host = Cache(1, 1, d, n, 32, fmt)
     for exponent in (4, 12, 20, 24):
@@ -245,8 +259,10 @@ def test_scores_of_any_size(fmt, L):
             near(lse[0, :, 0], np.full(L, x + np.log(len(top))), np.full(L, 5 * 2.0 ** -24 * abs(x) + 2.0 ** -20), "lse")
 
 
-def test_zero_scales_hide_nothing():
+@pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
+def test_zero_scales_hide_nothing(forced, form, parts):
     """A block of zeros has a scale of 0: its positions still draw weight, also in a unit's last tile."""
+    forced(form, parts)
     host = Cache(1, 1, 64, 50, 16, "int8")
     host.scales[0, 0, 1:] = 0.0
     q = torch.randn((1, 2, 2, 64), generator=torch.Generator().manual_seed(1)).to(BF)
@@ -257,7 +273,9 @@ def test_zero_scales_hide_nothing():
     near(lse, want["lse"], want["lse_tol"], "lse")
 
 
-def test_a_row_does_not_depend_on_what_other_sequences_hold():
+@pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
+def test_a_row_does_not_depend_on_what_other_sequences_hold(forced, form, parts):
+    forced(form, parts)
     g = torch.Generator().manual_seed(4)
     q, k, v = (torch.randn((4, 3, n, 64), generator=g).to(BF).to(DEV) for n in (4, 2, 2))
     host = Cache(2, 2, 64, 200, 32, "int8")

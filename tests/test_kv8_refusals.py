@@ -171,6 +171,30 @@ def test_calls_check_pointers_before_anything_runs(lib):
         refused(lib, attend(lib, **change), "lies on")
 
 
+def test_forms_that_there_are_not(lib):
+    for form, parts in ((-2, 0), (2, 0), (0, -1)):
+        refused(lib, lib.psd_debug_force_attention_kv8(form, parts))
+    try:
+        plan, sh = (C.c_int32 * 4)(), shape(S=4, L=16)
+        for form in (0, 1):
+            for parts in (1, 2, 100):
+                assert lib.psd_debug_force_attention_kv8(form, parts) == 0
+                assert lib.psd_debug_attention_kv8_plan(C.byref(sh), C.byref(cache(seqs_per_unit=4)), 1, plan) == 0
+                assert plan[0] == form and plan[1] == (2 if form else 8) and plan[2] == min(parts, 2 if form else 1) and plan[2] * plan[3] >= 100
+    finally:
+        assert lib.psd_debug_force_attention_kv8(-1, 0) == 0
+    refused(lib, lib.psd_debug_attention_kv8_plan(C.byref(sh), C.byref(cache(seqs_per_unit=4)), 1, None))
+
+
+def test_a_large_batch_takes_tiles_of_128_rows_and_a_small_one_of_32(lib):
+    heads = dict(n_heads=32, n_kv_heads=32, d_head=128, ld_q=4096, ld_out=4096)
+    for S, L, n, per, want in ((128, 64, 5120, 8, (1, 4, 1)), (16, 32, 1312, 1, (0, 1, 1)), (1, 1, 4096, 1, (0, 1, 8))):
+        plan = (C.c_int32 * 4)()
+        c = cache(n_kv_heads=32, d_head=128, capacity=n, len=n, stride_codes=n * 8192, stride_scales=n * 2, scales=1 << 50, seqs_per_unit=per)
+        assert lib.psd_debug_attention_kv8_plan(C.byref(shape(S=S, L=L, **heads)), C.byref(c), 1, plan) == 0
+        assert tuple(plan[:3]) == want and plan[2] * plan[3] >= n
+
+
 def test_the_workspace_is_checked(lib):
     long = dict(capacity=1 << 20, len=1 << 20, stride_codes=1 << 33, stride_scales=1 << 30)
     need = lib.psd_attention_kv8_bytes(C.byref(shape()), C.byref(cache(**long)), 1)
