@@ -112,19 +112,20 @@ struct Softmax {
                 for (int v = 0; v < 16; ++v) acc[ct][v] *= alpha;
         }
     }
-    // (the last words of reference(): scores scaled and rounded, scales of 1)
+    // (the last words of reference(): of a row that is far, scores scaled and rounded, scales of 1)
     template <int NT>
     __device__ __forceinline__ void scale_far(floatx16 (&x)[NT], Scale (&s)[2 * NT]) const {
         if (!far) return;
+        const bool row = fabsf(neg) > FAR;
 #pragma unroll
         for (int g = 0; g < 2 * NT; ++g) {
 #pragma unroll
             for (int v = 0; v < 8; ++v) {
                 float scaled = x[g >> 1][8 * (g & 1) + v] * s[g].k;
                 asm volatile("" : "+v"(scaled));   // (rounded: contracted into what follows it would not be)
-                x[g >> 1][8 * (g & 1) + v] = scaled;
+                x[g >> 1][8 * (g & 1) + v] = row ? scaled : x[g >> 1][8 * (g & 1) + v];
             }
-            s[g].k = 1.f;
+            s[g].k = row ? 1.f : s[g].k;
         }
     }
     // Scores into probabilities times value scales, 8 at a time as the second product takes them.
@@ -610,20 +611,19 @@ constexpr int attention_lds() {
     return MANY ? 2 * KT * DH * 4 : few_rows_lds<T, DH>();
 }
 
-// Workgroups are dealt to the XCDs in runs of equal length, the tiles of one unit, KV head and part behind one another, so that those that read the same
-// keys meet in one L2.
+// Every (unit, KV head, part) is dealt to an XCD, one after the other, with all of its tiles: those that read the same keys meet in one L2.  Parts are turned by
+// one from one unit and head to the next, so that no XCD has only first parts, which every unit fills, and another only last ones.
 template <typename T, int DH, int FORMAT, bool MANY>
 __global__ __launch_bounds__(NW * 64, 2) void attention_kv8_kernel(const T *__restrict__ q, SharedShape sh, Kv8Launch ln, float sl2) {
     extern __shared__ __align__(16) unsigned char lds[];
-    const int n = ln.units * sh.n_kv_heads * ln.splits * ln.tiles, run = (n + 7) / 8;
-    const int at = (blockIdx.x & 7) * run + (blockIdx.x >> 3);
-    if (at >= n) return;
-    const int tile = at % ln.tiles, split = at / ln.tiles % ln.splits, kvh = at / ln.tiles / ln.splits % sh.n_kv_heads, u = at / ln.tiles / ln.splits / sh.n_kv_heads;
+    const int tile = (int)(blockIdx.x >> 3) % ln.tiles, of = (int)(blockIdx.x >> 3) / ln.tiles * 8 + (int)(blockIdx.x & 7);
+    if (of >= ln.units * sh.n_kv_heads * ln.splits) return;
+    const int head = of / ln.splits, split = (of % ln.splits + head % ln.splits) % ln.splits, kvh = head % sh.n_kv_heads, u = head / sh.n_kv_heads;
     if constexpr (MANY) many_rows<DH, FORMAT>(q, sh, ln, u, kvh, tile, split, sl2, lds);
     else few_rows<T, DH, FORMAT>(q, sh, ln, u, kvh, tile, split, sl2, lds);
 }
 
-int64_t workgroups(const SharedShape &sh, const Kv8Launch &ln) { return (int64_t)ln.units * sh.n_kv_heads * ln.splits * ln.tiles; }
+int64_t workgroups(const SharedShape &sh, const Kv8Launch &ln) { return align_up((int64_t)ln.units * sh.n_kv_heads * ln.splits, 8) * ln.tiles; }
 
 template <typename T, int DH, int FORMAT, bool MANY>
 void run(const T *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st) {
@@ -631,7 +631,7 @@ void run(const T *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st)
     auto kern = attention_kv8_kernel<T, DH, FORMAT, MANY>;
     static std::atomic<uint64_t> lds_raised{0};   // one per instantiation
     ensure_dynamic_lds(reinterpret_cast<const void *>(kern), smem, lds_raised);
-    hipLaunchKernelGGL(kern, dim3((unsigned)align_up(workgroups(sh, ln), 8)), dim3(NW * 64), smem, st, q, sh, ln, LOG2E / sqrtf((float)DH));
+    hipLaunchKernelGGL(kern, dim3((unsigned)workgroups(sh, ln)), dim3(NW * 64), smem, st, q, sh, ln, LOG2E / sqrtf((float)DH));
 }
 template <typename T, int DH>
 void run(const T *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st) {
@@ -664,8 +664,8 @@ Price price(const SharedShape &sh, const Kv8 &c, bool own_rows, bool many, int u
     const bool fp32 = sh.dtype == PSD_DTYPE_FP32;
     const int64_t rows = (int64_t)c.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads);
     const int rows_of_tile = many ? MT : TR, keys = many ? KT : KV8_TILE * NW, steps = (int)((c.len + (int64_t)keys - 1) / keys);
-    const double size = sh.d_head / 128.0, step = fp32 ? 5.4 * size : many ? 1.36 * size : 0.93 * pow(size, 0.75);
-    const double shared = fp32 ? step : many ? 1.25 * size : (c.format == PSD_KV8_E4M3 ? 0.75 : 0.88) * pow(size, 0.75);
+    const double size = sh.d_head / 128.0, power = sqrt(size) * sqrt(sqrt(size)), step = fp32 ? 5.4 * size : many ? 1.36 * size : 0.93 * power;
+    const double shared = fp32 ? step : many ? 1.25 * size : (c.format == PSD_KV8_E4M3 ? 0.75 : 0.88) * power;
     const double fixed = many ? 5.0 : 2.0, full = c.lens ? 0.55 : 1.0;
     const double own = own_rows ? (sh.L + 31) / 32 * (many ? 0.7 : 0.35) * step : 0.0;
     const double memory = (double)units * sh.n_kv_heads * c.len * sh.d_head * 2 * full / 5.7e6, join_part = (double)sh.n_rows * sh.d_head * 8 / 4e6;
@@ -680,9 +680,12 @@ Price price(const SharedShape &sh, const Kv8 &c, bool own_rows, bool many, int u
     }
     for (int n = 1; n <= std::max(1, steps) && (n == 1 || (base * n <= 2048.0 && (double)n * sh.n_rows * sh.d_head * 4 <= 256e6)); n += 1 + n / 8) {
         const int each = std::max((steps + n - 1) / n, 1), splits = std::max((steps + each - 1) / each, 1);
-        const double work = base * splits * ((each * shared * full) + fixed * 0.8) / 256.0, alone = each * step + fixed;
+        // (a CU with one workgroup more than the others is the last; units of lengths of their own even that out)
+        const double wgs = c.lens ? base * splits / 256.0 : ceil(base * splits / 256.0);
+        const double work = wgs * (each * shared * full + fixed * 0.8), alone = each * step + fixed;
         const double us = 4.5 + std::max(std::max(alone, work), memory) + (c.lens ? 0.3 * each * step : 0.0) + own + (splits > 1 ? 4.0 + splits * join_part : 0.0);
         if (best.us < 0.0 || us < best.us) best.us = us, best.splits = splits, best.each = each;
+        if (steps * step < 4.0 + step) break;   // (less than a join takes)
     }
     return best;
 }
@@ -700,7 +703,7 @@ bool plan_attention_kv8(const SharedShape &sh, const Kv8 &cache, bool own_rows, 
     ln.units = sh.S / cache.seqs_per_unit;
     Price p = price(sh, cache, own_rows, false, ln.units);
     const int form = forced_form;
-    if (sh.dtype == PSD_DTYPE_BF16 && form != 0) {
+    if (sh.dtype == PSD_DTYPE_BF16 && (form == 1 || (form < 0 && (int64_t)cache.seqs_per_unit * sh.L * (sh.n_heads / sh.n_kv_heads) > MT / 2))) {
         const Price many = price(sh, cache, own_rows, true, ln.units);
         if (form == 1 || many.us < p.us) p = many, ln.tiled = 1;
     }
@@ -709,7 +712,7 @@ bool plan_attention_kv8(const SharedShape &sh, const Kv8 &cache, bool own_rows, 
     ln.chunk = std::max(p.each, 1) * (ln.tiled ? KT : KV8_TILE * NW);
     ln.parts = ln.splits > 1 ? ln.splits : 0;
     *out = ln;
-    return (double)ln.units * sh.n_kv_heads * ln.tiles * ln.splits < 0x1p31 && launchable(align_up(workgroups(sh, ln), 8), NW * 64) &&
+    return (double)ln.units * sh.n_kv_heads * ln.tiles * ln.splits < 0x1p31 && launchable(workgroups(sh, ln), NW * 64) &&
            (ln.parts == 0 || attention_join_launchable(sh, ln));
 }
 
