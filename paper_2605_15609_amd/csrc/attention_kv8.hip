@@ -159,11 +159,11 @@ __device__ __forceinline__ void hide(floatx16 (&x)[NT], Scale (&s)[2 * NT], int 
 #pragma unroll
     for (int g = 0; g < 2 * NT; ++g) {
         if (g * 16 >= left) s[g] = {1.f, 0.f};
-        const bool zero = s[g].k == 0.f;   // (0 x -inf is NaN)
+        const bool zero = s[g].k == 0.f;   // (0 x -inf is NaN: the scores are scaled here)
         if (zero) s[g].k = 1.f;
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
-            const float y = zero ? 0.f : x[g >> 1][8 * (g & 1) + v];
+            const float y = zero ? 0.f * x[g >> 1][8 * (g & 1) + v] : x[g >> 1][8 * (g & 1) + v];
             x[g >> 1][8 * (g & 1) + v] = 16 * g + 8 * (v >> 2) + 4 * half + (v & 3) >= left ? -INFINITY : y;
         }
     }
@@ -322,41 +322,37 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[ct][v] = 0.f;
     Softmax soft;
-    uint4 kc[KL], vc[CT];
-    float2 sc[2];
-    auto load = [&](int t) {
+    struct Codes {
+        uint4 k[KL], v[CT];
+        float2 scale[2];
+    } here, ahead;
+    auto load = [&](Codes &c, int t) {
         const uint8_t *at = head.codes + (int64_t)t * (64 * DH);
         if constexpr (DH < 32) {
-            kc[0] = *reinterpret_cast<const uint4 *>(at + lrow * 16);
-            vc[0] = *reinterpret_cast<const uint4 *>(at + 32 * DH + half * (16 * DH) + min(lrow, DH - 1) * 16);
+            c.k[0] = *reinterpret_cast<const uint4 *>(at + lrow * 16);
+            c.v[0] = *reinterpret_cast<const uint4 *>(at + 32 * DH + half * (16 * DH) + min(lrow, DH - 1) * 16);
         } else {
 #pragma unroll
-            for (int l = 0; l < KL; ++l) kc[l] = *reinterpret_cast<const uint4 *>(at + l * 1024 + lane * 16);
+            for (int l = 0; l < KL; ++l) c.k[l] = *reinterpret_cast<const uint4 *>(at + l * 1024 + lane * 16);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) vc[ct] = *reinterpret_cast<const uint4 *>(at + 32 * DH + ct * 1024 + lane * 16);
+            for (int ct = 0; ct < CT; ++ct) c.v[ct] = *reinterpret_cast<const uint4 *>(at + 32 * DH + ct * 1024 + lane * 16);
         }
 #pragma unroll
-        for (int g = 0; g < 2; ++g) sc[g] = head.scale(t, g);
+        for (int g = 0; g < 2; ++g) c.scale[g] = head.scale(t, g);
     };
-    if (wave < steps) load(t0 + wave);
-    for (int st = wave; st < steps; st += NW) {
+    auto step = [&](Codes &c, Codes &next, int st) {
         const int left = end - begin - st * KV8_TILE;
-        uint4 k[KL], v[CT];
         Scale scale[2];
 #pragma unroll
-        for (int l = 0; l < KL; ++l) k[l] = kc[l];
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) v[ct] = vc[ct];
-#pragma unroll
-        for (int g = 0; g < 2; ++g) scale[g] = {sc[g].x * sl2, sc[g].y};
-        if (st + NW < steps) load(t0 + st + NW);
+        for (int g = 0; g < 2; ++g) scale[g] = {c.scale[g].x * sl2, c.scale[g].y};
+        if (st + NW < steps) load(next, t0 + st + NW);
         floatx16 x[1];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[0][i] = 0.f;
 #pragma unroll
         for (int l = 0; l < KL; ++l) {
             Frag<T> a, b;
-            convert<FORMAT>(k[l], a, b);
+            convert<FORMAT>(c.k[l], a, b);
             if constexpr (DH < 32) {
                 if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -371,17 +367,22 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
         if (left < KV8_TILE) {
             hide(x, scale, left, half);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) v[ct] = keep(v[ct], left - 4 * half);
+            for (int ct = 0; ct < CT; ++ct) c.v[ct] = keep(c.v[ct], left - 4 * half);
         }
         Frag<T> p[2];
         soft.step(x, scale, acc, p);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             Frag<T> a, b;
-            convert<FORMAT>(v[ct], a, b);
+            convert<FORMAT>(c.v[ct], a, b);
             product(a, p[0], acc[ct]);
             product(b, p[1], acc[ct]);
         }
+    };
+    if (wave < steps) load(here, t0 + wave);
+    for (int st = wave; st < steps; st += 2 * NW) {
+        step(here, ahead, st);
+        if (st + NW < steps) step(ahead, here, st + NW);
     }
     if (ln.k && split == ln.splits - 1)
         own_blocks<T, DH, CT>(sh, ln, u, kvh, tile * TR, rows, row.token, (wave - steps) & (NW - 1), NW, sl2, [&](int ks) { return qf[ks]; }, soft, acc,

@@ -273,6 +273,53 @@ def test_zero_scales_hide_nothing(forced, form, parts):
     near(lse, want["lse"], want["lse_tol"], "lse")
 
 
+@pytest.mark.parametrize("form,parts", [(-1, 0), (0, 0), (1, 0), (0, 2), (1, 2)])
+def test_rows_without_a_number_and_lengths_out_of_range(forced, form, parts):
+    """A query of NaN spoils its own row alone, also where all that it sees has a scale of 0; lengths outside the cache are cut to it."""
+    forced(form, parts)
+    host = Cache(2, 1, 64, 150, 32, "e4m3", lens=[-5, 1000])
+    q = torch.randn((2, 8, 8, 64), generator=torch.Generator().manual_seed(6)).to(BF)
+    want = attention(q, host, 1)
+    q[1, 2, 3, 10] = float("nan")
+    for zero in (False, True):
+        if zero:
+            host.scales[:] = 0.0
+        lse = torch.empty((2, 8, 8), device=DEV)
+        out = psd.psd_attention_kv8(q.to(DEV), host.device(DEV), lse=lse)
+        assert (out[0] == 0).all() and torch.isneginf(lse[0]).all()
+        assert torch.isnan(out[1, 2, 3]).all() and torch.isnan(lse[1, 2, 3])
+        out[1, 2, 3], lse[1, 2, 3] = 0.0, 0.0
+        if zero:
+            assert (out == 0).all() and torch.allclose(lse[1].flatten()[lse[1].flatten() != 0], torch.tensor(float(np.log(150)), device=DEV), atol=2.0 ** -20)
+        else:
+            want["out"][1, 2, 3], want["lse"][1, 2, 3] = 0.0, 0.0
+            near(out, want["out"], want["out_tol"], "out")
+            near(lse, want["lse"], want["lse_tol"], "lse")
+
+
+def test_offsets_beyond_32_bits():
+    """A unit of more than 4 GB and units further apart than that: what the last head holds at both ends, and attention over its beginning."""
+    Hkv, d, n = 17, 128, 1 << 20                       # 268 MB a head
+    codes = torch.empty((2 * Hkv * 2 * n * d,), dtype=torch.uint8, device=DEV).view(2, Hkv, n // 32, 2, 32 * d)
+    cache = psd.Kv8Cache(codes, torch.empty((2, Hkv, n // 32, 2), device=DEV), d)
+    assert cache.codes.stride(0) > 2 ** 32 and Hkv * cache.codes.stride(1) > 2 ** 32
+    g = torch.Generator().manual_seed(5)
+    k, v = (torch.randn((2, 40, Hkv, d), generator=g).to(BF) for _ in range(2))
+    small = Cache(2, Hkv, d, 40, 32, "int8")
+    number, scales = stored(small, k.double().numpy(), v.double().numpy(), [0, 0], [40, 40])
+    for first in (n - 64, 0):
+        psd.psd_kv8_store(cache, k.to(DEV), v.to(DEV), first=first)
+        got = psd.psd_kv8_load(cache, first, 40, dtype=F32)
+        for i in (0, 1):
+            want = (number[i][:, :, :40] * scales[i][:, :, np.arange(40) // 32, None].astype(np.float64)).swapaxes(1, 2).astype(np.float32)
+            assert np.array_equal(got[i].cpu().numpy(), want)
+    small.codes, small.scales = codes[:, :, :2].cpu().numpy(), cache.scales[:, :, :2].cpu().numpy()
+    q = torch.randn((2, 2, 2 * Hkv, d), generator=g).to(BF)
+    want = attention(q, small, 1)
+    out = psd.psd_attention_kv8(q.to(DEV), psd.Kv8Cache(codes, cache.scales, d, length=n, lens=torch.tensor([40, 40], dtype=torch.int32, device=DEV)))
+    near(out, want["out"], want["out_tol"], "out")
+
+
 @pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
 def test_a_row_does_not_depend_on_what_other_sequences_hold(forced, form, parts):
     forced(form, parts)
