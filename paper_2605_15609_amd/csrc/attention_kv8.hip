@@ -7,6 +7,15 @@
 //
 // Per tile the problem is transposed as in the other attention kernels: S^T = K Q^T, O^T += V^T P^T.  A lane owns one row; the cache holds
 // codes in the order of the products' fragments (kv8_device.h), so a lane's 16 bytes are two fragments once they are converted.
+//
+// What bounds it, with bf16 heads of 128: single rows memory (32 requests of the 7B shape over 16384 positions each take 94 us, 5.7 TB/s of codes; of
+// lengths even over 1 .. 16384 64 us, where a part's last workgroups run alone); blocks of 16 requests over 1312 positions (8B shape) 40 us, of
+// which 32 are memory.  Drafts are bound by vector instructions: a tile of 32 keys and 32 rows has 16 products and, in int8, 192 instructions that convert
+// its codes (e4m3: 64) and some 130 of softmax.  128 drafts of 64 rows over 5120 + 64 keys (8B shape) take 760 - 815 us, 0.85 - 0.92 PFLOP/s: vector units busy 70 %
+// of the cycles, matrix cores 47 %, at a clock that power holds near 1.8 GHz.  Small calls are one chain of round trips: 6.5 us, 7.5 with the host's call.
+// Tried and slower: queries in LDS for three workgroups a CU, with one tile of codes under way a wavefront in place of two (32 requests, ragged: 58 -> 66);
+// 16x16 products for up to 16 rows, a third workgroup a CU (level with these, 64 us); value scales in the exponent and no maximum in front of the exponentials
+// (many rows: 776 -> 760, but 92 -> 101 at 32 drafts over 2000 keys: two ways through a stage, of which the careful one spills).
 #include <math.h>
 
 #include <algorithm>
@@ -297,7 +306,10 @@ __device__ __forceinline__ void own_blocks(const SharedShape &sh, const Kv8Launc
 }
 
 // Few rows: a tile of TR rows against a part of its unit's keys, and the last part against their own blocks too.  The wavefronts deal the keys, 32 at
-// a time, codes straight from memory a step ahead, and merge in LDS in wavefront order.
+// a time, codes straight from memory a step ahead (into two sets of registers in turn: copying one to the other took 36 of 210 instructions), and merge in
+// LDS in wavefront order.  No barrier in the loop, so a batch of tiles that fills the CUs little more than once is faster so than in tiles of MT
+// rows, although every wavefront converts its codes alone: 6 drafts of 4 requests over 2596 keys (7B shape) 48 - 50 us against 57, 8 drafts over 2000 (8B) 36
+// against 42; 32 drafts over 2000 it is 92 in tiles of MT rows against 130.
 template <typename T, int DH>
 constexpr int few_rows_lds() {
     constexpr int merge = NW * (2 + (DH + 31) / 32 * 16) * 64 * 4, own = NW * own_lds<T, DH>();

@@ -5,7 +5,9 @@
 // M = 127 (whole numbers) or 448 (floats of 4 and 3 bits), RN to the nearest code, ties to even.  Where s grows, kept codes are rounded again:
 // RN(code * s_kept / s).  The quotients are exact before they are rounded, so a code does not depend on how the division is done.
 //
-// Bound: memory (rows read once, codes written once); a single token a chain of round trips in one launch.
+// Bound: memory, rows read once and codes written once: 4 prompts of 1024 positions of the 8B shape (67 MB of rows, 34 of codes) are stored in 30 us and
+// read back in 24, where a copy of as many bytes takes 20.  In between: 9 instructions a number in the store, one wait for the largest of a block.  A token of 32
+// requests (7B shape) takes 6.8 us: lengths, then rows, scale and codes, then the largest of a block, each a round trip.
 #include "psd_internal.h"
 #include "kv8_device.h"
 
@@ -57,23 +59,29 @@ struct Rounding {
     }
     // the same where no t is next to a border or on it and nothing is lifted; else `again` is set
     __device__ __forceinline__ uint32_t quick(const float (&x)[4], bool &again) const {
-        float t[4], v[4];
-        uint32_t word = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = x[i] * inv;
         if constexpr (FORMAT == PSD_KV8_INT8) {
+            constexpr float WHOLE = 0x1.8p23f;   // a sum with it is rounded to a whole number, whose last byte is the code
+            const float half = 0.5f * s;
+            uint32_t r[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = rintf(t[i]);
-            word = pack_codes<FORMAT>(v[0], v[1], v[2], v[3]);
+            for (int i = 0; i < 4; ++i) {
+                const float t = __builtin_fmaf(x[i], inv, WHOLE);
+                again |= !(fabsf(__builtin_fmaf(WHOLE - t, s, x[i])) < half);
+                r[i] = __float_as_uint(t);
+            }
+            return __builtin_amdgcn_perm(__builtin_amdgcn_perm(r[3], r[2], 0x0c0c0400u), __builtin_amdgcn_perm(r[1], r[0], 0x0c0c0400u), 0x05040100u);
         } else {
-            word = pack_codes<FORMAT>(t[0], t[1], t[2], t[3]);
-            v[0] = __builtin_amdgcn_cvt_f32_fp8((int)word, 0), v[1] = __builtin_amdgcn_cvt_f32_fp8((int)word, 1);
-            v[2] = __builtin_amdgcn_cvt_f32_fp8((int)word, 2), v[3] = __builtin_amdgcn_cvt_f32_fp8((int)word, 3);
-        }
-        const float half = 0.5f * s;
+            // t by 2^-22 more and less: the same codes, or one is next to a border
+            float lo[4], hi[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) again |= !(fabsf(__builtin_fmaf(-v[i], s, x[i])) < (FORMAT == PSD_KV8_INT8 ? half : step_of(t[i]) * half));
-        return word;
+            for (int i = 0; i < 4; ++i) {
+                const float t = x[i] * inv;
+                lo[i] = __builtin_fmaf(t, -0x1p-22f, t), hi[i] = __builtin_fmaf(t, 0x1p-22f, t);
+            }
+            const uint32_t word = pack_codes<FORMAT>(lo[0], lo[1], lo[2], lo[3]);
+            again |= word != pack_codes<FORMAT>(hi[0], hi[1], hi[2], hi[3]);
+            return word;
+        }
     }
     // kept codes under a scale of `had` rounded again, the first n of four
     __device__ __forceinline__ uint32_t regrown(uint32_t codes, float had, int n) const {
@@ -86,6 +94,41 @@ struct Rounding {
         }
         const uint32_t first = n >= 4 ? ~0u : (1u << (8 * max(n, 0))) - 1;
         return (codes & ~first) | (pack_codes<FORMAT>(v[0], v[1], v[2], v[3]) & first);
+    }
+};
+
+// 8 numbers of a row as they were loaded
+template <typename T>
+struct Raw;
+template <>
+struct Raw<bf16_t> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const bf16_t *p) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    }
+    __device__ __forceinline__ float at(int e) const { return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16); }
+    // the largest magnitude's bits: infinities and NaN are above all numbers
+    typedef uint16_t pair __attribute__((ext_vector_type(2)));
+    __device__ __forceinline__ uint32_t top(uint32_t so_far) const {
+        pair m = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(pair, w[i] & 0x7fff7fffu));
+        return max(so_far, (uint32_t)max(m.x, m.y) << 16);
+    }
+};
+template <>
+struct Raw<float> {
+    float v[8];
+    __device__ __forceinline__ void load(const float *p) {
+        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+    __device__ __forceinline__ float at(int e) const { return v[e]; }
+    __device__ __forceinline__ uint32_t top(uint32_t so_far) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) so_far = max(so_far, __float_as_uint(v[e]) & 0x7fffffffu);
+        return so_far;
     }
 };
 
@@ -142,7 +185,7 @@ __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows,
     const int rg = t >> (ds - 3), c8 = (t & ((d >> 3) - 1)) * 8;   // the thread's positions 4 rg .. and channels c8 ..
     const bool partial = live && (lo > 0 || hi < block);
 
-    alignas(16) T raw[NB][4][8];
+    Raw<T> raw[NB][4];
     uint32_t top = 0;
     float had = 0.f;
     if (live) {
@@ -151,13 +194,7 @@ __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows,
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {   // (positions without a new row repeat one that has)
-                const T *from = x + min(max(n * KV8_TILE - row0 + 4 * rg + j, lo), hi - 1) * ld + c8;
-                if constexpr (sizeof(T) == 2) {
-                    *reinterpret_cast<uint4 *>(raw[n][j]) = *reinterpret_cast<const uint4 *>(from);
-                } else {
-                    *reinterpret_cast<float4 *>(raw[n][j]) = *reinterpret_cast<const float4 *>(from);
-                    *reinterpret_cast<float4 *>(raw[n][j] + 4) = *reinterpret_cast<const float4 *>(from + 4);
-                }
+                raw[n][j].load(x + min(max(n * KV8_TILE - row0 + 4 * rg + j, lo), hi - 1) * ld + c8);
             }
         if (partial)   // (codes that stay, and those behind the rows)
 #pragma unroll
@@ -173,8 +210,7 @@ __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows,
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(to_float(raw[n][j][e])) & 0x7fffffffu);   // (infinities and NaN are above all numbers)
+                top = raw[n][j].top(top);
     }
     for (int s = min(d, 64) >> 1; s > 0; s >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s, 64));
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
@@ -226,12 +262,12 @@ __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows,
                 for (int j = 0; j < 4; ++j) fresh |= p + j >= lo && p + j < hi ? 0xffu << (8 * j) : 0u;
                 put(n, [&](int i, float (&v)[4]) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = to_float(raw[n][j][i]);
+                    for (int j = 0; j < 4; ++j) v[j] = raw[n][j].at(i);
                 }, [&](int i, uint32_t code) { merge(to + value_word(rg & 1, c8 + i, rg >> 1, d), code, fresh, lo - p); });
             } else {
                 put(n, [&](int i, float (&v)[4]) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = to_float(raw[n][i >> 1][4 * (i & 1) + e]);
+                    for (int e = 0; e < 4; ++e) v[e] = raw[n][i >> 1].at(4 * (i & 1) + e);
                 }, [&](int i, uint32_t code) {
                     const int j = i >> 1;
                     merge(to + key_word(4 * rg + j, c8 + 4 * (i & 1), d), code, p + j >= lo && p + j < hi ? 0xffffffffu : 0u, p + j < lo ? 4 : 0);
@@ -258,17 +294,41 @@ __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows,
         }
 }
 
-// code * s to T: exact before it is rounded.  In fp32 the product is rounded already; bf16 takes it with the last bit set where something was cut off
-// (rounded to odd), which rounds as the exact product does.
-template <typename T>
-__device__ __forceinline__ T value_of(float code, float s) {
-    float p = code * s;
-    if constexpr (sizeof(T) == 2) {
-        const float rest = __builtin_fmaf(code, s, -p);
-        const uint32_t bits = __float_as_uint(p);
-        if (rest != 0.f && !(bits & 1)) p = __uint_as_float((rest > 0.f) == (p > 0.f) ? bits | 1 : bits - 1);
+// byte i of a word as a number
+template <int FORMAT>
+__device__ __forceinline__ float byte_of(uint32_t w, int i) {
+    if constexpr (FORMAT == PSD_KV8_INT8) return (float)(int8_t)(w >> (8 * i));
+    else return i == 0 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 0) : i == 1 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 1) : i == 2 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 2)
+                                                                                                            : __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+}
+// 8 codes times s, exact before they are rounded, to a row.  code * s in fp32 is rounded already, and bf16 rounds that once more: wrong only where the first
+// rounding ended halfway between two numbers of bf16.  Then (__any of the wavefront) all are rounded to odd first -- the last bit set where something was cut off --
+// which bf16 rounds as it would the exact product.
+template <int FORMAT>
+__device__ __forceinline__ void store_values(bf16_t *to, const float (&code)[8], float s) {
+    typedef uint16_t pair __attribute__((ext_vector_type(2)));
+    float p[8];
+    pair least = {0xffff, 0xffff};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        p[2 * i] = code[2 * i] * s, p[2 * i + 1] = code[2 * i + 1] * s;
+        const uint32_t ends = __builtin_amdgcn_perm(__float_as_uint(p[2 * i + 1]), __float_as_uint(p[2 * i]), 0x05040100u) ^ 0x80008000u;
+        least = __builtin_elementwise_min(least, __builtin_bit_cast(pair, ends));
     }
-    return from_float<T>(p);
+    if (__any(least.x == 0 || least.y == 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float rest = __builtin_fmaf(code[i], s, -p[i]);
+            const uint32_t bits = __float_as_uint(p[i]);
+            if (rest != 0.f && !(bits & 1)) p[i] = __uint_as_float((rest > 0.f) == (p[i] > 0.f) ? bits | 1 : bits - 1);
+        }
+    }
+    *reinterpret_cast<uint4 *>(to) = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+}
+template <int FORMAT>
+__device__ __forceinline__ void store_values(float *to, const float (&code)[8], float s) {
+    *reinterpret_cast<float4 *>(to) = make_float4(code[0] * s, code[1] * s, code[2] * s, code[3] * s);
+    *reinterpret_cast<float4 *>(to + 4) = make_float4(code[4] * s, code[5] * s, code[6] * s, code[7] * s);
 }
 
 // A task is one tile of a unit and KV head, keys or values, and d_head threads: codes into LDS as they lie in memory, and a thread takes 4
@@ -301,27 +361,26 @@ __global__ __launch_bounds__(THREADS) void kv8_load_kernel(Kv8 c, Kv8Rows rows, 
     }
     __syncthreads();
     if (!live) return;
-    uint32_t w[8];   // keys: 2 words of each position; values: one of each channel
     if (which) {
+        uint32_t w[8];   // a channel's 4 positions
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = lds[value_word(rg & 1, c8 + e, rg >> 1, d)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float code[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) code[e] = byte_of<FORMAT>(w[e], j);
+            if (4 * rg + j >= lo && 4 * rg + j < hi) store_values<FORMAT>(out + (4 * rg + j) * ld, code, s);
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t *from = lds + key_word(4 * rg + j, c8, d);
-            w[2 * j] = from[0], w[2 * j + 1] = from[1];
+            const uint32_t *from = lds + key_word(4 * rg + j, c8, d), w0 = from[0], w1 = from[1];   // a position's 8 channels
+            float code[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) code[e] = byte_of<FORMAT>(e < 4 ? w0 : w1, e & 3);
+            if (4 * rg + j >= lo && 4 * rg + j < hi) store_values<FORMAT>(out + (4 * rg + j) * ld, code, s);
         }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int p = 4 * rg + j;
-        if (p < lo || p >= hi) continue;
-        alignas(16) T v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = value_of<T>(number_of<FORMAT>((which ? w[e] >> (8 * j) : w[2 * j + (e >> 2)] >> (8 * (e & 3))) & 0xffu), s);
-        T *to = out + p * ld;
-        *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(v);
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(to + 4) = *reinterpret_cast<const uint4 *>(v + 4);
     }
 }
 
