@@ -5,9 +5,11 @@
 // M = 127 (whole numbers) or 448 (floats of 4 and 3 bits), RN to the nearest code, ties to even.  Where s grows, kept codes are rounded again:
 // RN(code * s_kept / s).  The quotients are exact before they are rounded, so a code does not depend on how the division is done.
 //
-// Bound: memory, rows read once and codes written once: 4 prompts of 1024 positions of the 8B shape (67 MB of rows, 34 of codes) are stored in 30 us and
-// read back in 24, where a copy of as many bytes takes 20.  In between: 9 instructions a number in the store, one wait for the largest of a block.  A token of 32
-// requests (7B shape) takes 6.8 us: lengths, then rows, scale and codes, then the largest of a block, each a round trip.
+// Bound: memory, rows read once and codes written once: 4 prompts of 1024 positions of the 8B shape (67 MB of rows, 34 of codes) are stored in 27 us and
+// read back in 17, where a copy of as many bytes takes 20 (what was just written is read from the caches).  The store's instructions take about half of its
+// time: 5 a number for the code, 1 for the largest, and a wait for the largest of a block between them.  Decided word by word, the quotients next to a border
+// cost 50 registers in all, so that a SIMD holds 8 wavefronts; decided for all 8 words at once they took 87 and 30 us.  A token of 32 requests (7B shape)
+// takes 5.7 us: lengths, then rows, scale and codes, then the largest of a block, each a round trip.
 #include "psd_internal.h"
 #include "kv8_device.h"
 
@@ -51,7 +53,7 @@ struct Rounding {
         const float t = x * inv, step = step_of(t), per = FORMAT == PSD_KV8_INT8 ? 1.f : __uint_as_float(0x7f000000u - __float_as_uint(step));
         const float n = rintf(t * per), v = n * step, rest = __builtin_fmaf(-v, s, x), half = 0.5f * step * s;
         const float over = (fabsf(rest) - half) + (rest < 0.f ? -low : low);
-        return over > 0.f || (over == 0.f && ((int)n & 1)) ? v + copysignf(step, rest) : v;
+        return (over > 0.f) | ((over == 0.f) & (((int)n & 1) != 0)) ? v + copysignf(step, rest) : v;
     }
     // four of them as bytes
     __device__ __forceinline__ uint32_t careful(const float (&x)[4]) const {
@@ -159,14 +161,21 @@ struct Task {
     }
 };
 
+// The thread's task among its workgroup's.  With heads of 64 and 128 (D; 0: any other) a wavefront has one, so what follows from it is kept once for all lanes.
+template <int D>
+__device__ __forceinline__ int task_in_group(int ds) {
+    if constexpr (D != 0) return __builtin_amdgcn_readfirstlane(threadIdx.x >> ds);
+    else return threadIdx.x >> ds;
+}
+
 // A task is what the rows of a unit put into one block of a KV head, keys or values; d_head threads take one, tile by tile, a thread 4 positions of 8
 // channels.  Their codes are words of a position's channels (keys) or of a channel's positions (values), put together in LDS and written as they
 // lie in the cache.
-template <typename T, int FORMAT, int NB>
+template <typename T, int FORMAT, int NB, int D>
 __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows, const int32_t *starts, const int32_t *counts, uint32_t blocks, uint32_t tasks) {
     extern __shared__ __align__(16) uint32_t words[];   // [tasks][NB][tile_words]
     __shared__ uint32_t tops[THREADS / 64];
-    const int ds = __ffs(c.d_head) - 1, d = 1 << ds, block = 1 << c.block_shift, mine = threadIdx.x >> ds, t = threadIdx.x & (d - 1);
+    const int ds = D ? __builtin_ctz(D | 256) : __ffs(c.d_head) - 1, d = 1 << ds, block = 1 << c.block_shift, mine = task_in_group<D>(ds), t = threadIdx.x & (d - 1);
     const Task of(blockIdx.x * (THREADS >> ds) + mine, tasks, blocks, c.n_kv_heads);
     const int which = of.which, b = of.part, head = of.head;
     const int64_t u = of.unit;
@@ -190,12 +199,20 @@ __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows,
     float had = 0.f;
     if (live) {
         if (lo > 0) had = *scale;   // (a block that begins with a new row starts afresh)
+        if (!partial) {
+            const T *from = x + (int64_t)(4 * rg - row0) * ld + c8;
+            if (block < KV8_TILE && (4 * rg < row0 || 4 * rg >= row0 + block)) from = x + c8;   // (the other half of a tile: any row)
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {   // (positions without a new row repeat one that has)
-                raw[n][j].load(x + min(max(n * KV8_TILE - row0 + 4 * rg + j, lo), hi - 1) * ld + c8);
-            }
+                for (int j = 0; j < 4; ++j) raw[n][j].load(from + (n * KV8_TILE + j) * ld);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)   // (positions without a new row repeat one that has)
+                    raw[n][j].load(x + min(max(n * KV8_TILE - row0 + 4 * rg + j, lo), hi - 1) * ld + c8);
+        }
         if (partial)   // (codes that stay, and those behind the rows)
 #pragma unroll
             for (int n = 0; n < NB; ++n)
@@ -222,56 +239,51 @@ __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows,
     const bool grown = finite && had > 0.f && s > had, some = finite && s > 0.f;
     if (live) {
         const Rounding<FORMAT> round(some ? s : 1.f);
-        auto put = [&](int n, auto numbers, auto place) {   // the 8 words of the thread in tile n
-            uint32_t code[8];
-            bool again = round.lift != 1.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float v[4];
-                numbers(i, v);
-                code[i] = round.quick(v, again);
-            }
-            if (__any(again)) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float v[4];
-                    numbers(i, v);
-                    code[i] = round.careful(v);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) place(i, some ? code[i] : 0u);
+        // word i of the thread's 8 in tile n: where it is, and which of its bytes (positions of a channel, or channels of a position) are new
+        auto word_at = [&](int n, int i) {
+            return lds + n * tile_words(d) + (which ? value_word(rg & 1, c8 + i, rg >> 1, d) : key_word(4 * rg + (i >> 1), c8 + 4 * (i & 1), d));
         };
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            uint32_t *to = lds + n * tile_words(d);
+        auto new_bytes = [&](int n, int i) {
             const int p = n * KV8_TILE - row0 + 4 * rg;   // of the thread's first position in the block
-            // a word whose bytes in `fresh` are new: of what it held in front of them `kept` bytes stay
-            auto merge = [&](uint32_t *word, uint32_t code, uint32_t fresh, int kept) {
-                if (fresh == 0xffffffffu) {
-                    *word = code;
-                } else if (partial && p >= 0 && p < block) {
-                    uint32_t old = *word;
-                    if (grown) old = round.regrown(old, had, kept);
-                    *word = (old & ~fresh) | (code & fresh);
-                }
-            };
-            if (which) {
-                uint32_t fresh = 0;
+            if (!which) return p + (i >> 1) >= lo && p + (i >> 1) < hi ? 0xffffffffu : 0u;
+            uint32_t fresh = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) fresh |= p + j >= lo && p + j < hi ? 0xffu << (8 * j) : 0u;
-                put(n, [&](int i, float (&v)[4]) {
+            for (int j = 0; j < 4; ++j) fresh |= p + j >= lo && p + j < hi ? 0xffu << (8 * j) : 0u;
+            return fresh;
+        };
+        auto put = [&](int n, int i, uint32_t code) {
+            uint32_t *word = word_at(n, i), fresh = partial ? new_bytes(n, i) : 0xffffffffu;
+            code = some ? code : 0u;
+            if (fresh == 0xffffffffu) *word = code;
+            else if (fresh != 0) *word = (*word & ~fresh) | (code & fresh);
+        };
+        if (partial && grown) {
+#pragma unroll 4
+            for (int i = 0; i < 8 * NB; ++i) {
+                const int p = (i >> 3) * KV8_TILE - row0 + 4 * rg;
+                uint32_t *word = word_at(i >> 3, i & 7);
+                if (p >= 0 && p < block) *word = round.regrown(*word, had, which ? lo - p : p + ((i & 7) >> 1) < lo ? 4 : 0);
+            }
+        }
+        auto code_of = [&](const float (&v)[4]) {
+            bool again = round.lift != 1.f;
+            uint32_t code = round.quick(v, again);
+            if (__any(again)) code = round.careful(v);
+            return code;
+        };
+        if (which) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = raw[n][j].at(i);
-                }, [&](int i, uint32_t code) { merge(to + value_word(rg & 1, c8 + i, rg >> 1, d), code, fresh, lo - p); });
-            } else {
-                put(n, [&](int i, float (&v)[4]) {
+            for (int i = 0; i < 8 * NB; ++i) {
+                const float v[4] = {raw[i >> 3][0].at(i & 7), raw[i >> 3][1].at(i & 7), raw[i >> 3][2].at(i & 7), raw[i >> 3][3].at(i & 7)};
+                put(i >> 3, i & 7, code_of(v));
+            }
+        } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = raw[n][i >> 1].at(4 * (i & 1) + e);
-                }, [&](int i, uint32_t code) {
-                    const int j = i >> 1;
-                    merge(to + key_word(4 * rg + j, c8 + 4 * (i & 1), d), code, p + j >= lo && p + j < hi ? 0xffffffffu : 0u, p + j < lo ? 4 : 0);
-                });
+            for (int i = 0; i < 8 * NB; ++i) {
+                const Raw<T> &from = raw[i >> 3][(i & 7) >> 1];
+                const int e = 4 * (i & 1);
+                const float v[4] = {from.at(e), from.at(e + 1), from.at(e + 2), from.at(e + 3)};
+                put(i >> 3, i & 7, code_of(v));
             }
         }
         if (t == 0) *scale = s;
@@ -333,10 +345,10 @@ __device__ __forceinline__ void store_values(float *to, const float (&code)[8], 
 
 // A task is one tile of a unit and KV head, keys or values, and d_head threads: codes into LDS as they lie in memory, and a thread takes 4
 // positions of 8 channels out of it.
-template <typename T, int FORMAT>
+template <typename T, int FORMAT, int D>
 __global__ __launch_bounds__(THREADS) void kv8_load_kernel(Kv8 c, Kv8Rows rows, uint32_t tiles, uint32_t tasks) {
     extern __shared__ __align__(16) uint32_t words[];   // [tasks][tile_words]
-    const int ds = __ffs(c.d_head) - 1, d = 1 << ds, mine = threadIdx.x >> ds, t = threadIdx.x & (d - 1);
+    const int ds = D ? __builtin_ctz(D | 256) : __ffs(c.d_head) - 1, d = 1 << ds, mine = task_in_group<D>(ds), t = threadIdx.x & (d - 1);
     const Task of(blockIdx.x * (THREADS >> ds) + mine, tasks, tiles, c.n_kv_heads);
     const int which = of.which, tile = rows.first / KV8_TILE + of.part, head = of.head;
     const int64_t u = of.unit;
@@ -392,16 +404,27 @@ int load_tiles(int first, int n) { return (first + n - 1) / KV8_TILE - first / K
 bool kv8_store_launchable(const Kv8 &c, int units, int n) { return n < 1 || (double)units * c.n_kv_heads * store_blocks(c, n) * 2 * THREADS < 0x1p32; }
 bool kv8_load_launchable(const Kv8 &c, int units, int n) { return (double)units * c.n_kv_heads * ((n + 30) / KV8_TILE + 1) * 2 * THREADS < 0x1p32; }
 
-#define PSD_KV8_DISPATCH(call)                                                   \
-    if (rows.dtype == PSD_DTYPE_BF16) {                                          \
-        using T = bf16_t;                                                        \
-        if (c.format == PSD_KV8_INT8) { constexpr int F = PSD_KV8_INT8; call; }  \
-        else { constexpr int F = PSD_KV8_E4M3; call; }                           \
-    } else {                                                                     \
-        using T = float;                                                         \
-        if (c.format == PSD_KV8_INT8) { constexpr int F = PSD_KV8_INT8; call; }  \
-        else { constexpr int F = PSD_KV8_E4M3; call; }                           \
-    }
+template <typename T, int FORMAT, int D>
+static void store_as(const dim3 &grid, int smem, int nb, hipStream_t st, const Kv8 &c, const Kv8Rows &rows, const int32_t *starts, const int32_t *counts, int blocks, uint32_t tasks) {
+    if (nb == 1) hipLaunchKernelGGL((kv8_store_kernel<T, FORMAT, 1, D>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks);
+    else if (nb == 2) hipLaunchKernelGGL((kv8_store_kernel<T, FORMAT, 2, D>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks);
+    else hipLaunchKernelGGL((kv8_store_kernel<T, FORMAT, 4, D>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks);
+}
+
+// call(T(), format, d): the types and the head width that kernels are built for
+template <int FORMAT, typename T, typename Call>
+static void kv8_by_width(int d_head, Call call) {
+    if (d_head == 128) call(T(), std::integral_constant<int, FORMAT>(), std::integral_constant<int, 128>());
+    else if (d_head == 64) call(T(), std::integral_constant<int, FORMAT>(), std::integral_constant<int, 64>());
+    else call(T(), std::integral_constant<int, FORMAT>(), std::integral_constant<int, 0>());
+}
+template <typename Call>
+static void kv8_dispatch(const Kv8 &c, int dtype, Call call) {
+    if (dtype == PSD_DTYPE_BF16 && c.format == PSD_KV8_INT8) kv8_by_width<PSD_KV8_INT8, bf16_t>(c.d_head, call);
+    else if (dtype == PSD_DTYPE_BF16) kv8_by_width<PSD_KV8_E4M3, bf16_t>(c.d_head, call);
+    else if (c.format == PSD_KV8_INT8) kv8_by_width<PSD_KV8_INT8, float>(c.d_head, call);
+    else kv8_by_width<PSD_KV8_E4M3, float>(c.d_head, call);
+}
 
 void launch_kv8_store(const Kv8 &c, int units, const Kv8Rows &rows, const int32_t *starts, const int32_t *counts, hipStream_t st) {
     if (rows.n < 1) return;
@@ -409,13 +432,9 @@ void launch_kv8_store(const Kv8 &c, int units, const Kv8Rows &rows, const int32_
     const uint32_t tasks = (uint32_t)(units * c.n_kv_heads * blocks * 2);
     const int smem = per * nb * tile_words(c.d_head) * 4;
     const dim3 grid((unsigned)((tasks + per - 1) / per));
-    if (nb == 1) {
-        PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_store_kernel<T, F, 1>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks))
-    } else if (nb == 2) {
-        PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_store_kernel<T, F, 2>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks))
-    } else {
-        PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_store_kernel<T, F, 4>), grid, dim3(THREADS), smem, st, c, rows, starts, counts, blocks, tasks))
-    }
+    kv8_dispatch(c, rows.dtype, [&](auto type, auto format, auto width) {
+        store_as<decltype(type), decltype(format)::value, decltype(width)::value>(grid, smem, nb, st, c, rows, starts, counts, blocks, tasks);
+    });
 }
 
 void launch_kv8_load(const Kv8 &c, int units, const Kv8Rows &rows, hipStream_t st) {
@@ -423,5 +442,7 @@ void launch_kv8_load(const Kv8 &c, int units, const Kv8Rows &rows, hipStream_t s
     const int tiles = load_tiles(rows.first, rows.n), per = THREADS / c.d_head;
     const uint32_t tasks = (uint32_t)(units * c.n_kv_heads * tiles * 2);
     const dim3 grid((unsigned)((tasks + per - 1) / per));
-    PSD_KV8_DISPATCH(hipLaunchKernelGGL((kv8_load_kernel<T, F>), grid, dim3(THREADS), per * tile_words(c.d_head) * 4, st, c, rows, tiles, tasks))
+    kv8_dispatch(c, rows.dtype, [&](auto type, auto format, auto width) {
+        hipLaunchKernelGGL((kv8_load_kernel<decltype(type), decltype(format)::value, decltype(width)::value>), grid, dim3(THREADS), per * tile_words(c.d_head) * 4, st, c, rows, tiles, tasks);
+    });
 }
