@@ -123,7 +123,8 @@ def attention(q, cache, per, k=None, v=None):
     A score is a sum of d products of exact inputs in fp32, off by at most d 2^-24 sum|q||k| / sqrt(d) (a code's scale is taken out of the sum), and
     is scaled, shifted and exponentiated with at most 2^-21 |x| + 2^-22 more, E together; so is the lse, whose sum of n positive terms adds n 2^-24.  A
     probability is off by a factor within 2 E + n 2^-24, the sum of n products with values by n 2^-24 more, an output by that much of sum p|v|.  A
-    probability times its value scale is rounded to fp32 (2^-24) and with bf16 to that (half a step), and so is the result."""
+    probability times its value scale is rounded to fp32 (2^-24) and with bf16 to that (half a step u: factors 1 + e_j), and so is the result.  With bf16 the
+    sum that divides has the same factors: sum p (1 + e) v / sum p (1 + e) is off by at most u sum p|v| + u |o| before it is rounded."""
     S, L, H, d = q.shape
     Hkv, u, x64 = cache.Hkv, U[q.dtype], q.double().numpy()
     out, lse = np.zeros((S, L, H, d)), np.full((S, L, H), -np.inf)
@@ -147,7 +148,8 @@ def attention(q, cache, per, k=None, v=None):
             rel = 2 * E + 2 * n * 2.0 ** -24
             o = p @ vv
             out[s, :, h], lse[s, :, h], lse_tol[s, :, h] = o, z[:, 0], rel[:, 0]
-            out_tol[s, :, h] = (rel + 2.0 ** -23 + (u if q.dtype == torch.bfloat16 else 0)) * (p @ np.abs(vv)) + u * np.abs(o) + 1e-30
+            given = u if q.dtype == torch.bfloat16 else 0
+            out_tol[s, :, h] = (rel + 2.0 ** -23 + given) * (p @ np.abs(vv)) + (u + given) * np.abs(o) + 1e-30
     return {"out": out, "lse": lse, "out_tol": out_tol, "lse_tol": lse_tol}
 
 

@@ -259,6 +259,34 @@ def test_scores_of_any_size(forced, form, parts, fmt, L):
             near(lse[0, :, 0], np.full(L, x + np.log(len(top))), np.full(L, 5 * 2.0 ** -24 * abs(x) + 2.0 ** -20), "lse")
 
 
+@pytest.mark.parametrize("fmt,positions", [("int8", 1), ("e4m3", 1), ("int8", 700), ("e4m3", 700)])
+@pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
+def test_a_row_with_one_key_has_its_value(forced, form, parts, fmt, positions):
+    """Where one key has all of the weight nothing is rounded but the result: half a step of it, 2^-18 for some forty steps of fp32, and 700 exp(-32)
+    < 2^-36 of the others' values: a query is stretched until its best key is 32 or more ahead."""
+    forced(form, parts)
+    S, L, H, Hkv, d = 3, 4, 8, 4, 64
+    host = Cache(S, Hkv, d, positions, 32, fmt, seed=3)
+    q = torch.randn((S, L, H, d), generator=torch.Generator().manual_seed(8))
+    want, best, size = np.empty((S, L, H, d)), np.empty((S, L, H)), np.empty((S, L, H))
+    for s in range(S):
+        keys, values = (torch.from_numpy(x) for x in host.read(s))
+        for h in range(H):
+            for stretch in (True, False):
+                x = q[s, :, h].double() @ keys[:, h // 2].T / d ** 0.5
+                top = torch.cat([x, torch.full((L, 1), -1e9)], 1).topk(2)
+                ahead = top.values[:, 0] - top.values[:, 1]
+                if stretch:
+                    q[s, :, h] = (q[s, :, h] * (33 / ahead.float()).clamp(min=1.0)[:, None] * 1.25).to(BF).float()
+            assert (ahead > 32).all()
+            want[s, :, h], best[s, :, h] = values[top.indices[:, 0], h // 2].numpy(), top.values[:, 0].numpy()
+            size[s, :, h] = (q[s, :, h].double().abs() @ keys[:, h // 2].abs().T / d ** 0.5).max(1).values.numpy()
+    lse = torch.empty((S, L, H), device=DEV)
+    out = psd.psd_attention_kv8(q.to(BF).to(DEV), host.device(DEV), lse=lse)
+    near(out, want, (2.0 ** -8 + 2.0 ** -18) * np.abs(want) + 2.0 ** -36 * np.nanmax(np.abs(want)), "out")
+    near(lse, best, (d + 16) * 2.0 ** -24 * size + 2.0 ** -20, "lse")
+
+
 @pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
 def test_zero_scales_hide_nothing(forced, form, parts):
     """A block of zeros has a scale of 0: its positions still draw weight, also in a unit's last tile."""
