@@ -5,11 +5,10 @@
 // M = 127 (whole numbers) or 448 (floats of 4 and 3 bits), RN to the nearest code, ties to even.  Where s grows, kept codes are rounded again:
 // RN(code * s_kept / s).  The quotients are exact before they are rounded, so a code does not depend on how the division is done.
 //
-// Bound: memory, rows read once and codes written once: 4 prompts of 1024 positions of the 8B shape (67 MB of rows, 34 of codes) are stored in 27 us and
-// read back in 17, where a copy of as many bytes takes 20 (what was just written is read from the caches).  The store's instructions take about half of its
-// time: 5 a number for the code, 1 for the largest, and a wait for the largest of a block between them.  Decided word by word, the quotients next to a border
-// cost 50 registers in all, so that a SIMD holds 8 wavefronts; decided for all 8 words at once they took 87 and 30 us.  A token of 32 requests (7B shape)
-// takes 5.7 us: lengths, then rows, scale and codes, then the largest of a block, each a round trip.
+// Bound: memory, rows read once and codes written once: 4 prompts of 1024 positions of the 8B shape (67 MB of rows, 34 of codes) are stored in 22.8 us and
+// read back in 17, where a copy of as many bytes takes 20 (what was just written is read from the caches).  The store's vector instructions, some 18 a number,
+// take most of its time beside that; deciding the quotients next to a border on a path of their own took 27 us, for in a third of the blocks some are.
+// A token of 32 requests (7B shape) takes 5.5 us: lengths, then rows, scale and codes, then the largest of a block, each a round trip.
 #include "psd_internal.h"
 #include "kv8_device.h"
 
@@ -55,34 +54,33 @@ struct Rounding {
         const float over = (fabsf(rest) - half) + (rest < 0.f ? -low : low);
         return (over > 0.f) | ((over == 0.f) & (((int)n & 1) != 0)) ? v + copysignf(step, rest) : v;
     }
-    // four of them as bytes
-    __device__ __forceinline__ uint32_t careful(const float (&x)[4]) const {
-        return pack_codes<FORMAT>(exact(x[0] * lift, 0.f), exact(x[1] * lift, 0.f), exact(x[2] * lift, 0.f), exact(x[3] * lift, 0.f));
-    }
-    // the same where no t is next to a border or on it and nothing is lifted; else `again` is set
-    __device__ __forceinline__ uint32_t quick(const float (&x)[4], bool &again) const {
+    // Four of them as bytes.  Numbers of bf16 are often next to a border: half of the largest, of which 127 codes make 63.5, or three quarters of it, 336 with
+    // 448.  So t is taken to b, the nearest half step -- a code or a border -- and a little to the side that x - b s is on, whose sign is exact: it is
+    // 2^-29 of b s or more, or nothing, and then b decides (ties to even).  A code is not left by that, nor is one next to it reached.
+    __device__ __forceinline__ uint32_t codes(float (&x)[4]) const {
+        if (lift != 1.f) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] *= lift;
+        }
+        const float far = inv * 0x1p24f;   // (a lifted scale is 2^-100 or more)
         if constexpr (FORMAT == PSD_KV8_INT8) {
-            constexpr float WHOLE = 0x1.8p23f;   // a sum with it is rounded to a whole number, whose last byte is the code
-            const float half = 0.5f * s;
+            constexpr float HALVES = 0x1.8p22f, WHOLE = 0x1.8p23f;   // sums with them are rounded to halves, and to whole numbers, whose last byte is the code
             uint32_t r[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float t = __builtin_fmaf(x[i], inv, WHOLE);
-                again |= !(fabsf(__builtin_fmaf(WHOLE - t, s, x[i])) < half);
-                r[i] = __float_as_uint(t);
+                const float b = __builtin_fmaf(x[i], inv, HALVES) - HALVES, side = __builtin_fmaf(-b, s, x[i]) * far;
+                r[i] = __float_as_uint((b + __builtin_amdgcn_fmed3f(side, -0.125f, 0.125f)) + WHOLE);
             }
             return __builtin_amdgcn_perm(__builtin_amdgcn_perm(r[3], r[2], 0x0c0c0400u), __builtin_amdgcn_perm(r[1], r[0], 0x0c0c0400u), 0x05040100u);
         } else {
-            // t by 2^-22 more and less: the same codes, or one is next to a border
-            float lo[4], hi[4];
+            float r[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float t = x[i] * inv;
-                lo[i] = __builtin_fmaf(t, -0x1p-22f, t), hi[i] = __builtin_fmaf(t, 0x1p-22f, t);
+                // (5 bits; below the normal numbers finer than half steps)
+                const float b = __uint_as_float((__float_as_uint(x[i] * inv) + 0x40000u) & 0xfff80000u), side = __builtin_fmaf(-b, s, x[i]) * far, most = fabsf(b) * 0x1p-8f;
+                r[i] = b + __builtin_amdgcn_fmed3f(side, -most, most);
             }
-            const uint32_t word = pack_codes<FORMAT>(lo[0], lo[1], lo[2], lo[3]);
-            again |= word != pack_codes<FORMAT>(hi[0], hi[1], hi[2], hi[3]);
-            return word;
+            return pack_codes<FORMAT>(r[0], r[1], r[2], r[3]);
         }
     }
     // kept codes under a scale of `had` rounded again, the first n of four
@@ -265,25 +263,19 @@ __global__ __launch_bounds__(THREADS) void kv8_store_kernel(Kv8 c, Kv8Rows rows,
                 if (p >= 0 && p < block) *word = round.regrown(*word, had, which ? lo - p : p + ((i & 7) >> 1) < lo ? 4 : 0);
             }
         }
-        auto code_of = [&](const float (&v)[4]) {
-            bool again = round.lift != 1.f;
-            uint32_t code = round.quick(v, again);
-            if (__any(again)) code = round.careful(v);
-            return code;
-        };
         if (which) {
 #pragma unroll
             for (int i = 0; i < 8 * NB; ++i) {
-                const float v[4] = {raw[i >> 3][0].at(i & 7), raw[i >> 3][1].at(i & 7), raw[i >> 3][2].at(i & 7), raw[i >> 3][3].at(i & 7)};
-                put(i >> 3, i & 7, code_of(v));
+                float v[4] = {raw[i >> 3][0].at(i & 7), raw[i >> 3][1].at(i & 7), raw[i >> 3][2].at(i & 7), raw[i >> 3][3].at(i & 7)};
+                put(i >> 3, i & 7, round.codes(v));
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 8 * NB; ++i) {
                 const Raw<T> &from = raw[i >> 3][(i & 7) >> 1];
                 const int e = 4 * (i & 1);
-                const float v[4] = {from.at(e), from.at(e + 1), from.at(e + 2), from.at(e + 3)};
-                put(i >> 3, i & 7, code_of(v));
+                float v[4] = {from.at(e), from.at(e + 1), from.at(e + 2), from.at(e + 3)};
+                put(i >> 3, i & 7, round.codes(v));
             }
         }
         if (t == 0) *scale = s;

@@ -72,7 +72,7 @@ def test_quotients_on_and_next_to_borders(fmt, dtype):
     t = t[np.abs(t) <= (127 if fmt == "int8" else 448)]
     middle = ((t[1:] + t[:-1]) / 2).astype(np.float64)
     host = Cache(1, 1, 128, 32, 32, fmt)
-    for scale in (1.0, 0.0371, 2.0 ** -130, 3e35):
+    for scale in (1.0, 0.0371, 2.0 ** -99, 2.0 ** -130, 3e35):
         s = np.float32(np.float32(scale) * t[-1]) / np.float64(t[-1])
         base = torch.from_numpy((middle * s)).to(dtype)
         x = torch.cat([base, torch.nextafter(base.float(), torch.full_like(base.float(), 1e38)).to(dtype),
