@@ -294,14 +294,21 @@ int32_t psd_attention_kv8(const psd_attention_shape *shape, const void *q, const
     const int64_t units = sh.S / c.seqs_per_unit;
     const Region to = rows_region(out, n_tokens, sh.ld_out, row, esz), sums = dense(lse, sh.n_rows * 4);
     if (!apart(to, sums)) PSD_FAIL(PSD_ERR_INVALID_ARG, "lse lies on out");
-    for (const Region &x : {rows_region(q, n_tokens, sh.ld_q, row, esz), rows_region(k, n_tokens, ld_k, width, esz), rows_region(v, n_tokens, ld_v, width, esz),
-                            codes_region(c, units), scales_region(c, units), dense(c.lens, units * 4)})
+    const Region read[] = {rows_region(q, n_tokens, sh.ld_q, row, esz), rows_region(k, n_tokens, ld_k, width, esz), rows_region(v, n_tokens, ld_v, width, esz),
+                           codes_region(c, units), scales_region(c, units), dense(c.lens, units * 4)};
+    for (const Region &x : read)
         if (!apart(x, to) || !apart(x, sums)) PSD_FAIL(PSD_ERR_INVALID_ARG, "out or lse lies on what is read");
     Kv8Launch ln;
     if (!plan_attention_kv8(sh, c, k != nullptr, &ln)) PSD_FAIL(PSD_ERR_SHAPE, "more workgroups than a launch takes");
     const int64_t need = attention_parts_bytes(sh, ln);
     if (need > 0 && (!ws || ws_bytes < need)) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
     if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 255) != 0) PSD_FAIL(PSD_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    if (need > 0) {
+        const Region scratch = dense(ws, need);
+        for (const Region &x : read)
+            if (!apart(x, scratch)) PSD_FAIL(PSD_ERR_WORKSPACE, "the workspace lies on what is read");
+        if (!apart(to, scratch) || !apart(sums, scratch)) PSD_FAIL(PSD_ERR_WORKSPACE, "the workspace lies on out or lse");
+    }
     ln.k = k;
     ln.v = v;
     ln.ld_k = ld_k;

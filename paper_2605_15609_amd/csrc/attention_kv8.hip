@@ -9,10 +9,10 @@
 // codes in the order of the products' fragments (kv8_device.h), so a lane's 16 bytes are two fragments once they are converted.
 //
 // What bounds it, with bf16 heads of 128: single rows memory (32 requests of the 7B shape over 16384 positions each take 94 us, 5.7 TB/s of codes; of
-// lengths even over 1 .. 16384 64 us, where a part's last workgroups run alone); blocks of 16 requests over 1312 positions (8B shape) 40 us, of
+// lengths even over 1 .. 16384 60 - 67 us, where a part's last workgroups run alone); blocks of 16 requests over 1312 positions (8B shape) 40 us, of
 // which 32 are memory.  Drafts are bound by vector instructions: a tile of 32 keys and 32 rows has 16 products and, in int8, 192 instructions that convert
-// its codes (e4m3: 64) and some 130 of softmax.  128 drafts of 64 rows over 5120 + 64 keys (8B shape) take 760 - 815 us, 0.85 - 0.92 PFLOP/s: vector units busy 70 %
-// of the cycles, matrix cores 47 %, at a clock that power holds near 1.8 GHz.  Small calls are one chain of round trips: 6.5 us, 7.5 with the host's call.
+// its codes (e4m3: 64) and some 150 of softmax.  128 drafts of 64 rows over 5120 + 64 keys (8B shape) take 783 - 829 us, 0.84 - 0.89 PFLOP/s: vector units busy 71 %
+// of the cycles, matrix cores 44 %, at a clock that power holds near 1.8 GHz.  Small calls are one chain of round trips: 6.5 us, 7.5 with the host's call.
 // Tried and slower: queries in LDS for three workgroups a CU, with one tile of codes under way a wavefront in place of two (32 requests, ragged: 58 -> 66);
 // 16x16 products for up to 16 rows, a third workgroup a CU (level with these, 64 us); value scales in the exponent and no maximum in front of the exponentials
 // (many rows: 776 -> 760, but 92 -> 101 at 32 drafts over 2000 keys: two ways through a stage, of which the careful one spills).
@@ -172,12 +172,12 @@ struct Softmax {
     // What the outputs of a row are multiplied by.  A probability times its value scale is rounded to bf16, and where one key has nearly all of a row that
     // is a factor of the whole row, half a step like the result's own rounding.  The sum of the rounded products over their scales has the same factor, so
     // it goes away, for 4 % of the time where vector instructions bound it (128 drafts 799 -> 829 us, drafts of 4 requests 47 -> 48.8) and 1 % where memory
-    // does.  Nothing is corrected where a scale of 0, infinite or NaN has been met, or products below the normal numbers.
+    // does.  It is within half a step; anything else comes from scales of 0, infinite or NaN, or products below the normal numbers, and corrects nothing.
     template <typename T>
     __device__ __forceinline__ float correction() const {
         if constexpr (sizeof(T) == 4) return 1.f;
         const float f = both_sum(l) / both_sum(given);
-        return fabsf(f - 1.f) < 0x1p-7f ? f : 1.f;
+        return fabsf(f - 1.f) < 0x1.02p-8f ? f : 1.f;
     }
     template <typename T, int NT, int CT>
     __device__ __forceinline__ void step(floatx16 (&x)[NT], Scale (&s)[2 * NT], floatx16 (&acc)[CT], Frag<T> (&p)[2 * NT]) {
@@ -333,7 +333,7 @@ __device__ __forceinline__ void own_blocks(const SharedShape &sh, const Kv8Launc
 // Few rows: a tile of TR rows against a part of its unit's keys, and the last part against their own blocks too.  The wavefronts deal the keys, 32 at
 // a time, codes straight from memory a step ahead (into two sets of registers in turn: copying one to the other took 36 of 210 instructions), and merge in
 // LDS in wavefront order.  No barrier in the loop, so a batch of tiles that fills the CUs little more than once is faster so than in tiles of MT
-// rows, although every wavefront converts its codes alone: 6 drafts of 4 requests over 2596 keys (7B shape) 48 - 50 us against 57, 8 drafts over 2000 (8B) 36
+// rows, although every wavefront converts its codes alone: 6 drafts of 4 requests over 2596 keys (7B shape) 46 - 50 us against 57, 8 drafts over 2000 (8B) 36
 // against 42; 32 drafts over 2000 it is 92 in tiles of MT rows against 130.
 template <typename T, int DH>
 constexpr int few_rows_lds() {
@@ -649,7 +649,8 @@ constexpr int attention_lds() {
 }
 
 // Every (unit, KV head, part) is dealt to an XCD, one after the other, with all of its tiles: those that read the same keys meet in one L2.  Parts are turned by
-// one from one unit and head to the next, so that no XCD has only first parts, which every unit fills, and another only last ones.
+// one from one unit and head to the next, so that no XCD has only first parts, which every unit fills, and another only last ones (32 caches of up to 16384
+// positions: 71 us dealt in order, 64 so).
 template <typename T, int DH, int FORMAT, bool MANY>
 __global__ __launch_bounds__(NW * 64, 2) void attention_kv8_kernel(const T *__restrict__ q, SharedShape sh, Kv8Launch ln, float sl2) {
     extern __shared__ __align__(16) unsigned char lds[];

@@ -205,6 +205,15 @@ def test_the_workspace_is_checked(lib):
 
 
 # ---------------------------------------------------------------------------------------------------------- binding
+def test_a_workspace_that_lies_on_something_is_refused(lib):
+    far = dict(sh=shape(S=4, L=1), capacity=32768, len=32768, lse=BASE + 5 * GB)
+    need = lib.psd_attention_kv8_bytes(C.byref(far["sh"]), C.byref(cache(capacity=32768, len=32768, lens=BASE + 8 * GB)), 1)
+    assert need > 0
+    own = dict(k=BASE + 6 * GB, v=BASE + 7 * GB, n=need, lens=BASE + 8 * GB)
+    for at in (BASE, BASE + 2 * GB, BASE + 3 * GB, BASE + 5 * GB, BASE + 6 * GB, BASE + 7 * GB, BASE + 8 * GB):
+        refused(lib, attend(lib, **{**far, **own, "ws": at}), "the workspace lies on")
+
+
 def test_caches_that_the_binding_refuses():
     codes, scales = torch.zeros((2, 3, 4, 2, 32 * 64), dtype=torch.uint8), torch.zeros((2, 3, 4, 2))
     c = psd.Kv8Cache(codes, scales, 64)
