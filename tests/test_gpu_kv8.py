@@ -119,6 +119,29 @@ def test_what_is_read_back_is_rounded_once(fmt, dtype):
                 assert (got[u, m:] == -7.0).all()
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+def test_every_width_and_block_there_and_back(fmt, dtype, d, block):
+    """Rows that begin and end inside blocks: codes and scales, and what is read back, exactly."""
+    host = Cache(3, 3, d, 290, block, fmt, seed=block + d)
+    dev = host.device(DEV, length=host.n)
+    g = torch.Generator().manual_seed(block * d)
+    k, v = ((2.0 ** torch.randn((3, 150, 1, 1), generator=g) * torch.randn((3, 150, 3, d), generator=g)).to(dtype) for _ in range(2))
+    starts, counts = [0, 37, 128], [150, 149, 131]
+    number, scales = stored(host, k.double().numpy(), v.double().numpy(), starts, counts)
+    check_store(host, dev, k, v, starts, counts, pad=8, call=dict(starts=torch.tensor(starts, dtype=torch.int32, device=DEV),
+                                                                  counts=torch.tensor(counts, dtype=torch.int32, device=DEV)))
+    got = psd.psd_kv8_load(dev, 3, 180, dtype=dtype)
+    for u in range(3):
+        held = range(max(starts[u], 3), min(starts[u] + counts[u], 183))
+        at = np.array(held)
+        for i in (0, 1):
+            want = number[i][u][:, at] * scales[i][u].astype(np.float64)[:, at // block, None]
+            assert torch.equal(got[i][u, at - 3].cpu(), torch.from_numpy(np.swapaxes(want, 0, 1).copy()).to(dtype)), (u, i)
+
+
 def test_token_by_token_is_the_same_as_rules_say():
     """One token at a time: a block's scale grows step by step, and what it holds is rounded again each time."""
     host = Cache(2, 2, 64, 64, 32, "int8")
