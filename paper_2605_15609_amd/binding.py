@@ -977,7 +977,8 @@ def rotary_frequencies(rotated: int, theta: float, kind: str = "plain", stretch:
 
 
 def _layout(t: Optional[torch.Tensor]):
-    return None if t is None else (t.shape, t.stride(), t.dtype, t.device)
+    # (the device's number, not the device, whose hash is slow; whatever is not on a GPU is -1 and never passes a check beside what is)
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
 
 
 def _dense_on(t: torch.Tensor, what: str, dtype, shape, device) -> None:
