@@ -32,9 +32,10 @@ __device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float 
     }
 }
 
-// RN(x / s) to a code, x / s at most M (1 + 2^-23).  t = x * fl(1 / s) is off by 2^-23 of itself, so the nearest code v to t is the right one or next to
-// it; x - v s tells which, and in fp32 it is exact: v has 8 bits at most and x is v s or more than half a step away, so the difference is a
-// multiple of 2^-25 steps and hardly more than half a step.  (Scales below 2^-100, where it might not be, are lifted with x.)
+// RN(x / s) to a code, the largest where x / s is beyond it: M (1 + 2^-23) at most, or, where s is below the normal numbers and off by up to half of its
+// last place, 1.5 M at most (190 * 2^-149 has a scale of 2^-149 in int8).  t = x * fl(1 / s) is off by 2^-23 of itself, so the nearest code v to t
+// is the right one or next to it; x - v s tells which, and in fp32 it is exact: v is 0 and it is x, or x is hardly less than half a step and it is a
+// multiple of 2^-25 steps that is hardly more than half a step.  (Scales below 2^-100, where it might not be, are lifted with x.)
 template <int FORMAT>
 struct Rounding {
     float s, inv, lift;
@@ -59,8 +60,9 @@ struct Rounding {
     // 2^-29 of b s or more, or nothing, and then b decides (ties to even).  A code is not left by that, nor is one next to it reached.
     __device__ __forceinline__ uint32_t codes(float (&x)[4]) const {
         if (lift != 1.f) {
+            const float most = s * kv8_most(FORMAT);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] *= lift;
+            for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_fmed3f(x[i] * lift, -most, most);
         }
         const float far = inv * 0x1p24f;   // (a lifted scale is 2^-100 or more)
         if constexpr (FORMAT == PSD_KV8_INT8) {

@@ -1,0 +1,40 @@
+"""8-bit caches and rotation on the GPU where numbers, lengths and forms end."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_15609_amd as psd
+from tests.gpu_common import DEV
+from tests.kv8_common import Cache, stored
+from tests.test_gpu_kv8 import check_store
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+#: largest magnitudes of a block, in units of the smallest number: quotients by a scale of so few bits pass the largest code by up to half of it
+TINY = [1, 2, 63, 64, 65, 127, 150, 190, 191, 223, 224, 225, 337, 449, 465, 500, 671, 672, 1119, 1121, 5000, 6047, 8953, 9999, 16385, 123457, 2 ** 19 - 1, 2 ** 19,
+        2 ** 21 + 1, 2 ** 22 + 3, 2 ** 23 - 1, 2 ** 23 + 5]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("d", [16, 64, 128])
+def test_blocks_of_the_smallest_numbers(fmt, d):
+    """fp32 rows whose scales are below the normal numbers, in fresh blocks and behind kept rows: codes and scales are exact, and what is read back is
+    code * scale (a whole number of smallest ones in int8; rounded to one in e4m3)."""
+    units, rng = len(TINY), np.random.default_rng(d)
+    host = Cache(units, 1, d, 32, 32, fmt, seed=d)
+    dev = host.device(DEV)
+
+    def rows(tops):
+        x = np.stack([rng.integers(-t, t + 1, (16, 1, d)) for t in tops]).astype(np.float64)
+        for u, t in enumerate(tops):
+            x[u, 5, 0, 7], x[u, 6, 0, 9] = t, -t
+        return torch.from_numpy(x * 2.0 ** -149).to(F32)
+    for start, tops in ((0, TINY), (16, TINY[::-1])):
+        k, v = rows(tops), rows(tops[1:] + tops[:1])
+        number, scales = stored(host, k.double().numpy(), v.double().numpy(), [start] * units, [16] * units)
+        check_store(host, dev, k, v, [start] * units, [16] * units, call=dict(first=start))
+        host.codes, host.scales = dev.codes.cpu().numpy(), dev.scales.cpu().numpy()
+        for got, n, s in zip(psd.psd_kv8_load(dev, 0, start + 16, dtype=F32), number, scales):
+            want = (n[:, :, :start + 16] * s.astype(np.float64)[..., None]).swapaxes(1, 2).astype(np.float32)
+            assert np.isfinite(want).all() and np.array_equal(got.cpu().numpy(), want)
