@@ -309,7 +309,7 @@ __device__ __forceinline__ float byte_of(uint32_t w, int i) {
 }
 // 8 codes times s, exact before they are rounded, to a row.  code * s in fp32 is rounded already, and bf16 rounds that once more: wrong only where the first
 // rounding ended halfway between two numbers of bf16.  Then (__any of the wavefront) all are rounded to odd first -- the last bit set where something was cut off --
-// which bf16 rounds as it would the exact product.
+// which bf16 rounds as it would the exact product.  (What was cut off a product below the normal numbers may be below the smallest one: lifted.)
 template <int FORMAT>
 __device__ __forceinline__ void store_values(bf16_t *to, const float (&code)[8], float s) {
     typedef uint16_t pair __attribute__((ext_vector_type(2)));
@@ -322,11 +322,12 @@ __device__ __forceinline__ void store_values(bf16_t *to, const float (&code)[8],
         least = __builtin_elementwise_min(least, __builtin_bit_cast(pair, ends));
     }
     if (__any(least.x == 0 || least.y == 0)) {
+        const float lift = s < 1.f ? 0x1p64f : 1.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float rest = __builtin_fmaf(code[i], s, -p[i]);
+            const float rest = __builtin_fmaf(code[i], s * lift, -(p[i] * lift));
             const uint32_t bits = __float_as_uint(p[i]);
-            if (rest != 0.f && !(bits & 1)) p[i] = __uint_as_float((rest > 0.f) == (p[i] > 0.f) ? bits | 1 : bits - 1);
+            if (rest != 0.f && p[i] != 0.f && !(bits & 1)) p[i] = __uint_as_float((rest > 0.f) == (p[i] > 0.f) ? bits | 1 : bits - 1);
         }
     }
     *reinterpret_cast<uint4 *>(to) = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));

@@ -5,7 +5,7 @@ import torch
 
 import paper_2605_15609_amd as psd
 from tests.gpu_common import DEV
-from tests.kv8_common import Cache, stored
+from tests.kv8_common import Cache, spots, stored, table
 from tests.test_gpu_kv8 import check_store
 
 pytestmark = pytest.mark.gpu
@@ -38,3 +38,29 @@ def test_blocks_of_the_smallest_numbers(fmt, d):
         for got, n, s in zip(psd.psd_kv8_load(dev, 0, start + 16, dtype=F32), number, scales):
             want = (n[:, :, :start + 16] * s.astype(np.float64)[..., None]).swapaxes(1, 2).astype(np.float32)
             assert np.isfinite(want).all() and np.array_equal(got.cpu().numpy(), want)
+
+
+def test_products_below_the_normal_numbers_are_rounded_once():
+    """e4m3 codes times scales of 2^-149 whole numbers, next to a border between two numbers of bf16 by less than fp32 has there."""
+    t = table("e4m3")
+    host, pairs = Cache(1, 1, 16, 64 * 16, 16, "e4m3"), []
+    for byte in (0x0b, 0x14, 0x1d, 0x25, 0x2b, 0x33, 0x35, 0x37):
+        for m in range(12):
+            # code * k 2^-149 beside (2 m + 1) 2^-134, by half of 2^-149 at most
+            k = round((2 * m + 1) * 2 ** 15 / t[byte])
+            if 0 < k < 2 ** 23 and k * t[byte] != (2 * m + 1) * 2 ** 15:
+                pairs.append((byte, k))
+    pairs = pairs[:64]
+    assert len(pairs) == 64
+    flat = host.codes.reshape(1, 1, -1)
+    for b, (byte, k) in enumerate(pairs):
+        for at in spots(host.n, 16):
+            flat[0, 0, at[16 * b:16 * b + 16]] = byte
+            flat[0, 0, at[16 * b + 3]] = byte | 0x80
+        host.scales[0, 0, b] = np.float32(k * 2.0 ** -149)
+    want = host.read(0)[0]
+    # exact, and rounded to whole numbers of 2^-133, ties to even
+    want = np.sign(want) * np.rint(np.abs(want) * 2.0 ** 133) * 2.0 ** -133
+    assert (want != 0).any()
+    for got in psd.psd_kv8_load(host.device(DEV), 0, 16 * len(pairs)):
+        assert np.array_equal(got[0].double().cpu().numpy(), want[:16 * len(pairs)])
