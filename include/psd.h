@@ -531,8 +531,9 @@ int32_t psd_kv8_load(const psd_kv8_cache *cache, int32_t units, int32_t first, i
  *   own sequence (row i of sequence s: k + (s*L + i) * ld_k, in the dtype of the call, 16-byte aligned rows), which are not in the cache: a block attends
  *   to all of itself.  Shape, out, lse and rows without a key as for psd_attention_shared (S a multiple of cache->seqs_per_unit; cache->len may be
  *   0, then codes and scales may be NULL with capacity 0).  Codes are used as they are: a key's scale multiplies its score, a value's its probability, which with
- *   bf16 is rounded after that (outputs are divided by the sum of the rounded ones, lse is of the others).  Sums and statistics are fp32.  ws: device, 256-byte aligned, psd_attention_kv8_bytes of the same shape and cache (own_rows: 1
- *   where k is set; it does not look at device memory); calls that overlap need one each.
+ *   bf16 is rounded after that.  Outputs are divided by the sum of the rounded ones (where a value scale is 0 or below the normal numbers, of the others); lse is of
+ *   the others.  Sums and statistics are fp32.  ws: device, 256-byte aligned, psd_attention_kv8_bytes of the same shape and cache (own_rows: 1 where k is set; it
+ *   does not look at device memory); calls that overlap need one each.
  * psd_debug_attention_kv8_plan: form (0: tiles of 32 rows, 1: of 128), tiles of rows of a unit and KV head, parts of the keys, keys of a part.
  * psd_debug_force_attention_kv8: the form (-1: by price; fp32 has form 0 only) and the parts (0: by price; cut to what there is) of the calls that
  *   follow, workspaces included.  Process-wide. */

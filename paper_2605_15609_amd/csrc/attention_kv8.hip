@@ -80,9 +80,16 @@ __device__ __forceinline__ uint4 keep(uint4 c, int left) {
     return c;
 }
 
-// 16 positions of a head's scales: key scale times 1 / sqrt(d) in units of log 2, value scale
+// 16 positions of a head's scales, the same in all lanes: key scale times 1 / sqrt(d) in units of log 2, value scale
 struct Scale {
     float k, v;
+    float inv;   // what products are multiplied by that tell what probabilities were rounded to (see weigh)
+    bool told;
+    __device__ Scale() {}
+    __device__ Scale(float key, float value, float reciprocal) : k(key), v(value), inv(reciprocal), told(tells(value)) {}
+    // the reciprocal of a value scale holds what it has to: 2^-126 .. 2^126
+    static __device__ __forceinline__ bool tells(float value) { return __float_as_uint(value) - 0x00800000u < 0x7e000000u; }
+    static __device__ __forceinline__ float reciprocal(float value) { return tells(value) ? __builtin_amdgcn_rcpf(value) : 1.f; }
 };
 
 // The softmax of a lane's row, kept relative to a running reference that is raised only where the maximum has grown by more than 2^SLACK in a
@@ -139,11 +146,12 @@ struct Softmax {
             s[g].k = row ? 1.f : s[g].k;
         }
     }
-    // 8 probabilities times value scales as the second product takes them
+    // 8 probabilities, whose sum is l8, times value scales as the second product takes them.  The products over their scale say what the probabilities were
+    // rounded to; where a scale does not (a block of zeros has 0) these count as they are, so that what the products of others say stays.
     template <typename T>
-    __device__ __forceinline__ void weigh(float (&e)[8], float value_scale, Frag<T> &p) {
+    __device__ __forceinline__ void weigh(float (&e)[8], float l8, const Scale &s, Frag<T> &p) {
 #pragma unroll
-        for (int v = 0; v < 8; ++v) e[v] *= value_scale;
+        for (int v = 0; v < 8; ++v) e[v] *= s.v;
         probabilities(e, p);
         if constexpr (sizeof(T) == 2) {
             typedef __bf16 pair __attribute__((ext_vector_type(2)));
@@ -151,28 +159,28 @@ struct Softmax {
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, (&p.v.x)[i]), ones, sum, false);
-            given = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(value_scale), given);
+            given = __builtin_fmaf(s.told ? sum : l8, s.inv, given);
         }
     }
     template <typename T, int NT>
     __device__ __forceinline__ void weights(const floatx16 (&x)[NT], const Scale (&s)[2 * NT], Frag<T> (&p)[2 * NT]) {
-        float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int g = 0; g < 2 * NT; ++g) {
-            float e[8];
+            float e[8], sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int v = 0; v < 8; ++v) {
                 e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g >> 1][8 * (g & 1) + v], s[g].k, neg));
-                sum[v & 1] += e[v];
+                sum[v & 1] = v < 2 ? e[v] : sum[v & 1] + e[v];
             }
-            weigh(e, s[g].v, p[g]);
+            l += sum[0] + sum[1];
+            weigh(e, sum[0] + sum[1], s[g], p[g]);
         }
-        l += sum[0] + sum[1];
     }
     // What the outputs of a row are multiplied by.  A probability times its value scale is rounded to bf16, and where one key has nearly all of a row that
     // is a factor of the whole row, half a step like the result's own rounding.  The sum of the rounded products over their scales has the same factor, so
     // it goes away, for 4 % of the time where vector instructions bound it (128 drafts 799 -> 829 us, drafts of 4 requests 47 -> 48.8) and 1 % where memory
-    // does.  It is within half a step; anything else comes from scales of 0, infinite or NaN, or products below the normal numbers, and corrects nothing.
+    // does.  It is within half a step; anything else comes from scales that are infinite or NaN, or products below the normal numbers, and corrects nothing.
+    // (Blocks of scale 0 looked for in front of the exponentials instead, in a branch that is hardly ever taken: 128 drafts 830 -> 840 us.)
     template <typename T>
     __device__ __forceinline__ float correction() const {
         if constexpr (sizeof(T) == 4) return 1.f;
@@ -192,7 +200,7 @@ template <int NT>
 __device__ __forceinline__ void hide(floatx16 (&x)[NT], Scale (&s)[2 * NT], int left, int half) {
 #pragma unroll
     for (int g = 0; g < 2 * NT; ++g) {
-        if (g * 16 >= left) s[g] = {1.f, 1.f};
+        if (g * 16 >= left) s[g] = Scale(1.f, 1.f, 1.f);
         const bool zero = s[g].k == 0.f;   // (0 x -inf is NaN: the scores are scaled here)
         if (zero) s[g].k = 1.f;
 #pragma unroll
@@ -285,7 +293,7 @@ __device__ __forceinline__ void own_step(const SharedShape &sh, const Kv8Launch 
 #pragma unroll
     for (int i = 0; i < 16; ++i)
         if (8 * (i >> 2) + 4 * half + (i & 3) >= left || !sees) x[0][i] = -INFINITY;
-    Scale scale[2] = {{sl2, 1.f}, {sl2, 1.f}};
+    Scale scale[2] = {{sl2, 1.f, 1.f}, {sl2, 1.f, 1.f}};
     Frag<T> p[2];
     soft.step(x, scale, acc, p);
     asm volatile("" ::: "memory");
@@ -381,7 +389,7 @@ __device__ __forceinline__ void few_rows(const T *__restrict__ q, const SharedSh
         const int left = end - begin - st * KV8_TILE;
         Scale scale[2];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) scale[g] = {c.scale[g].x * sl2, c.scale[g].y};
+        for (int g = 0; g < 2; ++g) scale[g] = Scale(c.scale[g].x * sl2, c.scale[g].y, Scale::reciprocal(c.scale[g].y));
         if (st + NW < steps) load(next, t0 + st + NW);
         floatx16 x[1];
 #pragma unroll
@@ -556,9 +564,10 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
         };
         read(f[0], ak, 0, KS);
         Scale scale[4];
+        const float inv = Scale::reciprocal(sc.y);   // of lane g: group g
+        auto of_lane = [](float x, int g) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), g)); };
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            scale[g] = {__int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.x), g)) * sl2, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), g))};
+        for (int g = 0; g < 4; ++g) scale[g] = Scale(of_lane(sc.x, g) * sl2, of_lane(sc.y, g), of_lane(inv, g));
         sc = head.scale(t0 + 2 * (st + 1), lane & 3);
         const int left = end - begin - st * KT;
         if (left < KT) hide(x, scale, left, half);
@@ -582,12 +591,14 @@ __device__ __forceinline__ void many_rows(const bf16_t *__restrict__ q, const Sh
 #pragma unroll
             for (int i = ks * N; i < ks * N + N; ++i) {
                 e[i >> 3][i & 7] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 4][i & 15], scale[i >> 3].k, soft.neg));
-                sum[i & 1] += e[i >> 3][i & 7];
-                if ((i & 7) == 7) soft.weigh(e[i >> 3], scale[i >> 3].v, p[i >> 3]);
+                sum[i & 1] = (i & 7) < 2 ? e[i >> 3][i & 7] : sum[i & 1] + e[i >> 3][i & 7];
+                if ((i & 7) == 7) {
+                    soft.l += sum[0] + sum[1];
+                    soft.weigh(e[i >> 3], sum[0] + sum[1], scale[i >> 3], p[i >> 3]);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        soft.l += sum[0] + sum[1];
         // product j of the values: 16 positions g = j / CT, channels j % CT, whose fragment is the one at 2 (g / 2 CT + j % CT) + g % 2
         auto value_at = [](int j) { return ((j / CT >> 1) * CT + j % CT) * 2 + (j / CT & 1); };
 #pragma unroll

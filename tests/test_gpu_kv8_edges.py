@@ -6,7 +6,8 @@ import torch
 import paper_2605_15609_amd as psd
 from tests.gpu_common import DEV
 from tests.kv8_common import Cache, spots, stored, table
-from tests.test_gpu_kv8 import check_store
+from tests.shared_common import near
+from tests.test_gpu_kv8 import check_store, forced  # noqa: F401 (a fixture)
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -64,3 +65,28 @@ def test_products_below_the_normal_numbers_are_rounded_once():
     assert (want != 0).any()
     for got in psd.psd_kv8_load(host.device(DEV), 0, 16 * len(pairs)):
         assert np.array_equal(got[0].double().cpu().numpy(), want[:16 * len(pairs)])
+
+
+@pytest.mark.parametrize("none", [0.0, 2.0 ** -130, 2.0 ** -149])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("L,positions", [(4, 200), (64, 200), (64, 700)])
+@pytest.mark.parametrize("form,parts", [(0, 0), (1, 0), (0, 2), (1, 2)])
+def test_a_row_with_one_key_beside_blocks_without_values(forced, form, parts, fmt, L, positions, none):
+    """Blocks whose values are all zero (a scale of 0), or too small for a reciprocal of their scale: a row that a key of another block has all of is still
+    rounded once -- half a step, 2^-18 for some forty steps of fp32, and 700 exp(-32) < 2^-36 of the others' values."""
+    forced(form, parts)
+    d = 64
+    host = Cache(1, 1, d, positions, 16, fmt, seed=11)
+    without = np.arange(host.n // 16) % 2 == 1                  # every second block, so every step of every wavefront has one
+    host.scales[0, 0, without & ~np.isnan(host.scales[0, 0, :, 1]), 1] = none
+    host.scales[0, 0, ~np.isnan(host.scales[0, 0, :, 0]), 0] = 0.02
+    keys, values = (torch.from_numpy(x[:, 0]) for x in host.read(0))
+    # each row asks for a key of its own, of a block that has values
+    held = torch.from_numpy(np.flatnonzero(~without[np.arange(positions) // 16]))
+    best = held[torch.arange(2 * L) * 37 % len(held)]
+    q = (keys[best] * (1000 / (keys[best] ** 2).sum(1, keepdim=True))).to(BF)
+    top = (q.double() @ keys.T / d ** 0.5).topk(2)
+    assert torch.equal(top.indices[:, 0], best) and (top.values[:, 0] - top.values[:, 1] > 33).all()
+    want = values[best].view(1, L, 2, d).numpy()
+    out = psd.psd_attention_kv8(q.view(1, L, 2, d).to(DEV), host.device(DEV))
+    near(out, want, (2.0 ** -8 + 2.0 ** -18) * np.abs(want) + 2.0 ** -36 * np.abs(values.numpy()).max(), "out")
