@@ -976,6 +976,10 @@ def rotary_frequencies(rotated: int, theta: float, kind: str = "plain", stretch:
     return out, factor.value
 
 
+def _address(t: Optional[torch.Tensor]):
+    return None if t is None or t.numel() == 0 else t.data_ptr()
+
+
 def _layout(t: Optional[torch.Tensor]):
     # (the device's number, not the device, whose hash is slow; whatever is not on a GPU is -1 and never passes a check beside what is)
     return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
@@ -1047,7 +1051,8 @@ class Kv8Cache:
 
     codes uint8 [units, n_kv_heads, positions / 32, 2, 32 * d_head] and scales float32 [units, n_kv_heads, positions / block, 2], each unit dense
     (include/psd.h has the order of the codes); format "int8" or "e4m3".  The first `length` positions (default: all) of a unit are held, or lens[unit]
-    of them (int32 [units], what is outside 0 .. length is cut); seqs_per_unit consecutive sequences attend to a unit."""
+    of them (int32 [units], what is outside 0 .. length is cut); seqs_per_unit consecutive sequences attend to a unit.  These three may be set anew (a
+    workspace kept for a shorter length may then be too small, which the call says); everything else stays as the cache was made."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, d_head: int, format: str = "int8", length: Optional[int] = None,
                  lens: Optional[torch.Tensor] = None, seqs_per_unit: int = 1):
@@ -1063,22 +1068,33 @@ class Kv8Cache:
         block = positions // blocks if blocks else 32
         if block * blocks != positions:
             raise PsdError(f"{blocks} scales for {positions} positions")
-        n = positions if length is None else int(length)
-        if not 0 <= n <= positions:
-            raise PsdError(f"{n} positions of {positions}")
-        if lens is not None:
-            _dense_on(lens, "lens", torch.int32, (units,), codes.device)
         if scales.device != codes.device:
             raise PsdError(f"a cache on {codes.device} and {scales.device}")
-        self.codes, self.scales, self.lens, self.format = codes, scales, lens, format
-        self.units, self.n_kv_heads, self.d_head, self.capacity, self.block, self.length = units, heads, int(d_head), positions, block, n
-        self.seqs_per_unit, self.device = int(seqs_per_unit), codes.device
-        def address(t):
-            return None if t is None or t.numel() == 0 else t.data_ptr()
-        self.c = _Kv8Cache(address(codes), address(scales), address(lens), codes.stride(0) if units > 1 else 0, scales.stride(0) if units > 1 else 0,
-                           _int32(positions, "positions"), _int32(n, "length"), _int32(block, "block"), _KV8_FORMATS[format],
-                           _int32(heads, "KV heads"), _int32(d_head, "d_head"), _int32(self.seqs_per_unit, "seqs_per_unit"), 0)
+        self.codes, self.scales, self.format, self.device = codes, scales, format, codes.device
+        self.units, self.n_kv_heads, self.d_head, self.capacity, self.block = units, heads, int(d_head), positions, block
+        self.c = _Kv8Cache(_address(codes), _address(scales), None, codes.stride(0) if units > 1 else 0, scales.stride(0) if units > 1 else 0,
+                           _int32(positions, "positions"), 0, _int32(block, "block"), _KV8_FORMATS[format], _int32(heads, "KV heads"),
+                           _int32(d_head, "d_head"), 1, 0)
         self.shapes: dict = {}      # (see rows and _kv8_shape)
+        self.length, self.lens, self.seqs_per_unit = positions if length is None else length, lens, seqs_per_unit
+
+    def __setattr__(self, name, value):
+        """What the calls read is self.c, so that says what the attributes say."""
+        if name == "length":
+            value = int(value)
+            if not 0 <= value <= self.capacity:
+                raise PsdError(f"{value} positions of {self.capacity}")
+            self.c.len = value
+        elif name == "lens":
+            if value is not None:
+                _dense_on(value, "lens", torch.int32, (self.units,), self.device)
+            self.c.lens = _address(value)
+        elif name == "seqs_per_unit":
+            value = self.c.seqs_per_unit = _int32(value, "seqs_per_unit")
+            self.shapes.clear()
+        elif name in self.__dict__:
+            raise PsdError(f"{name} stays as the cache was made")
+        super().__setattr__(name, value)
 
     @classmethod
     def empty(cls, units: int, n_kv_heads: int, d_head: int, positions: int, block: int = 32, format: str = "int8", device="cuda:0",
