@@ -39,6 +39,8 @@ int32_t check_cache(const psd_kv8_cache *a, int32_t units, Kv8 *out) {
         PSD_FAIL(PSD_ERR_SHAPE, "cache: %d positions are not whole blocks of %d", a->capacity, std::max(a->block, KV8_TILE));
     if (a->len < 0 || a->len > a->capacity) PSD_FAIL(PSD_ERR_SHAPE, "cache: %d positions of %d", a->len, a->capacity);
     if (a->stride_codes < 0 || a->stride_scales < 0) PSD_FAIL(PSD_ERR_SHAPE, "cache: negative stride");
+    if (units > 1 && (double)units * std::max((double)a->stride_codes, 4.0 * a->stride_scales) >= 0x1p60)
+        PSD_FAIL(PSD_ERR_SHAPE, "cache: %d units %lld bytes and %lld floats apart", units, (long long)a->stride_codes, (long long)a->stride_scales);
     if (a->capacity > 0) {
         if (!a->codes || !a->scales) PSD_FAIL(PSD_ERR_INVALID_ARG, "cache: codes or scales are NULL");
         if (misaligned16(a->codes) || a->stride_codes % 16) PSD_FAIL(PSD_ERR_SHAPE, "cache: codes must be 16-byte aligned");
