@@ -4,10 +4,11 @@ import pytest
 import torch
 
 import paper_2605_15609_amd as psd
+from paper_2605_15609_amd import binding as B
 from tests.gpu_common import DEV
 from tests.kv8_common import Cache, spots, stored, table
 from tests.shared_common import near
-from tests.test_gpu_kv8 import check_store, forced  # noqa: F401 (a fixture)
+from tests.test_gpu_kv8 import check_store, forced, run_attention  # noqa: F401 (forced: a fixture)
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -90,3 +91,53 @@ def test_a_row_with_one_key_beside_blocks_without_values(forced, form, parts, fm
     want = values[best].view(1, L, 2, d).numpy()
     out = psd.psd_attention_kv8(q.view(1, L, 2, d).to(DEV), host.device(DEV))
     near(out, want, (2.0 ** -8 + 2.0 ** -18) * np.abs(want) + 2.0 ** -36 * np.abs(values.numpy()).max(), "out")
+
+
+def parts_of(form, positions, parts):
+    """Parts that a call of so many positions has when `parts` are asked for: whole steps of 128 (form 0) or 64 positions, evenly."""
+    steps = max(1, -(-positions // (64 if form else 128)))
+    each = -(-steps // min(parts, steps))
+    return -(-steps // each)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("parts", [1, 2, 3, 5])
+@pytest.mark.parametrize("dtype,form,H,Hkv,d,S,L,per,positions,lens,own", [
+    (BF, 0, 28, 4, 128, 2, 1, 1, 1000, [1000, 129], True), (BF, 1, 8, 2, 64, 4, 33, 2, 700, [700, 65], True), (BF, 1, 4, 1, 128, 2, 64, 2, 449, None, False),
+    (F32, 0, 4, 4, 16, 2, 5, 1, 600, [600, 1], True), (F32, 0, 2, 1, 128, 2, 64, 1, 900, None, True), (F32, 0, 8, 8, 64, 4, 3, 2, 385, [385, 0], False)])
+def test_as_many_parts_as_were_asked_for(forced, fmt, parts, dtype, form, H, Hkv, d, S, L, per, positions, lens, own):
+    forced(form, parts)
+    plan = run_attention(dtype, H, Hkv, d, S, L, per, positions, 32, fmt, lens, own, seed=positions + parts)
+    assert (plan[0], plan[2]) == (form, parts_of(form, positions, parts)) and (parts == 1) == (plan[2] == 1)
+
+
+@pytest.mark.parametrize("form,parts", [(0, 1), (1, 1), (0, 2), (1, 2)])
+def test_every_position_of_a_cache_of_zeros_counts(forced, form, parts):
+    """All scales are 0: every score is 0, so lse is the log of the number of positions in every row."""
+    forced(form, parts)
+    host = Cache(2, 1, 64, 150, 32, "e4m3", lens=[33, 150])
+    host.scales[:] = 0.0
+    q = torch.randn((2, 8, 8, 64), generator=torch.Generator().manual_seed(6)).to(BF).to(DEV)
+    lse = torch.full((2, 8, 8), float("nan"), device=DEV)
+    out = psd.psd_attention_kv8(q, host.device(DEV), lse=lse)
+    assert (out == 0).all()
+    near(lse, np.log(np.array([33.0, 150.0]))[:, None, None] * np.ones((1, 8, 8)), np.full((2, 8, 8), 2.0 ** -20), "lse")
+
+
+def test_two_calls_at_once_that_both_need_a_workspace():
+    host = Cache(2, 2, 128, 5000, 32, "int8")
+    q = torch.randn((2, 1, 8, 128), generator=torch.Generator().manual_seed(2)).to(BF).to(DEV)
+    cache = host.device(DEV)
+    assert B.attention_kv8_plan(q, cache)[2] > 1
+    spaces = [psd.psd_attention_kv8_workspace(q, cache) for _ in range(2)]
+    assert spaces[0].numel() > 256
+    others = q.flip(0).contiguous()
+    want = [psd.psd_attention_kv8(x, cache) for x in (q, others)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.full_like(q, float("nan")) for _ in range(12)]
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        with torch.cuda.stream(streams[i % 2]):
+            psd.psd_attention_kv8((q, others)[i % 2], cache, out=out, ws=spaces[i % 2])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i % 2]) for i, o in enumerate(outs))
