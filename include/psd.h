@@ -465,7 +465,8 @@ int32_t psd_decode_block_shared(psd_handle *h, int32_t *tokens, int32_t B, int32
  * psd_rotary_frequencies: theta^(-2j / rotated), host double [rotated / 2], plain or scaled for contexts `stretch` times as long as a model was
  *   trained for: PSD_ROTARY_LINEAR divides all by stretch; PSD_ROTARY_BASE uses theta * stretch^(rotated / (rotated - 2)), which keeps the
  *   fastest and divides the slowest by stretch; PSD_ROTARY_PARTS divides those that turn less than `slow` times over `trained` positions by stretch, keeps
- *   those that turn more than `fast` times, goes linearly between, and has a factor of 0.1 ln(stretch) + 1 (else *factor is 1; it may be NULL). */
+ *   those that turn more than `fast` times, goes linearly between, and has a factor of 0.1 ln(stretch) + 1 (else *factor is 1; it may be NULL).  "Between" is in turns:
+ *   a model whose ramp goes by the pair's index between two cut-offs needs frequencies of the caller's own. */
 #define PSD_MAX_ROTARY_HEAD 256
 #define PSD_ROTARY_PLAIN 0
 #define PSD_ROTARY_LINEAR 1

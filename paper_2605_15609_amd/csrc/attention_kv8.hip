@@ -9,9 +9,9 @@
 // codes in the order of the products' fragments (kv8_device.h), so a lane's 16 bytes are two fragments once they are converted.
 //
 // What bounds it, with bf16 heads of 128: single rows memory (32 requests of the 7B shape over 16384 positions each take 94 us, 5.7 TB/s of codes; of
-// lengths even over 1 .. 16384 60 - 67 us, where a part's last workgroups run alone); blocks of 16 requests over 1312 positions (8B shape) 40 us, of
+// lengths even over 1 .. 16384 60 - 73 us, where a part's last workgroups run alone); blocks of 16 requests over 1312 positions (8B shape) 40 us, of
 // which 32 are memory.  Drafts are bound by vector instructions: a tile of 32 keys and 32 rows has 16 products and, in int8, 192 instructions that convert
-// its codes (e4m3: 64) and some 150 of softmax.  128 drafts of 64 rows over 5120 + 64 keys (8B shape) take 783 - 829 us, 0.84 - 0.89 PFLOP/s: vector units busy 71 %
+// its codes (e4m3: 64) and some 150 of softmax.  128 drafts of 64 rows over 5120 + 64 keys (8B shape) take 783 - 845 us, 0.82 - 0.89 PFLOP/s: vector units busy 70 %
 // of the cycles, matrix cores 44 %, at a clock that power holds near 1.8 GHz.  Small calls are one chain of round trips: 6.5 us, 7.5 with the host's call.
 // Tried and slower: queries in LDS for three workgroups a CU, with one tile of codes under way a wavefront in place of two (32 requests, ragged: 58 -> 66);
 // 16x16 products for up to 16 rows, a third workgroup a CU (level with these, 64 us); value scales in the exponent and no maximum in front of the exponentials
@@ -325,7 +325,8 @@ __device__ __forceinline__ void own_step(const SharedShape &sh, const Kv8Launch 
     asm volatile("" ::: "memory");
 }
 
-// A tile of up to 32 rows of a unit and KV head (r_first ..) against the own blocks of their sequences, every W-th step from `first` on
+// A tile of up to 32 rows of a unit and KV head (r_first ..) against the own blocks of their sequences, every W-th step from `first` on.  A step is of one
+// sequence, so many drafts of one row take 3 - 6 us of their call (8 requests of 8 drafts over 2000 positions, 8B shape: 30 us, 24 without own rows).
 template <typename T, int DH, int CT, typename Q>
 __device__ __forceinline__ void own_blocks(const SharedShape &sh, const Kv8Launch &ln, int u, int kvh, int r_first, int rows, int64_t token, int first, int W, float sl2,
                                            const Q &query, Softmax &soft, floatx16 (&acc)[CT], unsigned char *lds) {
@@ -700,6 +701,7 @@ void run(const T *q, const SharedShape &sh, const Kv8Launch &ln, hipStream_t st)
 //   a workgroup alone on a CU  few rows: 0.93 for 128 keys (32768 keys of 4 requests, 16 workgroups), 0.55 with heads of 64, 2.7 in fp32 with heads of 64;
 //                              many rows: 1.36 for 64 keys (2000 keys, 8 drafts of 64 rows)
 //   two and more               few rows: 0.88 a workgroup, 0.75 with e4m3, whose conversion is shorter (one unit of 512 rows a KV head; 4 of 1344); many rows: 1.25
+//                              (fp32 in proportion from heads of 64: of 128 it is 32 us against 18 for 4 blocks of 16 rows of 8 heads over 4000 keys)
 //   fixed                      4.5 for the call, 2 or 5 for a workgroup, 4 for the join
 //   memory                     5.7 TB/s (32 caches of 16384 keys: 94 us)
 // and units of lengths of their own, which are taken to be about half full, by how long the last of them runs.

@@ -5,9 +5,10 @@
 // M = 127 (whole numbers) or 448 (floats of 4 and 3 bits), RN to the nearest code, ties to even.  Where s grows, kept codes are rounded again:
 // RN(code * s_kept / s).  The quotients are exact before they are rounded, so a code does not depend on how the division is done.
 //
-// Bound: memory, rows read once and codes written once: 4 prompts of 1024 positions of the 8B shape (67 MB of rows, 34 of codes) are stored in 22.8 us and
-// read back in 17, where a copy of as many bytes takes 20 (what was just written is read from the caches).  The store's vector instructions, some 18 a number,
-// take most of its time beside that; deciding the quotients next to a border on a path of their own took 27 us, for in a third of the blocks some are.
+// Bound: memory, rows read once and codes written once: 4 prompts of 1024 positions of the 8B shape (67 MB of rows, 34 of codes) are stored in 20 - 23 us and
+// read back in 17 where they have just been written and 22 out of memory (12 such caches in turn); a copy of as many bytes takes 20.  The store's vector
+// instructions, some 17 a number, take most of its time beside that; deciding the quotients next to a border on a path of their own took 27 us, for in a third
+// of the blocks some are.
 // A token of 32 requests (7B shape) takes 5.5 us: lengths, then rows, scale and codes, then the largest of a block, each a round trip.
 #include "psd_internal.h"
 #include "kv8_device.h"
@@ -57,7 +58,7 @@ struct Rounding {
     }
     // Four of them as bytes.  Numbers of bf16 are often next to a border: half of the largest, of which 127 codes make 63.5, or three quarters of it, 336 with
     // 448.  So t is taken to b, the nearest half step -- a code or a border -- and a little to the side that x - b s is on, whose sign is exact: it is
-    // 2^-29 of b s or more, or nothing, and then b decides (ties to even).  A code is not left by that, nor is one next to it reached.
+    // 2^-25 of s or more (int8), 2^-29 of b s (e4m3), or nothing, and then b decides (ties to even).  A code is not left by that, nor is one next to it reached.
     __device__ __forceinline__ uint32_t codes(float (&x)[4]) const {
         if (lift != 1.f) {
             const float most = s * kv8_most(FORMAT);

@@ -3,14 +3,8 @@
 #include "psd_internal.h"
 #include "device_types.h"
 
-// Where the code of a position (0 .. 31 of its tile) and channel lies among the 32 * d bytes of a tile's keys, or of its values.  Both are the
-// order in which a lane of a 32x32 product takes them, 16 bytes at a time: keys 16 channels of one position, values 16 positions of one
-// channel, those that the scores of the lane's half are of (8 b + 4 h + j).
-__host__ __device__ __forceinline__ int kv8_key_at(int position, int c) { return (c >> 4) * 512 + position * 16 + (c & 15); }
-__host__ __device__ __forceinline__ int kv8_value_at(int position, int c, int d) {
-    const int w = d < 32 ? d : 32;
-    return c / w * (32 * w) + ((position >> 2) & 1) * (16 * w) + c % w * 16 + (position >> 3) * 4 + (position & 3);
-}
+// The codes of a tile lie in the order in which a lane of a 32x32 product takes them, 16 bytes at a time (psd.h): keys 16 channels of one position, values 16
+// positions of one channel, those that the scores of the lane's half are of (8 b + 4 h + j).
 
 // the largest code
 __host__ __device__ constexpr float kv8_most(int format) { return format == PSD_KV8_INT8 ? 127.f : 448.f; }

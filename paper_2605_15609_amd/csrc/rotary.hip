@@ -4,10 +4,13 @@
 // for the pairs (j, j + r/2) or (2j, 2j + 1) of the first r channels; the others stay as they are.
 //
 // An angle of a far position has more turns than fp32 can count, so position * frequency / 2 pi is taken in 64 bits and only what is left of
-// whole turns is rounded: off by at most 2^-25 of a turn.  Everything else is fp32, rounded to the type once.
+// whole turns is rounded: off by 2^-25 of a turn and, for the three products in 64 bits, 2^-51 of the angle's turns (as much at 2^26 of them).
+// Everything else is fp32, rounded to the type once.
 //
 // Bound: memory, every channel read and written once: 20480 rows of 64 heads of 128 take 115 - 122 us (671 MB, 5.5 - 5.8 TB/s; a copy has 5.2),
 // normed; 6126 rows of 32 heads, half of each turned, 17 - 19 us (100 MB).  One block of the small model 3.5 us, a launch.
+// Heads or halves that are not whole pieces of 16 bytes go by wavefronts, which turn the angles of every head anew and are bound by that: 20480 rows of 64
+// heads of 128 with 120 channels turned in halves take 636 us, 16 heads of 64 with 24 channels 97 (with 32, by pieces, 15).
 #include "psd_internal.h"
 #include "device_types.h"
 
