@@ -1079,22 +1079,28 @@ class Kv8Cache:
         self.length, self.lens, self.seqs_per_unit = positions if length is None else length, lens, seqs_per_unit
 
     def __setattr__(self, name, value):
-        """What the calls read is self.c, so that says what the attributes say."""
+        """What the calls read is self.c, so that says what the attributes say (anew: a copy of the cache has its own)."""
         if name == "length":
             value = int(value)
             if not 0 <= value <= self.capacity:
                 raise PsdError(f"{value} positions of {self.capacity}")
-            self.c.len = value
+            self._describe("len", value)
         elif name == "lens":
             if value is not None:
                 _dense_on(value, "lens", torch.int32, (self.units,), self.device)
-            self.c.lens = _address(value)
+            self._describe("lens", _address(value))
         elif name == "seqs_per_unit":
-            value = self.c.seqs_per_unit = _int32(value, "seqs_per_unit")
-            self.shapes.clear()
+            value = _int32(value, "seqs_per_unit")
+            self._describe("seqs_per_unit", value)
+            self.__dict__["shapes"] = {}
         elif name in self.__dict__:
             raise PsdError(f"{name} stays as the cache was made")
         super().__setattr__(name, value)
+
+    def _describe(self, field, value):
+        c = _Kv8Cache.from_buffer_copy(self.c)
+        setattr(c, field, value)
+        self.__dict__["c"] = c
 
     @classmethod
     def empty(cls, units: int, n_kv_heads: int, d_head: int, positions: int, block: int = 32, format: str = "int8", device="cuda:0",

@@ -1,4 +1,6 @@
 """A Kv8Cache says what the calls that take it read, also after its attributes are set; nothing is launched, so no GPU is needed."""
+import copy
+
 import pytest
 import torch
 
@@ -57,3 +59,15 @@ def test_what_a_cache_was_made_with_stays(name):
     c = cache()
     with pytest.raises(psd.PsdError):
         setattr(c, name, getattr(c, name))
+
+
+def test_a_copy_has_a_length_and_sequences_of_its_own():
+    lens = torch.ones(2, dtype=torch.int32)
+    one = cache(lens=lens)
+    q = torch.zeros((2, 4, 6, 64), dtype=torch.bfloat16)
+    other = copy.copy(one)
+    other.length, other.lens, other.seqs_per_unit = 64, None, 2
+    assert (one.length, one.c.len, one.c.lens, one.c.seqs_per_unit) == (20000, 20000, lens.data_ptr(), 1) and (other.c.len, other.c.lens, other.c.seqs_per_unit) == (64, None, 2)
+    assert B.attention_kv8_plan(q, one)[1] > 0
+    with pytest.raises(psd.PsdError):
+        B.attention_kv8_plan(q, other)
