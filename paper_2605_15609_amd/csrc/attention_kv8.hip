@@ -179,7 +179,7 @@ struct Softmax {
     // What the outputs of a row are multiplied by.  A probability times its value scale is rounded to bf16, and where one key has nearly all of a row that
     // is a factor of the whole row, half a step like the result's own rounding.  The sum of the rounded products over their scales has the same factor, so
     // it goes away, for 4 % of the time where vector instructions bound it (128 drafts 799 -> 829 us, drafts of 4 requests 47 -> 48.8) and 1 % where memory
-    // does.  It is within half a step; anything else comes from scales that are infinite or NaN, or products below the normal numbers, and corrects nothing.
+    // does.  It is within half a step; anything else comes from rows without a number or products below the normal numbers, and corrects nothing.
     // (Blocks of scale 0 looked for in front of the exponentials instead, in a branch that is hardly ever taken: 128 drafts 830 -> 840 us.)
     template <typename T>
     __device__ __forceinline__ float correction() const {
